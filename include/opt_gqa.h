@@ -71,6 +71,17 @@ extern "C" {
 #define OPT_GQA_ERR_TIMEOUT (-6) /* a bounded device-side wait ran out (device status)    */
 #define OPT_GQA_ERR_SCRATCH (-7) /* the call needs more than OPT_GQA_STATIC_SCRATCH_BYTES  */
 
+/* Rotary positions: which elements of a head form pair i (R = the number of rotated dims). */
+#define OPT_GQA_ROTARY_HALF 0        /* i and i + R/2   */
+#define OPT_GQA_ROTARY_INTERLEAVED 1 /* 2i and 2i + 1   */
+
+/* Frequency scaling for contexts longer than the trained one (opt_gqa_rotary_frequencies). */
+#define OPT_GQA_ROTARY_NONE 0
+#define OPT_GQA_ROTARY_LINEAR 1
+#define OPT_GQA_ROTARY_NTK 2
+#define OPT_GQA_ROTARY_PARTS 3
+#define OPT_GQA_ROTARY_RAMP 4
+
 /* Size of the scratch array built into the library for opt_gqa_paged_attention_decode_no_alloc. */
 #define OPT_GQA_STATIC_SCRATCH_BYTES (8u << 20)
 
@@ -331,6 +342,63 @@ int opt_gqa_int4_prepack(void* packed, const uint32_t* qweight, const void* scal
 int opt_gqa_qkv_project_int4(void* q_out, void* k_out, void* v_out, void* k_cache, void* v_cache,
                              const int64_t* slot_mapping, const void* x, const void* packed, int T, int K, int Hq,
                              int Hkv, int D, int bs, int64_t num_blocks, int gs, void* stream);
+
+/*
+ * Rotary positions, for models that encode positions by rotating q and k instead of adding the ALiBi bias (the
+ * attention calls then get alibi_slopes = NULL).  The first R = rot_dim dims of every head are rotated in R/2 pairs,
+ *
+ *     (a, b) -> amplitude * (a cos t - b sin t,  b cos t + a sin t),    t = position * f_i  for pair i,
+ *
+ * the dims past R pass through.  layout says which elements are pair i (OPT_GQA_ROTARY_HALF / _INTERLEAVED).
+ *
+ * The frequencies are prepared once, on the host:
+ * opt_gqa_rotary_frequencies writes f_0 .. f_{R/2-1} (HOST, radians per position, 64 bits) for base^(-2i/R) and
+ *   NONE    as it is
+ *   LINEAR  f / factor
+ *   NTK     the base becomes base * factor^(R/(R-2))                                                  (R > 2)
+ *   PARTS   r = original_len f / 2pi turns over the original context, w = (r - low_turns) / (high_turns - low_turns)
+ *           held in [0, 1]:  f (w + (1 - w) / factor)
+ *   RAMP    with i(r) = R ln(original_len / (2pi r)) / (2 ln base), lo = max(floor i(high_turns), 0),
+ *           hi = min(ceil i(low_turns), R - 1), w = 1 - (i - lo) / (hi - lo) held in [0, 1]:  f (w + (1 - w) / factor);
+ *           the amplitude that goes with it, 0.1 ln(factor) + 1, is the caller's to pass
+ *   (arguments a scaling does not name are ignored; OPT_GQA_ERR_SHAPE for an odd R, base or factor <= 0, PARTS or RAMP
+ *   with original_len <= 0 or not 0 < low_turns < high_turns, RAMP with base <= 1, or a frequency that is not finite).
+ * opt_gqa_rotary_table turns n frequencies -- these or the caller's own -- into the table the kernels read (HOST to
+ *   HOST; copy it to the device): f / 2pi mod 1 in 64-bit fixed point.  position * table[i] mod 2^64 is then the angle
+ *   reduced to one turn without a rounding, at any position of either sign.
+ *
+ * opt_gqa_rotary: q -> q_out [T, Hq, D] and k -> k_out [T, Hkv, D] in one launch (Hkv = 0: q alone, k and k_out are
+ *   not read).  inverse != 0 turns the angles around (same amplitude): with gradients in the place of q and k this is
+ *   the gradient of the forward call.
+ * opt_gqa_rotary_append: the same forward rotation of q and k, with the rotated keys and the values stored to
+ *   slot_mapping [T] of the paged pool as in opt_gqa_cache_append (a negative slot, or one past the pool, stores
+ *   nothing; the slots of one call are distinct) and, when k_out is not NULL, the rotated keys to k_out [T, Hkv, D]
+ *   as well (for opt_gqa_prompt_attention).  Hq = 0: keys and values alone.
+ *
+ *   positions   [T] int32;  freq  [rot_dim/2] uint64 (DEVICE, from opt_gqa_rotary_table)
+ *               both are read before the wait for the preceding kernel, like block_tables (see the ordering contract)
+ *   *_stride    HOST values, elements from one token to the next, so that q, k and v may be slices of wider rows (the
+ *               fused projection's output); >= heads * D and a multiple of 16 bytes (OPT_GQA_ERR_SHAPE / _ALIGN).
+ *               k_out of the append form is contiguous, as is its q_out.
+ *   q_out may be q and k_out may be k (same stride): the rotation is then done in place.  Other overlaps are errors
+ *   that are not detected.
+ * dtype fp32 or bf16; D 64 or 128; rot_dim even, 2 .. D.  Angles, sines and products are fp32 or better, results are
+ * rounded once.  T = 0 returns OK without a launch.
+ */
+int opt_gqa_rotary_frequencies(double* freq_host, int rot_dim, double base, int scaling, double factor,
+                               double original_len, double low_turns, double high_turns);
+
+int opt_gqa_rotary_table(uint64_t* table_host, const double* freq_host, int n);
+
+int opt_gqa_rotary(void* q_out, const void* q, void* k_out, const void* k, const int32_t* positions,
+                   const uint64_t* freq, int rot_dim, int layout, float amplitude, int inverse, int T, int Hq, int Hkv,
+                   int D, int64_t q_out_stride, int64_t q_stride, int64_t k_out_stride, int64_t k_stride, int dtype,
+                   void* stream);
+
+int opt_gqa_rotary_append(void* q_out, const void* q, void* k_out, const void* k, const void* v, void* k_cache,
+                          void* v_cache, const int64_t* slot_mapping, const int32_t* positions, const uint64_t* freq,
+                          int rot_dim, int layout, float amplitude, int T, int Hq, int Hkv, int D, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, int bs, int64_t num_blocks, int dtype, void* stream);
 
 /*
  * One decode step of the attention layer, Algorithm 2 from "Store reshaped K, V

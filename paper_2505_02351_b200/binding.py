@@ -20,8 +20,12 @@ LIB_PATH = os.path.join(_PKG, "libopt_gqa.so")
 FP32, BF16 = 0, 1
 _DTYPE_CODE = {torch.float32: FP32, torch.bfloat16: BF16}
 
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+_ROTARY_SCALING = {"none": 0, "linear": 1, "ntk": 2, "parts": 3, "ramp": 4}
+
 _c = ctypes
 _vp, _i, _i64, _f, _sz = _c.c_void_p, _c.c_int, _c.c_int64, _c.c_float, _c.c_size_t
+_d = _c.c_double
 
 SIGNATURES = {
     "opt_gqa_int4_packed_bytes": (ctypes.c_size_t, [_i, _i, _i]),
@@ -47,6 +51,12 @@ SIGNATURES = {
     "opt_gqa_paged_attention_prefill_local": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i,
                                                    _i, _i, _i64, _i, _i, _vp]),
     "opt_gqa_prompt_attention": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _f, _i, _i, _i, _i, _i, _vp]),
+    "opt_gqa_rotary_frequencies": (_i, [_vp, _i, _d, _i, _d, _d, _d, _d]),
+    "opt_gqa_rotary_table": (_i, [_vp, _vp, _i]),
+    "opt_gqa_rotary": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _f, _i, _i, _i, _i, _i, _i64, _i64, _i64, _i64, _i,
+                            _vp]),
+    "opt_gqa_rotary_append": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _f, _i, _i, _i, _i, _i64,
+                                   _i64, _i64, _i, _i64, _i, _vp]),
     "opt_gqa_decode_step": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i, _i, _i, _i64,
                                  _i, _vp, _sz, _i, _i, _vp]),
     "opt_gqa_decode_step_host": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _f, _i, _i, _i, _i,
@@ -290,6 +300,98 @@ def qkv_project_int4(q_out, x, packed, Hq: int, Hkv: int, D: int, gs: int, k_out
     _check(load().opt_gqa_qkv_project_int4(
         _ptr(q_out), _ptr(k_out), _ptr(v_out), _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), _ptr(x),
         _ptr(packed), T, K, Hq, Hkv, D, bs, num_blocks, gs, _stream(stream)), "opt_gqa_qkv_project_int4")
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_len: float = 0.0, low_turns: float = 0.0, high_turns: float = 0.0) -> torch.Tensor:
+    """Radians per position of the rot_dim / 2 pairs (host, float64); scaling "none", "linear", "ntk", "parts", "ramp"."""
+    f = torch.empty(max(rot_dim, 0) // 2, dtype=torch.float64)
+    _check(load().opt_gqa_rotary_frequencies(f.data_ptr() or None, rot_dim, base, _ROTARY_SCALING[scaling], factor,
+                                             original_len, low_turns, high_turns), "opt_gqa_rotary_frequencies")
+    return f
+
+
+def rotary_table(frequencies: torch.Tensor, device) -> torch.Tensor:
+    """The rotary calls' table of the given radians per position (host, float64) on `device`: int64 words that hold
+    unsigned 64-bit fractions of a turn."""
+    if frequencies.is_cuda or frequencies.dtype != torch.float64 or not frequencies.is_contiguous():
+        raise ValueError("expected a contiguous float64 host tensor")
+    table = torch.empty(frequencies.numel(), dtype=torch.int64)
+    _check(load().opt_gqa_rotary_table(table.data_ptr(), frequencies.data_ptr(), frequencies.numel()),
+           "opt_gqa_rotary_table")
+    return table.to(device)
+
+
+def _rows(t: Optional[torch.Tensor]):
+    """(address, elements from token to token) of a CUDA tensor [T, heads, D] whose heads lie side by side."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError("expected a CUDA tensor of the current device")
+    T, H, D = t.shape
+    st, sh, sd = t.stride()
+    if (D > 1 and sd != 1) or (H > 1 and sh != D):
+        raise ValueError("expected the heads of a token side by side")
+    return t.data_ptr(), st if T > 1 else H * D      # the stride of a single token says nothing
+
+
+def _same_rows(name: str, t: Optional[torch.Tensor], like: torch.Tensor) -> None:
+    if t is None or t.shape != like.shape or t.dtype != like.dtype:
+        raise ValueError(f"{name}: expected a tensor of shape {tuple(like.shape)} and dtype {like.dtype}")
+
+
+def _rotary_index(positions, freq, T: int) -> None:
+    if positions.dtype != torch.int32 or positions.numel() != T:
+        raise ValueError("positions: expected int32, one per token")
+    if freq.dtype != torch.int64:
+        raise ValueError("freq: expected the table made by rotary_table")
+
+
+def rotary(q_out, q, positions, freq, layout: int, k_out=None, k=None, amplitude: float = 1.0, inverse: bool = False,
+           stream=None) -> None:
+    """q_out = rotated q and, where k is given, k_out = rotated k; outputs may be their inputs.  freq: rotary_table."""
+    T, Hq, D = q.shape
+    _same_rows("q_out", q_out, q)
+    _rotary_index(positions, freq, T)
+    Hkv = 0
+    if k is not None:
+        Hkv = k.shape[1]
+        if k.shape[0] != T or k.shape[2] != D or k.dtype != q.dtype:
+            raise ValueError("k: expected as many tokens, dims and the dtype of q")
+        _same_rows("k_out", k_out, k)
+    (qp, qs), (qop, qos), (kp, ks), (kop, kos) = _rows(q), _rows(q_out), _rows(k), _rows(k_out)
+    _check(load().opt_gqa_rotary(
+        qop, qp, kop, kp, _ptr(positions), _ptr(freq), 2 * freq.numel(), layout, amplitude, int(inverse), T, Hq, Hkv, D,
+        qos, qs, kos, ks, _DTYPE_CODE[q.dtype], _stream(stream)), "opt_gqa_rotary")
+
+
+def rotary_append(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freq, layout: int, amplitude: float = 1.0,
+                  k_out=None, stream=None) -> None:
+    """q_out = rotated q; rotated k and v go to slot_mapping of the paged cache (and rotated k to k_out, if given).
+    q and q_out may both be None (keys and values alone); q, k, v may be slices of wider rows."""
+    T, Hkv, D = k.shape
+    num_blocks, _, bs, _ = k_cache.shape
+    if k_cache.shape != (num_blocks, Hkv, bs, D) or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
+        raise ValueError("expected k_cache and v_cache of one shape and dtype, with the heads and dims of k")
+    if k.dtype != k_cache.dtype:
+        raise ValueError("k: expected the dtype of the cache")
+    _same_rows("v", v, k)
+    _rotary_index(positions, freq, T)
+    if slot_mapping.dtype != torch.int64 or slot_mapping.numel() != T:
+        raise ValueError("slot_mapping: expected int64, one per token")
+    Hq = 0
+    if q is not None:
+        Hq = q.shape[1]
+        if q.shape[0] != T or q.shape[2] != D or q.dtype != k.dtype:
+            raise ValueError("q: expected as many tokens, dims and the dtype of k")
+        _same_rows("q_out", q_out, q)
+    if k_out is not None:
+        _same_rows("k_out", k_out, k)
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q), _rows(k), _rows(v)
+    _check(load().opt_gqa_rotary_append(
+        _ptr(q_out), qp, _ptr(k_out), kp, vp, _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), _ptr(positions),
+        _ptr(freq), 2 * freq.numel(), layout, amplitude, T, Hq, Hkv, D, qs, ks, vs, bs, num_blocks,
+        _DTYPE_CODE[k.dtype], _stream(stream)), "opt_gqa_rotary_append")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

@@ -287,6 +287,92 @@ int opt_gqa_prompt_attention(void* out, const void* q, const void* k, const void
                               status, static_cast<cudaStream_t>(stream));
 }
 
+int opt_gqa_rotary_frequencies(double* freq_host, int rot_dim, double base, int scaling, double factor,
+                               double original_len, double low_turns, double high_turns) {
+    if (!freq_host) return OPT_GQA_ERR_NULL;
+    if (rot_dim < 2 || rot_dim % 2 != 0 || !(base > 0.0)) return OPT_GQA_ERR_SHAPE;
+    if (scaling < OPT_GQA_ROTARY_NONE || scaling > OPT_GQA_ROTARY_RAMP) return OPT_GQA_ERR_SHAPE;
+    if (scaling != OPT_GQA_ROTARY_NONE && !(factor > 0.0)) return OPT_GQA_ERR_SHAPE;
+    if (scaling == OPT_GQA_ROTARY_NTK && rot_dim == 2) return OPT_GQA_ERR_SHAPE;
+    if (scaling == OPT_GQA_ROTARY_PARTS || scaling == OPT_GQA_ROTARY_RAMP) {
+        if (!(original_len > 0.0) || !(low_turns > 0.0) || !(high_turns > low_turns)) return OPT_GQA_ERR_SHAPE;
+        if (scaling == OPT_GQA_ROTARY_RAMP && !(base > 1.0)) return OPT_GQA_ERR_SHAPE;
+    }
+    return rotary_frequencies(freq_host, rot_dim, base, scaling, factor, original_len, low_turns, high_turns);
+}
+
+int opt_gqa_rotary_table(uint64_t* table_host, const double* freq_host, int n) {
+    if (n < 0) return OPT_GQA_ERR_SHAPE;
+    if (n == 0) return OPT_GQA_OK;
+    if (!table_host || !freq_host) return OPT_GQA_ERR_NULL;
+    for (int i = 0; i < n; ++i)
+        if (!(freq_host[i] - freq_host[i] == 0.0)) return OPT_GQA_ERR_SHAPE;      // not finite
+    for (int i = 0; i < n; ++i) table_host[i] = rotary_turns(freq_host[i]);
+    return OPT_GQA_OK;
+}
+
+// The checks the two rotary calls share, of what is present (heads > 0 wherever a tensor is read).
+static int rotary_checked(const RotaryArgs& a, void* stream) {
+    if (!dtype_ok(a.dtype)) return OPT_GQA_ERR_DTYPE;
+    if (a.T < 0 || a.Hq < 0 || a.Hkv < 0 || a.Hq > 65535 || a.Hkv > 65535 || (a.D != 64 && a.D != 128)) return OPT_GQA_ERR_SHAPE;
+    if (a.rot_dim < 2 || a.rot_dim > a.D || a.rot_dim % 2 != 0) return OPT_GQA_ERR_SHAPE;
+    if (a.layout != OPT_GQA_ROTARY_HALF && a.layout != OPT_GQA_ROTARY_INTERLEAVED) return OPT_GQA_ERR_SHAPE;
+    if (a.T == 0 || (a.Hq == 0 && a.Hkv == 0)) return OPT_GQA_OK;
+    if (!a.positions || !a.freq || (a.Hq > 0 && (!a.q || !a.q_out)) || (a.Hkv > 0 && (!a.k || (!a.k_out && !a.k_cache))))
+        return OPT_GQA_ERR_NULL;
+    const int64_t qw = (int64_t)a.Hq * a.D, kw = (int64_t)a.Hkv * a.D, vec = a.dtype == OPT_GQA_FP32 ? 4 : 8;
+    const int64_t most = INT64_MAX / 8 / (a.T > 0 ? a.T : 1);       // no offset in bytes passes 63 bits
+    auto stride_ok = [&](int64_t st, int64_t width) { return st >= width && st <= most; };
+    if (a.Hq > 0 && (!stride_ok(a.q_stride, qw) || !stride_ok(a.q_out_stride, qw))) return OPT_GQA_ERR_SHAPE;
+    if (a.Hkv > 0 && (!stride_ok(a.k_stride, kw) || (a.k_out && !stride_ok(a.k_out_stride, kw)) ||
+                      (a.v && !stride_ok(a.v_stride, kw))))
+        return OPT_GQA_ERR_SHAPE;
+    if (a.T > 1 && ((a.Hq > 0 && a.q_out == a.q && a.q_out_stride != a.q_stride) ||
+                    (a.Hkv > 0 && a.k_out == a.k && a.k_out_stride != a.k_stride)))
+        return OPT_GQA_ERR_SHAPE;                                   // in place means token by token in place
+    if (a.Hq > 0 && (!aligned16(a.q) || !aligned16(a.q_out) || a.q_stride % vec || a.q_out_stride % vec)) return OPT_GQA_ERR_ALIGN;
+    if (a.Hkv > 0 && (!aligned16(a.k) || !aligned16(a.k_out) || !aligned16(a.v) || !aligned16(a.k_cache) ||
+                      !aligned16(a.v_cache) || a.k_stride % vec || (a.k_out && a.k_out_stride % vec) ||
+                      (a.v && a.v_stride % vec)))
+        return OPT_GQA_ERR_ALIGN;
+    return launch_rotary(a, static_cast<cudaStream_t>(stream));
+}
+
+int opt_gqa_rotary(void* q_out, const void* q, void* k_out, const void* k, const int32_t* positions,
+                   const uint64_t* freq, int rot_dim, int layout, float amplitude, int inverse, int T, int Hq, int Hkv,
+                   int D, int64_t q_out_stride, int64_t q_stride, int64_t k_out_stride, int64_t k_stride, int dtype,
+                   void* stream) {
+    RotaryArgs a = {};
+    a.q = q, a.q_out = q_out, a.k = k, a.k_out = k_out;
+    a.positions = positions, a.freq = freq;
+    a.q_stride = q_stride, a.q_out_stride = q_out_stride, a.k_stride = k_stride, a.k_out_stride = k_out_stride;
+    a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.rot_dim = rot_dim, a.layout = layout;
+    a.amplitude = amplitude, a.inverse = inverse, a.dtype = dtype;
+    return rotary_checked(a, stream);
+}
+
+int opt_gqa_rotary_append(void* q_out, const void* q, void* k_out, const void* k, const void* v, void* k_cache,
+                          void* v_cache, const int64_t* slot_mapping, const int32_t* positions, const uint64_t* freq,
+                          int rot_dim, int layout, float amplitude, int T, int Hq, int Hkv, int D, int64_t q_stride,
+                          int64_t k_stride, int64_t v_stride, int bs, int64_t num_blocks, int dtype, void* stream) {
+    if (!dtype_ok(dtype)) return OPT_GQA_ERR_DTYPE;
+    if (T < 0 || Hkv <= 0 || Hq < 0 || (D != 64 && D != 128) || (bs != 16 && bs != 32) || num_blocks < 0 ||
+        num_blocks > INT64_MAX / 32)
+        return OPT_GQA_ERR_SHAPE;
+    RotaryArgs a = {};
+    a.q = q, a.q_out = q_out, a.k = k, a.k_out = k_out, a.v = v, a.k_cache = k_cache, a.v_cache = v_cache;
+    a.slots = slot_mapping, a.positions = positions, a.freq = freq;
+    a.q_stride = q_stride, a.q_out_stride = (int64_t)Hq * D, a.k_stride = k_stride, a.k_out_stride = (int64_t)Hkv * D;
+    a.v_stride = v_stride, a.num_blocks = num_blocks, a.bs = bs;
+    a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.D = D, a.rot_dim = rot_dim, a.layout = layout;
+    a.amplitude = amplitude, a.dtype = dtype;
+    if (T > 0) {
+        if (!v || !k_cache || !v_cache || !slot_mapping) return OPT_GQA_ERR_NULL;
+        if (num_blocks == 0) return OPT_GQA_ERR_SHAPE;
+    }
+    return rotary_checked(a, stream);
+}
+
 // Bytes of `workspace` a decode step of these sizes uses: the balanced split's layout for bf16 caches, one
 // (D + 1)-float row per (sequence, head, partition) for fp32 caches, nothing for a single pass.
 static size_t step_workspace_need(int B, int Hq, int Hkv, int D, int partition_size, int max_partitions, int dtype) {

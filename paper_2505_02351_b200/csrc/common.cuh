@@ -192,6 +192,23 @@ int launch_cache_append(const void* k_new, const void* v_new, void* k_cache, voi
                         const int64_t* slot_mapping, int T, int Hkv, int D, int bs, int dtype,
                         cudaStream_t stream);
 
+// Rotary positions, alone or with the slot-mapped write (rotary.cu).  v null: no values; k_cache null: no cache;
+// Hkv 0: q alone.  Strides in elements.
+struct RotaryArgs {
+    const void *q, *k, *v;
+    void *q_out, *k_out, *k_cache, *v_cache;
+    const int64_t* slots;
+    const int32_t* positions;
+    const uint64_t* freq;
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, num_blocks;
+    int T, Hq, Hkv, D, bs, rot_dim, layout, inverse, dtype;
+    float amplitude;
+};
+int launch_rotary(const RotaryArgs& a, cudaStream_t stream);
+int rotary_frequencies(double* f, int R, double base, int scaling, double factor, double original_len, double low_turns,
+                       double high_turns);
+uint64_t rotary_turns(double f);
+
 int launch_decode(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
                   int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale,
                   int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks, int partition_size, float* partial_out,

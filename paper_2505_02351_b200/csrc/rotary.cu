@@ -1,0 +1,283 @@
+// Rotary positions: the first R dims of every query and key head are rotated in pairs by angles that grow with the
+// token's position, y = amplitude * R(pos * f_i) x, and -- in the append form -- the rotated keys and the values are
+// written to their slots of the paged cache on the way (Algorithm 1, "Reshape and store K, V into C_K, C_V", for
+// models whose positions are rotary instead of ALiBi).
+//
+// Angles.  The caller hands over f_i as a fraction of a turn in 64-bit fixed point, F_i = f_i / 2pi * 2^64 mod 2^64,
+// so that pos * F_i mod 2^64 -- one wrapping integer product -- is the angle reduced to a turn, exactly, at any
+// position: no 64-bit floating point, no argument reduction, no table over positions.  Its upper 32 bits go through
+// one conversion (off by at most 2^-25 of half a turn, 9e-8 rad) and sincospi; cos, sin and the products are fp32,
+// the result is rounded once when stored.
+//
+// Bound by memory: every element is read once and written once, about one flop per byte.  A CTA takes kTokens tokens;
+// their cos/sin pairs are computed once into shared memory (before the wait for the preceding kernel) and used by all
+// heads: computed per head they would cost as much as the copy itself (30 instructions against 6 per pair).
+// A unit of work is P pairs of one row, two 16-byte vectors: vectors P u and R/2 + P u of the half layout, two
+// adjacent ones of the interleaved layout and of the dims past R, which pass through unchanged.  A thread requests
+// kBatch units before it uses the first, so 256 threads keep 32 KB in flight.  Where R is no multiple of two vectors,
+// a unit is one pair of elements (P = 1).
+#include <math.h>
+
+#include "common.cuh"
+
+namespace optgqa {
+
+namespace {
+
+constexpr int kRotThreads = 256;
+constexpr int kBatch = 4;              // units a thread has in flight
+
+struct RotaryParams {
+    const void* q;
+    const void* k;
+    const void* v;                     // null: no values (the rotation alone)
+    void* q_out;
+    void* k_out;                       // may be null when there is a cache
+    void* k_cache;                     // null: no cache
+    void* v_cache;
+    const int64_t* slots;
+    const int32_t* positions;
+    const uint64_t* freq;
+    long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;   // elements from token to token
+    long long num_slots;
+    int T, Hq, Hk, Hv, R, bs_log2;
+    float cos_amp, sin_amp;            // amplitude, and with the direction's sign
+};
+
+// P adjacent elements as fp32; 16 bytes at once unless P is 1.
+template <typename T, int P>
+struct Chunk {
+    uint4 raw;
+    __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = raw; }
+    __device__ __forceinline__ void get(float (&f)[P]) const {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2) {
+                const float2 v = bf16x2_to_float2(w[i]);
+                f[2 * i] = v.x;
+                f[2 * i + 1] = v.y;
+            } else {
+                f[i] = __uint_as_float(w[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[P]) {
+        if constexpr (sizeof(T) == 2)
+            raw = make_uint4(float2_to_bf16x2(f[0], f[1]), float2_to_bf16x2(f[2], f[3]), float2_to_bf16x2(f[4], f[5]),
+                             float2_to_bf16x2(f[6], f[7]));
+        else
+            raw = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+template <typename T>
+struct Chunk<T, 1> {
+    T raw;
+    __device__ __forceinline__ void load(const T* p) { raw = *p; }
+    __device__ __forceinline__ void store(T* p) const { *p = raw; }
+    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = static_cast<float>(raw); }
+    __device__ __forceinline__ void set(const float (&f)[1]) { raw = static_cast<T>(f[0]); }
+};
+
+template <typename T, int D, int P, bool kInterleaved, int kTokens>
+__global__ void __launch_bounds__(kRotThreads)
+rotary_kernel(const RotaryParams p) {
+    constexpr int U = D / (2 * P);                    // units per row
+    __shared__ __align__(16) float s_cos[kTokens][D / 2], s_sin[kTokens][D / 2];
+    grid_dependency_launch();
+    const long long t0 = (long long)blockIdx.x * kTokens;
+    const int tokens = (int)min((long long)kTokens, p.T - t0), half = p.R / 2;
+    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+        const int tok = i / half, pair = i - tok * half;
+        const uint64_t turn = (uint64_t)(int64_t)__ldg(p.positions + t0 + tok) * __ldg(p.freq + pair);
+        float s, c;
+        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);     // half turns, in [-1, 1]
+        s_cos[tok][pair] = c * p.cos_amp;
+        s_sin[tok][pair] = s * p.sin_amp;
+    }
+    __syncthreads();
+    grid_dependency_wait();     // q, k, v may come from the preceding kernel, which may also still read what is written here
+
+    const int H = p.Hq + p.Hk + p.Hv, units = tokens * H * U;
+    for (int base = threadIdx.x; base < units; base += kBatch * kRotThreads) {
+        Chunk<T, P> a[kBatch], b[kBatch];
+        // element offsets of a unit's two halves inside its row
+        auto offsets = [&](int u, int& e0, int& e1) {
+            const bool split = !kInterleaved && P * u < half;
+            e0 = split ? P * u : 2 * P * u;
+            e1 = split ? half + P * u : 2 * P * u + P;
+        };
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+            const int i = base + n * kRotThreads;
+            if (i < units) {
+                const int row = i / U, tok = row / H, h = row - tok * H;
+                const long long t = t0 + tok;
+                int e0, e1;
+                offsets(i % U, e0, e1);
+                const T* src = h < p.Hq             ? static_cast<const T*>(p.q) + t * p.q_stride + (long long)h * D
+                               : h < p.Hq + p.Hk    ? static_cast<const T*>(p.k) + t * p.k_stride + (long long)(h - p.Hq) * D
+                                                    : static_cast<const T*>(p.v) + t * p.v_stride + (long long)(h - p.Hq - p.Hk) * D;
+                a[n].load(src + e0);
+                b[n].load(src + e1);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kBatch; ++n) {
+            const int i = base + n * kRotThreads;
+            if (i < units) {
+                const int u = i % U, row = i / U, tok = row / H, h = row - tok * H;
+                const long long t = t0 + tok;
+                int e0, e1;
+                offsets(u, e0, e1);
+                if (h < p.Hq + p.Hk && P * u < half) {
+                    const float* cs = &s_cos[tok][P * u];
+                    const float* sn = &s_sin[tok][P * u];
+                    float x[P], y[P];
+                    a[n].get(x);
+                    b[n].get(y);
+                    if constexpr (kInterleaved && P > 1) {
+                        // the P pairs are (2i, 2i + 1) of the 2 P adjacent elements x, y
+#pragma unroll
+                        for (int e = 0; e < P / 2; ++e) {
+                            const float x0 = x[2 * e], x1 = x[2 * e + 1], y0 = y[2 * e], y1 = y[2 * e + 1];
+                            x[2 * e] = x0 * cs[e] - x1 * sn[e];
+                            x[2 * e + 1] = x1 * cs[e] + x0 * sn[e];
+                            y[2 * e] = y0 * cs[P / 2 + e] - y1 * sn[P / 2 + e];
+                            y[2 * e + 1] = y1 * cs[P / 2 + e] + y0 * sn[P / 2 + e];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            const float x0 = x[e], y0 = y[e];
+                            x[e] = x0 * cs[e] - y0 * sn[e];
+                            y[e] = y0 * cs[e] + x0 * sn[e];
+                        }
+                    }
+                    a[n].set(x);
+                    b[n].set(y);
+                }
+                if (h < p.Hq) {
+                    T* dst = static_cast<T*>(p.q_out) + t * p.q_out_stride + (long long)h * D;
+                    a[n].store(dst + e0);
+                    b[n].store(dst + e1);
+                    continue;
+                }
+                const bool is_v = h >= p.Hq + p.Hk;
+                const int kh = is_v ? h - p.Hq - p.Hk : h - p.Hq;
+                if (!is_v && p.k_out) {
+                    T* dst = static_cast<T*>(p.k_out) + t * p.k_out_stride + (long long)kh * D;
+                    a[n].store(dst + e0);
+                    b[n].store(dst + e1);
+                }
+                if (p.k_cache) {
+                    const long long slot = p.slots[t];
+                    if (slot >= 0 && slot < p.num_slots) {
+                        const long long page = slot >> p.bs_log2, off = slot & ((1 << p.bs_log2) - 1);
+                        T* dst = static_cast<T*>(is_v ? p.v_cache : p.k_cache) + (((page * p.Hk + kh) << p.bs_log2) + off) * D;
+                        a[n].store(dst + e0);
+                        b[n].store(dst + e1);
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int D, int P, bool kInterleaved>
+int launch_tokens(const RotaryParams& p, cudaStream_t stream) {
+    // Four tokens per CTA once that still gives every multiprocessor several CTAs; one below (a decode batch).
+    if (p.T >= 4096)
+        return launch_dependent(rotary_kernel<T, D, P, kInterleaved, 4>, dim3((unsigned)((p.T + 3ll) / 4)), dim3(kRotThreads), 0,
+                                stream, p);
+    return launch_dependent(rotary_kernel<T, D, P, kInterleaved, 1>, dim3((unsigned)p.T), dim3(kRotThreads), 0, stream, p);
+}
+
+template <typename T, int D>
+int launch_typed(const RotaryParams& p, int layout, cudaStream_t stream) {
+    constexpr int kVec = 16 / sizeof(T);
+    // whole vectors on both sides of every pair: R / 2 elements are whole 16-byte vectors
+    const bool wide = p.R % (2 * kVec) == 0;
+    if (layout == OPT_GQA_ROTARY_INTERLEAVED)
+        return wide ? launch_tokens<T, D, kVec, true>(p, stream) : launch_tokens<T, D, 1, true>(p, stream);
+    return wide ? launch_tokens<T, D, kVec, false>(p, stream) : launch_tokens<T, D, 1, false>(p, stream);
+}
+
+}  // namespace
+
+int launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
+    RotaryParams p;
+    p.q = a.q;
+    p.k = a.k;
+    p.v = a.v;
+    p.q_out = a.q_out;
+    p.k_out = a.k_out;
+    p.k_cache = a.k_cache;
+    p.v_cache = a.v_cache;
+    p.slots = a.slots;
+    p.positions = a.positions;
+    p.freq = a.freq;
+    p.q_stride = a.q_stride;
+    p.k_stride = a.k_stride;
+    p.v_stride = a.v_stride;
+    p.q_out_stride = a.q_out_stride;
+    p.k_out_stride = a.k_out_stride;
+    p.num_slots = a.num_blocks * a.bs;
+    p.T = a.T;
+    p.Hq = a.Hq;
+    p.Hk = a.Hkv;
+    p.Hv = a.v ? a.Hkv : 0;
+    p.R = a.rot_dim;
+    p.bs_log2 = a.bs == 32 ? 5 : 4;
+    p.cos_amp = a.amplitude;
+    p.sin_amp = a.inverse ? -a.amplitude : a.amplitude;
+    if (a.dtype == OPT_GQA_BF16)
+        return a.D == 128 ? launch_typed<__nv_bfloat16, 128>(p, a.layout, stream) : launch_typed<__nv_bfloat16, 64>(p, a.layout, stream);
+    return a.D == 128 ? launch_typed<float, 128>(p, a.layout, stream) : launch_typed<float, 64>(p, a.layout, stream);
+}
+
+// ----------------------------------------------------------------------------- host arithmetic
+// Radians per position of pair i, i < R / 2, in 64 bits.
+int rotary_frequencies(double* f, int R, double base, int scaling, double factor, double original_len, double low_turns,
+                       double high_turns) {
+    constexpr double kTwoPi = 6.283185307179586476925;
+    for (int i = 0; i < R / 2; ++i) {
+        const double plain = pow(base, -2.0 * i / R);
+        switch (scaling) {
+            case OPT_GQA_ROTARY_NONE: f[i] = plain; break;
+            case OPT_GQA_ROTARY_LINEAR: f[i] = plain / factor; break;
+            case OPT_GQA_ROTARY_NTK: f[i] = pow(base * pow(factor, (double)R / (R - 2)), -2.0 * i / R); break;
+            case OPT_GQA_ROTARY_PARTS: {
+                const double turns = original_len * plain / kTwoPi;
+                const double w = fmin(fmax((turns - low_turns) / (high_turns - low_turns), 0.0), 1.0);
+                f[i] = plain * (w + (1.0 - w) / factor);
+                break;
+            }
+            case OPT_GQA_ROTARY_RAMP: {
+                // the (real) pair index at which a dimension makes `turns` turns over the original context
+                const double lo_at = R * log(original_len / (kTwoPi * high_turns)) / (2.0 * log(base));
+                const double hi_at = R * log(original_len / (kTwoPi * low_turns)) / (2.0 * log(base));
+                const double lo = fmax(floor(lo_at), 0.0), hi = fmin(ceil(hi_at), R - 1.0);
+                const double w = 1.0 - fmin(fmax((i - lo) / fmax(hi - lo, 0.001), 0.0), 1.0);
+                f[i] = plain * (w + (1.0 - w) / factor);
+                break;
+            }
+            default: return OPT_GQA_ERR_SHAPE;
+        }
+        if (!isfinite(f[i])) return OPT_GQA_ERR_SHAPE;
+    }
+    return OPT_GQA_OK;
+}
+
+// f radians per position -> the fraction of a turn in 64-bit fixed point (whole turns per position drop out: positions
+// are whole numbers).
+uint64_t rotary_turns(double f) {
+    constexpr double kTwoPi = 6.283185307179586476925;
+    const double turns = f / kTwoPi, frac = turns - floor(turns);      // [0, 1]
+    const double hi = floor(ldexp(frac, 32));                          // two exact halves of the 64 bits
+    const double lo = floor(ldexp(ldexp(frac, 32) - hi, 32));
+    return ((uint64_t)hi << 32) + (uint64_t)lo;
+}
+
+}  // namespace optgqa
