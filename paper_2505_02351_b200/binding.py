@@ -106,8 +106,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# The current stream's handle without building a Stream object (0.3 us per call against 3.3).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    device = torch.cuda.current_device()
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _check(code: int, where: str) -> None:
@@ -322,76 +329,77 @@ def rotary_table(frequencies: torch.Tensor, device) -> torch.Tensor:
     return table.to(device)
 
 
-def _rows(t: Optional[torch.Tensor]):
+def _rows(name: str, t: torch.Tensor, shape, dtype, device: int):
     """(address, elements from token to token) of a CUDA tensor [T, heads, D] whose heads lie side by side."""
-    if t is None:
-        return None, 0
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError("expected a CUDA tensor of the current device")
-    T, H, D = t.shape
+    if t is None or t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current CUDA device")
+    T, H, D = shape
     st, sh, sd = t.stride()
-    if (D > 1 and sd != 1) or (H > 1 and sh != D):
-        raise ValueError("expected the heads of a token side by side")
+    if sd != 1 or (sh != D and H > 1):
+        raise ValueError(f"{name}: expected the heads of a token side by side")
     return t.data_ptr(), st if T > 1 else H * D      # the stride of a single token says nothing
 
 
-def _same_rows(name: str, t: Optional[torch.Tensor], like: torch.Tensor) -> None:
-    if t is None or t.shape != like.shape or t.dtype != like.dtype:
-        raise ValueError(f"{name}: expected a tensor of shape {tuple(like.shape)} and dtype {like.dtype}")
+def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
+    if t.dtype != dtype or (n >= 0 and t.numel() != n) or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {'any number of' if n < 0 else n} contiguous {dtype} values on the current "
+                         "CUDA device")
+    return t.data_ptr()
 
 
-def _rotary_index(positions, freq, T: int) -> None:
-    if positions.dtype != torch.int32 or positions.numel() != T:
-        raise ValueError("positions: expected int32, one per token")
-    if freq.dtype != torch.int64:
-        raise ValueError("freq: expected the table made by rotary_table")
+def _current_device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    return torch.cuda.current_device()
 
 
 def rotary(q_out, q, positions, freq, layout: int, k_out=None, k=None, amplitude: float = 1.0, inverse: bool = False,
            stream=None) -> None:
     """q_out = rotated q and, where k is given, k_out = rotated k; outputs may be their inputs.  freq: rotary_table."""
-    T, Hq, D = q.shape
-    _same_rows("q_out", q_out, q)
-    _rotary_index(positions, freq, T)
-    Hkv = 0
+    shape, dtype, dev = q.shape, q.dtype, _current_device(q)
+    T, Hq, D = shape
+    qp, qs = _rows("q", q, shape, dtype, dev)
+    qop, qos = _rows("q_out", q_out, shape, dtype, dev)
+    Hkv, kp, ks, kop, kos = 0, None, 0, None, 0
     if k is not None:
         Hkv = k.shape[1]
-        if k.shape[0] != T or k.shape[2] != D or k.dtype != q.dtype:
-            raise ValueError("k: expected as many tokens, dims and the dtype of q")
-        _same_rows("k_out", k_out, k)
-    (qp, qs), (qop, qos), (kp, ks), (kop, kos) = _rows(q), _rows(q_out), _rows(k), _rows(k_out)
+        kp, ks = _rows("k", k, (T, Hkv, D), dtype, dev)
+        kop, kos = _rows("k_out", k_out, (T, Hkv, D), dtype, dev)
     _check(load().opt_gqa_rotary(
-        qop, qp, kop, kp, _ptr(positions), _ptr(freq), 2 * freq.numel(), layout, amplitude, int(inverse), T, Hq, Hkv, D,
-        qos, qs, kos, ks, _DTYPE_CODE[q.dtype], _stream(stream)), "opt_gqa_rotary")
+        qop, qp, kop, kp, _index("positions", positions, torch.int32, T, dev), _index("freq", freq, torch.int64, -1, dev),
+        2 * freq.numel(), layout, amplitude, inverse, T, Hq, Hkv, D, qos, qs, kos, ks, _DTYPE_CODE[dtype],
+        _stream(stream)), "opt_gqa_rotary")
 
 
 def rotary_append(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freq, layout: int, amplitude: float = 1.0,
                   k_out=None, stream=None) -> None:
     """q_out = rotated q; rotated k and v go to slot_mapping of the paged cache (and rotated k to k_out, if given).
     q and q_out may both be None (keys and values alone); q, k, v may be slices of wider rows."""
-    T, Hkv, D = k.shape
-    num_blocks, _, bs, _ = k_cache.shape
-    if k_cache.shape != (num_blocks, Hkv, bs, D) or v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype:
-        raise ValueError("expected k_cache and v_cache of one shape and dtype, with the heads and dims of k")
-    if k.dtype != k_cache.dtype:
-        raise ValueError("k: expected the dtype of the cache")
-    _same_rows("v", v, k)
-    _rotary_index(positions, freq, T)
-    if slot_mapping.dtype != torch.int64 or slot_mapping.numel() != T:
-        raise ValueError("slot_mapping: expected int64, one per token")
-    Hq = 0
+    shape, pool, dtype, dev = k.shape, k_cache.shape, k.dtype, _current_device(k)
+    T, Hkv, D = shape
+    num_blocks, _, bs, _ = pool
+    if pool != (num_blocks, Hkv, bs, D) or v_cache.shape != pool:
+        raise ValueError("expected k_cache and v_cache [blocks, heads of k, block size, dims of k]")
+    kcp = _index("k_cache", k_cache, dtype, -1, dev)
+    vcp = _index("v_cache", v_cache, dtype, -1, dev)
+    kp, ks = _rows("k", k, shape, dtype, dev)
+    vp, vs = _rows("v", v, shape, dtype, dev)
+    Hq, qp, qs, qop, kop = 0, None, 0, None, None
     if q is not None:
         Hq = q.shape[1]
-        if q.shape[0] != T or q.shape[2] != D or q.dtype != k.dtype:
-            raise ValueError("q: expected as many tokens, dims and the dtype of k")
-        _same_rows("q_out", q_out, q)
+        qp, qs = _rows("q", q, (T, Hq, D), dtype, dev)
+        qop, qos = _rows("q_out", q_out, (T, Hq, D), dtype, dev)
+        if qos != Hq * D:
+            raise ValueError("q_out: expected a contiguous tensor")
     if k_out is not None:
-        _same_rows("k_out", k_out, k)
-    (qp, qs), (kp, ks), (vp, vs) = _rows(q), _rows(k), _rows(v)
+        kop, kos = _rows("k_out", k_out, shape, dtype, dev)
+        if kos != Hkv * D:
+            raise ValueError("k_out: expected a contiguous tensor")
     _check(load().opt_gqa_rotary_append(
-        _ptr(q_out), qp, _ptr(k_out), kp, vp, _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), _ptr(positions),
-        _ptr(freq), 2 * freq.numel(), layout, amplitude, T, Hq, Hkv, D, qs, ks, vs, bs, num_blocks,
-        _DTYPE_CODE[k.dtype], _stream(stream)), "opt_gqa_rotary_append")
+        qop, qp, kop, kp, vp, kcp, vcp, _index("slot_mapping", slot_mapping, torch.int64, T, dev),
+        _index("positions", positions, torch.int32, T, dev), _index("freq", freq, torch.int64, -1, dev),
+        2 * freq.numel(), layout, amplitude, T, Hq, Hkv, D, qs, ks, vs, bs, num_blocks, _DTYPE_CODE[dtype],
+        _stream(stream)), "opt_gqa_rotary_append")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

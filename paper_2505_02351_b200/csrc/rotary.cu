@@ -14,7 +14,8 @@
 // heads: computed per head they would cost as much as the copy itself (30 instructions against 6 per pair).
 // A unit of work is P pairs of one row, two 16-byte vectors: vectors P u and R/2 + P u of the half layout, two
 // adjacent ones of the interleaved layout and of the dims past R, which pass through unchanged.  A thread requests
-// kBatch units before it uses the first, so 256 threads keep 32 KB in flight.  Where R is no multiple of two vectors,
+// kBatch units before it uses the first; registers are held to five CTAs per multiprocessor (80 KB in flight; four
+// units per thread at two CTAs took 40 us where this takes 29).  Where R is no multiple of two vectors,
 // a unit is one pair of elements (P = 1).
 #include <math.h>
 
@@ -25,7 +26,7 @@ namespace optgqa {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kBatch = 4;              // units a thread has in flight
+constexpr int kRotCtas = 5;            // resident CTAs per multiprocessor the registers are held to
 
 struct RotaryParams {
     const void* q;
@@ -80,8 +81,8 @@ struct Chunk<T, 1> {
     __device__ __forceinline__ void set(const float (&f)[1]) { raw = static_cast<T>(f[0]); }
 };
 
-template <typename T, int D, int P, bool kInterleaved, int kTokens>
-__global__ void __launch_bounds__(kRotThreads)
+template <typename T, int D, int P, bool kInterleaved, int kTokens, int kBatch>
+__global__ void __launch_bounds__(kRotThreads, kRotCtas)
 rotary_kernel(const RotaryParams p) {
     constexpr int U = D / (2 * P);                    // units per row
     __shared__ __align__(16) float s_cos[kTokens][D / 2], s_sin[kTokens][D / 2];
@@ -100,7 +101,8 @@ rotary_kernel(const RotaryParams p) {
     grid_dependency_wait();     // q, k, v may come from the preceding kernel, which may also still read what is written here
 
     const int H = p.Hq + p.Hk + p.Hv, units = tokens * H * U;
-    for (int base = threadIdx.x; base < units; base += kBatch * kRotThreads) {
+    const int step = kRotThreads * gridDim.y;         // the CTAs of one token in y take its units in turns
+    for (int base = threadIdx.x + kRotThreads * blockIdx.y; base < units; base += kBatch * step) {
         Chunk<T, P> a[kBatch], b[kBatch];
         // element offsets of a unit's two halves inside its row
         auto offsets = [&](int u, int& e0, int& e1) {
@@ -110,7 +112,7 @@ rotary_kernel(const RotaryParams p) {
         };
 #pragma unroll
         for (int n = 0; n < kBatch; ++n) {
-            const int i = base + n * kRotThreads;
+            const int i = base + n * step;
             if (i < units) {
                 const int row = i / U, tok = row / H, h = row - tok * H;
                 const long long t = t0 + tok;
@@ -125,7 +127,7 @@ rotary_kernel(const RotaryParams p) {
         }
 #pragma unroll
         for (int n = 0; n < kBatch; ++n) {
-            const int i = base + n * kRotThreads;
+            const int i = base + n * step;
             if (i < units) {
                 const int u = i % U, row = i / U, tok = row / H, h = row - tok * H;
                 const long long t = t0 + tok;
@@ -187,11 +189,21 @@ rotary_kernel(const RotaryParams p) {
 
 template <typename T, int D, int P, bool kInterleaved>
 int launch_tokens(const RotaryParams& p, cudaStream_t stream) {
-    // Four tokens per CTA once that still gives every multiprocessor several CTAs; one below (a decode batch).
-    if (p.T >= 4096)
-        return launch_dependent(rotary_kernel<T, D, P, kInterleaved, 4>, dim3((unsigned)((p.T + 3ll) / 4)), dim3(kRotThreads), 0,
-                                stream, p);
-    return launch_dependent(rotary_kernel<T, D, P, kInterleaved, 1>, dim3((unsigned)p.T), dim3(kRotThreads), 0, stream, p);
+    constexpr int U = D / (2 * P);
+    const int units = (p.Hq + p.Hk + p.Hv) * U;
+    auto launch = [&](auto kernel, long long x, int y) {
+        return launch_dependent(kernel, dim3((unsigned)x, (unsigned)y), dim3(kRotThreads), 0, stream, p);
+    };
+    // Few tokens (a decode batch): latency counts, every thread takes one unit and a token as many CTAs as that needs
+    // (256 tokens of 80 heads, bf16: 3.2 us against 3.8 with two units per thread).
+    if (p.T <= 512)
+        return launch(rotary_kernel<T, D, P, kInterleaved, 1, 1>, p.T, (units + kRotThreads - 1) / kRotThreads);
+    // Many tokens whose rows do not fill a CTA's two units per thread: four per CTA (8192 tokens of 40 heads, bf16: 28.7
+    // us against 40 with one); but not where one token fills it (4095 tokens of 72 heads, fp32: 47 us against 63 with four),
+    // nor where the grid would end up below a few CTAs per multiprocessor (1999 tokens of 24 heads: 5.6 against 6.4).
+    if (p.T >= 4096 && units <= 2 * kRotThreads)
+        return launch(rotary_kernel<T, D, P, kInterleaved, 4, 2>, (p.T + 3ll) / 4, 1);
+    return launch(rotary_kernel<T, D, P, kInterleaved, 1, 2>, p.T, 1);
 }
 
 template <typename T, int D>
