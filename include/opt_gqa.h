@@ -226,6 +226,37 @@ int opt_gqa_paged_attention_decode_no_alloc(void* out, const void* q, const void
                                             int partition_size, int max_partitions, int dtype, void* stream);
 
 /*
+ * Decode attention for a batch in which sequences share long prefixes -- many questions about one document, many samples
+ * of one prompt -- computed once per prefix for all sequences that share it (no counterpart in the paper; the result is
+ * that of opt_gqa_paged_attention_decode).  The batch is described as for the other decode calls, plus
+ *
+ *   group_start  [num_groups + 1] int32  increasing; group g is the sequences group_start[g] .. group_start[g+1] - 1.
+ *                Sequences before group_start[0] or from group_start[num_groups] on belong to no group (padding rows of a
+ *                captured batch, say) and share nothing.
+ *   prefix_lens  [B] int32  sequence s has its first prefix_lens[s] tokens in common with its group: wherever two
+ *                sequences of a group both have a position below their prefix_lens, their block tables name the same
+ *                page for it.  Values may differ inside a group (0: this one shares nothing), may exceed context_lens[s]
+ *                and need not be multiples of a page; the shared pass takes whole tiles of 64 tokens,
+ *                e_s = floor(min(prefix_lens[s], context_lens[s]) / 64) * 64, and only those have to agree.
+ *                prefix_lens of a sequence of no group is not looked at.
+ *   num_groups   1 .. 512 (a group of one sequence gains nothing: leave it out of the groups)
+ *   alibi_slopes, scale, partition_size, max_partitions  as in opt_gqa_paged_attention_decode_balanced
+ *   workspace    opt_gqa_shared_workspace_bytes(...) bytes (host arithmetic; 0 for bad arguments), 16-byte aligned; contents
+ *                need no initialisation.  Calls that can overlap on the GPU need a workspace each.
+ * group_start and prefix_lens are read before the wait for the preceding kernel, like block_tables.
+ * context_lens[s] == 0 gives a zero row.  bf16 only.  What a sequence does not see never reaches its row, whatever it holds.
+ */
+int opt_gqa_paged_attention_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache,
+                                          const int32_t* block_tables, int max_blocks_per_seq,
+                                          const int32_t* context_lens, const int32_t* group_start,
+                                          const int32_t* prefix_lens, int num_groups, const float* alibi_slopes,
+                                          float scale, int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks,
+                                          int partition_size, void* workspace, size_t workspace_bytes,
+                                          int max_partitions, int dtype, void* stream);
+
+size_t opt_gqa_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions);
+
+/*
  * Multi-token (chunked-prefill) variant on tensor cores: the prompt branch of
  * Algorithms 1 and 2 run over the paged cache with a causal mask plus the ALiBi
  * bias ("Create ALiBi bias"; Eq. 3-5).  Sequence s contributes

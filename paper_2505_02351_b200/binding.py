@@ -51,6 +51,9 @@ SIGNATURES = {
     "opt_gqa_paged_attention_prefill_local": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i,
                                                    _i, _i, _i64, _i, _i, _vp]),
     "opt_gqa_prompt_attention": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _f, _i, _i, _i, _i, _i, _vp]),
+    "opt_gqa_paged_attention_decode_shared": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _f, _i, _i, _i, _i,
+                                                   _i, _i64, _i, _vp, _sz, _i, _i, _vp]),
+    "opt_gqa_shared_workspace_bytes": (_c.c_size_t, [_i, _i, _i, _i, _i, _i]),
     "opt_gqa_rotary_frequencies": (_i, [_vp, _i, _d, _i, _d, _d, _d, _d]),
     "opt_gqa_rotary_table": (_i, [_vp, _vp, _i]),
     "opt_gqa_rotary": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _f, _i, _i, _i, _i, _i, _i64, _i64, _i64, _i64, _i,
@@ -400,6 +403,32 @@ def rotary_append(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, fre
         _index("positions", positions, torch.int32, T, dev), _index("freq", freq, torch.int64, -1, dev),
         2 * freq.numel(), layout, amplitude, T, Hq, Hkv, D, qs, ks, vs, bs, num_blocks, _DTYPE_CODE[dtype],
         _stream(stream)), "opt_gqa_rotary_append")
+
+
+def shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, num_groups: int, max_partitions: int) -> int:
+    return int(load().opt_gqa_shared_workspace_bytes(B, Hq, Hkv, D, num_groups, max_partitions))
+
+
+def paged_attention_decode_shared(out, q, k_cache, v_cache, block_tables, context_lens, group_start, prefix_lens,
+                                  alibi_slopes, scale: float, partition_size: int, workspace, max_partitions: int,
+                                  stream=None) -> None:
+    """Decode of a batch whose groups of sequences share prefixes, each prefix read once for its group."""
+    shape, pool, dtype, dev = q.shape, k_cache.shape, q.dtype, _current_device(q)
+    B, Hq, D = shape
+    num_blocks, Hkv, bs, _ = pool
+    num_groups = group_start.numel() - 1
+    if out.shape != shape or pool != (num_blocks, Hkv, bs, D) or v_cache.shape != pool:
+        raise ValueError("expected out like q and k_cache, v_cache [blocks, heads, block size, dims of q]")
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError("block_tables: expected a row per sequence")
+    _check(load().opt_gqa_paged_attention_decode_shared(
+        _index("out", out, dtype, -1, dev), _index("q", q, dtype, -1, dev), _index("k_cache", k_cache, dtype, -1, dev),
+        _index("v_cache", v_cache, dtype, -1, dev), _index("block_tables", block_tables, torch.int32, -1, dev),
+        block_tables.shape[1], _index("context_lens", context_lens, torch.int32, B, dev),
+        _index("group_start", group_start, torch.int32, -1, dev), _index("prefix_lens", prefix_lens, torch.int32, B, dev),
+        num_groups, None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale,
+        B, Hq, Hkv, D, bs, num_blocks, partition_size, _ptr(workspace), _nbytes(workspace), max_partitions,
+        _DTYPE_CODE[dtype], _stream(stream)), "opt_gqa_paged_attention_decode_shared")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

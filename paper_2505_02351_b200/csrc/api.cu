@@ -215,6 +215,40 @@ int opt_gqa_paged_attention_decode_local(void* out, const void* q, const void* k
                                    max_partitions, window, dtype, stream);
 }
 
+size_t opt_gqa_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
+    if (B <= 0 || B > 65535 || !shape_ok(Hq, Hkv, D, 16) || Hkv > 65535 || num_groups <= 0 || num_groups > kMaxGroups ||
+        max_partitions <= 0 || max_partitions > 65535)
+        return 0;
+    return shared_layout(B, Hq, Hkv, D, num_groups, max_partitions).total;
+}
+
+int opt_gqa_paged_attention_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache,
+                                          const int32_t* block_tables, int max_blocks_per_seq,
+                                          const int32_t* context_lens, const int32_t* group_start,
+                                          const int32_t* prefix_lens, int num_groups, const float* alibi_slopes,
+                                          float scale, int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks,
+                                          int partition_size, void* workspace, size_t workspace_bytes,
+                                          int max_partitions, int dtype, void* stream) {
+    if (dtype != OPT_GQA_BF16) return OPT_GQA_ERR_DTYPE;
+    if (B < 0 || !shape_ok(Hq, Hkv, D, bs) || max_blocks_per_seq < 0 || num_blocks < 0 || partition_size <= 0 ||
+        partition_size % 16 != 0 || max_partitions <= 0 || num_groups < 0)
+        return OPT_GQA_ERR_SHAPE;
+    if (B > 65535 || Hkv > 65535 || max_partitions > 65535 || num_groups > kMaxGroups) return OPT_GQA_ERR_SHAPE;
+    if (B == 0) return OPT_GQA_OK;
+    if (!out || !q || !k_cache || !v_cache || !block_tables || !context_lens || !group_start || !prefix_lens || !workspace)
+        return OPT_GQA_ERR_NULL;
+    if (num_blocks == 0 || max_blocks_per_seq == 0 || num_groups == 0) return OPT_GQA_ERR_SHAPE;
+    if (workspace_bytes < shared_layout(B, Hq, Hkv, D, num_groups, max_partitions).total) return OPT_GQA_ERR_SHAPE;
+    if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace))
+        return OPT_GQA_ERR_ALIGN;
+    int* status = device_status_ptr();
+    if (!status) return OPT_GQA_ERR_CUDA;
+    const SharedPrefix shared = {group_start, prefix_lens, num_groups};
+    return launch_decode_shared(out, q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, shared,
+                                alibi_slopes, scale, B, Hq, Hkv, D, bs, num_blocks, partition_size, workspace,
+                                max_partitions, status, static_cast<cudaStream_t>(stream));
+}
+
 static int prefill_checked(bool allow_umma, int window, void* out, const void* q, const int32_t* q_start_loc, int total_q_tokens,
                            int max_q_len, const void* k_cache, const void* v_cache, const int32_t* block_tables,
                            int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes,

@@ -256,13 +256,58 @@ int launch_decode_tc(void* out, const void* q, const void* k_cache, const void* 
                      float* partial_out, float* partial_lse, int max_partitions, int* device_status,
                      cudaStream_t stream, const FusedAppend* append = nullptr);
 
+// A batch whose sequences share prefixes: group g is the sequences group_start[g] .. group_start[g + 1] - 1, and
+// sequence s has its first prefix_lens[s] tokens in common with its group.  The group pass works on whole tiles of
+// kSharedTile keys; what is left of the prefix behind them belongs to the sequences' own pass.
+struct SharedPrefix {
+    const int32_t* group_start;     // [num_groups + 1]
+    const int32_t* prefix_lens;     // [B]
+    int num_groups;
+};
+constexpr int kSharedTile = 64;
+constexpr int kMaxGroups = 512;
+// Tokens of a sequence of length n that the group pass attends to.
+__device__ __forceinline__ int shared_tokens(int prefix, int n) { return max(min(prefix, n), 0) & ~(kSharedTile - 1); }
+
+// Workspace of the shared-prefix decode: the own pass's balanced layout, then per group {items, tiles of one head before
+// it} and {tiles, row blocks}, and the group pass's pieces.  An item is (group, KV head, block of 128 rows), a row being
+// (sequence, head of the KV head's group); the tiles of the items laid end to end are cut into one range per worker, and
+// the piece of item i inside worker w's range owns rows (i + w) * 128 .. + 127.
+constexpr int kSharedRows = 128;
+constexpr int kSharedMaxWorkers = 296;
+struct SharedLayout {
+    BalancedLayout own;
+    size_t header, groups, lse, out, total;
+    unsigned long long rows;
+};
+inline SharedLayout shared_layout(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
+    SharedLayout L;
+    L.own = balanced_layout(B, Hq, Hkv, D, max_partitions);
+    const unsigned long long G = (unsigned long long)(Hq / Hkv);
+    const unsigned long long items = (unsigned long long)Hkv * ((unsigned long long)num_groups + (unsigned long long)B * G / kSharedRows);
+    L.rows = (items + kSharedMaxWorkers) * kSharedRows;
+    L.header = round_up_256(L.own.total);
+    L.groups = L.header + 256;
+    L.lse = L.groups + round_up_256((size_t)num_groups * 32);
+    L.out = L.lse + round_up_256((size_t)L.rows * 4);
+    L.total = L.out + (size_t)L.rows * D * 4;
+    return L;
+}
+
+// Pieces and merge of the group pass (decode_shared.cu); the own pass is launch_decode_stream with the same SharedPrefix.
+int launch_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                         int max_blocks_per_seq, const int32_t* context_lens, const SharedPrefix& shared,
+                         const float* alibi_slopes, float scale, int B, int Hq, int Hkv, int D, int bs,
+                         int64_t num_blocks, int partition_size, void* workspace, int max_partitions,
+                         int* device_status, cudaStream_t stream);
+
 // bf16, partition_size > 0, balanced split into `workspace`: persistent streaming kernel, one worker per warp
 // (decode_stream.cu).  append != nullptr: see FusedAppend.
 int launch_decode_stream(const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
                          int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale,
                          int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks, int partition_size,
                          void* workspace, int max_partitions, int window, int* device_status, cudaStream_t stream,
-                         const FusedAppend* append = nullptr);
+                         const FusedAppend* append = nullptr, const SharedPrefix* shared = nullptr);
 
 // Workers (warps) of the grid that launch_decode_stream uses for the balanced split of these sizes on the current
 // device; 0 if the device cannot be queried.
