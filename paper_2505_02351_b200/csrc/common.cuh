@@ -176,13 +176,18 @@ constexpr int kMaxDevices = 64;
 
 // Raises the dynamic shared memory limit of `kernel` once per device.  `done` is the launcher's own
 // `static std::atomic<bool> [kMaxDevices]`.
+// `whole_sm`: ask for the largest shared memory of a multiprocessor, not the least that holds this kernel's CTAs, so that
+// another kernel's CTAs find room beside them.
 template <typename Kernel>
-inline bool ensure_smem_limit(Kernel kernel, int bytes, std::atomic<bool>* done) {
+inline bool ensure_smem_limit(Kernel kernel, int bytes, std::atomic<bool>* done, bool whole_sm = false) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
     const bool cached = dev >= 0 && dev < kMaxDevices;
     if (cached && done[dev].load(std::memory_order_acquire)) return true;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    if (whole_sm && cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                         cudaSharedmemCarveoutMaxShared) != cudaSuccess)
+        return false;
     if (cached) done[dev].store(true, std::memory_order_release);
     return true;
 }
@@ -263,21 +268,25 @@ struct SharedPrefix {
     const int32_t* group_start;     // [num_groups + 1]
     const int32_t* prefix_lens;     // [B]
     int num_groups;
+    int32_t* info = nullptr;        // [B * Hkv][kInfoWords], see SharedLayout
 };
 constexpr int kSharedTile = 64;
 constexpr int kMaxGroups = 512;
 // Tokens of a sequence of length n that the group pass attends to.
 __device__ __forceinline__ int shared_tokens(int prefix, int n) { return max(min(prefix, n), 0) & ~(kSharedTile - 1); }
 
-// Workspace of the shared-prefix decode: the own pass's balanced layout, then per group {items, tiles of one head before
-// it} and {tiles, row blocks}, and the group pass's pieces.  An item is (group, KV head, block of 128 rows), a row being
-// (sequence, head of the KV head's group); the tiles of the items laid end to end are cut into one range per worker, and
-// the piece of item i inside worker w's range owns rows (i + w) * 128 .. + 127.
+// Workspace of the shared-prefix decode: the own pass's balanced layout, then the bookkeeping the two passes leave for the
+// merge and the group pass's pieces.  An item is (group, KV head, block of 128 rows), a row being (sequence, head of the KV
+// head's group); the tiles of the items laid end to end are cut into one range per worker, and the part of item i inside
+// worker w's range is piece i + w: its log-sum-exps are partial_lse[piece][128], its rows partial_out[piece][D][128].
+// info, per (sequence, KV head): {first piece, row of the group's first head, last piece, -, first and last piece row / G of
+// the own pass, -, -}; a pass writes its words for the streams it has keys for.
 constexpr int kSharedRows = 128;
-constexpr int kSharedMaxWorkers = 296;
+constexpr int kSharedMaxWorkers = 148;
+constexpr int kInfoWords = 8;
 struct SharedLayout {
     BalancedLayout own;
-    size_t header, groups, lse, out, total;
+    size_t info, lse, out, total;
     unsigned long long rows;
 };
 inline SharedLayout shared_layout(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
@@ -286,9 +295,8 @@ inline SharedLayout shared_layout(int B, int Hq, int Hkv, int D, int num_groups,
     const unsigned long long G = (unsigned long long)(Hq / Hkv);
     const unsigned long long items = (unsigned long long)Hkv * ((unsigned long long)num_groups + (unsigned long long)B * G / kSharedRows);
     L.rows = (items + kSharedMaxWorkers) * kSharedRows;
-    L.header = round_up_256(L.own.total);
-    L.groups = L.header + 256;
-    L.lse = L.groups + round_up_256((size_t)num_groups * 32);
+    L.info = round_up_256(L.own.total);
+    L.lse = L.info + round_up_256((size_t)B * Hkv * kInfoWords * 4);
     L.out = L.lse + round_up_256((size_t)L.rows * 4);
     L.total = L.out + (size_t)L.rows * D * 4;
     return L;

@@ -20,10 +20,10 @@
 // the last one backwards) a row that has not begun simply discards what it accumulated: its O is set to zero, not
 // multiplied by zero, at its first tile, and nothing it does not see can reach it, not even a NaN.
 //
-// Six warps as in the prefill kernel: 0-3 one thread per row (softmax), 4 the TMA producer, 5 issues the tensor-core work.
-// All of them walk the same list of pieces.  Every wait is a bounded mbarrier wait.
-#include <type_traits>
-
+// Eight warps: 0-3 one thread per row (softmax), 4 and 6 the TMA producers of Q, K and of V, 5 and 7 issue S = Q K^T and
+// O += P V.  All of them walk the same list of pieces.  Every wait is a bounded mbarrier wait.  (A single producer was what
+// the pass waited for: a copy of 16 rows costs its warp about 90 cycles, 16 of them a tile; and a single issuing thread
+// adds the waits for K, V and P up, 1690 cycles a tile against 1100 of softmax.)
 #include "umma.cuh"
 
 namespace optgqa {
@@ -32,10 +32,10 @@ namespace {
 
 constexpr int kRows = kSharedRows;
 constexpr int kTN = kSharedTile;
-constexpr int kSub = 16;                   // token rows per TMA box
-constexpr int kKvStages = 2;
-constexpr int kCtasPerSm = 2;
-constexpr int kThreads = 192;
+constexpr int kKStages = 3;
+constexpr int kVStages = 2;
+constexpr int kThreads = 256;
+constexpr int kMaxRegs = 160;              // two of these warps and one of the own pass's (184) share a scheduler's 512
 constexpr int kMinTiles = 2;               // tiles a worker gets at least
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
@@ -48,7 +48,7 @@ constexpr int kExtRowGroupBytes = 256;
 constexpr int kQxBytes = kRows / 8 * kExtRowGroupBytes;
 constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
 // barriers: q_full, q_empty, qx_full, o_empty, k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2]
-constexpr int kNumBars = 4 + 4 * kKvStages + 4;
+constexpr int kNumBars = 4 + 2 * kKStages + 2 * kVStages + 4;
 
 template <int D>
 struct ShLayout {
@@ -57,8 +57,8 @@ struct ShLayout {
     static constexpr int kQBytes = kHalves * kQHalfBytes;
     static constexpr int kOffQ = 0;
     static constexpr int kOffK = kQBytes;
-    static constexpr int kOffV = kOffK + kKvStages * kTileBytes;
-    static constexpr int kOffQx = kOffV + kKvStages * kTileBytes;
+    static constexpr int kOffV = kOffK + kKStages * kTileBytes;
+    static constexpr int kOffQx = kOffV + kVStages * kTileBytes;
     static constexpr int kOffKp = kOffQx + kQxBytes;
     static constexpr int kOffBar = kOffKp + kKpBytes;
     static constexpr int kOffGroups = kOffBar + kNumBars * 8 + 16;      // tiles before (8 B), tiles, leader, items before (2 B)
@@ -77,8 +77,7 @@ struct SharedParams {
     const float* slopes;
     float* partial_out;
     float* partial_lse;
-    long long* header;          // {tiles of all items, workers}
-    long long* groups;          // per group {tiles of one head before it, items of one head before it, tiles, row blocks}
+    int32_t* info;              // per (sequence, KV head): see SharedLayout
     int* status;
     float scale;
     int num_groups, B, max_blocks, Hq, Hkv, bs, lanes_log2;
@@ -93,7 +92,7 @@ struct PieceCursor {
 };
 
 template <int D, int G>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+__global__ void __maxnreg__(kMaxRegs)
 decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const SharedParams p) {
     using L = ShLayout<D>;
@@ -108,10 +107,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* qx_full = bars + 2;
     uint64_t* o_empty = bars + 3;
     uint64_t* k_full = bars + 4;
-    uint64_t* k_empty = k_full + kKvStages;
-    uint64_t* v_full = k_empty + kKvStages;
-    uint64_t* v_empty = v_full + kKvStages;
-    uint64_t* s_full = v_empty + kKvStages;
+    uint64_t* k_empty = k_full + kKStages;
+    uint64_t* v_full = k_empty + kKStages;
+    uint64_t* v_empty = v_full + kVStages;
+    uint64_t* s_full = v_empty + kVStages;
     uint64_t* p_full = s_full + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
     long long* g_tiles = reinterpret_cast<long long*>(smem + L::kOffGroups);     // exclusive sums over the groups, one head
@@ -119,17 +118,22 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     int* g_lead = g_kt + kMaxGroups;
     uint16_t* g_items = reinterpret_cast<uint16_t*>(g_lead + kMaxGroups);        // at most kMaxGroups + 65535 * 8 / 128
 
-    grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int N = p.num_groups;
+    if (threadIdx.x == 128) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
     auto group_lo = [&](int g) { return min(max(__ldg(p.group_start + g), 0), p.B); };
     auto blocks_of = [&](int g) { return max(group_lo(g + 1) - group_lo(g), 0) * G / kRows +
                                          (max(group_lo(g + 1) - group_lo(g), 0) * G % kRows != 0); };
 
     // ------------------------------------------------------------------ the groups: longest shared run, whose it is
-    {
+    // (the index arrays are read before the wait for the preceding kernel: see the ordering contract in the header)
+    if (warp < 4) {
         const int lanes = 1 << p.lanes_log2, sub = lane & (lanes - 1), per_warp = 32 >> p.lanes_log2;
-        for (int g0 = warp * per_warp; g0 < N; g0 += kThreads / 32 * per_warp) {
+        for (int g0 = warp * per_warp; g0 < N; g0 += 4 * per_warp) {
             const int g = g0 + (lane >> p.lanes_log2);
             int best = 0, lead = 0;
             if (g < N) {
@@ -149,15 +153,18 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
         }
     }
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 128) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
         mbar_init(qx_full, kRows);
         mbar_init(o_empty, kRows);
 #pragma unroll
-        for (int i = 0; i < kKvStages; ++i) {
+        for (int i = 0; i < kKStages; ++i) {
             mbar_init(&k_full[i], 1);
             mbar_init(&k_empty[i], 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kVStages; ++i) {
             mbar_init(&v_full[i], 1);
             mbar_init(&v_empty[i], 1);
         }
@@ -228,19 +235,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const long long total = s_total, me = blockIdx.x;
     const long long by_size = total / kMinTiles > 0 ? total / kMinTiles : (total > 0 ? 1 : 0);
     const long long workers = by_size < gridDim.x ? by_size : gridDim.x;
-    grid_dependency_wait();     // the cache and q may still be written, the workspace still read, by the preceding kernel
-    if (me == 0) {
-        if (threadIdx.x == 0) {
-            p.header[0] = total;
-            p.header[1] = workers;
-        }
-        for (int g = threadIdx.x; g < N; g += kThreads) {
-            p.groups[4 * g] = g_tiles[g];
-            p.groups[4 * g + 1] = g_items[g];
-            p.groups[4 * g + 2] = g_kt[g];
-            p.groups[4 * g + 3] = blocks_of(g);
-        }
-    }
+    // The cache and q may still be written, the workspace still read, by the preceding kernel: the producer waits for it
+    // before its first copy, and everything this CTA writes follows from that copy.  The kernel after this one (the own
+    // pass) is let go only behind that wait: it then runs beside this grid without a wait of its own.
+    if (total == 0) grid_dependency_wait();         // a grid none of whose CTAs waited could finish before its predecessor
 
     if (me < workers) {
         const long long lo = total * me / workers, hi = total * (me + 1) / workers;
@@ -281,102 +279,88 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             cur.item = (long long)g_items[cur.g] * p.Hkv;
         };
 
-        if (warp == 4) {
-            // -------------------------------------------------------------- producer
-            const int sub = lane & 3;                           // lanes 0-3 fetch one 16-token slice each
-            int it = 0, pc = 0;
+        if (warp == 4 || warp == 6) {
+            // -------------------------------------------------------------- producers: warp 4 Q and K, warp 6 V
+            // A slice is the bs tokens of a page.  K: one box of bs rows x 64 dims per slice and half, so that the 64 rows of
+            // a half lie together; V: one box of all of a slice (see issue_pv for its layout).
+            const bool is_k = warp == 4;
+            const int slices = kTN / p.bs, sub = lane % slices, hf = lane / slices;
+            const bool issues = lane < (is_k ? slices * L::kHalves : slices);
+            uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
+            const int stages = is_k ? kKStages : kVStages;
+            char* ring = smem + (is_k ? kOffK + hf * kHalfBytes + sub * p.bs * 128 : kOffV + sub * p.bs * (D * 2));
+            int pc = 0, st = 0;
+            uint32_t ph = 1;                                    // parity of a stage's last release (none yet: passes)
             bool ok = true;
             while (ok && cur.pos < hi) {
                 const int len = piece_len(), kvh = cur.kvh;
-                const int s0 = group_lo(cur.g) + cur.mt * TQ;
                 const int32_t* table = p.block_tables + (size_t)g_lead[cur.g] * p.max_blocks;
                 const int tile_hi = cur.jt + len - 1;
                 auto page_of = [&](int j) {
-                    return lane < 4 ? __ldg(table + min(((tile_hi - j) * kTN + sub * kSub) / p.bs, p.max_blocks - 1)) : 0;
+                    return issues ? __ldg(table + min((tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
                 };
                 int page = page_of(0);
-                if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
-                if (!ok) break;
-                if (lane == 0) {
-                    mbar_expect_tx(q_full, L::kQBytes);
-#pragma unroll
-                    for (int hf = 0; hf < L::kHalves; ++hf)
-                        tma_load_3d(smem + kOffQ + hf * kQHalfBytes, &map_q, 64 * hf, kvh * G, s0, q_full);
+                if (pc == 0) {
+                    grid_dependency_wait();
+                    if (is_k) grid_dependency_launch();
                 }
-                for (int j = 0; j < len; ++j, ++it) {
-                    const int st = it % kKvStages;
-                    const int page_next = j + 1 < len ? page_of(j + 1) : 0;
-                    const int tok = (tile_hi - j) * kTN + sub * kSub;
-                    const int row = (page * p.Hkv + kvh) * p.bs + tok % p.bs;          // row of the [rows, D] view
-                    if (it >= kKvStages) ok = mbar_wait(&k_empty[st], ((it / kKvStages) - 1) & 1, p.status);
-                    if (!__all_sync(kFull, ok)) break;
-                    if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)kTileBytes);
-                    __syncwarp();
-                    if (lane < 4) {
-                        char* dst = smem + kOffK + st * kTileBytes + sub * (kSub * 128);
+                if (is_k) {
+                    if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(q_full, L::kQBytes);
 #pragma unroll
-                        for (int hf = 0; hf < L::kHalves; ++hf) tma_load_2d(dst + hf * kHalfBytes, &map_k, 64 * hf, row, &k_full[st]);
+                        for (int h = 0; h < L::kHalves; ++h)
+                            tma_load_3d(smem + kOffQ + h * kQHalfBytes, &map_q, 64 * h, kvh * G, group_lo(cur.g) + cur.mt * TQ, q_full);
                     }
-                    if (it >= kKvStages) ok = mbar_wait(&v_empty[st], ((it / kKvStages) - 1) & 1, p.status);
-                    if (!__all_sync(kFull, ok)) break;
-                    if (lane == 0) mbar_expect_tx(&v_full[st], (uint32_t)kTileBytes);
+                }
+                for (int j = 0; j < len; ++j) {
+                    const int page_next = j + 1 < len ? page_of(j + 1) : 0;
+                    const int row = (page * p.Hkv + kvh) * p.bs;                       // row of the [rows, D] view
+                    ok = __all_sync(kFull, mbar_wait(&empty[st], ph, p.status));
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(&full[st], (uint32_t)kTileBytes);
                     __syncwarp();
-                    if (lane < 4) {
-                        char* dst = smem + kOffV + st * kTileBytes + sub * (kSub * 128);
-#pragma unroll
-                        for (int hf = 0; hf < L::kHalves; ++hf) tma_load_2d(dst + hf * kHalfBytes, &map_v, 64 * hf, row, &v_full[st]);
+                    if (issues) {
+                        if (is_k) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &full[st]);
+                        else tma_load_3d(ring + st * kTileBytes, &map_v, 0, row, 0, &full[st]);
                     }
                     page = page_next;
+                    if (++st == stages) st = 0, ph ^= 1;
                 }
-                ok = __all_sync(kFull, ok);
                 next_piece(len);
                 ++pc;
             }
         } else if (warp == 5) {
-            // -------------------------------------------------------------- tensor-core issue (one thread)
+            // -------------------------------------------------------------- one thread issues S = Q K^T
             if (lane == 0) {
-                constexpr uint32_t idesc_s = instr_desc(false, kTN), idesc_pv = instr_desc(true, D);
+                constexpr uint32_t idesc_s = instr_desc(false, kTN);
                 const uint32_t idesc_qk = p.scale < 0.f ? instr_desc(false, kTN, true) : idesc_s;
                 const bool dots = p.scale != 0.f;
-                uint64_t q_desc[D / 16], k_desc0[kKvStages], v_desc0[kKvStages];
+                uint64_t q_desc[D / 16];
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
                     q_desc[ks] = smem_desc(smem_u32(smem + kOffQ) + (ks >> 2) * kQHalfBytes + (ks & 3) * 32, 16, 1024);
-#pragma unroll
-                for (int st = 0; st < kKvStages; ++st) {
-                    k_desc0[st] = smem_desc(smem_u32(smem + kOffK + st * kTileBytes), 16, 1024);
-                    v_desc0[st] = smem_desc(smem_u32(smem + kOffV + st * kTileBytes), kHalfBytes, 1024);
-                }
+                const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
                 const uint64_t qx_desc = smem_desc_plain(smem_u32(smem + kOffQx), 128, kExtRowGroupBytes);
                 const uint64_t kp_desc = smem_desc_plain(smem_u32(smem + kOffKp), 128, kExtRowGroupBytes);
+                int it = 0, pc = 0, st = 0, vst = 0;
+                uint32_t ph = 0, vph = 1;
                 bool ok = true;
-                // O (+)= P V of tile t; `first`: the first one of its piece (O of the piece before must have been read)
-                auto issue_pv = [&](int t, bool first, int piece) -> bool {
-                    const int st = t % kKvStages, sb = t & 1;
-                    if (!mbar_wait(&p_full[sb], (t >> 1) & 1, p.status)) return false;
-                    if (!mbar_wait(&v_full[st], (t / kKvStages) & 1, p.status)) return false;
-                    if (first && piece > 0 && !mbar_wait(o_empty, (piece - 1) & 1, p.status)) return false;
-                    tc_fence_after();
-                    const uint64_t vd = st == 0 ? v_desc0[0] : v_desc0[kKvStages - 1];
-                    const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
-                    umma_ts(tmem_base + kColO, p_tmem, vd, idesc_pv, !first);
-#pragma unroll
-                    for (int kk = 1; kk < kTN / 16; ++kk)
-                        umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, kk * 2048), idesc_pv, true);
-                    tc_commit(&v_empty[st]);
-                    return true;
-                };
-                int it = 0, pc = 0;
-                bool last_first = false;            // whether tile it - 1 was the first one of its piece
                 while (ok && cur.pos < hi) {
                     const int len = piece_len();
                     ok = mbar_wait(q_full, pc & 1, p.status) && (!alibi || mbar_wait(qx_full, pc & 1, p.status));
                     for (int j = 0; ok && j < len; ++j, ++it) {
-                        const int st = it % kKvStages, sb = it & 1;
-                        ok = mbar_wait(&k_full[st], (it / kKvStages) & 1, p.status);
+                        const int sb = it & 1;
+                        // the score buffer is free once the P V of the tile before the last one has read its weights there
+                        if (it >= 2) {
+                            ok = mbar_wait(&v_empty[vst], vph ^ 1, p.status);
+                            if (++vst == kVStages) vst = 0, vph ^= 1;
+                        }
+                        ok = ok && mbar_wait(&k_full[st], ph, p.status);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint64_t kd = st == 0 ? k_desc0[0] : k_desc0[kKvStages - 1];
+                        const uint64_t kd = desc_advance(k_desc0, st * kTileBytes);
                         const uint32_t s_tmem = tmem_base + kColS + sb * kTN;
                         if (dots) {
 #pragma unroll
@@ -387,13 +371,43 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         tc_commit(&s_full[sb]);
                         tc_commit(&k_empty[st]);
                         if (j == len - 1) tc_commit(q_empty);
-                        if (it >= 1) ok = issue_pv(it - 1, last_first, j == 0 ? pc - 1 : pc);
-                        last_first = j == 0;
+                        if (++st == kKStages) st = 0, ph ^= 1;
                     }
                     next_piece(len);
                     ++pc;
                 }
-                if (ok) issue_pv(it - 1, last_first, pc - 1);
+            }
+        } else if (warp == 7) {
+            // -------------------------------------------------------------- one thread issues O (+)= P V
+            if (lane == 0) {
+                constexpr uint32_t idesc_pv = instr_desc(true, D);
+                // V is MN-major, in slices of bs keys with the 64-dim halves of a slice side by side: halves bs * 128 bytes
+                // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
+                const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
+                int it = 0, pc = 0, st = 0;
+                uint32_t ph = 0;
+                bool ok = true;
+                while (ok && cur.pos < hi) {
+                    const int len = piece_len();
+                    for (int j = 0; ok && j < len; ++j, ++it) {
+                        const int sb = it & 1;
+                        ok = mbar_wait(&v_full[st], ph, p.status) && mbar_wait(&p_full[sb], (it >> 1) & 1, p.status) &&
+                             (j > 0 || pc == 0 || mbar_wait(o_empty, (pc - 1) & 1, p.status));    // O of the piece before is read
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t vd = desc_advance(v_desc0, st * kTileBytes);
+                        const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
+#pragma unroll
+                        for (int kk = 0; kk < kTN / 16; ++kk) {
+                            const uint32_t at = p.bs == 16 ? kk * 16 * (D * 2) : (kk >> 1) * 32 * (D * 2) + (kk & 1) * 2048;
+                            umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, at), idesc_pv, j > 0 || kk > 0);
+                        }
+                        tc_commit(&v_empty[st]);
+                        if (++st == kVStages) st = 0, ph ^= 1;
+                    }
+                    next_piece(len);
+                    ++pc;
+                }
             }
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
@@ -414,7 +428,13 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 mbar_arrive(qx_full);
             };
             if (alibi) write_qx(cur.kvh);
-            int it = 0;
+            int it = 0, st = 0;                     // tile, and the stage and parity of its V
+            uint32_t ph = 0;
+            // waits for the P V of the tile before this one
+            auto prev_pv_done = [&]() {
+                const int ps = st == 0 ? kVStages - 1 : st - 1;
+                return __all_sync(kFull, mbar_wait(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
+            };
             bool ok = true;
             while (ok && cur.pos < hi) {
                 const int len = piece_len(), tile_hi = cur.jt + len - 1;
@@ -425,10 +445,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const int n = valid ? __ldg(p.context_lens + s) : 0;
                 const int e_row = valid ? shared_tokens(__ldg(p.prefix_lens + s), n) : 0;      // keys the row sees
                 const float slope2 = p.slopes ? __ldg(p.slopes + kvh * G + hg) * kLog2e : 0.f;
+                const bool opens = cur.jt == 0, closes = cur.jt + len == cur.kt;
                 next_piece(len);                    // `cur` is the piece after this one from here on
                 float m_used = -INFINITY, l = 0.f;
 
-                for (int j = 0; j < len; ++j, ++it) {
+                auto next_tile = [&]() {
+                    ++it;
+                    if (++st == kVStages) st = 0, ph ^= 1;
+                };
+                for (int j = 0; j < len; ++j, next_tile()) {
                     const int sb = it & 1, j0 = (tile_hi - j) * kTN;
                     ok = __all_sync(kFull, mbar_wait(&s_full[sb], (it >> 1) & 1, p.status));
                     if (!ok) break;
@@ -469,7 +494,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const float m_new = need ? m_tile : m_used;
                     const float f = need ? ex2(m_used - m_new) : 1.f;
                     if (j > 0 && __any_sync(kFull, need || begins)) {
-                        ok = __all_sync(kFull, mbar_wait(&v_empty[(it - 1) % kKvStages], ((it - 1) / kKvStages) & 1, p.status));
+                        ok = prev_pv_done();
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
@@ -511,24 +536,28 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (!ok) break;
 
                 // ---- the piece is complete once its last P V is: normalise, store, hand O back
-                ok = __all_sync(kFull, mbar_wait(&v_empty[(it - 1) % kKvStages], ((it - 1) / kKvStages) & 1, p.status));
+                ok = prev_pv_done();
                 if (!ok) break;
                 tc_fence_after();
                 if (__any_sync(kFull, valid)) {
                     const float inv = 1.f / l;
                     const bool begun = (tile_hi - len + 1) * kTN < e_row;          // the row saw a tile of the piece
-                    float4* orow = reinterpret_cast<float4*>(p.partial_out + (row0 + r) * D);
+                    float* po = p.partial_out + row0 * D + r;                       // [D][kRows]: 32 rows are one line
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c) {
                         float o[32];
                         tmem_ld32(lane_addr + kColO + c * 32, o);
                         if (begun) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                orow[c * 8 + e] = make_float4(o[4 * e] * inv, o[4 * e + 1] * inv, o[4 * e + 2] * inv, o[4 * e + 3] * inv);
+                            for (int e = 0; e < 32; ++e) po[(c * 32 + e) * kRows] = o[e] * inv;
                         }
                     }
                     // a row that saw nothing of the piece: weight zero
+                    if (e_row > 0 && hg == 0) {
+                        int32_t* info = p.info + ((size_t)s * p.Hkv + kvh) * kInfoWords;
+                        if (opens) info[0] = (int)(row0 / kRows), info[1] = r;
+                        if (closes) info[2] = (int)(row0 / kRows);
+                    }
                     if (valid) p.partial_lse[row0 + r] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
                 }
                 tc_fence_before();
@@ -552,8 +581,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 }
 
 // ----------------------------------------------------------------------------- merge
-// One row (sequence, query head): the group pass's pieces that cover the sequence's item (rows (item + w) * 128 + r for
-// consecutive workers w) and the own pass's (consecutive piece rows, see reduce.cu), swept as one list by WPR warps.
+// A CTA merges 32 rows: 32 / G consecutive sequences times the G heads of one KV head, a lane per row, so that the group
+// pass's pieces ([D][128 rows]) are read as whole lines.  Per row the pieces are one list: the group pass's that cover the
+// sequence's item (numbers item + w, w consecutive workers), then the own pass's (consecutive rows, see reduce.cu).  kWP of
+// the CTA's eight warps share the list, the others (and the grid's y) take other columns, C of them per lane.
 constexpr int kMergeWarps = 8;
 
 struct MergeParams {
@@ -561,122 +592,106 @@ struct MergeParams {
     const int32_t* context_lens;
     const int32_t* prefix_lens;
     const int32_t* group_start;
-    const long long* sh_header;
-    const long long* sh_groups;
+    const int32_t* info;
     const float* sh_lse;
     const float* sh_out;
-    const long long* own_header;
-    const long long* seq_info;
     const float* own_lse;
     const float* own_out;
-    int num_groups, rows, Hq, Hkv, partition_size;
+    int num_groups, B, Hq, Hkv;
 };
 
-template <int D, int WPR>
+template <int D, int G, int kWP, int C>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 merge_shared_kernel(const MergeParams p) {
-    constexpr int V = D / 32, RPB = kMergeWarps / WPR;
-    using Vec = typename std::conditional<V == 4, float4, float2>::type;
-    __shared__ float s_num[kMergeWarps][D];
-    __shared__ float s_den[kMergeWarps];
-    __shared__ float s_max[kMergeWarps];
+    constexpr int kSeqs = 32 / G;
+    __shared__ float s_max[kWP > 1 ? kMergeWarps : 1][32];
+    __shared__ float s_den[kWP > 1 ? kMergeWarps : 1][32];
+    __shared__ float s_num[kWP > 1 ? kMergeWarps : 1][C][32];
     grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rib = warp / WPR, sub = warp % WPR;
-    const int row = blockIdx.x * RPB + rib;
-    const bool active = row < p.rows;
-    const int s = active ? row / p.Hq : 0, h = active ? row % p.Hq : 0, G = p.Hq / p.Hkv, kvh = h / G, hh = h % G;
+    const int wp = warp % kWP, d0 = (blockIdx.z * (kMergeWarps / kWP) + warp / kWP) * C;
+    const int s = blockIdx.x * kSeqs + lane / G, kvh = blockIdx.y, hh = lane % G;
+    const bool active = s < p.B;
     const int n = active ? __ldg(p.context_lens + s) : 0;
-    // the sequence's group: group_start increases, so it is the number of starts at or before s
-    int g = -1;
-    for (int g0 = 0; g0 <= p.num_groups; g0 += 32) {
-        const bool at = g0 + lane <= p.num_groups && __ldg(p.group_start + g0 + lane) <= s;
-        g += __popc(__ballot_sync(kFull, at));
-    }
-    const bool grouped = g >= 0 && g < p.num_groups;
+    const bool grouped = active && s >= __ldg(p.group_start) && s < __ldg(p.group_start + p.num_groups);
     const int shared = grouped ? shared_tokens(__ldg(p.prefix_lens + s), n) : 0;
-    const int first = grouped ? min(max(__ldg(p.group_start + g), 0), s) : 0;
-    const int P16 = p.partition_size / 16, tiles = (n + 15) / 16 - shared / 16, np = (tiles + P16 - 1) / P16;
+    const bool has1 = shared > 0, has2 = n > shared;
     grid_dependency_wait();
 
-    // group pass: R1 rows kRows apart; own pass: R2 rows G apart
-    int R1 = 0, R2 = 0;
-    const float *lse1 = p.sh_lse, *po1 = p.sh_out, *lse2 = p.own_lse, *po2 = p.own_out;
-    if (shared > 0) {
-        const long long total = p.sh_header[0], workers = p.sh_header[1];
-        const long long before = p.sh_groups[4 * g], items = p.sh_groups[4 * g + 1], kt = p.sh_groups[4 * g + 2],
-                        blocks = p.sh_groups[4 * g + 3];
-        const int at = (s - first) * G + hh;
-        // (the two minima hold for every group_start that increases; with one that does not they keep the reads inside)
-        const long long in_group = kvh * blocks + min((long long)(at / kRows), blocks - 1);
-        if (kt > 0) {
-            // the sequence sees the first shared / kTN tiles of its item
-            const long long f0 = before * p.Hkv + in_group * kt, f1 = f0 + min((long long)(shared / kTN), kt);
-            const long long w0 = ((f0 + 1) * workers - 1) / total, w1 = (f1 * workers - 1) / total;
-            const long long r0 = (items * p.Hkv + in_group + w0) * kRows + at % kRows;
-            R1 = (int)(w1 - w0 + 1);
-            lse1 += r0;
-            po1 += r0 * D + lane * V;
-        }
-    }
-    if (np > 0) {
-        const long long total = p.own_header[0], workers = p.own_header[1];
-        const long long f0 = p.seq_info[2 * s] * p.Hkv + (long long)kvh * tiles;
-        const long long first_part = p.seq_info[2 * s + 1] * p.Hkv + (long long)kvh * np;
-        const long long r0 = first_part + ((f0 + 1) * workers - 1) / total;
-        const long long r1 = first_part + np - 1 + ((f0 + tiles) * workers - 1) / total;
-        R2 = (int)(r1 - r0 + 1);
-        lse2 += r0 * G + hh;
-        po2 += (r0 * G + hh) * D + lane * V;
-    }
+    // group pass: R1 pieces of kRows rows; own pass: R2 pieces of G rows
+    const int32_t* info = p.info + ((size_t)(active ? s : 0) * p.Hkv + kvh) * kInfoWords;
+    const int4 i0 = *reinterpret_cast<const int4*>(info);
+    const int2 i1 = *reinterpret_cast<const int2*>(info + 4);
+    const int R1 = has1 ? i0.z - i0.x + 1 : 0, R2 = has2 ? i1.y - i1.x + 1 : 0;
+    const float* lse1 = p.sh_lse + (has1 ? (size_t)i0.x * kRows + i0.y + hh : 0);
+    const float* po1 = p.sh_out + (has1 ? ((size_t)i0.x * D + d0) * kRows + i0.y + hh : 0);
+    const float* lse2 = p.own_lse + (has2 ? (size_t)i1.x * G + hh : 0);
+    const float* po2 = p.own_out + (has2 ? ((size_t)i1.x * G + hh) * D + d0 : 0);
     const int R = R1 + R2;
-    auto lse_at = [&](int i) { return i < R1 ? lse1[(size_t)i * kRows] : lse2[(size_t)(i - R1) * G]; };
-    auto row_at = [&](int i) {
-        return *reinterpret_cast<const Vec*>(i < R1 ? po1 + (size_t)i * kRows * D : po2 + (size_t)(i - R1) * G * D);
-    };
     float M = -INFINITY;
-    for (int i = sub * 32 + lane; i < R; i += WPR * 32) M = fmaxf(M, lse_at(i));
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kFull, M, o));
-    if (WPR > 1) {
-        if (lane == 0) s_max[warp] = M;
+    for (int i = wp; i < R1; i += kWP) M = fmaxf(M, lse1[(size_t)i * kRows]);
+    for (int i = wp; i < R2; i += kWP) M = fmaxf(M, lse2[(size_t)i * G]);
+    if (kWP > 1) {
+        s_max[warp][lane] = M;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) M = fmaxf(M, s_max[rib * WPR + w]);
+        for (int w = 0; w < kWP; ++w) M = fmaxf(M, s_max[warp - wp + w][lane]);
     }
-    float num[V], den = 0.f;
+    float num[C], den = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) num[v] = 0.f;
-#pragma unroll 4
-    for (int i = sub; i < R; i += WPR) {
-        const float lw = lse_at(i);
-        const Vec x = row_at(i);
-        if (lw != -INFINITY) {                                 // a row that holds nothing (a NaN is carried on)
-            const float w = ex2((lw - M) * kLog2e);
-            den += w;
-            num[0] = fmaf(w, x.x, num[0]);
-            num[1] = fmaf(w, x.y, num[1]);
-            if constexpr (V == 4) {
-                num[2] = fmaf(w, x.z, num[2]);
-                num[3] = fmaf(w, x.w, num[3]);
-            }
+    for (int c = 0; c < C; ++c) num[c] = 0.f;
+    // (loads do not wait for the weight: a row that holds nothing, lse -inf, is selected away; a NaN is carried on)
+#pragma unroll 2
+    for (int i = wp; i < R1; i += kWP) {
+        const float lw = lse1[(size_t)i * kRows];
+        const float* x = po1 + (size_t)i * kRows * D;
+        float y[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) y[c] = x[c * kRows];
+        const bool holds = lw != -INFINITY;
+        const float w = holds ? ex2((lw - M) * kLog2e) : 0.f;
+        den += w;
+#pragma unroll
+        for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? y[c] : 0.f, num[c]);
+    }
+#pragma unroll 2
+    for (int i = wp; i < R2; i += kWP) {
+        const float lw = lse2[(size_t)i * G];
+        const float4* x = reinterpret_cast<const float4*>(po2 + (size_t)i * G * D);
+        float4 y[C / 4];
+#pragma unroll
+        for (int c = 0; c < C / 4; ++c) y[c] = x[c];
+        const bool holds = lw != -INFINITY;
+        const float w = holds ? ex2((lw - M) * kLog2e) : 0.f;
+        den += w;
+#pragma unroll
+        for (int c = 0; c < C / 4; ++c) {
+            num[4 * c] = fmaf(w, holds ? y[c].x : 0.f, num[4 * c]);
+            num[4 * c + 1] = fmaf(w, holds ? y[c].y : 0.f, num[4 * c + 1]);
+            num[4 * c + 2] = fmaf(w, holds ? y[c].z : 0.f, num[4 * c + 2]);
+            num[4 * c + 3] = fmaf(w, holds ? y[c].w : 0.f, num[4 * c + 3]);
         }
     }
+    if constexpr (kWP > 1) {
+        s_den[warp][lane] = den;
 #pragma unroll
-    for (int v = 0; v < V; ++v) s_num[warp][lane * V + v] = num[v];
-    if (lane == 0) s_den[warp] = den;
-    __syncthreads();
+        for (int c = 0; c < C; ++c) s_num[warp][c][lane] = num[c];
+        __syncthreads();
+        if (wp != 0) return;
+#pragma unroll
+        for (int w = 1; w < kWP; ++w) {
+            den += s_den[warp + w][lane];
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c] += s_num[warp + w][c][lane];
+        }
+    }
     if (!active) return;
-    __nv_bfloat16* o = p.out + (size_t)row * D;
-    for (int d = sub * 32 + lane; d < D; d += WPR * 32) {
-        float a = 0.f, b = 0.f;
+    const float inv = R > 0 ? 1.f / den : 0.f;                  // an empty sequence gives a zero row
+    uint4* o = reinterpret_cast<uint4*>(p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0);
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) {
-            a += s_num[rib * WPR + w][d];
-            b += s_den[rib * WPR + w];
-        }
-        o[d] = __float2bfloat16_rn(R > 0 ? a / b : 0.f);       // an empty sequence gives a zero row
-    }
+    for (int c = 0; c < C / 8; ++c)
+        o[c] = make_uint4(pack2(num[8 * c] * inv, num[8 * c + 1] * inv), pack2(num[8 * c + 2] * inv, num[8 * c + 3] * inv),
+                          pack2(num[8 * c + 4] * inv, num[8 * c + 5] * inv), pack2(num[8 * c + 6] * inv, num[8 * c + 7] * inv));
 }
 
 // ----------------------------------------------------------------------------- host
@@ -688,11 +703,19 @@ bool make_q_map(CUtensorMap* map, const void* q, int B, int Hq, int G, int D) {
     return make_bf16_map(map, q, 3, dims, strides, box);
 }
 
+// The cache as a 3-D tensor [64-dim halves, rows, 64]; a box is the bs token rows of a page, half after half.
+bool make_slice_map(CUtensorMap* map, const void* cache, uint64_t rows, int D, int bs) {
+    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(D / 64)};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, 128};
+    const cuuint32_t box[3] = {64, (cuuint32_t)bs, (cuuint32_t)(D / 64)};
+    return make_bf16_map(map, cache, 3, dims, strides, box);
+}
+
 template <int D, int G>
 int launch_pass(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const SharedParams& p, unsigned ctas,
                 cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
-    if (!ensure_smem_limit(decode_shared_kernel<D, G>, ShLayout<D>::kSmemBytes, configured)) return OPT_GQA_ERR_CUDA;
+    if (!ensure_smem_limit(decode_shared_kernel<D, G>, ShLayout<D>::kSmemBytes, configured, true)) return OPT_GQA_ERR_CUDA;
     return launch_dependent(decode_shared_kernel<D, G>, dim3(ctas), dim3(kThreads), ShLayout<D>::kSmemBytes, stream, mq, mk,
                             mv, p);
 }
@@ -709,20 +732,26 @@ int launch_pass_g(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
     return OPT_GQA_ERR_SHAPE;
 }
 
-template <int D, int WPR>
-int launch_merge_w(const MergeParams& p, cudaStream_t stream) {
-    constexpr int rpb = kMergeWarps / WPR;
-    return launch_dependent(merge_shared_kernel<D, WPR>, dim3((unsigned)((p.rows + rpb - 1) / rpb)), dim3(kMergeWarps * 32), 0,
-                            stream, p);
+template <int D, int G>
+int launch_merge(const MergeParams& p, cudaStream_t stream) {
+    const unsigned slabs = (unsigned)((p.B + 32 / G - 1) / (32 / G));
+    auto launch = [&](auto kernel, unsigned z) {
+        return launch_dependent(kernel, dim3(slabs, (unsigned)p.Hkv, z), dim3(kMergeWarps * 32), 0, stream, p);
+    };
+    // Few rows: eight warps share a row's pieces and a CTA takes 8 columns; many rows: a CTA takes all of a row.
+    if ((long long)slabs * p.Hkv <= 128) return launch(merge_shared_kernel<D, G, 8, 8>, D / 8);
+    return launch(merge_shared_kernel<D, G, 1, D / 8>, 1);
 }
 
 template <int D>
-int launch_merge(const MergeParams& p, cudaStream_t stream) {
-    // about 8192 warps in all, as in the balanced merge
-    if (p.rows <= 1024) return launch_merge_w<D, 8>(p, stream);
-    if (p.rows <= 2048) return launch_merge_w<D, 4>(p, stream);
-    if (p.rows <= 4096) return launch_merge_w<D, 2>(p, stream);
-    return launch_merge_w<D, 1>(p, stream);
+int launch_merge_g(const MergeParams& p, int G, cudaStream_t stream) {
+    switch (G) {
+        case 1: return launch_merge<D, 1>(p, stream);
+        case 2: return launch_merge<D, 2>(p, stream);
+        case 4: return launch_merge<D, 4>(p, stream);
+        case 8: return launch_merge<D, 8>(p, stream);
+    }
+    return OPT_GQA_ERR_SHAPE;
 }
 
 }  // namespace
@@ -736,12 +765,12 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     if (rows == 0 || rows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
     const int G = Hq / Hkv, N = shared.num_groups;
     const SharedLayout L = shared_layout(B, Hq, Hkv, D, N, max_partitions);
-    if (L.own.rows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
+    if (L.own.rows > 0x7fffffffull || L.rows / kSharedRows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
     const int sms = sm_count();
     if (sms <= 0) return OPT_GQA_ERR_CUDA;
     CUtensorMap mq, mk, mv;
-    if (!make_q_map(&mq, q, B, Hq, G, D) || !make_cache_map(&mk, k_cache, rows, D, kSub) ||
-        !make_cache_map(&mv, v_cache, rows, D, kSub))
+    if (!make_q_map(&mq, q, B, Hq, G, D) || !make_cache_map(&mk, k_cache, rows, D, bs) ||
+        !make_slice_map(&mv, v_cache, rows, D, bs))
         return OPT_GQA_ERR_CUDA;
     char* ws = static_cast<char*>(workspace);
     SharedParams p;
@@ -752,8 +781,7 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     p.slopes = alibi_slopes;
     p.partial_out = reinterpret_cast<float*>(ws + L.out);
     p.partial_lse = reinterpret_cast<float*>(ws + L.lse);
-    p.header = reinterpret_cast<long long*>(ws + L.header);
-    p.groups = reinterpret_cast<long long*>(ws + L.groups);
+    p.info = reinterpret_cast<int32_t*>(ws + L.info);
     p.status = device_status;
     p.scale = scale;
     p.num_groups = N;
@@ -764,38 +792,32 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     p.bs = bs;
     p.lanes_log2 = 0;           // lanes that scan one group's sequences: about the mean size of a group
     while (p.lanes_log2 < 5 && ((long long)N << p.lanes_log2) < B) ++p.lanes_log2;
-    // one resident wave; no more workers than tiles there can be (max_partitions * partition_size bounds every context)
-    const long long most = (long long)Hkv * (N + (long long)B * G / kRows) *
-                           (((long long)max_partitions * partition_size + kTN - 1) / kTN);
-    long long ctas = (long long)sms * kCtasPerSm;
-    if (ctas > kSharedMaxWorkers) ctas = kSharedMaxWorkers;
-    if (ctas > most) ctas = most;
+    // one CTA per multiprocessor, beside one of the own pass
+    const int ctas = sms < kSharedMaxWorkers ? sms : kSharedMaxWorkers;
     int rc = D == 128 ? launch_pass_g<128>(mq, mk, mv, p, G, (unsigned)ctas, stream)
                       : launch_pass_g<64>(mq, mk, mv, p, G, (unsigned)ctas, stream);
     if (rc != OPT_GQA_OK) return rc;
+    SharedPrefix own = shared;
+    own.info = p.info;
     rc = launch_decode_stream(q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, alibi_slopes, scale, B, Hq,
                               Hkv, D, bs, num_blocks, partition_size, workspace, max_partitions, 0, device_status, stream,
-                              nullptr, &shared);
+                              nullptr, &own);
     if (rc != OPT_GQA_OK) return rc;
     MergeParams m;
     m.out = static_cast<__nv_bfloat16*>(out);
     m.context_lens = context_lens;
     m.prefix_lens = shared.prefix_lens;
     m.group_start = shared.group_start;
-    m.sh_header = p.header;
-    m.sh_groups = p.groups;
+    m.info = p.info;
     m.sh_lse = p.partial_lse;
     m.sh_out = p.partial_out;
-    m.own_header = reinterpret_cast<const long long*>(ws + L.own.header);
-    m.seq_info = reinterpret_cast<const long long*>(ws + L.own.seq_info);
     m.own_lse = reinterpret_cast<const float*>(ws + L.own.lse);
     m.own_out = reinterpret_cast<const float*>(ws + L.own.out);
     m.num_groups = N;
-    m.rows = B * Hq;
+    m.B = B;
     m.Hq = Hq;
     m.Hkv = Hkv;
-    m.partition_size = partition_size;
-    return D == 128 ? launch_merge<128>(m, stream) : launch_merge<64>(m, stream);
+    return D == 128 ? launch_merge_g<128>(m, G, stream) : launch_merge_g<64>(m, G, stream);
 }
 
 }  // namespace optgqa

@@ -35,6 +35,7 @@ namespace {
 
 constexpr int kTileTok = 16;                     // tokens per tile (one ring stage holds a K tile and a V tile)
 constexpr int kWarps = 4;                        // workers per CTA
+constexpr int kSharedWarps = 4;                  // and beside the group pass, one CTA per multiprocessor
 constexpr int kStages = 2;                       // ring depth per worker
 constexpr int kCtasPerSm = 2;
 constexpr int kDescSlots = 4;                    // item descriptors a worker keeps (>= items between prefetch and use)
@@ -70,17 +71,19 @@ struct StreamParams {
     const int32_t* prefix_lens;
     const int32_t* group_start;
     int num_groups;
+    int32_t* info;          // see SharedLayout
 };
 
-template <int D>
+template <int D, bool kShared>
 struct StreamCfg {
+    static constexpr int WARPS = kShared ? kSharedWarps : kWarps;
     static constexpr int NBOX = D / 64;                   // 128-byte-wide boxes per token row
     static constexpr int BOX_BYTES = kTileTok * 128;      // 16 rows x 128 B
     static constexpr int TILE_BYTES = NBOX * BOX_BYTES;   // K (or V) bytes per tile
     static constexpr int WARP_RING = kStages * 2 * TILE_BYTES;
-    static constexpr int OFF_DESC = kWarps * WARP_RING;
-    static constexpr int OFF_BAR = OFF_DESC + kWarps * kDescSlots * 32;
-    static constexpr int SMEM = OFF_BAR + kWarps * kStages * 8 + 1024;   // + slack to align the ring to 1 KB
+    static constexpr int OFF_DESC = WARPS * WARP_RING;
+    static constexpr int OFF_BAR = OFF_DESC + WARPS * kDescSlots * 32;
+    static constexpr int SMEM = OFF_BAR + WARPS * kStages * 8 + 1024;   // + slack to align the ring to 1 KB
 };
 
 // Transposes an 8x8 matrix of 16-bit elements held one row pair per thread (the ldmatrix layout).
@@ -121,12 +124,14 @@ struct StreamCursor {
 };
 
 // kShared: the first shared_tokens() of every sequence of a group are left out; the group pass of decode_shared.cu
-// attends to them.
+// attends to them.  That pass precedes this kernel in the stream, works on other rows of the workspace, and lets this kernel
+// start only when everything before both of them is complete; so nothing here waits for it, the two share the GPU, and
+// worker 0 alone waits for it at its end, so that this grid's completion tells the merge of both.
 template <int D, int G, bool kShared>
-__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
+__global__ void __launch_bounds__((kShared ? kSharedWarps : kWarps) * 32, kCtasPerSm)
 decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const StreamParams p) {
-    using C = StreamCfg<D>;
+    using C = StreamCfg<D, kShared>;
     constexpr int KS = D / 16;    // k-steps of K q^T
     constexpr int MT = D / 16;    // m-tiles of V^T p^T
     extern __shared__ char smem_raw[];
@@ -172,16 +177,19 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     total *= p.Hkv;
     // Never more workers than tiles, so that every worker's range holds at least one tile.
-    const long long grid_workers = (long long)gridDim.x * kWarps, me = (long long)blockIdx.x * kWarps + warp;
+    const long long grid_workers = (long long)gridDim.x * C::WARPS, me = (long long)blockIdx.x * C::WARPS + warp;
     const long long workers = total < grid_workers ? (total > 0 ? total : 1) : grid_workers;
     if (me == 0) {
-        grid_dependency_wait();     // the previous reader of the workspace must be done
+        if constexpr (!kShared) grid_dependency_wait();     // the previous reader of the workspace must be done
         if (lane == 0) {
             p.header[0] = total;
             p.header[1] = workers;
         }
     }
-    if (total == 0 || me >= workers) return;
+    if (total == 0 || me >= workers) {
+        if (kShared && me == 0) grid_dependency_wait();
+        return;
+    }
     const long long lo = total * me / workers, hi = total * (me + 1) / workers;
 
     StreamCursor cur;       // the next piece to be described (runs one piece ahead of the issue side)
@@ -215,7 +223,7 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 acc_p += __shfl_sync(kFull, incl_p, 31);
             }
         }
-        if (cur.s < 0) return;                               // cannot happen: lo < total
+            if (cur.s < 0) return;                               // cannot happen: lo < total
         const int r = (int)(lo - cur.tiles_before * p.Hkv);
         cur.kvh = r / cur.tiles;
         cur.jt = r - cur.kvh * cur.tiles;
@@ -275,6 +283,13 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         if (lane == 0 && cur.kvh == 0 && cur.jt == 0) {
             p.seq_info[2 * cur.s] = cur.tiles_before;
             p.seq_info[2 * cur.s + 1] = cur.parts_before;
+        }
+        if constexpr (kShared) {
+            if (lane == 0) {
+                int32_t* info = p.info + ((size_t)cur.s * p.Hkv + cur.kvh) * kInfoWords;
+                if (cur.jt == 0) info[4] = obase / G;
+                if (cur.jt + len == cur.tiles) info[5] = obase / G;
+            }
         }
         // Where this range and a partition end together inside a stream, the next piece is two numbers on:
         // mark the number in between as empty, so that the merge can sweep the stream's numbers without gaps.
@@ -393,7 +408,7 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             asm volatile("prefetch.global.L2 [%0];" ::"l"(
                 reinterpret_cast<const char*>(p.q + ((size_t)cur.s * p.Hq + (size_t)cur.kvh * G) * D) + lane * 128));
     }
-    grid_dependency_wait();     // the cache may still be receiving this step's appended tokens
+    if constexpr (!kShared) grid_dependency_wait();     // the cache may still be receiving this step's appended tokens
     describe_next();            // piece 0
     while (issue_allowed()) issue_one();
 
@@ -558,6 +573,7 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         // chance to land before this CTA's shared memory is released.
         for (uint32_t kk = consumed; kk != issued; ++kk) mbar_wait(&bars[kk % kStages], (kk / kStages) & 1, p.status);
     }
+    if (kShared && me == 0) grid_dependency_wait();
 }
 
 // One resident wave; never more workers than there could be 16-token tiles (the ranges are cut at tile granularity),
@@ -575,12 +591,12 @@ long long stream_grid_ctas(int B, int Hkv, int max_partitions, int partition_siz
 
 template <int D, int G, bool kShared>
 int launch_one(const CUtensorMap& mk, const CUtensorMap& mv, const StreamParams& p, cudaStream_t stream) {
-    using C = StreamCfg<D>;
+    using C = StreamCfg<D, kShared>;
     static std::atomic<bool> configured[kMaxDevices];
-    if (!ensure_smem_limit(decode_stream_kernel<D, G, kShared>, C::SMEM, configured)) return OPT_GQA_ERR_CUDA;
-    const long long ctas = stream_grid_ctas(p.B, p.Hkv, p.max_partitions, p.partition_size);
+    if (!ensure_smem_limit(decode_stream_kernel<D, G, kShared>, C::SMEM, configured, kShared)) return OPT_GQA_ERR_CUDA;
+    const long long ctas = kShared ? sm_count() : stream_grid_ctas(p.B, p.Hkv, p.max_partitions, p.partition_size);
     if (ctas <= 0) return OPT_GQA_ERR_CUDA;
-    return launch_dependent(decode_stream_kernel<D, G, kShared>, dim3((unsigned)ctas), dim3(kWarps * 32), C::SMEM, stream, mk,
+    return launch_dependent(decode_stream_kernel<D, G, kShared>, dim3((unsigned)ctas), dim3(C::WARPS * 32), C::SMEM, stream, mk,
                             mv, p);
 }
 
@@ -656,6 +672,7 @@ int launch_decode_stream(const void* q, const void* k_cache, const void* v_cache
     p.prefix_lens = shared ? shared->prefix_lens : nullptr;
     p.group_start = shared ? shared->group_start : nullptr;
     p.num_groups = shared ? shared->num_groups : 0;
+    p.info = shared ? shared->info : nullptr;
     const int G = Hq / Hkv;
     if (shared) {
         if (D == 128) return launch_g<128, true>(mk, mv, p, G, stream);

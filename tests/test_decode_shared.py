@@ -16,9 +16,11 @@ def lib():
 def test_workspace_holds_every_piece_of_both_passes(lib):
     B, Hq, Hkv, D, N, P = 256, 64, 8, 128, 12, 20
     own = binding.workspace_bytes(B, Hq, D, P)
-    rows = (Hkv * (N + B * 8 // 128) + 296) * 128
+    items = Hkv * (N + B * 8 // 128) * 128                  # rows of every (group, KV head, block of 128 rows)
     need = binding.shared_workspace_bytes(B, Hq, Hkv, D, N, P)
-    assert own - 4096 + rows * (D + 1) * 4 + N * 32 <= need <= own + rows * (D + 1) * 4 + N * 32 + 4096
+    # and of at most two more pieces per multiprocessor, 32 bytes per (sequence, KV head), rounding
+    assert own + items * (D + 1) * 4 <= need + 4096
+    assert need <= own + (items + 2 * 148 * 128) * (D + 1) * 4 + B * Hkv * 32 + 4096
     for bad in ((0, Hq, Hkv, D, N, P), (B, 63, Hkv, D, N, P), (B, Hq, Hkv, 96, N, P), (B, Hq, Hkv, D, 0, P),
                 (B, Hq, Hkv, D, 513, P), (B, Hq, Hkv, D, N, 0), (1 << 17, Hq, Hkv, D, N, P), (B, 48, 3, D, N, P)):
         assert binding.shared_workspace_bytes(*bad) == 0, bad
