@@ -219,7 +219,7 @@ size_t opt_gqa_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int num_gro
     if (B <= 0 || B > 65535 || !shape_ok(Hq, Hkv, D, 16) || Hkv > 65535 || num_groups <= 0 || num_groups > kMaxGroups ||
         max_partitions <= 0 || max_partitions > 65535)
         return 0;
-    return shared_layout(B, Hq, Hkv, D, num_groups, max_partitions).total;
+    return shared_layout(B, Hq, Hkv, D, num_groups).total;
 }
 
 int opt_gqa_paged_attention_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache,
@@ -238,15 +238,15 @@ int opt_gqa_paged_attention_decode_shared(void* out, const void* q, const void* 
     if (!out || !q || !k_cache || !v_cache || !block_tables || !context_lens || !group_start || !prefix_lens || !workspace)
         return OPT_GQA_ERR_NULL;
     if (num_blocks == 0 || max_blocks_per_seq == 0 || num_groups == 0) return OPT_GQA_ERR_SHAPE;
-    if (workspace_bytes < shared_layout(B, Hq, Hkv, D, num_groups, max_partitions).total) return OPT_GQA_ERR_SHAPE;
+    if (workspace_bytes < shared_layout(B, Hq, Hkv, D, num_groups).total) return OPT_GQA_ERR_SHAPE;
     if (!aligned16(out) || !aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace))
         return OPT_GQA_ERR_ALIGN;
     int* status = device_status_ptr();
     if (!status) return OPT_GQA_ERR_CUDA;
-    const SharedPrefix shared = {group_start, prefix_lens, num_groups};
-    return launch_decode_shared(out, q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, shared,
-                                alibi_slopes, scale, B, Hq, Hkv, D, bs, num_blocks, partition_size, workspace,
-                                max_partitions, status, static_cast<cudaStream_t>(stream));
+    return launch_decode_shared(out, q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, group_start,
+                                prefix_lens, num_groups, alibi_slopes, scale, B, Hq, Hkv, D, bs, num_blocks,
+                                (int64_t)max_partitions * partition_size, workspace, status,
+                                static_cast<cudaStream_t>(stream));
 }
 
 static int prefill_checked(bool allow_umma, int window, void* out, const void* q, const int32_t* q_start_loc, int total_q_tokens,

@@ -176,18 +176,13 @@ constexpr int kMaxDevices = 64;
 
 // Raises the dynamic shared memory limit of `kernel` once per device.  `done` is the launcher's own
 // `static std::atomic<bool> [kMaxDevices]`.
-// `whole_sm`: ask for the largest shared memory of a multiprocessor, not the least that holds this kernel's CTAs, so that
-// another kernel's CTAs find room beside them.
 template <typename Kernel>
-inline bool ensure_smem_limit(Kernel kernel, int bytes, std::atomic<bool>* done, bool whole_sm = false) {
+inline bool ensure_smem_limit(Kernel kernel, int bytes, std::atomic<bool>* done) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
     const bool cached = dev >= 0 && dev < kMaxDevices;
     if (cached && done[dev].load(std::memory_order_acquire)) return true;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    if (whole_sm && cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout,
-                                         cudaSharedmemCarveoutMaxShared) != cudaSuccess)
-        return false;
     if (cached) done[dev].store(true, std::memory_order_release);
     return true;
 }
@@ -262,51 +257,46 @@ int launch_decode_tc(void* out, const void* q, const void* k_cache, const void* 
                      cudaStream_t stream, const FusedAppend* append = nullptr);
 
 // A batch whose sequences share prefixes: group g is the sequences group_start[g] .. group_start[g + 1] - 1, and
-// sequence s has its first prefix_lens[s] tokens in common with its group.  The group pass works on whole tiles of
-// kSharedTile keys; what is left of the prefix behind them belongs to the sequences' own pass.
-struct SharedPrefix {
-    const int32_t* group_start;     // [num_groups + 1]
-    const int32_t* prefix_lens;     // [B]
-    int num_groups;
-    int32_t* info = nullptr;        // [B * Hkv][kInfoWords], see SharedLayout
-};
+// sequence s has its first prefix_lens[s] tokens in common with its group.  What is shared is taken in whole tiles of
+// kSharedTile keys; the rest of the prefix behind them belongs to the sequence alone.
 constexpr int kSharedTile = 64;
 constexpr int kMaxGroups = 512;
-// Tokens of a sequence of length n that the group pass attends to.
+// Tokens of a sequence of length n that are attended to together with its group.
 __device__ __forceinline__ int shared_tokens(int prefix, int n) { return max(min(prefix, n), 0) & ~(kSharedTile - 1); }
 
-// Workspace of the shared-prefix decode: the own pass's balanced layout, then the bookkeeping the two passes leave for the
-// merge and the group pass's pieces.  An item is (group, KV head, block of 128 rows), a row being (sequence, head of the KV
-// head's group); the tiles of the items laid end to end are cut into one range per worker, and the part of item i inside
-// worker w's range is piece i + w: its log-sum-exps are partial_lse[piece][128], its rows partial_out[piece][D][128].
-// info, per (sequence, KV head): {first piece, row of the group's first head, last piece, -, first and last piece row / G of
-// the own pass, -, -}; a pass writes its words for the streams it has keys for.
+// Workspace of the shared-prefix decode.  An item is (group, KV head, block of 128 rows), a row being (sequence, head of
+// the KV head's group), over the group's shared tiles; or (sequence, KV head), G rows, over the tiles that are the
+// sequence's own.  The tiles of all items laid end to end are cut into one range per worker; the part of item i inside worker
+// w's range is a piece: number i + w, counted for the two kinds apart, log-sum-exps lse[piece][rows], normalised partial
+// results out[piece], [D][128] of a group's, [G][D] of a sequence's own.
+// info, per (sequence, KV head): {first piece of its group item, row of the first head in it, last piece, -, first and last
+// own piece, -, -}; only the words of what the sequence has are written.
 constexpr int kSharedRows = 128;
-constexpr int kSharedMaxWorkers = 148;
+constexpr int kSharedMaxWorkers = 296;
 constexpr int kInfoWords = 8;
 struct SharedLayout {
-    BalancedLayout own;
-    size_t info, lse, out, total;
-    unsigned long long rows;
+    size_t info, group_lse, group_out, own_lse, own_out, total;
+    unsigned long long group_pieces, own_pieces;
 };
-inline SharedLayout shared_layout(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
+inline SharedLayout shared_layout(int B, int Hq, int Hkv, int D, int num_groups) {
     SharedLayout L;
-    L.own = balanced_layout(B, Hq, Hkv, D, max_partitions);
     const unsigned long long G = (unsigned long long)(Hq / Hkv);
-    const unsigned long long items = (unsigned long long)Hkv * ((unsigned long long)num_groups + (unsigned long long)B * G / kSharedRows);
-    L.rows = (items + kSharedMaxWorkers) * kSharedRows;
-    L.info = round_up_256(L.own.total);
-    L.lse = L.info + round_up_256((size_t)B * Hkv * kInfoWords * 4);
-    L.out = L.lse + round_up_256((size_t)L.rows * 4);
-    L.total = L.out + (size_t)L.rows * D * 4;
+    L.group_pieces = (unsigned long long)Hkv * ((unsigned long long)num_groups + (unsigned long long)B * G / kSharedRows) + kSharedMaxWorkers;
+    L.own_pieces = (unsigned long long)B * Hkv + kSharedMaxWorkers;
+    L.info = 0;
+    L.group_lse = round_up_256((size_t)B * Hkv * kInfoWords * 4);
+    L.group_out = L.group_lse + round_up_256((size_t)L.group_pieces * kSharedRows * 4);
+    L.own_lse = L.group_out + (size_t)L.group_pieces * kSharedRows * D * 4;
+    L.own_out = L.own_lse + round_up_256((size_t)L.own_pieces * G * 4);
+    L.total = L.own_out + round_up_256((size_t)L.own_pieces * G * D * 4);
     return L;
 }
 
-// Pieces and merge of the group pass (decode_shared.cu); the own pass is launch_decode_stream with the same SharedPrefix.
+// bf16: decode_shared.cu.  max_context bounds every context length (it sizes the grid).
 int launch_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
-                         int max_blocks_per_seq, const int32_t* context_lens, const SharedPrefix& shared,
-                         const float* alibi_slopes, float scale, int B, int Hq, int Hkv, int D, int bs,
-                         int64_t num_blocks, int partition_size, void* workspace, int max_partitions,
+                         int max_blocks_per_seq, const int32_t* context_lens, const int32_t* group_start,
+                         const int32_t* prefix_lens, int num_groups, const float* alibi_slopes, float scale, int B, int Hq,
+                         int Hkv, int D, int bs, int64_t num_blocks, int64_t max_context, void* workspace,
                          int* device_status, cudaStream_t stream);
 
 // bf16, partition_size > 0, balanced split into `workspace`: persistent streaming kernel, one worker per warp
@@ -315,7 +305,7 @@ int launch_decode_stream(const void* q, const void* k_cache, const void* v_cache
                          int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale,
                          int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks, int partition_size,
                          void* workspace, int max_partitions, int window, int* device_status, cudaStream_t stream,
-                         const FusedAppend* append = nullptr, const SharedPrefix* shared = nullptr);
+                         const FusedAppend* append = nullptr);
 
 // Workers (warps) of the grid that launch_decode_stream uses for the balanced split of these sizes on the current
 // device; 0 if the device cannot be queried.

@@ -3,27 +3,32 @@
 //
 // Softmax over disjoint sets of keys merges exactly from each set's normalised result and log-sum-exp, so
 //     out = (e^{lse_P} o_P + e^{lse_S} o_S) / (e^{lse_P} + e^{lse_S}),
-// P the shared keys (this file), S the sequence's own (decode_stream.cu with a first tile per sequence).  In the group
-// pass the n_g sequences of a group times the G query heads of a KV head are the rows of one product with the prefix's
-// keys -- a real matrix product, with 2 n_g G flops per byte of the cache -- so it runs on tcgen05: per item (group, KV head,
-// block of 128 rows) S = Q K^T and O += P V over 64-key tiles, accumulators in tensor memory, exactly as a query block of
-// the chunked prefill without its causal mask.  Up to 128 rows the pass is bound by reading the cache (a 32 KB tile takes
-// an SM's share of the bandwidth 1480 cycles, the two resident CTAs need about 900 for its arithmetic); beyond, by the
-// special-function unit and the tensor core as the prefill is.
+// P the keys a sequence shares, S its own.  Both are items of one kernel: over the shared keys of a group the n_g sequences
+// times the G query heads of a KV head are the rows (in blocks of 128), a real matrix product with 2 n_g G flops per byte
+// of the cache; over a sequence's own keys the G heads are the rows.  Per item S = Q K^T and O += P V run on tcgen05 over
+// 64-key tiles, accumulators in tensor memory, as a query block of the chunked prefill does.  For an own item most of a
+// 128-row tile is idle, and that costs nothing that counts: a 32 KB tile takes an SM's share of the memory bandwidth 1480
+// cycles, and the two resident CTAs need fewer for its arithmetic, idle rows or not (warps none of whose rows are live skip
+// the softmax).  So own contexts and prefixes of up to 128 rows are bound by reading the cache; prefixes of more rows by the
+// special-function unit and the tensor core, as the prefill is.
 //
-// The tiles of all items are laid end to end and cut into one contiguous range per worker (two CTAs per SM), so that one
-// long prefix fills the GPU as well as many short ones.  A worker's part of an item is a piece: 128 normalised partial
-// rows and log-sum-exps in the workspace, merged with the own pass's pieces by merge_shared_kernel.
+// The tiles of all items are laid end to end and cut into one contiguous range per worker (a CTA, two per SM), so that one
+// long prefix fills the GPU as well as many short ones, whatever the mix.  A worker's part of an item is a piece: normalised
+// partial rows and log-sum-exps in the workspace, merged by merge_shared_kernel.  (The own contexts were first left to
+// decode_stream.cu, beside or behind the group pass: 113 against 70 us for 256 sequences in 12 groups; its mma.sync work
+// takes issue slots and tensor cycles from the group pass, and its workers drain between two 16-token tiles.)
 //
-// Rows see whole tiles only: sequence s attends to the first e_s = floor(min(prefix, n_s) / 64) * 64 tokens here and to the
-// rest in its own pass.  So no tile is masked inside, and where sequences of a group differ in e_s (the tiles are taken from
-// the last one backwards) a row that has not begun simply discards what it accumulated: its O is set to zero, not
-// multiplied by zero, at its first tile, and nothing it does not see can reach it, not even a NaN.
+// A sequence sees whole tiles of its group only: the first e_s = floor(min(prefix, n_s) / 64) * 64 tokens, the rest is its
+// own.  So no group tile is masked inside, and where sequences of a group differ in e_s (the tiles are taken from the last
+// one backwards) a row that has not begun simply discards what it accumulated: its O is set to zero, not multiplied by zero,
+// at its first tile, and nothing it does not see can reach it, not even a NaN.
 //
-// Eight warps: 0-3 one thread per row (softmax), 4 and 6 the TMA producers of Q, K and of V, 5 and 7 issue S = Q K^T and
-// O += P V.  All of them walk the same list of pieces.  Every wait is a bounded mbarrier wait.  (A single producer was what
-// the pass waited for: a copy of 16 rows costs its warp about 90 cycles, 16 of them a tile; and a single issuing thread
-// adds the waits for K, V and P up, 1690 cycles a tile against 1100 of softmax.)
+// Eight warps: 0-3 one thread per row (softmax), 4 the list of pieces and the TMA copies of Q and K, 6 those of V, 5 and 7
+// issue S = Q K^T and O += P V.  (One producer was what everything waited for: a copy of 16 rows costs its warp about 90
+// cycles, 16 of them a tile; and one issuing thread adds the waits for K, V and P up, 1690 cycles a tile.)  Every wait is a
+// bounded mbarrier wait.
+#include <type_traits>
+
 #include "umma.cuh"
 
 namespace optgqa {
@@ -32,23 +37,28 @@ namespace {
 
 constexpr int kRows = kSharedRows;
 constexpr int kTN = kSharedTile;
-constexpr int kKStages = 3;
-constexpr int kVStages = 2;
+constexpr int kStages = 2;                 // of the K ring and of the V ring
+constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
-constexpr int kMaxRegs = 160;              // two of these warps and one of the own pass's (184) share a scheduler's 512
-constexpr int kMinTiles = 2;               // tiles a worker gets at least
+// What the even cut counts, in units of about 550 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp),
+// and what an own item costs besides (Q, the wait for its last P V, storing the piece).
+constexpr int kGroupTile = 4, kOwnTile = 3, kOwnItem = 5;
+constexpr int kMinUnits = 4;               // a worker's share at least: every share holds a tile of each item it touches
+constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
 
-constexpr int kHalfBytes = kTN * 128;      // one 64-dim column half of a K or V tile
+constexpr int kHalfBytes = kTN * 128;      // one 64-dim column half of a K tile
 constexpr int kQHalfBytes = kRows * 128;   // one 64-dim column half of the Q tile
 // The ALiBi term inside a tile rides on the tensor core as one more k-step (see prefill_umma.cu): slope / |scale| as
 // three bf16 values against the key's index in the tile.
 constexpr int kExtRowGroupBytes = 256;
 constexpr int kQxBytes = kRows / 8 * kExtRowGroupBytes;
 constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
-// barriers: q_full, q_empty, qx_full, o_empty, k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2]
-constexpr int kNumBars = 4 + 2 * kKStages + 2 * kVStages + 4;
+// barriers: q_full, q_empty, o_empty, k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
+// desc_full[], desc_empty[]
+constexpr int kNumBars = 4 + 4 * kStages + 4 + 2 * kDescs;          // (one to spare: an even number)
+constexpr int kDescReaders = 7;            // warps that read a descriptor: all but the one that writes it
 
 template <int D>
 struct ShLayout {
@@ -57,11 +67,12 @@ struct ShLayout {
     static constexpr int kQBytes = kHalves * kQHalfBytes;
     static constexpr int kOffQ = 0;
     static constexpr int kOffK = kQBytes;
-    static constexpr int kOffV = kOffK + kKStages * kTileBytes;
-    static constexpr int kOffQx = kOffV + kVStages * kTileBytes;
+    static constexpr int kOffV = kOffK + kStages * kTileBytes;
+    static constexpr int kOffQx = kOffV + kStages * kTileBytes;
     static constexpr int kOffKp = kOffQx + kQxBytes;
     static constexpr int kOffBar = kOffKp + kKpBytes;
-    static constexpr int kOffGroups = kOffBar + kNumBars * 8 + 16;      // tiles before (8 B), tiles, leader, items before (2 B)
+    static constexpr int kOffDesc = kOffBar + kNumBars * 8 + 16;
+    static constexpr int kOffGroups = kOffDesc + kDescs * 48;           // tiles before (8 B), tiles, leader, items before (2 B)
     static constexpr int kSmemBytes = kOffGroups + kMaxGroups * 18 + 1024;
 };
 
@@ -75,26 +86,28 @@ struct SharedParams {
     const int32_t* prefix_lens;
     const int32_t* group_start;
     const float* slopes;
-    float* partial_out;
-    float* partial_lse;
-    int32_t* info;              // per (sequence, KV head): see SharedLayout
+    int32_t* info;              // see SharedLayout, as the pieces below
+    float* group_lse;
+    float* group_out;
+    float* own_lse;
+    float* own_out;
     int* status;
     float scale;
     int num_groups, B, max_blocks, Hq, Hkv, bs, lanes_log2;
 };
 
-// A worker's place in the items laid end to end: (group, KV head, row block), row block fastest, so that the blocks of one
-// prefix are worked on at the same time and its tiles come from L2 after their first reading.
-struct PieceCursor {
-    int g, kvh, mt;             // the item
-    int kt, blocks, jt;         // its tiles, the group's row blocks, the tile inside the item
-    long long item, pos;        // number of the item, position in the tiles of all items
+// What the other warps need to know of a piece.
+struct Piece {
+    int s0, rows, kvh, table;       // first sequence, live rows, KV head, sequence whose page table is walked
+    int tile_hi, len, n, piece;     // last tile (of the sequence's 64-key tiles) and how many, keys there are, number
+    int own, opens, closes, pad;    // own item or a group's; whether the piece holds the item's first and last tile
 };
 
 template <int D, int G>
-__global__ void __maxnreg__(kMaxRegs)
-decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                     const __grid_constant__ CUtensorMap map_v, const SharedParams p) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q1,
+                     const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                     const SharedParams p) {
     using L = ShLayout<D>;
     constexpr int kTileBytes = L::kTileBytes, kOffQ = L::kOffQ, kOffK = L::kOffK, kOffV = L::kOffV, kOffQx = L::kOffQx,
                   kOffKp = L::kOffKp;
@@ -104,34 +117,60 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
     uint64_t* q_full = bars;
     uint64_t* q_empty = bars + 1;
-    uint64_t* qx_full = bars + 2;
-    uint64_t* o_empty = bars + 3;
-    uint64_t* k_full = bars + 4;
-    uint64_t* k_empty = k_full + kKStages;
-    uint64_t* v_full = k_empty + kKStages;
-    uint64_t* v_empty = v_full + kVStages;
-    uint64_t* s_full = v_empty + kVStages;
+    uint64_t* o_empty = bars + 2;
+    uint64_t* k_full = bars + 3;
+    uint64_t* k_empty = k_full + kStages;
+    uint64_t* v_full = k_empty + kStages;
+    uint64_t* v_empty = v_full + kStages;
+    uint64_t* s_full = v_empty + kStages;
     uint64_t* p_full = s_full + 2;
+    uint64_t* desc_full = p_full + 2;
+    uint64_t* desc_empty = desc_full + kDescs;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+    const int4* descs = reinterpret_cast<const int4*>(smem + L::kOffDesc);
     long long* g_tiles = reinterpret_cast<long long*>(smem + L::kOffGroups);     // exclusive sums over the groups, one head
     int* g_kt = reinterpret_cast<int*>(g_tiles + kMaxGroups);
     int* g_lead = g_kt + kMaxGroups;
     uint16_t* g_items = reinterpret_cast<uint16_t*>(g_lead + kMaxGroups);        // at most kMaxGroups + 65535 * 8 / 128
+    // units of the own items (one head) of the sequences of each thread's chunk, then exclusive sums; gone once the K ring is
+    // in use
+    long long* c_units = reinterpret_cast<long long*>(smem + kOffK);
 
+    grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int N = p.num_groups;
-    if (threadIdx.x == 128) {
+    if (threadIdx.x == 192) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q1) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
     auto group_lo = [&](int g) { return min(max(__ldg(p.group_start + g), 0), p.B); };
-    auto blocks_of = [&](int g) { return max(group_lo(g + 1) - group_lo(g), 0) * G / kRows +
-                                         (max(group_lo(g + 1) - group_lo(g), 0) * G % kRows != 0); };
+    auto blocks_of = [&](int g) {
+        const int rows = max(group_lo(g + 1) - group_lo(g), 0) * G;
+        return rows / kRows + (rows % kRows != 0);
+    };
+    const int grouped_lo = __ldg(p.group_start), grouped_hi = __ldg(p.group_start + N);
+    // tiles of sequence s (of length n) at which its own begin and end
+    auto own_begin = [&](int s, int n) {
+        return s >= grouped_lo && s < grouped_hi ? shared_tokens(__ldg(p.prefix_lens + s), n) / kTN : 0;
+    };
+    auto own_end = [&](int n) { return (max(n, 0) + kTN - 1) / kTN; };
+    auto item_units = [&](int tiles) { return tiles > 0 ? kOwnItem + kOwnTile * (long long)tiles : 0ll; };
 
-    // ------------------------------------------------------------------ the groups: longest shared run, whose it is
-    // (the index arrays are read before the wait for the preceding kernel: see the ordering contract in the header)
+    // ------------------------------------------------------------------ the items (the index arrays are read before the
+    // wait for the preceding kernel: see the ordering contract in the header)
+    const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
+    {
+        long long sum = 0;
+        for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) {
+            const int n = __ldg(p.context_lens + s);
+            sum += item_units(own_end(n) - own_begin(s, n));
+        }
+        c_units[threadIdx.x] = sum;
+    }
     if (warp < 4) {
+        // of each group the longest shared run, and whose it is: 2^lanes_log2 lanes per group
         const int lanes = 1 << p.lanes_log2, sub = lane & (lanes - 1), per_warp = 32 >> p.lanes_log2;
         for (int g0 = warp * per_warp; g0 < N; g0 += 4 * per_warp) {
             const int g = g0 + (lane >> p.lanes_log2);
@@ -156,15 +195,11 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (threadIdx.x == 128) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
-        mbar_init(qx_full, kRows);
         mbar_init(o_empty, kRows);
 #pragma unroll
-        for (int i = 0; i < kKStages; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&k_full[i], 1);
             mbar_init(&k_empty[i], 1);
-        }
-#pragma unroll
-        for (int i = 0; i < kVStages; ++i) {
             mbar_init(&v_full[i], 1);
             mbar_init(&v_empty[i], 1);
         }
@@ -173,19 +208,23 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], kRows);
         }
+#pragma unroll
+        for (int i = 0; i < kDescs; ++i) {
+            mbar_init(&desc_full[i], 1);
+            mbar_init(&desc_empty[i], kDescReaders);
+        }
         tmem_slot[1] = 0;
         fence_barrier_init();
     }
     // The scale may have any sign (see prefill_umma.cu).
     const float sabs = p.scale == 0.f ? 1.f : fabsf(p.scale);
     const bool alibi = p.slopes != nullptr || p.scale == 0.f;
-    if (alibi && threadIdx.x >= kRows) {
-        for (int e = threadIdx.x - kRows; e < kTN; e += kThreads - kRows) {
-            const uint32_t eb = __bfloat16_as_ushort(__float2bfloat16_rn((float)e));      // exact: e < 256
-            char* row = smem + kOffKp + (e >> 3) * kExtRowGroupBytes + (e & 7) * 16;
-            *reinterpret_cast<uint4*>(row) = make_uint4(eb | (eb << 16), eb, 0u, 0u);
-            *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
-        }
+    if (alibi && threadIdx.x >= kThreads - kTN) {
+        const int e = threadIdx.x - (kThreads - kTN);
+        const uint32_t eb = __bfloat16_as_ushort(__float2bfloat16_rn((float)e));      // exact: e < 256
+        char* row = smem + kOffKp + (e >> 3) * kExtRowGroupBytes + (e & 7) * 16;
+        *reinterpret_cast<uint4*>(row) = make_uint4(eb | (eb << 16), eb, 0u, 0u);
+        *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
         fence_proxy_async();
     }
     if (warp == 5) {
@@ -194,169 +233,297 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    __syncthreads();
-    // Exclusive sums over the groups, by one warp.  A group_start that is not increasing may name more row blocks than the
-    // workspace has room for: the groups past it are left out (a wrong row, never a write outside).
-    __shared__ long long s_total;
-    if (warp == 0) {
-        long long tiles = 0;
-        int items = 0;
-        const int most = N + (int)((long long)p.B * G / kRows);
-        for (int g0 = 0; g0 < N; g0 += 32) {
-            const int g = g0 + lane;
-            int b = g < N && g_kt[g] > 0 ? blocks_of(g) : 0, kt = g < N ? g_kt[g] : 0;
-            int incl = b;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(kFull, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (items + incl > most) b = 0, kt = 0;       // (items + incl only grows: all later ones too)
-            long long incl_t = (long long)b * kt;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(kFull, incl_t, o);
-                if (lane >= o) incl_t += v;
-            }
-            if (g < N) {
-                g_tiles[g] = tiles + incl_t - (long long)b * kt;
-                g_items[g] = (uint16_t)min(items + incl - b, most);
-                g_kt[g] = kt;
-            }
-            tiles += __shfl_sync(kFull, incl_t, 31);
-            items += __shfl_sync(kFull, incl, 31);
-        }
-        if (lane == 0) s_total = tiles * p.Hkv;
-    }
+    fence_proxy_async();                // c_units lies where the copies of K will land
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    const long long total = s_total, me = blockIdx.x;
-    const long long by_size = total / kMinTiles > 0 ? total / kMinTiles : (total > 0 ? 1 : 0);
-    const long long workers = by_size < gridDim.x ? by_size : gridDim.x;
-    // The cache and q may still be written, the workspace still read, by the preceding kernel: the producer waits for it
-    // before its first copy, and everything this CTA writes follows from that copy.  The kernel after this one (the own
-    // pass) is let go only behind that wait: it then runs beside this grid without a wait of its own.
-    if (total == 0) grid_dependency_wait();         // a grid none of whose CTAs waited could finish before its predecessor
 
-    if (me < workers) {
-        const long long lo = total * me / workers, hi = total * (me + 1) / workers;
-        PieceCursor cur;
-        auto enter_group = [&]() {
-            cur.kt = g_kt[cur.g];
-            cur.blocks = blocks_of(cur.g);
-        };
+    if (warp == 4) {
+        // ------------------------------------------------------------------ the list of pieces, Q and K
+        // Exclusive sums over the groups.  A group_start that is not increasing may name more row blocks than the workspace
+        // has room for: the groups past it are left out (a wrong row, never a write outside).
+        long long group_total = 0, own_total = 0;
         {
-            int a = 0, b = N - 1;           // the last group whose tiles begin at or before lo and that has any
+            int items = 0;
+            const int most = N + (int)((long long)p.B * G / kRows);
+            for (int g0 = 0; g0 < N; g0 += 32) {
+                const int g = g0 + lane;
+                int b = g < N && g_kt[g] > 0 ? blocks_of(g) : 0, kt = g < N ? g_kt[g] : 0;
+                int incl = b;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int v = __shfl_up_sync(kFull, incl, o);
+                    if (lane >= o) incl += v;
+                }
+                if (items + incl > most) b = 0, kt = 0;       // (items + incl only grows: all later ones too)
+                long long incl_t = (long long)b * kt;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long v = __shfl_up_sync(kFull, incl_t, o);
+                    if (lane >= o) incl_t += v;
+                }
+                if (g < N) {
+                    g_tiles[g] = group_total + incl_t - (long long)b * kt;
+                    g_items[g] = (uint16_t)min(items + incl - b, most);
+                    g_kt[g] = kt;
+                }
+                group_total += __shfl_sync(kFull, incl_t, 31);
+                items += __shfl_sync(kFull, incl, 31);
+            }
+            group_total *= kGroupTile * p.Hkv;
+            for (int c0 = 0; c0 < kThreads; c0 += 32) {
+                const long long mine = c_units[c0 + lane];
+                long long incl = mine;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const long long v = __shfl_up_sync(kFull, incl, o);
+                    if (lane >= o) incl += v;
+                }
+                c_units[c0 + lane] = own_total + incl - mine;
+                own_total += __shfl_sync(kFull, incl, 31);
+            }
+            own_total *= p.Hkv;
+            __syncwarp();
+        }
+        const long long total = group_total + own_total, me = blockIdx.x;
+        const long long by_size = total / kMinUnits > 0 ? total / kMinUnits : (total > 0 ? 1 : 0);
+        const long long workers = by_size < gridDim.x ? by_size : gridDim.x;
+        const long long lo = me < workers ? total * me / workers : 0, hi = me < workers ? total * (me + 1) / workers : 0;
+        long long pos = hi;                 // unit at which the next tile to be described lies; a tile belongs to the share it lies in
+        // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
+        // at the same time and its tiles come from L2 after their first reading; then (sequence, KV head)
+        int g = 0, kvh = 0, mt = 0, blocks = 1, s = 0, n = 0, jt = 0, t0 = 0, t1 = 0;    // the item's tiles t0 .. t1 - 1
+        long long item = 0;
+        auto enter_group = [&]() {
+            t0 = 0;
+            t1 = g_kt[g];
+            blocks = blocks_of(g);
+        };
+        auto enter_sequence = [&]() {       // s, or the first one behind it that has tiles of its own
+            for (;; ++s) {
+                n = s < p.B ? __ldg(p.context_lens + s) : 0;
+                t0 = s < p.B ? own_begin(s, n) : 0;
+                t1 = own_end(n);
+                if (t1 > t0 || s >= p.B) return;
+            }
+        };
+        const long long first_tile = (lo + kGroupTile - 1) / kGroupTile;       // of the groups' tiles
+        if (lo < hi && first_tile * kGroupTile < group_total) {
+            int a = 0, b = N - 1;           // the last group that begins at or before it (and so one that has tiles)
             while (a < b) {
                 const int m = (a + b + 1) >> 1;
-                if (g_tiles[m] * p.Hkv <= lo) a = m;
+                if (g_tiles[m] * p.Hkv <= first_tile) a = m;
                 else b = m - 1;
             }
-            cur.g = a;
+            g = a;
             enter_group();
-            const long long r = lo - g_tiles[a] * p.Hkv;
-            const int in_group = (int)(r / cur.kt);
-            cur.jt = (int)(r - (long long)in_group * cur.kt);
-            cur.kvh = in_group / cur.blocks;
-            cur.mt = in_group - cur.kvh * cur.blocks;
-            cur.item = (long long)g_items[a] * p.Hkv + in_group;
-            cur.pos = lo;
-        }
-        auto piece_len = [&]() { return (int)min((long long)(cur.kt - cur.jt), hi - cur.pos); };
-        auto next_piece = [&](int len) {
-            cur.pos += len;
-            cur.jt = 0;
-            ++cur.item;
-            if (cur.pos >= hi || ++cur.mt < cur.blocks) return;
-            cur.mt = 0;
-            if (++cur.kvh < p.Hkv) return;
-            cur.kvh = 0;
-            do ++cur.g;
-            while (cur.g < N - 1 && g_kt[cur.g] == 0);
-            enter_group();
-            cur.item = (long long)g_items[cur.g] * p.Hkv;
-        };
-
-        if (warp == 4 || warp == 6) {
-            // -------------------------------------------------------------- producers: warp 4 Q and K, warp 6 V
-            // A slice is the bs tokens of a page.  K: one box of bs rows x 64 dims per slice and half, so that the 64 rows of
-            // a half lie together; V: one box of all of a slice (see issue_pv for its layout).
-            const bool is_k = warp == 4;
-            const int slices = kTN / p.bs, sub = lane % slices, hf = lane / slices;
-            const bool issues = lane < (is_k ? slices * L::kHalves : slices);
-            uint64_t *full = is_k ? k_full : v_full, *empty = is_k ? k_empty : v_empty;
-            const int stages = is_k ? kKStages : kVStages;
-            char* ring = smem + (is_k ? kOffK + hf * kHalfBytes + sub * p.bs * 128 : kOffV + sub * p.bs * (D * 2));
-            int pc = 0, st = 0;
-            uint32_t ph = 1;                                    // parity of a stage's last release (none yet: passes)
-            bool ok = true;
-            while (ok && cur.pos < hi) {
-                const int len = piece_len(), kvh = cur.kvh;
-                const int32_t* table = p.block_tables + (size_t)g_lead[cur.g] * p.max_blocks;
-                const int tile_hi = cur.jt + len - 1;
-                auto page_of = [&](int j) {
-                    return issues ? __ldg(table + min((tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
-                };
-                int page = page_of(0);
-                if (pc == 0) {
-                    grid_dependency_wait();
-                    if (is_k) grid_dependency_launch();
+            const long long r = first_tile - g_tiles[g] * p.Hkv;
+            const int in_group = (int)(r / t1);
+            jt = (int)(r - (long long)in_group * t1);
+            kvh = in_group / blocks;
+            mt = in_group - kvh * blocks;
+            item = (long long)g_items[g] * p.Hkv + in_group;
+            pos = first_tile * kGroupTile;
+        } else if (lo < hi && own_total > 0) {
+            const long long x = max(lo - group_total, 0ll);
+            int a = 0, b = kThreads - 1;    // the last chunk that begins at or before it
+            while (a < b) {
+                const int m = (a + b + 1) >> 1;
+                if (c_units[m] * p.Hkv <= x) a = m;
+                else b = m - 1;
+            }
+            long long before = c_units[a] * p.Hkv;
+            s = a * chunk;
+            for (;; ++s) {
+                enter_sequence();
+                if (s >= p.B || before + item_units(t1 - t0) * p.Hkv > x) break;
+                before += item_units(t1 - t0) * p.Hkv;
+            }
+            if (s < p.B) {                  // (always: x < own_total)
+                kvh = (int)((x - before) / item_units(t1 - t0));
+                const long long r = x - before - kvh * item_units(t1 - t0) - kOwnItem;      // tile j lies at kOwnTile * j
+                jt = r > 0 ? (int)((r + kOwnTile - 1) / kOwnTile) : 0;                         // < t1 - t0 unless the item is over
+                pos = group_total + x - r + (long long)jt * kOwnTile;
+                if (jt == t1 - t0) {
+                    jt = 0;
+                    pos += kOwnItem;
+                    if (++kvh == p.Hkv) {
+                        kvh = 0;
+                        ++s;
+                        enter_sequence();
+                        if (s >= p.B) pos = hi;
+                    }
                 }
-                if (is_k) {
+            }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        grid_dependency_wait();             // q and the cache may still be written, the workspace still read, by the preceding kernel
+
+        const int slices = kTN / p.bs, sub = lane % slices, hf = lane / slices;
+        const bool issues = lane < slices * L::kHalves;
+        char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
+        int st = 0;
+        uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
+        bool ok = true;
+        for (int pc = 0; ok; ++pc) {
+            const bool own = pos >= group_total;
+            const int weight = own ? kOwnTile : kGroupTile;
+            const int len = pos < hi ? (int)min((long long)(t1 - t0 - jt), (hi - pos + weight - 1) / weight) : 0;
+            const int s0 = own ? s : group_lo(g) + mt * TQ;
+            const int rows = own ? G : min(kRows, (group_lo(g + 1) - s0) * G);
+            const int table_of = own ? s : g_lead[g], tile_hi = t0 + jt + len - 1, keys = own ? n : t1 * kTN;
+            ok = __all_sync(kFull, mbar_wait(&desc_empty[pc % kDescs], ((pc / kDescs) & 1) ^ 1, p.status));
+            if (!ok) break;
+            if (lane == 0) {
+                int4* d = reinterpret_cast<int4*>(smem + L::kOffDesc) + 3 * (pc % kDescs);
+                d[0] = make_int4(s0, rows, kvh, table_of);
+                d[1] = make_int4(tile_hi, len, keys, (int)((own ? (long long)s * p.Hkv + kvh : item) + me));
+                d[2] = make_int4(own, jt == 0, jt + len == t1 - t0, 0);
+                mbar_arrive(&desc_full[pc % kDescs]);
+            }
+            if (len == 0) break;
+            const int32_t* table = p.block_tables + (size_t)table_of * p.max_blocks;
+            auto page_of = [&](int j) {
+                return issues ? __ldg(table + min((tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
+            };
+            int page = page_of(0);
+            for (int j = 0; j < len; ++j) {
+                const int page_next = j + 1 < len ? page_of(j + 1) : 0;
+                const int row = (page * p.Hkv + kvh) * p.bs;                       // row of the [rows, D] view
+                const int live = min(slices, (keys - (tile_hi - j) * kTN + p.bs - 1) / p.bs);    // slices that hold keys
+                ok = __all_sync(kFull, mbar_wait(&k_empty[st], ph, p.status));
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)(live * p.bs * D * 2));
+                __syncwarp();
+                if (issues && sub < live) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st]);
+                page = page_next;
+                if (++st == kStages) st = 0, ph ^= 1;
+                if (j == 0) {               // Q behind the first K tile, which does not have to wait for the piece before
                     if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
                     if (!ok) break;
                     if (lane == 0) {
-                        mbar_expect_tx(q_full, L::kQBytes);
+                        // an own item's G rows alone: what the other rows of the tile hold reaches no live row
+                        mbar_expect_tx(q_full, own ? (uint32_t)(G * D * 2) : (uint32_t)L::kQBytes);
 #pragma unroll
                         for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_3d(smem + kOffQ + h * kQHalfBytes, &map_q, 64 * h, kvh * G, group_lo(cur.g) + cur.mt * TQ, q_full);
+                            tma_load_3d(smem + kOffQ + h * kQHalfBytes, own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, q_full);
                     }
                 }
-                for (int j = 0; j < len; ++j) {
-                    const int page_next = j + 1 < len ? page_of(j + 1) : 0;
-                    const int row = (page * p.Hkv + kvh) * p.bs;                       // row of the [rows, D] view
-                    ok = __all_sync(kFull, mbar_wait(&empty[st], ph, p.status));
+            }
+            // on to the next piece
+            pos += (long long)weight * len;
+            jt = 0;
+            if (own) {
+                pos += kOwnItem;
+                if (pos < hi && ++kvh == p.Hkv) {
+                    kvh = 0;
+                    ++s;
+                    enter_sequence();
+                    if (s >= p.B) pos = hi;
+                }
+            } else if (pos < hi) {
+                ++item;
+                if (pos >= group_total) {
+                    pos += kOwnItem;
+                    kvh = 0;
+                    s = 0;
+                    enter_sequence();
+                    if (s >= p.B) pos = hi;
+                } else if (++mt == blocks) {
+                    mt = 0;
+                    if (++kvh == p.Hkv) {
+                        kvh = 0;
+                        do ++g;
+                        while (g < N - 1 && g_kt[g] == 0);
+                        enter_group();
+                        item = (long long)g_items[g] * p.Hkv;
+                    }
+                }
+            }
+        }
+    } else {
+        // what every other warp does first with the next piece; false at the end of the list
+        Piece d;
+        auto next_piece = [&](int pc, bool& ok) -> bool {
+            ok = __all_sync(kFull, mbar_wait(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
+            if (!ok) return false;
+            const int4 *at = descs + 3 * (pc % kDescs), a = at[0], b = at[1], c = at[2];
+            d.s0 = a.x, d.rows = a.y, d.kvh = a.z, d.table = a.w;
+            d.tile_hi = b.x, d.len = b.y, d.n = b.z, d.piece = b.w;
+            d.own = c.x, d.opens = c.y, d.closes = c.z;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&desc_empty[pc % kDescs]);
+            return d.len > 0;
+        };
+        bool ok = true;
+        if (warp == 6) {
+            // -------------------------------------------------------------- V
+            // A box is all of a slice (the bs tokens of a page), half after half: see the issuing thread for the layout.
+            const int slices = kTN / p.bs, sub = lane % slices;
+            const bool issues = lane < slices;
+            char* ring = smem + kOffV + sub * p.bs * (D * 2);
+            int st = 0;
+            uint32_t ph = 1;
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const int32_t* table = p.block_tables + (size_t)d.table * p.max_blocks;
+                auto page_of = [&](int j) {
+                    return issues ? __ldg(table + min((d.tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
+                };
+                int page = page_of(0);
+                if (pc == 0) grid_dependency_wait();
+                for (int j = 0; j < d.len; ++j) {
+                    const int page_next = j + 1 < d.len ? page_of(j + 1) : 0;
+                    const int row = (page * p.Hkv + d.kvh) * p.bs;
+                    const int live = min(slices, (d.n - (d.tile_hi - j) * kTN + p.bs - 1) / p.bs);
+                    ok = __all_sync(kFull, mbar_wait(&v_empty[st], ph, p.status));
                     if (!ok) break;
-                    if (lane == 0) mbar_expect_tx(&full[st], (uint32_t)kTileBytes);
+                    if (lane == 0) mbar_expect_tx(&v_full[st], (uint32_t)(live * p.bs * D * 2));
                     __syncwarp();
-                    if (issues) {
-                        if (is_k) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &full[st]);
-                        else tma_load_3d(ring + st * kTileBytes, &map_v, 0, row, 0, &full[st]);
-                    }
+                    if (issues && sub < live) tma_load_3d(ring + st * kTileBytes, &map_v, 0, row, 0, &v_full[st]);
                     page = page_next;
-                    if (++st == stages) st = 0, ph ^= 1;
+                    if (++st == kStages) st = 0, ph ^= 1;
                 }
-                next_piece(len);
-                ++pc;
+                if (!ok) break;
             }
         } else if (warp == 5) {
             // -------------------------------------------------------------- one thread issues S = Q K^T
-            if (lane == 0) {
-                constexpr uint32_t idesc_s = instr_desc(false, kTN);
-                const uint32_t idesc_qk = p.scale < 0.f ? instr_desc(false, kTN, true) : idesc_s;
-                const bool dots = p.scale != 0.f;
-                uint64_t q_desc[D / 16];
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    q_desc[ks] = smem_desc(smem_u32(smem + kOffQ) + (ks >> 2) * kQHalfBytes + (ks & 3) * 32, 16, 1024);
-                const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
-                const uint64_t qx_desc = smem_desc_plain(smem_u32(smem + kOffQx), 128, kExtRowGroupBytes);
-                const uint64_t kp_desc = smem_desc_plain(smem_u32(smem + kOffKp), 128, kExtRowGroupBytes);
-                int it = 0, pc = 0, st = 0, vst = 0;
-                uint32_t ph = 0, vph = 1;
-                bool ok = true;
-                while (ok && cur.pos < hi) {
-                    const int len = piece_len();
-                    ok = mbar_wait(q_full, pc & 1, p.status) && (!alibi || mbar_wait(qx_full, pc & 1, p.status));
-                    for (int j = 0; ok && j < len; ++j, ++it) {
+            constexpr uint32_t idesc_s = instr_desc(false, kTN);
+            const uint32_t idesc_qk = p.scale < 0.f ? instr_desc(false, kTN, true) : idesc_s;
+            const bool dots = p.scale != 0.f;
+            const uint64_t q_desc0 = smem_desc(smem_u32(smem + kOffQ), 16, 1024);
+            const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
+            const uint64_t qx_desc = smem_desc_plain(smem_u32(smem + kOffQx), 128, kExtRowGroupBytes);
+            const uint64_t kp_desc = smem_desc_plain(smem_u32(smem + kOffKp), 128, kExtRowGroupBytes);
+            int it = 0, st = 0;
+            uint32_t ph = 0;
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                if (alibi) {
+                    // The ALiBi step's operand for this KV head: slope / |scale| as a sum of three bf16 values, the rows a head
+                    // each in turn.  Nothing reads the one before once that piece's last scores are there.
+                    if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
+                    if (!ok) break;
+                    for (int r = lane; r < kRows; r += 32) {
+                        const float a = p.slopes ? __ldg(p.slopes + d.kvh * G + r % G) / sabs : 0.f;
+                        const __nv_bfloat16 a0 = __float2bfloat16_rn(a);
+                        const __nv_bfloat16 a1 = __float2bfloat16_rn(a - __bfloat162float(a0));
+                        const __nv_bfloat16 a2 = __float2bfloat16_rn(a - __bfloat162float(a0) - __bfloat162float(a1));
+                        char* row = smem + kOffQx + (r >> 3) * kExtRowGroupBytes + (r & 7) * 16;
+                        *reinterpret_cast<uint4*>(row) = make_uint4((uint32_t)__bfloat16_as_ushort(a0) | ((uint32_t)__bfloat16_as_ushort(a1) << 16),
+                                                                    (uint32_t)__bfloat16_as_ushort(a2), 0u, 0u);
+                        *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                if (lane == 0) {
+                    ok = mbar_wait(q_full, pc & 1, p.status);
+                    for (int j = 0; ok && j < d.len; ++j, ++it) {
                         const int sb = it & 1;
                         // the score buffer is free once the P V of the tile before the last one has read its weights there
-                        if (it >= 2) {
-                            ok = mbar_wait(&v_empty[vst], vph ^ 1, p.status);
-                            if (++vst == kVStages) vst = 0, vph ^= 1;
-                        }
+                        // (kStages is 2: that tile's V stage is this tile's)
+                        if (it >= 2) ok = mbar_wait(&v_empty[st], ph ^ 1, p.status);
                         ok = ok && mbar_wait(&k_full[st], ph, p.status);
                         if (!ok) break;
                         tc_fence_after();
@@ -365,102 +532,96 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         if (dots) {
 #pragma unroll
                             for (int ks = 0; ks < D / 16; ++ks)
-                                umma_ss(s_tmem, q_desc[ks], desc_advance(kd, (ks >> 2) * kHalfBytes + (ks & 3) * 32), idesc_qk, ks > 0);
+                                umma_ss(s_tmem, desc_advance(q_desc0, (ks >> 2) * kQHalfBytes + (ks & 3) * 32),
+                                        desc_advance(kd, (ks >> 2) * kHalfBytes + (ks & 3) * 32), idesc_qk, ks > 0);
                         }
                         if (alibi) umma_ss(s_tmem, qx_desc, kp_desc, idesc_s, dots);
                         tc_commit(&s_full[sb]);
                         tc_commit(&k_empty[st]);
-                        if (j == len - 1) tc_commit(q_empty);
-                        if (++st == kKStages) st = 0, ph ^= 1;
+                        if (j == d.len - 1) tc_commit(q_empty);
+                        if (++st == kStages) st = 0, ph ^= 1;
                     }
-                    next_piece(len);
-                    ++pc;
                 }
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
             }
         } else if (warp == 7) {
             // -------------------------------------------------------------- one thread issues O (+)= P V
-            if (lane == 0) {
-                constexpr uint32_t idesc_pv = instr_desc(true, D);
-                // V is MN-major, in slices of bs keys with the 64-dim halves of a slice side by side: halves bs * 128 bytes
-                // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
-                const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
-                int it = 0, pc = 0, st = 0;
-                uint32_t ph = 0;
-                bool ok = true;
-                while (ok && cur.pos < hi) {
-                    const int len = piece_len();
-                    for (int j = 0; ok && j < len; ++j, ++it) {
-                        const int sb = it & 1;
-                        ok = mbar_wait(&v_full[st], ph, p.status) && mbar_wait(&p_full[sb], (it >> 1) & 1, p.status) &&
-                             (j > 0 || pc == 0 || mbar_wait(o_empty, (pc - 1) & 1, p.status));    // O of the piece before is read
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t vd = desc_advance(v_desc0, st * kTileBytes);
-                        const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
+            // V is MN-major, in slices of bs keys with the 64-dim halves of a slice side by side: halves bs * 128 bytes
+            // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
+            constexpr uint32_t idesc_pv = instr_desc(true, D);
+            const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
+            int it = 0, st = 0;
+            uint32_t ph = 0;
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                for (int j = 0; j < d.len; ++j, ++it) {
+                    const int sb = it & 1, live = d.n - (d.tile_hi - j) * kTN;      // keys of the tile that exist
+                    ok = __all_sync(kFull, mbar_wait(&v_full[st], ph, p.status));
+                    if (!ok) break;
+                    if (live < kTN) {
+                        // Rows past the sequence's end hold whatever the page held, or stale shared memory where no page
+                        // exists: zero them, so that a weight of 0 times garbage cannot be NaN.
+                        for (int r = live + (lane >> 3); r < kTN; r += 4) {
+                            char* vrow = smem + kOffV + st * kTileBytes + (r / p.bs) * p.bs * (D * 2) + (r % p.bs) * 128 + (lane & 7) * 16;
 #pragma unroll
-                        for (int kk = 0; kk < kTN / 16; ++kk) {
-                            const uint32_t at = p.bs == 16 ? kk * 16 * (D * 2) : (kk >> 1) * 32 * (D * 2) + (kk & 1) * 2048;
-                            umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, at), idesc_pv, j > 0 || kk > 0);
+                            for (int b = 0; b < L::kHalves; ++b)
+                                *reinterpret_cast<uint4*>(vrow + b * p.bs * 128) = make_uint4(0, 0, 0, 0);
                         }
-                        tc_commit(&v_empty[st]);
-                        if (++st == kVStages) st = 0, ph ^= 1;
+                        fence_proxy_async();
+                        __syncwarp();
                     }
-                    next_piece(len);
-                    ++pc;
+                    if (lane == 0) {
+                        ok = mbar_wait(&p_full[sb], (it >> 1) & 1, p.status) &&
+                             (j > 0 || pc == 0 || mbar_wait(o_empty, (pc - 1) & 1, p.status));    // O of the piece before is read
+                        if (ok) {
+                            tc_fence_after();
+                            const uint64_t vd = desc_advance(v_desc0, st * kTileBytes);
+                            const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
+#pragma unroll
+                            for (int kk = 0; kk < kTN / 16; ++kk) {
+                                const uint32_t at = p.bs == 16 ? kk * 16 * (D * 2) : (kk >> 1) * 32 * (D * 2) + (kk & 1) * 2048;
+                                umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, at), idesc_pv, j > 0 || kk > 0);
+                            }
+                            tc_commit(&v_empty[st]);
+                        }
+                    }
+                    ok = __all_sync(kFull, ok);
+                    if (!ok) break;
+                    if (++st == kStages) st = 0, ph ^= 1;
                 }
+                if (!ok) break;
             }
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
             const int r = threadIdx.x, hg = r % G;
             const float qscale = sabs * kLog2e;
             const uint32_t lane_addr = tmem_base + ((uint32_t)(warp * 32) << 16);
-            // The row of the ALiBi step's operand for KV head kvh: slope / |scale| as a sum of three bf16 values.
-            auto write_qx = [&](int kvh) {
-                const float a = p.slopes ? p.slopes[kvh * G + hg] / sabs : 0.f;
-                const __nv_bfloat16 a0 = __float2bfloat16_rn(a);
-                const __nv_bfloat16 a1 = __float2bfloat16_rn(a - __bfloat162float(a0));
-                const __nv_bfloat16 a2 = __float2bfloat16_rn(a - __bfloat162float(a0) - __bfloat162float(a1));
-                char* row = smem + kOffQx + (r >> 3) * kExtRowGroupBytes + (r & 7) * 16;
-                *reinterpret_cast<uint4*>(row) = make_uint4((uint32_t)__bfloat16_as_ushort(a0) | ((uint32_t)__bfloat16_as_ushort(a1) << 16),
-                                                            (uint32_t)__bfloat16_as_ushort(a2), 0u, 0u);
-                *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
-                fence_proxy_async();
-                mbar_arrive(qx_full);
-            };
-            if (alibi) write_qx(cur.kvh);
             int it = 0, st = 0;                     // tile, and the stage and parity of its V
             uint32_t ph = 0;
             // waits for the P V of the tile before this one
             auto prev_pv_done = [&]() {
-                const int ps = st == 0 ? kVStages - 1 : st - 1;
+                const int ps = st == 0 ? kStages - 1 : st - 1;
                 return __all_sync(kFull, mbar_wait(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
             };
-            bool ok = true;
-            while (ok && cur.pos < hi) {
-                const int len = piece_len(), tile_hi = cur.jt + len - 1;
-                const int kvh = cur.kvh;
-                const long long row0 = (cur.item + me) * kRows;
-                const int i = cur.mt * TQ + r / G, s = group_lo(cur.g) + i;
-                const bool valid = s < group_lo(cur.g + 1);
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const int s = d.s0 + r / G;
+                const bool valid = r < d.rows;
                 const int n = valid ? __ldg(p.context_lens + s) : 0;
-                const int e_row = valid ? shared_tokens(__ldg(p.prefix_lens + s), n) : 0;      // keys the row sees
-                const float slope2 = p.slopes ? __ldg(p.slopes + kvh * G + hg) * kLog2e : 0.f;
-                const bool opens = cur.jt == 0, closes = cur.jt + len == cur.kt;
-                next_piece(len);                    // `cur` is the piece after this one from here on
+                // keys the row sees: of a group's item whole tiles
+                const int e_row = !valid ? 0 : d.own ? n : shared_tokens(__ldg(p.prefix_lens + s), n);
+                const float slope2 = p.slopes ? __ldg(p.slopes + d.kvh * G + hg) * kLog2e : 0.f;
                 float m_used = -INFINITY, l = 0.f;
-
                 auto next_tile = [&]() {
                     ++it;
-                    if (++st == kVStages) st = 0, ph ^= 1;
+                    if (++st == kStages) st = 0, ph ^= 1;
                 };
-                for (int j = 0; j < len; ++j, next_tile()) {
-                    const int sb = it & 1, j0 = (tile_hi - j) * kTN;
+                for (int j = 0; j < d.len; ++j, next_tile()) {
+                    const int sb = it & 1, j0 = (d.tile_hi - j) * kTN;
                     ok = __all_sync(kFull, mbar_wait(&s_full[sb], (it >> 1) & 1, p.status));
                     if (!ok) break;
                     tc_fence_after();
-                    // the piece's last scores are there: nothing reads its ALiBi operand any more
-                    if (alibi && j == len - 1 && cur.pos < hi) write_qx(cur.kvh);
                     const bool sees = j0 < e_row;
+                    const bool masked = j0 + kTN > d.n;             // an own item's sequence ends inside the tile
                     if (!__any_sync(kFull, sees)) {
                         // no row of the warp has begun: what the tensor core adds to their O from this tile's scores,
                         // read as if they were weights, is discarded when they do
@@ -483,6 +644,13 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                             for (int e = 0; e < 32; ++e) v[c][e] = __uint_as_float(raw[c][e]);
                         }
                     }
+                    if (masked) {
+                        // -inf in the place of what lies past the end: both passes then run as they are
+                        const int live = d.n - j0;
+#pragma unroll
+                        for (int e = 0; e < kTN; ++e)
+                            if (e >= live) v[e / 32][e % 32] = -INFINITY;
+                    }
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                     for (int c = 0; c < kTN / 32; ++c) chunk_max<false>(v[c], 0, 0, 0, mx);
@@ -497,7 +665,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         ok = prev_pv_done();
                         if (!ok) break;
                         tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D / 32; ++c) {
                             float o[32];
                             uint32_t w[32];
@@ -541,24 +709,36 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 tc_fence_after();
                 if (__any_sync(kFull, valid)) {
                     const float inv = 1.f / l;
-                    const bool begun = (tile_hi - len + 1) * kTN < e_row;          // the row saw a tile of the piece
-                    float* po = p.partial_out + row0 * D + r;                       // [D][kRows]: 32 rows are one line
-#pragma unroll
+                    const bool begun = (d.tile_hi - d.len + 1) * kTN < e_row;      // the row saw a tile of the piece
+                    // a group's piece is [D][128 rows], so that 32 neighbouring rows are one line; an own piece [G][D]
+#pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         float o[32];
                         tmem_ld32(lane_addr + kColO + c * 32, o);
-                        if (begun) {
+                        if (begun && d.own) {
+                            float4* po = reinterpret_cast<float4*>(p.own_out + ((size_t)d.piece * G + r) * D + c * 32);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) po[(c * 32 + e) * kRows] = o[e] * inv;
+                            for (int e = 0; e < 8; ++e)
+                                po[e] = make_float4(o[4 * e] * inv, o[4 * e + 1] * inv, o[4 * e + 2] * inv, o[4 * e + 3] * inv);
+                        } else if (begun) {
+                            float* po = p.group_out + ((size_t)d.piece * D + c * 32) * kRows + r;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) po[e * kRows] = o[e] * inv;
+                        }
+                    }
+                    if (e_row > 0 && hg == 0) {
+                        int32_t* info = p.info + ((size_t)s * p.Hkv + d.kvh) * kInfoWords;
+                        if (d.own) {
+                            if (d.opens) info[4] = d.piece;
+                            if (d.closes) info[5] = d.piece;
+                        } else {
+                            if (d.opens) info[0] = d.piece, info[1] = r;
+                            if (d.closes) info[2] = d.piece;
                         }
                     }
                     // a row that saw nothing of the piece: weight zero
-                    if (e_row > 0 && hg == 0) {
-                        int32_t* info = p.info + ((size_t)s * p.Hkv + kvh) * kInfoWords;
-                        if (opens) info[0] = (int)(row0 / kRows), info[1] = r;
-                        if (closes) info[2] = (int)(row0 / kRows);
-                    }
-                    if (valid) p.partial_lse[row0 + r] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
+                    if (valid)
+                        (d.own ? p.own_lse + (size_t)d.piece * G : p.group_lse + (size_t)d.piece * kRows)[r] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
                 }
                 tc_fence_before();
                 mbar_arrive(o_empty);
@@ -581,10 +761,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 }
 
 // ----------------------------------------------------------------------------- merge
-// A CTA merges 32 rows: 32 / G consecutive sequences times the G heads of one KV head, a lane per row, so that the group
-// pass's pieces ([D][128 rows]) are read as whole lines.  Per row the pieces are one list: the group pass's that cover the
-// sequence's item (numbers item + w, w consecutive workers), then the own pass's (consecutive rows, see reduce.cu).  kWP of
-// the CTA's eight warps share the list, the others (and the grid's y) take other columns, C of them per lane.
+// A CTA merges 32 rows: 32 / G consecutive sequences times the G heads of one KV head, a lane per row, so that a group's
+// pieces ([D][rows]) are read as whole lines.  Per row the pieces are two runs of consecutive numbers, its group item's and its
+// own.  kWP of the CTA's eight warps share the runs, the others (and the grid's z) take other columns, C of them per lane;
+// a warp keeps a running maximum, so that log-sum-exps and rows are requested together, kBatch pieces at a time.
 constexpr int kMergeWarps = 8;
 
 struct MergeParams {
@@ -593,17 +773,17 @@ struct MergeParams {
     const int32_t* prefix_lens;
     const int32_t* group_start;
     const int32_t* info;
-    const float* sh_lse;
-    const float* sh_out;
+    const float* group_lse;
+    const float* group_out;
     const float* own_lse;
     const float* own_out;
-    int num_groups, B, Hq, Hkv;
+    int num_groups, B, Hq, Hkv, group_pieces, own_pieces;
 };
 
 template <int D, int G, int kWP, int C>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 merge_shared_kernel(const MergeParams p) {
-    constexpr int kSeqs = 32 / G;
+    constexpr int kSeqs = 32 / G, kBatch = 32 / C;
     __shared__ float s_max[kWP > 1 ? kMergeWarps : 1][32];
     __shared__ float s_den[kWP > 1 ? kMergeWarps : 1][32];
     __shared__ float s_num[kWP > 1 ? kMergeWarps : 1][C][32];
@@ -618,75 +798,94 @@ merge_shared_kernel(const MergeParams p) {
     const bool has1 = shared > 0, has2 = n > shared;
     grid_dependency_wait();
 
-    // group pass: R1 pieces of kRows rows; own pass: R2 pieces of G rows
     const int32_t* info = p.info + ((size_t)(active ? s : 0) * p.Hkv + kvh) * kInfoWords;
-    const int4 i0 = *reinterpret_cast<const int4*>(info);
-    const int2 i1 = *reinterpret_cast<const int2*>(info + 4);
-    const int R1 = has1 ? i0.z - i0.x + 1 : 0, R2 = has2 ? i1.y - i1.x + 1 : 0;
-    const float* lse1 = p.sh_lse + (has1 ? (size_t)i0.x * kRows + i0.y + hh : 0);
-    const float* po1 = p.sh_out + (has1 ? ((size_t)i0.x * D + d0) * kRows + i0.y + hh : 0);
-    const float* lse2 = p.own_lse + (has2 ? (size_t)i1.x * G + hh : 0);
-    const float* po2 = p.own_out + (has2 ? ((size_t)i1.x * G + hh) * D + d0 : 0);
-    const int R = R1 + R2;
-    float M = -INFINITY;
-    for (int i = wp; i < R1; i += kWP) M = fmaxf(M, lse1[(size_t)i * kRows]);
-    for (int i = wp; i < R2; i += kWP) M = fmaxf(M, lse2[(size_t)i * G]);
-    if (kWP > 1) {
-        s_max[warp][lane] = M;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWP; ++w) M = fmaxf(M, s_max[warp - wp + w][lane]);
-    }
-    float num[C], den = 0.f;
+    int4 i0 = *reinterpret_cast<const int4*>(info);
+    int2 i1 = *reinterpret_cast<const int2*>(info + 4);
+    // Always so, where the index arrays keep their promises; where they do not (a sequence that no group of a group_start
+    // that does not increase covers), the words were never written and the row is wrong, but nothing outside is read.
+    i0.x = min(max(i0.x, 0), p.group_pieces - 1);
+    i0.y = min(max(i0.y, 0), kRows - G);
+    i0.z = min(min(max(i0.z, i0.x), i0.x + kSharedMaxWorkers), p.group_pieces - 1);
+    i1.x = min(max(i1.x, 0), p.own_pieces - 1);
+    i1.y = min(min(max(i1.y, i1.x), i1.x + kSharedMaxWorkers), p.own_pieces - 1);
+
+    float M = -INFINITY, den = 0.f, num[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) num[c] = 0.f;
-    // (loads do not wait for the weight: a row that holds nothing, lse -inf, is selected away; a NaN is carried on)
-#pragma unroll 2
-    for (int i = wp; i < R1; i += kWP) {
-        const float lw = lse1[(size_t)i * kRows];
-        const float* x = po1 + (size_t)i * kRows * D;
-        float y[C];
+    // R pieces of `rows` rows each, log-sum-exps `rows` apart
+    auto sweep = [&](auto is_own, int R, int rows, const float* lse, const float* po) {
+        for (int i = wp; i < R; i += kWP * kBatch) {
+            float lw[kBatch];
+            __align__(16) float x[kBatch][C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) y[c] = x[c * kRows];
-        const bool holds = lw != -INFINITY;
-        const float w = holds ? ex2((lw - M) * kLog2e) : 0.f;
-        den += w;
+            for (int u = 0; u < kBatch; ++u) {
+                const int k = i + u * kWP;
+                lw[u] = -INFINITY;
+                if (k < R) {
+                    lw[u] = lse[(size_t)k * rows];
 #pragma unroll
-        for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? y[c] : 0.f, num[c]);
-    }
-#pragma unroll 2
-    for (int i = wp; i < R2; i += kWP) {
-        const float lw = lse2[(size_t)i * G];
-        const float4* x = reinterpret_cast<const float4*>(po2 + (size_t)i * G * D);
-        float4 y[C / 4];
+                    for (int c = 0; c < C; c += 4) {
+                        if constexpr (decltype(is_own)::value) {        // [rows][D]
+                            *reinterpret_cast<float4*>(&x[u][c]) = *reinterpret_cast<const float4*>(po + (size_t)k * rows * D + c);
+                        } else {                                        // [D][rows]
 #pragma unroll
-        for (int c = 0; c < C / 4; ++c) y[c] = x[c];
-        const bool holds = lw != -INFINITY;
-        const float w = holds ? ex2((lw - M) * kLog2e) : 0.f;
-        den += w;
+                            for (int e = 0; e < 4; ++e) x[u][c + e] = po[((size_t)k * D + c + e) * rows];
+                        }
+                    }
+                }
+            }
+            float top = M;
 #pragma unroll
-        for (int c = 0; c < C / 4; ++c) {
-            num[4 * c] = fmaf(w, holds ? y[c].x : 0.f, num[4 * c]);
-            num[4 * c + 1] = fmaf(w, holds ? y[c].y : 0.f, num[4 * c + 1]);
-            num[4 * c + 2] = fmaf(w, holds ? y[c].z : 0.f, num[4 * c + 2]);
-            num[4 * c + 3] = fmaf(w, holds ? y[c].w : 0.f, num[4 * c + 3]);
+            for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u]);
+            if (top > M) {
+                const float f = ex2((M - top) * kLog2e);        // 0 the first time
+                den *= f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) num[c] *= f;
+                M = top;
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                // -inf: no piece, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
+                const bool holds = lw[u] != -INFINITY;
+                const float w = holds ? ex2((lw[u] - M) * kLog2e) : 0.f;
+                den += w;
+#pragma unroll
+                for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? x[u][c] : 0.f, num[c]);
+            }
         }
-    }
+    };
+    if (has1)
+        sweep(std::false_type(), i0.z - i0.x + 1, kRows, p.group_lse + (size_t)i0.x * kRows + i0.y + hh,
+              p.group_out + ((size_t)i0.x * D + d0) * kRows + i0.y + hh);
+    if (has2)
+        sweep(std::true_type(), i1.y - i1.x + 1, G, p.own_lse + (size_t)i1.x * G + hh,
+              p.own_out + ((size_t)i1.x * G + hh) * D + d0);
     if constexpr (kWP > 1) {
+        s_max[warp][lane] = M;
         s_den[warp][lane] = den;
 #pragma unroll
         for (int c = 0; c < C; ++c) s_num[warp][c][lane] = num[c];
         __syncthreads();
         if (wp != 0) return;
+        float top = M;
+#pragma unroll
+        for (int w = 1; w < kWP; ++w) top = fmaxf(top, s_max[warp + w][lane]);
+        const float sub = top == -INFINITY ? 0.f : top;         // nothing anywhere: 0 weights
+        const float f = ex2((M - sub) * kLog2e);
+        den *= f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) num[c] *= f;
 #pragma unroll
         for (int w = 1; w < kWP; ++w) {
-            den += s_den[warp + w][lane];
+            const float fw = ex2((s_max[warp + w][lane] - sub) * kLog2e);
+            den = fmaf(fw, s_den[warp + w][lane], den);
 #pragma unroll
-            for (int c = 0; c < C; ++c) num[c] += s_num[warp + w][c][lane];
+            for (int c = 0; c < C; ++c) num[c] = fmaf(fw, s_num[warp + w][c][lane], num[c]);
         }
     }
     if (!active) return;
-    const float inv = R > 0 ? 1.f / den : 0.f;                  // an empty sequence gives a zero row
+    const float inv = has1 || has2 ? 1.f / den : 0.f;           // an empty sequence gives a zero row
     uint4* o = reinterpret_cast<uint4*>(p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0);
 #pragma unroll
     for (int c = 0; c < C / 8; ++c)
@@ -695,11 +894,11 @@ merge_shared_kernel(const MergeParams p) {
 }
 
 // ----------------------------------------------------------------------------- host
-// q [B, Hq, D] as a 3-D tensor; a box is 64 dims x the G heads of a group x 128 / G sequences.
-bool make_q_map(CUtensorMap* map, const void* q, int B, int Hq, int G, int D) {
+// q [B, Hq, D] as a 3-D tensor; a box is 64 dims x the G heads of a group x `seqs` sequences.
+bool make_q_map(CUtensorMap* map, const void* q, int B, int Hq, int G, int D, int seqs) {
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)B};
     const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)Hq * D * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)(kRows / G)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)seqs};
     return make_bf16_map(map, q, 3, dims, strides, box);
 }
 
@@ -711,45 +910,33 @@ bool make_slice_map(CUtensorMap* map, const void* cache, uint64_t rows, int D, i
     return make_bf16_map(map, cache, 3, dims, strides, box);
 }
 
+struct Maps {
+    CUtensorMap q, q1, k, v;
+};
+
 template <int D, int G>
-int launch_pass(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const SharedParams& p, unsigned ctas,
-                cudaStream_t stream) {
+int launch_both(const Maps& maps, const SharedParams& p, const MergeParams& m, unsigned ctas, cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
-    if (!ensure_smem_limit(decode_shared_kernel<D, G>, ShLayout<D>::kSmemBytes, configured, true)) return OPT_GQA_ERR_CUDA;
-    return launch_dependent(decode_shared_kernel<D, G>, dim3(ctas), dim3(kThreads), ShLayout<D>::kSmemBytes, stream, mq, mk,
-                            mv, p);
-}
-
-template <int D>
-int launch_pass_g(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const SharedParams& p, int G,
-                  unsigned ctas, cudaStream_t stream) {
-    switch (G) {
-        case 1: return launch_pass<D, 1>(mq, mk, mv, p, ctas, stream);
-        case 2: return launch_pass<D, 2>(mq, mk, mv, p, ctas, stream);
-        case 4: return launch_pass<D, 4>(mq, mk, mv, p, ctas, stream);
-        case 8: return launch_pass<D, 8>(mq, mk, mv, p, ctas, stream);
-    }
-    return OPT_GQA_ERR_SHAPE;
-}
-
-template <int D, int G>
-int launch_merge(const MergeParams& p, cudaStream_t stream) {
+    if (!ensure_smem_limit(decode_shared_kernel<D, G>, ShLayout<D>::kSmemBytes, configured)) return OPT_GQA_ERR_CUDA;
+    const int rc = launch_dependent(decode_shared_kernel<D, G>, dim3(ctas), dim3(kThreads), ShLayout<D>::kSmemBytes, stream,
+                                    maps.q, maps.q1, maps.k, maps.v, p);
+    if (rc != OPT_GQA_OK) return rc;
     const unsigned slabs = (unsigned)((p.B + 32 / G - 1) / (32 / G));
-    auto launch = [&](auto kernel, unsigned z) {
-        return launch_dependent(kernel, dim3(slabs, (unsigned)p.Hkv, z), dim3(kMergeWarps * 32), 0, stream, p);
+    auto merge = [&](auto kernel, unsigned z) {
+        return launch_dependent(kernel, dim3(slabs, (unsigned)p.Hkv, z), dim3(kMergeWarps * 32), 0, stream, m);
     };
     // Few rows: eight warps share a row's pieces and a CTA takes 8 columns; many rows: a CTA takes all of a row.
-    if ((long long)slabs * p.Hkv <= 128) return launch(merge_shared_kernel<D, G, 8, 8>, D / 8);
-    return launch(merge_shared_kernel<D, G, 1, D / 8>, 1);
+    if ((long long)slabs * p.Hkv <= 128) return merge(merge_shared_kernel<D, G, 8, 8>, D / 8);
+    return merge(merge_shared_kernel<D, G, 1, D / 8>, 1);
 }
 
 template <int D>
-int launch_merge_g(const MergeParams& p, int G, cudaStream_t stream) {
+int launch_g(const Maps& maps, const SharedParams& p, const MergeParams& m, int G, unsigned ctas, cudaStream_t stream) {
     switch (G) {
-        case 1: return launch_merge<D, 1>(p, stream);
-        case 2: return launch_merge<D, 2>(p, stream);
-        case 4: return launch_merge<D, 4>(p, stream);
-        case 8: return launch_merge<D, 8>(p, stream);
+        case 1: return launch_both<D, 1>(maps, p, m, ctas, stream);
+        case 2: return launch_both<D, 2>(maps, p, m, ctas, stream);
+        case 4: return launch_both<D, 4>(maps, p, m, ctas, stream);
+        case 8: return launch_both<D, 8>(maps, p, m, ctas, stream);
     }
     return OPT_GQA_ERR_SHAPE;
 }
@@ -757,31 +944,33 @@ int launch_merge_g(const MergeParams& p, int G, cudaStream_t stream) {
 }  // namespace
 
 int launch_decode_shared(void* out, const void* q, const void* k_cache, const void* v_cache, const int32_t* block_tables,
-                         int max_blocks_per_seq, const int32_t* context_lens, const SharedPrefix& shared,
-                         const float* alibi_slopes, float scale, int B, int Hq, int Hkv, int D, int bs,
-                         int64_t num_blocks, int partition_size, void* workspace, int max_partitions,
+                         int max_blocks_per_seq, const int32_t* context_lens, const int32_t* group_start,
+                         const int32_t* prefix_lens, int num_groups, const float* alibi_slopes, float scale, int B, int Hq,
+                         int Hkv, int D, int bs, int64_t num_blocks, int64_t max_context, void* workspace,
                          int* device_status, cudaStream_t stream) {
     const uint64_t rows = (uint64_t)num_blocks * (uint64_t)Hkv * (uint64_t)bs;
     if (rows == 0 || rows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
-    const int G = Hq / Hkv, N = shared.num_groups;
-    const SharedLayout L = shared_layout(B, Hq, Hkv, D, N, max_partitions);
-    if (L.own.rows > 0x7fffffffull || L.rows / kSharedRows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
+    const int G = Hq / Hkv, N = num_groups;
+    const SharedLayout L = shared_layout(B, Hq, Hkv, D, N);
+    if (L.group_pieces > 0x7fffffffull || L.own_pieces > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
     const int sms = sm_count();
     if (sms <= 0) return OPT_GQA_ERR_CUDA;
-    CUtensorMap mq, mk, mv;
-    if (!make_q_map(&mq, q, B, Hq, G, D) || !make_cache_map(&mk, k_cache, rows, D, bs) ||
-        !make_slice_map(&mv, v_cache, rows, D, bs))
+    Maps maps;
+    if (!make_q_map(&maps.q, q, B, Hq, G, D, kRows / G) || !make_q_map(&maps.q1, q, B, Hq, G, D, 1) ||
+        !make_cache_map(&maps.k, k_cache, rows, D, bs) || !make_slice_map(&maps.v, v_cache, rows, D, bs))
         return OPT_GQA_ERR_CUDA;
     char* ws = static_cast<char*>(workspace);
     SharedParams p;
     p.block_tables = block_tables;
     p.context_lens = context_lens;
-    p.prefix_lens = shared.prefix_lens;
-    p.group_start = shared.group_start;
+    p.prefix_lens = prefix_lens;
+    p.group_start = group_start;
     p.slopes = alibi_slopes;
-    p.partial_out = reinterpret_cast<float*>(ws + L.out);
-    p.partial_lse = reinterpret_cast<float*>(ws + L.lse);
     p.info = reinterpret_cast<int32_t*>(ws + L.info);
+    p.group_lse = reinterpret_cast<float*>(ws + L.group_lse);
+    p.group_out = reinterpret_cast<float*>(ws + L.group_out);
+    p.own_lse = reinterpret_cast<float*>(ws + L.own_lse);
+    p.own_out = reinterpret_cast<float*>(ws + L.own_out);
     p.status = device_status;
     p.scale = scale;
     p.num_groups = N;
@@ -792,32 +981,28 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     p.bs = bs;
     p.lanes_log2 = 0;           // lanes that scan one group's sequences: about the mean size of a group
     while (p.lanes_log2 < 5 && ((long long)N << p.lanes_log2) < B) ++p.lanes_log2;
-    // one CTA per multiprocessor, beside one of the own pass
-    const int ctas = sms < kSharedMaxWorkers ? sms : kSharedMaxWorkers;
-    int rc = D == 128 ? launch_pass_g<128>(mq, mk, mv, p, G, (unsigned)ctas, stream)
-                      : launch_pass_g<64>(mq, mk, mv, p, G, (unsigned)ctas, stream);
-    if (rc != OPT_GQA_OK) return rc;
-    SharedPrefix own = shared;
-    own.info = p.info;
-    rc = launch_decode_stream(q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, alibi_slopes, scale, B, Hq,
-                              Hkv, D, bs, num_blocks, partition_size, workspace, max_partitions, 0, device_status, stream,
-                              nullptr, &own);
-    if (rc != OPT_GQA_OK) return rc;
     MergeParams m;
     m.out = static_cast<__nv_bfloat16*>(out);
     m.context_lens = context_lens;
-    m.prefix_lens = shared.prefix_lens;
-    m.group_start = shared.group_start;
+    m.prefix_lens = prefix_lens;
+    m.group_start = group_start;
     m.info = p.info;
-    m.sh_lse = p.partial_lse;
-    m.sh_out = p.partial_out;
-    m.own_lse = reinterpret_cast<const float*>(ws + L.own.lse);
-    m.own_out = reinterpret_cast<const float*>(ws + L.own.out);
+    m.group_lse = p.group_lse;
+    m.group_out = p.group_out;
+    m.own_lse = p.own_lse;
+    m.own_out = p.own_out;
     m.num_groups = N;
     m.B = B;
     m.Hq = Hq;
     m.Hkv = Hkv;
-    return D == 128 ? launch_merge_g<128>(m, G, stream) : launch_merge_g<64>(m, G, stream);
+    m.group_pieces = (int)L.group_pieces;
+    m.own_pieces = (int)L.own_pieces;
+    // one resident wave, and no more workers than there can be tiles
+    const long long most = (long long)Hkv * (N + (long long)B * G / kRows + B) * ((max_context + kTN - 1) / kTN);
+    long long ctas = (long long)sms * kCtasPerSm;
+    if (ctas > kSharedMaxWorkers) ctas = kSharedMaxWorkers;
+    if (ctas > most) ctas = most;
+    return D == 128 ? launch_g<128>(maps, p, m, G, (unsigned)ctas, stream) : launch_g<64>(maps, p, m, G, (unsigned)ctas, stream);
 }
 
 }  // namespace optgqa

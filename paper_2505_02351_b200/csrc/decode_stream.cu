@@ -35,7 +35,6 @@ namespace {
 
 constexpr int kTileTok = 16;                     // tokens per tile (one ring stage holds a K tile and a V tile)
 constexpr int kWarps = 4;                        // workers per CTA
-constexpr int kSharedWarps = 4;                  // and beside the group pass, one CTA per multiprocessor
 constexpr int kStages = 2;                       // ring depth per worker
 constexpr int kCtasPerSm = 2;
 constexpr int kDescSlots = 4;                    // item descriptors a worker keeps (>= items between prefetch and use)
@@ -67,23 +66,17 @@ struct StreamParams {
     uint4* k_cache_w;
     uint4* v_cache_w;
     const int64_t* slot_mapping;
-    // the pass over what sequences do not share (kShared): sequence s starts behind its shared tokens
-    const int32_t* prefix_lens;
-    const int32_t* group_start;
-    int num_groups;
-    int32_t* info;          // see SharedLayout
 };
 
-template <int D, bool kShared>
+template <int D>
 struct StreamCfg {
-    static constexpr int WARPS = kShared ? kSharedWarps : kWarps;
     static constexpr int NBOX = D / 64;                   // 128-byte-wide boxes per token row
     static constexpr int BOX_BYTES = kTileTok * 128;      // 16 rows x 128 B
     static constexpr int TILE_BYTES = NBOX * BOX_BYTES;   // K (or V) bytes per tile
     static constexpr int WARP_RING = kStages * 2 * TILE_BYTES;
-    static constexpr int OFF_DESC = WARPS * WARP_RING;
-    static constexpr int OFF_BAR = OFF_DESC + WARPS * kDescSlots * 32;
-    static constexpr int SMEM = OFF_BAR + WARPS * kStages * 8 + 1024;   // + slack to align the ring to 1 KB
+    static constexpr int OFF_DESC = kWarps * WARP_RING;
+    static constexpr int OFF_BAR = OFF_DESC + kWarps * kDescSlots * 32;
+    static constexpr int SMEM = OFF_BAR + kWarps * kStages * 8 + 1024;   // + slack to align the ring to 1 KB
 };
 
 // Transposes an 8x8 matrix of 16-bit elements held one row pair per thread (the ldmatrix layout).
@@ -117,21 +110,16 @@ struct StreamCursor {
     int s, kvh, n;          // sequence, KV head, context length of s
     int tiles, parts;       // tiles and partitions of one stream of s
     int jt;                 // tile inside the stream
-    int first;              // tile of the sequence the stream starts at (kShared)
     long long pos;          // the same position in the end-to-end numbering
     long long tiles_before; // sum of `tiles` over earlier sequences (one head)
     long long parts_before; // sum of `parts` over earlier sequences (one head)
 };
 
-// kShared: the first shared_tokens() of every sequence of a group are left out; the group pass of decode_shared.cu
-// attends to them.  That pass precedes this kernel in the stream, works on other rows of the workspace, and lets this kernel
-// start only when everything before both of them is complete; so nothing here waits for it, the two share the GPU, and
-// worker 0 alone waits for it at its end, so that this grid's completion tells the merge of both.
-template <int D, int G, bool kShared>
-__global__ void __launch_bounds__((kShared ? kSharedWarps : kWarps) * 32, kCtasPerSm)
+template <int D, int G>
+__global__ void __launch_bounds__(kWarps * 32, kCtasPerSm)
 decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const StreamParams p) {
-    using C = StreamCfg<D, kShared>;
+    using C = StreamCfg<D>;
     constexpr int KS = D / 16;    // k-steps of K q^T
     constexpr int MT = D / 16;    // m-tiles of V^T p^T
     extern __shared__ char smem_raw[];
@@ -145,18 +133,8 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     const int P = p.partition_size, P16 = P / kTileTok;    // tiles per full partition
     // A sequence's stream starts at the tile that holds its first attended key (tile 0 without a window) and its
     // partitions are counted from there.
-    int grouped_lo = 0, grouped_hi = 0;                    // the sequences that belong to a group
-    if constexpr (kShared) {
-        grouped_lo = __ldg(p.group_start);
-        grouped_hi = __ldg(p.group_start + p.num_groups);
-    }
-    auto first_tile_of = [&](int s, int n) {
-        if constexpr (kShared)
-            return n > 0 && s >= grouped_lo && s < grouped_hi ? shared_tokens(__ldg(p.prefix_lens + s), n) / kTileTok : 0;
-        else
-            return p.window > 0 ? max(0, n - p.window) / kTileTok : 0;
-    };
-    auto tiles_of = [&](int s, int n) { return (n + kTileTok - 1) / kTileTok - first_tile_of(s, n); };
+    auto first_tile_of = [&](int n) { return p.window > 0 ? max(0, n - p.window) / kTileTok : 0; };
+    auto tiles_of = [&](int n) { return (n + kTileTok - 1) / kTileTok - first_tile_of(n); };
     const int* __restrict__ lens = p.context_lens;         // read before the dependency wait: see the ordering contract
     // Entry of a sequence's page table that holds token `tok`.  Held below max_blocks, so that a context length that
     // breaks the caller's promise (n_s <= max_blocks * bs) gives a wrong row and not an access outside the table.
@@ -170,26 +148,23 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     long long total = 0;
     for (int s0 = 0; s0 < p.B; s0 += 32) {
         const int n = s0 + lane < p.B ? __ldg(lens + s0 + lane) : 0;
-        int tl = tiles_of(s0 + lane, n);
+        int tl = tiles_of(n);
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) tl += __shfl_xor_sync(kFull, tl, o);
         total += tl;
     }
     total *= p.Hkv;
     // Never more workers than tiles, so that every worker's range holds at least one tile.
-    const long long grid_workers = (long long)gridDim.x * C::WARPS, me = (long long)blockIdx.x * C::WARPS + warp;
+    const long long grid_workers = (long long)gridDim.x * kWarps, me = (long long)blockIdx.x * kWarps + warp;
     const long long workers = total < grid_workers ? (total > 0 ? total : 1) : grid_workers;
     if (me == 0) {
-        if constexpr (!kShared) grid_dependency_wait();     // the previous reader of the workspace must be done
+        grid_dependency_wait();     // the previous reader of the workspace must be done
         if (lane == 0) {
             p.header[0] = total;
             p.header[1] = workers;
         }
     }
-    if (total == 0 || me >= workers) {
-        if (kShared && me == 0) grid_dependency_wait();
-        return;
-    }
+    if (total == 0 || me >= workers) return;
     const long long lo = total * me / workers, hi = total * (me + 1) / workers;
 
     StreamCursor cur;       // the next piece to be described (runs one piece ahead of the issue side)
@@ -199,7 +174,7 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         cur.s = -1;
         for (int s0 = 0; s0 < p.B && cur.s < 0; s0 += 32) {
             const int n = s0 + lane < p.B ? __ldg(lens + s0 + lane) : 0;
-            const int tl = tiles_of(s0 + lane, n), np = (tl + P16 - 1) / P16;
+            const int tl = tiles_of(n), np = (tl + P16 - 1) / P16;
             int incl_t = tl, incl_p = np;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -223,12 +198,11 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
                 acc_p += __shfl_sync(kFull, incl_p, 31);
             }
         }
-            if (cur.s < 0) return;                               // cannot happen: lo < total
+        if (cur.s < 0) return;                               // cannot happen: lo < total
         const int r = (int)(lo - cur.tiles_before * p.Hkv);
         cur.kvh = r / cur.tiles;
         cur.jt = r - cur.kvh * cur.tiles;
         cur.pos = lo;
-        if constexpr (kShared) cur.first = first_tile_of(cur.s, cur.n);
     }
     auto next_stream = [&]() {
         cur.jt = 0;
@@ -236,26 +210,13 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             cur.kvh = 0;
             cur.tiles_before += cur.tiles;
             cur.parts_before += cur.parts;
-            if constexpr (kShared) {
-                do {
-                    ++cur.s;
-                    cur.n = cur.s < p.B ? __ldg(lens + cur.s) : 0;
-                    cur.first = first_tile_of(cur.s, cur.n);
-                    cur.tiles = (cur.n + kTileTok - 1) / kTileTok - cur.first;
-                } while (cur.s < p.B && cur.tiles == 0);       // nothing of its own: all of it is shared
-            } else {
-                do {
-                    ++cur.s;
-                    cur.n = cur.s < p.B ? __ldg(lens + cur.s) : 0;
-                } while (cur.s < p.B && cur.n == 0);
-                cur.tiles = tiles_of(cur.s, cur.n);
-            }
+            do {
+                ++cur.s;
+                cur.n = cur.s < p.B ? __ldg(lens + cur.s) : 0;
+            } while (cur.s < p.B && cur.n == 0);
+            cur.tiles = tiles_of(cur.n);
             cur.parts = (cur.tiles + P16 - 1) / P16;
         }
-    };
-    auto cur_first = [&]() {
-        if constexpr (kShared) return cur.first;
-        else return first_tile_of(cur.s, cur.n);
     };
     auto cur_valid = [&]() { return cur.s < p.B && cur.pos < hi; };
     if (!cur_valid()) return;
@@ -284,24 +245,17 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
             p.seq_info[2 * cur.s] = cur.tiles_before;
             p.seq_info[2 * cur.s + 1] = cur.parts_before;
         }
-        if constexpr (kShared) {
-            if (lane == 0) {
-                int32_t* info = p.info + ((size_t)cur.s * p.Hkv + cur.kvh) * kInfoWords;
-                if (cur.jt == 0) info[4] = obase / G;
-                if (cur.jt + len == cur.tiles) info[5] = obase / G;
-            }
-        }
         // Where this range and a partition end together inside a stream, the next piece is two numbers on:
         // mark the number in between as empty, so that the merge can sweep the stream's numbers without gaps.
         if (cur.pos + len == hi && cur.jt + len < cur.tiles && (cur.jt + len) % P16 == 0 && lane < G)
             p.partial_lse[obase + G + lane] = -INFINITY;
         if (lane == 0) {
-            desc[2 * (pieces & (kDescSlots - 1))] = make_int4(cur.s, cur.kvh, cur.n, cur_first() + cur.jt);
+            desc[2 * (pieces & (kDescSlots - 1))] = make_int4(cur.s, cur.kvh, cur.n, first_tile_of(cur.n) + cur.jt);
             desc[2 * (pieces & (kDescSlots - 1)) + 1] = make_int4(len, obase, 0, 0);
         }
         // the piece is streamed from its last tile backwards: page ids of its last block of 32 tiles first
         const int blk = (len - 1) & ~31;
-        const int tok = (cur_first() + cur.jt + blk + lane) * kTileTok;
+        const int tok = (first_tile_of(cur.n) + cur.jt + blk + lane) * kTileTok;
         pages_nxt = blk + lane < len ? __ldg(p.block_tables + (size_t)cur.s * p.max_blocks + table_index(tok)) : 0;
         ++pieces;
         cur.pos += len;
@@ -401,14 +355,14 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         const int part = cur.jt / P16;
         const int len = (int)min((long long)(min((part + 1) * P16, cur.tiles) - cur.jt), hi - cur.pos);
         const int blk = (len - 1) & ~31;
-        const int tok = (cur_first() + cur.jt + blk + lane) * kTileTok;
+        const int tok = (first_tile_of(cur.n) + cur.jt + blk + lane) * kTileTok;
         if (blk + lane < len)
             asm volatile("prefetch.global.L1 [%0];" ::"l"(p.block_tables + (size_t)cur.s * p.max_blocks + table_index(tok)));
         if (lane < G * D * 2 / 128)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(
                 reinterpret_cast<const char*>(p.q + ((size_t)cur.s * p.Hq + (size_t)cur.kvh * G) * D) + lane * 128));
     }
-    if constexpr (!kShared) grid_dependency_wait();     // the cache may still be receiving this step's appended tokens
+    grid_dependency_wait();     // the cache may still be receiving this step's appended tokens
     describe_next();            // piece 0
     while (issue_allowed()) issue_one();
 
@@ -573,7 +527,6 @@ decode_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
         // chance to land before this CTA's shared memory is released.
         for (uint32_t kk = consumed; kk != issued; ++kk) mbar_wait(&bars[kk % kStages], (kk / kStages) & 1, p.status);
     }
-    if (kShared && me == 0) grid_dependency_wait();
 }
 
 // One resident wave; never more workers than there could be 16-token tiles (the ranges are cut at tile granularity),
@@ -589,24 +542,24 @@ long long stream_grid_ctas(int B, int Hkv, int max_partitions, int partition_siz
     return ctas;
 }
 
-template <int D, int G, bool kShared>
+template <int D, int G>
 int launch_one(const CUtensorMap& mk, const CUtensorMap& mv, const StreamParams& p, cudaStream_t stream) {
-    using C = StreamCfg<D, kShared>;
+    using C = StreamCfg<D>;
     static std::atomic<bool> configured[kMaxDevices];
-    if (!ensure_smem_limit(decode_stream_kernel<D, G, kShared>, C::SMEM, configured, kShared)) return OPT_GQA_ERR_CUDA;
-    const long long ctas = kShared ? sm_count() : stream_grid_ctas(p.B, p.Hkv, p.max_partitions, p.partition_size);
+    if (!ensure_smem_limit(decode_stream_kernel<D, G>, C::SMEM, configured)) return OPT_GQA_ERR_CUDA;
+    const long long ctas = stream_grid_ctas(p.B, p.Hkv, p.max_partitions, p.partition_size);
     if (ctas <= 0) return OPT_GQA_ERR_CUDA;
-    return launch_dependent(decode_stream_kernel<D, G, kShared>, dim3((unsigned)ctas), dim3(C::WARPS * 32), C::SMEM, stream, mk,
+    return launch_dependent(decode_stream_kernel<D, G>, dim3((unsigned)ctas), dim3(kWarps * 32), C::SMEM, stream, mk,
                             mv, p);
 }
 
-template <int D, bool kShared>
+template <int D>
 int launch_g(const CUtensorMap& mk, const CUtensorMap& mv, const StreamParams& p, int G, cudaStream_t stream) {
     switch (G) {
-        case 1: return launch_one<D, 1, kShared>(mk, mv, p, stream);
-        case 2: return launch_one<D, 2, kShared>(mk, mv, p, stream);
-        case 4: return launch_one<D, 4, kShared>(mk, mv, p, stream);
-        case 8: return launch_one<D, 8, kShared>(mk, mv, p, stream);
+        case 1: return launch_one<D, 1>(mk, mv, p, stream);
+        case 2: return launch_one<D, 2>(mk, mv, p, stream);
+        case 4: return launch_one<D, 4>(mk, mv, p, stream);
+        case 8: return launch_one<D, 8>(mk, mv, p, stream);
     }
     return OPT_GQA_ERR_SHAPE;
 }
@@ -635,7 +588,7 @@ int launch_decode_stream(const void* q, const void* k_cache, const void* v_cache
                          int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale,
                          int B, int Hq, int Hkv, int D, int bs, int64_t num_blocks, int partition_size,
                          void* workspace, int max_partitions, int window, int* device_status, cudaStream_t stream,
-                         const FusedAppend* append, const SharedPrefix* shared) {
+                         const FusedAppend* append) {
     if (!workspace) return OPT_GQA_ERR_NULL;
     const uint64_t rows = (uint64_t)num_blocks * (uint64_t)Hkv * (uint64_t)bs;
     if (rows == 0 || rows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
@@ -669,18 +622,9 @@ int launch_decode_stream(const void* q, const void* k_cache, const void* v_cache
     p.k_cache_w = append ? static_cast<uint4*>(append->k_cache) : nullptr;
     p.v_cache_w = append ? static_cast<uint4*>(append->v_cache) : nullptr;
     p.slot_mapping = append ? append->slot_mapping : nullptr;
-    p.prefix_lens = shared ? shared->prefix_lens : nullptr;
-    p.group_start = shared ? shared->group_start : nullptr;
-    p.num_groups = shared ? shared->num_groups : 0;
-    p.info = shared ? shared->info : nullptr;
     const int G = Hq / Hkv;
-    if (shared) {
-        if (D == 128) return launch_g<128, true>(mk, mv, p, G, stream);
-        if (D == 64) return launch_g<64, true>(mk, mv, p, G, stream);
-        return OPT_GQA_ERR_SHAPE;
-    }
-    if (D == 128) return launch_g<128, false>(mk, mv, p, G, stream);
-    if (D == 64) return launch_g<64, false>(mk, mv, p, G, stream);
+    if (D == 128) return launch_g<128>(mk, mv, p, G, stream);
+    if (D == 64) return launch_g<64>(mk, mv, p, G, stream);
     return OPT_GQA_ERR_SHAPE;
 }
 

@@ -15,12 +15,12 @@ def lib():
 
 def test_workspace_holds_every_piece_of_both_passes(lib):
     B, Hq, Hkv, D, N, P = 256, 64, 8, 128, 12, 20
-    own = binding.workspace_bytes(B, Hq, D, P)
-    items = Hkv * (N + B * 8 // 128) * 128                  # rows of every (group, KV head, block of 128 rows)
+    G = Hq // Hkv
+    rows = Hkv * (N + B * G // 128) * 128 + B * Hq          # of every (group, KV head, block of 128 rows) and every sequence
     need = binding.shared_workspace_bytes(B, Hq, Hkv, D, N, P)
-    # and of at most two more pieces per multiprocessor, 32 bytes per (sequence, KV head), rounding
-    assert own + items * (D + 1) * 4 <= need + 4096
-    assert need <= own + (items + 2 * 148 * 128) * (D + 1) * 4 + B * Hkv * 32 + 4096
+    # and of at most two more pieces of either kind per multiprocessor, 32 bytes per (sequence, KV head), rounding
+    assert rows * (D + 1) * 4 <= need
+    assert need <= (rows + 2 * 148 * (128 + G)) * (D + 1) * 4 + B * Hkv * 32 + 4096
     for bad in ((0, Hq, Hkv, D, N, P), (B, 63, Hkv, D, N, P), (B, Hq, Hkv, 96, N, P), (B, Hq, Hkv, D, 0, P),
                 (B, Hq, Hkv, D, 513, P), (B, Hq, Hkv, D, N, 0), (1 << 17, Hq, Hkv, D, N, P), (B, 48, 3, D, N, P)):
         assert binding.shared_workspace_bytes(*bad) == 0, bad
