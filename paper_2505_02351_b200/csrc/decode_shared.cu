@@ -42,7 +42,7 @@ constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
 // What the even cut counts, in units of about 550 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp),
 // and what an own item costs besides (Q, the wait for its last P V, storing the piece).
-constexpr int kGroupTile = 4, kOwnTile = 3, kOwnItem = 5;
+constexpr int kGroupTile = 4, kOwnTile = 4, kOwnItem = 7;
 constexpr int kMinUnits = 4;               // a worker's share at least: every share holds a tile of each item it touches
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
@@ -132,9 +132,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     int* g_kt = reinterpret_cast<int*>(g_tiles + kMaxGroups);
     int* g_lead = g_kt + kMaxGroups;
     uint16_t* g_items = reinterpret_cast<uint16_t*>(g_lead + kMaxGroups);        // at most kMaxGroups + 65535 * 8 / 128
-    // units of the own items (one head) of the sequences of each thread's chunk, then exclusive sums; gone once the K ring is
-    // in use
+    // units of the own items (one head) of the sequences before each thread's chunk, from its warp's first on, and of each
+    // warp's chunks; gone once the K ring is in use
     long long* c_units = reinterpret_cast<long long*>(smem + kOffK);
+    long long* w_units = c_units + kThreads;
 
     grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -153,7 +154,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const int grouped_lo = __ldg(p.group_start), grouped_hi = __ldg(p.group_start + N);
     // tiles of sequence s (of length n) at which its own begin and end
     auto own_begin = [&](int s, int n) {
-        return s >= grouped_lo && s < grouped_hi ? shared_tokens(__ldg(p.prefix_lens + s), n) / kTN : 0;
+        const int e = shared_tokens(__ldg(p.prefix_lens + s), n) / kTN;
+        return s >= grouped_lo && s < grouped_hi ? e : 0;
     };
     auto own_end = [&](int n) { return (max(n, 0) + kTN - 1) / kTN; };
     auto item_units = [&](int tiles) { return tiles > 0 ? kOwnItem + kOwnTile * (long long)tiles : 0ll; };
@@ -167,7 +169,14 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const int n = __ldg(p.context_lens + s);
             sum += item_units(own_end(n) - own_begin(s, n));
         }
-        c_units[threadIdx.x] = sum;
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += v;
+        }
+        c_units[threadIdx.x] = incl - sum;
+        if (lane == 31) w_units[warp] = incl;
     }
     if (warp < 4) {
         // of each group the longest shared run, and whose it is: 2^lanes_log2 lanes per group
@@ -272,17 +281,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 items += __shfl_sync(kFull, incl, 31);
             }
             group_total *= kGroupTile * p.Hkv;
-            for (int c0 = 0; c0 < kThreads; c0 += 32) {
-                const long long mine = c_units[c0 + lane];
-                long long incl = mine;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const long long v = __shfl_up_sync(kFull, incl, o);
-                    if (lane >= o) incl += v;
-                }
-                c_units[c0 + lane] = own_total + incl - mine;
-                own_total += __shfl_sync(kFull, incl, 31);
-            }
+            for (int w = 0; w < kThreads / 32; ++w) own_total += w_units[w];
             own_total *= p.Hkv;
             __syncwarp();
         }
@@ -327,13 +326,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             pos = first_tile * kGroupTile;
         } else if (lo < hi && own_total > 0) {
             const long long x = max(lo - group_total, 0ll);
-            int a = 0, b = kThreads - 1;    // the last chunk that begins at or before it
-            while (a < b) {
-                const int m = (a + b + 1) >> 1;
-                if (c_units[m] * p.Hkv <= x) a = m;
-                else b = m - 1;
-            }
-            long long before = c_units[a] * p.Hkv;
+            // the last chunk that begins at or before it
+            long long before = 0;
+            int a = 0;
+            while (a < kThreads / 32 - 1 && before + w_units[a] * p.Hkv <= x) before += w_units[a++] * p.Hkv;
+            a = a * 32 + __popc(__ballot_sync(kFull, before + c_units[a * 32 + lane] * p.Hkv <= x)) - 1;
+            before += c_units[a] * p.Hkv;
             s = a * chunk;
             for (;; ++s) {
                 enter_sequence();
@@ -359,8 +357,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
         fence_proxy_async();
         __syncwarp();
-        grid_dependency_wait();             // q and the cache may still be written, the workspace still read, by the preceding kernel
-
+        if (pos >= hi) grid_dependency_wait();      // a grid none of whose CTAs waited could finish before its predecessor
         const int slices = kTN / p.bs, sub = lane % slices, hf = lane / slices;
         const bool issues = lane < slices * L::kHalves;
         char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
@@ -395,6 +392,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const int live = min(slices, (keys - (tile_hi - j) * kTN + p.bs - 1) / p.bs);    // slices that hold keys
                 ok = __all_sync(kFull, mbar_wait(&k_empty[st], ph, p.status));
                 if (!ok) break;
+                // q and the cache may still be written, the workspace still read, by the preceding kernel
+                if (pc == 0 && j == 0) grid_dependency_wait();
                 if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)(live * p.bs * D * 2));
                 __syncwarp();
                 if (issues && sub < live) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st]);
@@ -783,7 +782,7 @@ struct MergeParams {
 template <int D, int G, int kWP, int C>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 merge_shared_kernel(const MergeParams p) {
-    constexpr int kSeqs = 32 / G, kBatch = 32 / C;
+    constexpr int kSeqs = 32 / G, kBatch = 32 / C;      // (C 4, 8 or 16)
     __shared__ float s_max[kWP > 1 ? kMergeWarps : 1][32];
     __shared__ float s_den[kWP > 1 ? kMergeWarps : 1][32];
     __shared__ float s_num[kWP > 1 ? kMergeWarps : 1][C][32];
@@ -886,11 +885,10 @@ merge_shared_kernel(const MergeParams p) {
     }
     if (!active) return;
     const float inv = has1 || has2 ? 1.f / den : 0.f;           // an empty sequence gives a zero row
-    uint4* o = reinterpret_cast<uint4*>(p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0);
+    uint2* o = reinterpret_cast<uint2*>(p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0);
 #pragma unroll
-    for (int c = 0; c < C / 8; ++c)
-        o[c] = make_uint4(pack2(num[8 * c] * inv, num[8 * c + 1] * inv), pack2(num[8 * c + 2] * inv, num[8 * c + 3] * inv),
-                          pack2(num[8 * c + 4] * inv, num[8 * c + 5] * inv), pack2(num[8 * c + 6] * inv, num[8 * c + 7] * inv));
+    for (int c = 0; c < C / 4; ++c)
+        o[c] = make_uint2(pack2(num[4 * c] * inv, num[4 * c + 1] * inv), pack2(num[4 * c + 2] * inv, num[4 * c + 3] * inv));
 }
 
 // ----------------------------------------------------------------------------- host
@@ -925,8 +923,14 @@ int launch_both(const Maps& maps, const SharedParams& p, const MergeParams& m, u
     auto merge = [&](auto kernel, unsigned z) {
         return launch_dependent(kernel, dim3(slabs, (unsigned)p.Hkv, z), dim3(kMergeWarps * 32), 0, stream, m);
     };
-    // Few rows: eight warps share a row's pieces and a CTA takes 8 columns; many rows: a CTA takes all of a row.
-    if ((long long)slabs * p.Hkv <= 128) return merge(merge_shared_kernel<D, G, 8, 8>, D / 8);
+    // About 512 CTAs, a wave of them: of few rows many warps share the pieces and a CTA takes few columns, of many rows a
+    // CTA takes all of them.
+    const long long cells = (long long)slabs * p.Hkv;
+    if (cells <= 16) return merge(merge_shared_kernel<D, G, 8, 4>, D / 4);
+    if (cells <= 32) return merge(merge_shared_kernel<D, G, 8, 8>, D / 8);
+    if (cells <= 64) return merge(merge_shared_kernel<D, G, 8, D / 8>, 8);
+    if (cells <= 128) return merge(merge_shared_kernel<D, G, 4, D / 8>, 4);
+    if (cells <= 256) return merge(merge_shared_kernel<D, G, 2, D / 8>, 2);
     return merge(merge_shared_kernel<D, G, 1, D / 8>, 1);
 }
 
