@@ -12,9 +12,12 @@
 // the softmax).  So own contexts and prefixes of up to 128 rows are bound by reading the cache; prefixes of more rows by the
 // special-function unit and the tensor core, as the prefill is.
 //
-// The tiles of all items are laid end to end and cut into one contiguous range per worker (a CTA, two per SM), so that one
-// long prefix fills the GPU as well as many short ones, whatever the mix.  A worker's part of an item is a piece: normalised
-// partial rows and log-sum-exps in the workspace, merged by merge_shared_kernel.  (The own contexts were first left to
+// The tiles of the groups' items, laid end to end, are cut into one contiguous range per worker (a CTA, two per SM), and so
+// are those of the sequences' own, so that one long prefix fills the GPU as well as many short ones, whatever the mix.  Each
+// worker gets of both: half of them, one of the two on each SM, begin with the groups' (bound by arithmetic, where they have
+// many rows), the others with the sequences' own (bound by memory), 256 sequences in 12 groups: 108 us with all groups' tiles
+// first.  A worker's part of an item is a piece: normalised partial rows and log-sum-exps in the workspace, merged by
+// merge_shared_kernel.  (The own contexts were first left to
 // decode_stream.cu, beside or behind the group pass: 113 against 70 us for 256 sequences in 12 groups; its mma.sync work
 // takes issue slots and tensor cycles from the group pass, and its workers drain between two 16-token tiles.)
 //
@@ -40,10 +43,11 @@ constexpr int kTN = kSharedTile;
 constexpr int kStages = 2;                 // of the K ring and of the V ring
 constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
-// What the even cut counts, in units of about 550 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp),
-// and what an own item costs besides (Q, the wait for its last P V, storing the piece).
-constexpr int kGroupTile = 4, kOwnTile = 4, kOwnItem = 7;
-constexpr int kMinUnits = 4;               // a worker's share at least: every share holds a tile of each item it touches
+// What the cut counts, in units of about 270 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp), and
+// what an own item costs besides (Q, the wait for its last P V, storing the piece).
+constexpr int kGroupTile = 8, kOwnTile = 7, kOwnItem = 10;
+constexpr int kMinGroupTiles = 2;          // a worker's share of the groups' tiles at least (a piece of theirs is 64 KB)
+constexpr int kMinOwnUnits = 16;           // and of the own units: every share then holds a tile of each item it reaches into
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
@@ -55,9 +59,9 @@ constexpr int kQHalfBytes = kRows * 128;   // one 64-dim column half of the Q ti
 constexpr int kExtRowGroupBytes = 256;
 constexpr int kQxBytes = kRows / 8 * kExtRowGroupBytes;
 constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
-// barriers: q_full, q_empty, o_empty, k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
+// barriers: q_full, q_empty, o_empty[4], k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
 // desc_full[], desc_empty[]
-constexpr int kNumBars = 4 + 4 * kStages + 4 + 2 * kDescs;          // (one to spare: an even number)
+constexpr int kNumBars = 6 + 4 * kStages + 4 + 2 * kDescs;
 constexpr int kDescReaders = 7;            // warps that read a descriptor: all but the one that writes it
 
 template <int D>
@@ -93,14 +97,22 @@ struct SharedParams {
     float* own_out;
     int* status;
     float scale;
-    int num_groups, B, max_blocks, Hq, Hkv, bs, lanes_log2;
+    int num_groups, B, max_blocks, Hq, Hkv, bs, bs_log2, lanes_log2;
 };
+
+// mbar_wait with its waiting loop in one place: this kernel waits at some twenty, its warps run all over it, and its time
+// goes with the instruction cache's misses (as inlined: 86 KB, the caches' shared port busy 74 % of the time).
+__noinline__ __device__ bool wait_long(uint64_t* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* status) {
+    return mbar_try_wait(bar, parity) || wait_long(bar, parity, status);
+}
 
 // What the other warps need to know of a piece.
 struct Piece {
     int s0, rows, kvh, table;       // first sequence, live rows, KV head, sequence whose page table is walked
     int tile_hi, len, n, piece;     // last tile (of the sequence's 64-key tiles) and how many, keys there are, number
-    int own, opens, closes, pad;    // own item or a group's; whether the piece holds the item's first and last tile
+    int own, opens, closes, warp0;  // own item or a group's; whether the piece holds the item's first and last tile; the row
+                                    // warp whose lanes are the first rows
 };
 
 template <int D, int G>
@@ -117,8 +129,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
     uint64_t* q_full = bars;
     uint64_t* q_empty = bars + 1;
-    uint64_t* o_empty = bars + 2;
-    uint64_t* k_full = bars + 3;
+    uint64_t* o_empty = bars + 2;               // [4], one per row warp
+    uint64_t* k_full = bars + 6;
     uint64_t* k_empty = k_full + kStages;
     uint64_t* v_full = k_empty + kStages;
     uint64_t* v_empty = v_full + kStages;
@@ -204,7 +216,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (threadIdx.x == 128) {
         mbar_init(q_full, 1);
         mbar_init(q_empty, 1);
-        mbar_init(o_empty, kRows);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mbar_init(&o_empty[i], 32);
 #pragma unroll
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&k_full[i], 1);
@@ -280,16 +293,29 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 group_total += __shfl_sync(kFull, incl_t, 31);
                 items += __shfl_sync(kFull, incl, 31);
             }
-            group_total *= kGroupTile * p.Hkv;
+            group_total *= p.Hkv;
             for (int w = 0; w < kThreads / 32; ++w) own_total += w_units[w];
             own_total *= p.Hkv;
             __syncwarp();
         }
-        const long long total = group_total + own_total, me = blockIdx.x;
-        const long long by_size = total / kMinUnits > 0 ? total / kMinUnits : (total > 0 ? 1 : 0);
-        const long long workers = by_size < gridDim.x ? by_size : gridDim.x;
-        const long long lo = me < workers ? total * me / workers : 0, hi = me < workers ? total * (me + 1) / workers : 0;
-        long long pos = hi;                 // unit at which the next tile to be described lies; a tile belongs to the share it lies in
+        // This worker's shares.  The groups' tiles go to the first `gw` workers evenly; a worker with such a share gets that
+        // much less of the own units, or none where little would be left.
+        const long long W = gridDim.x, me = blockIdx.x;
+        const long long gw = min(W, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
+        const long long g_lo = me < gw ? group_total * me / gw : 0, g_hi = me < gw ? group_total * (me + 1) / gw : 0;
+        long long o_lo = 0, o_hi = 0;
+        {
+            const long long left = (kGroupTile * group_total + own_total) / W - (gw > 0 ? kGroupTile * group_total / gw : 0);
+            const bool both = left >= kMinOwnUnits && gw < W;           // workers with a group share get `left` own units
+            const long long before = both ? gw * left : 0, first = gw < W ? gw : 0;
+            const long long ow = both ? W - gw : max(min(W - first, own_total / kMinOwnUnits), 1ll);    // the other own workers
+            auto own_at = [&](long long i) {
+                if (both && i < gw) return left * i;
+                return before + (own_total - before) * min(max(i - first, 0ll), ow) / ow;
+            };
+            o_lo = own_at(me);
+            o_hi = own_at(me + 1);
+        }
         // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
         // at the same time and its tiles come from L2 after their first reading; then (sequence, KV head)
         int g = 0, kvh = 0, mt = 0, blocks = 1, s = 0, n = 0, jt = 0, t0 = 0, t1 = 0;    // the item's tiles t0 .. t1 - 1
@@ -299,85 +325,113 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             t1 = g_kt[g];
             blocks = blocks_of(g);
         };
-        auto enter_sequence = [&]() {       // s, or the first one behind it that has tiles of its own
-            for (;; ++s) {
-                n = s < p.B ? __ldg(p.context_lens + s) : 0;
-                t0 = s < p.B ? own_begin(s, n) : 0;
-                t1 = own_end(n);
-                if (t1 > t0 || s >= p.B) return;
-            }
-        };
-        const long long first_tile = (lo + kGroupTile - 1) / kGroupTile;       // of the groups' tiles
-        if (lo < hi && first_tile * kGroupTile < group_total) {
+        long long pos = 0, hi = 0;          // in the list at hand: the next tile's place and the end of the share
+        // a group's tile lies at its number in the groups' tiles
+        auto locate_group = [&]() {
+            pos = g_lo;
+            hi = g_hi;
+            if (pos >= hi) return;
             int a = 0, b = N - 1;           // the last group that begins at or before it (and so one that has tiles)
             while (a < b) {
                 const int m = (a + b + 1) >> 1;
-                if (g_tiles[m] * p.Hkv <= first_tile) a = m;
+                if (g_tiles[m] * p.Hkv <= pos) a = m;
                 else b = m - 1;
             }
             g = a;
             enter_group();
-            const long long r = first_tile - g_tiles[g] * p.Hkv;
+            const long long r = pos - g_tiles[g] * p.Hkv;
             const int in_group = (int)(r / t1);
             jt = (int)(r - (long long)in_group * t1);
             kvh = in_group / blocks;
             mt = in_group - kvh * blocks;
             item = (long long)g_items[g] * p.Hkv + in_group;
-            pos = first_tile * kGroupTile;
-        } else if (lo < hi && own_total > 0) {
-            const long long x = max(lo - group_total, 0ll);
-            // the last chunk that begins at or before it
-            long long before = 0;
-            int a = 0;
-            while (a < kThreads / 32 - 1 && before + w_units[a] * p.Hkv <= x) before += w_units[a++] * p.Hkv;
-            a = a * 32 + __popc(__ballot_sync(kFull, before + c_units[a * 32 + lane] * p.Hkv <= x)) - 1;
-            before += c_units[a] * p.Hkv;
-            s = a * chunk;
-            for (;; ++s) {
-                enter_sequence();
-                if (s >= p.B || before + item_units(t1 - t0) * p.Hkv > x) break;
-                before += item_units(t1 - t0) * p.Hkv;
-            }
-            if (s < p.B) {                  // (always: x < own_total)
-                kvh = (int)((x - before) / item_units(t1 - t0));
-                const long long r = x - before - kvh * item_units(t1 - t0) - kOwnItem;      // tile j lies at kOwnTile * j
-                jt = r > 0 ? (int)((r + kOwnTile - 1) / kOwnTile) : 0;                         // < t1 - t0 unless the item is over
-                pos = group_total + x - r + (long long)jt * kOwnTile;
-                if (jt == t1 - t0) {
-                    jt = 0;
-                    pos += kOwnItem;
-                    if (++kvh == p.Hkv) {
-                        kvh = 0;
-                        ++s;
-                        enter_sequence();
-                        if (s >= p.B) pos = hi;
-                    }
-                }
-            }
+        };
+        // tile j of an own item lies kOwnItem + kOwnTile * j units behind the item's begin
+        int own_chunk = 0;                  // the last thread's chunk that begins at or before o_lo, and its begin
+        long long chunk_begin = 0;
+        if (o_lo < o_hi) {
+            while (own_chunk < kThreads / 32 - 1 && chunk_begin + w_units[own_chunk] * p.Hkv <= o_lo)
+                chunk_begin += w_units[own_chunk++] * p.Hkv;
+            own_chunk = own_chunk * 32 + __popc(__ballot_sync(kFull, chunk_begin + c_units[own_chunk * 32 + lane] * p.Hkv <= o_lo)) - 1;
+            chunk_begin += c_units[own_chunk] * p.Hkv;
         }
         fence_proxy_async();
         __syncwarp();
-        if (pos >= hi) grid_dependency_wait();      // a grid none of whose CTAs waited could finish before its predecessor
-        const int slices = kTN / p.bs, sub = lane % slices, hf = lane / slices;
+        const int slices = kTN >> p.bs_log2, sub = lane & (slices - 1), hf = lane >> (6 - p.bs_log2);
         const bool issues = lane < slices * L::kHalves;
         char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
         int st = 0;
         uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
-        bool ok = true;
-        for (int pc = 0; ok; ++pc) {
-            const bool own = pos >= group_total;
-            const int weight = own ? kOwnTile : kGroupTile;
-            const int len = pos < hi ? (int)min((long long)(t1 - t0 - jt), (hi - pos + weight - 1) / weight) : 0;
+        // The CTAs of a multiprocessor are numbers b and b + half the grid: one begins with the groups, the other with its own.
+        // (One place for each of the steps below, for the sake of the instruction cache.)
+        bool own = me >= W / 2, open_list = true, walk = false, seek = false;
+        int lists = 0;                      // lists done
+        long long before = 0;
+        for (int pc = 0;;) {
+            if (open_list) {
+                open_list = false;
+                if (own) {
+                    pos = hi = o_hi;
+                    if (o_lo < o_hi) {
+                        walk = seek = true;
+                        s = own_chunk * chunk;
+                        before = chunk_begin;
+                    }
+                } else {
+                    locate_group();
+                }
+            }
+            if (walk) {                     // s, or the first one behind it that has tiles of its own -- or holds o_lo
+                walk = false;
+                for (; s < p.B; ++s) {
+                    n = __ldg(p.context_lens + s);
+                    t0 = own_begin(s, n);
+                    t1 = own_end(n);
+                    if (t1 <= t0) continue;
+                    if (!seek || before + item_units(t1 - t0) * p.Hkv > o_lo) break;
+                    before += item_units(t1 - t0) * p.Hkv;
+                }
+                if (s >= p.B) {
+                    pos = hi;               // cannot happen: the shares end where the items do
+                } else if (seek) {
+                    // tile j of an item lies kOwnItem + kOwnTile * j units behind the item's begin
+                    seek = false;
+                    kvh = (int)((o_lo - before) / item_units(t1 - t0));
+                    const int r = (int)(o_lo - before - kvh * item_units(t1 - t0)) - kOwnItem;
+                    jt = r > 0 ? (r + kOwnTile - 1) / kOwnTile : 0;
+                    pos = o_lo - r + (long long)jt * kOwnTile;
+                    if (jt == t1 - t0) {    // the item is over: the next one
+                        jt = 0;
+                        pos += kOwnItem;
+                        if (++kvh == p.Hkv) {
+                            kvh = 0;
+                            ++s;
+                            walk = true;
+                            continue;
+                        }
+                    }
+                }
+            }
+            if (pos >= hi && ++lists < 2) {
+                own = !own;
+                open_list = true;
+                continue;
+            }
+            const unsigned room = (unsigned)max(min(hi - pos, (long long)0x3fffffff), 0ll);
+            const int len = (int)min((unsigned)(t1 - t0 - jt), own ? (room + kOwnTile - 1) / kOwnTile : room);    // 0: the end
             const int s0 = own ? s : group_lo(g) + mt * TQ;
             const int rows = own ? G : min(kRows, (group_lo(g + 1) - s0) * G);
+            // Own items take the row warps in turns: while one waits for its item's last P V and stores the piece, the next is
+            // at the next item's weights.
+            const int warp0 = own ? pc & 3 : 0;
             const int table_of = own ? s : g_lead[g], tile_hi = t0 + jt + len - 1, keys = own ? n : t1 * kTN;
-            ok = __all_sync(kFull, mbar_wait(&desc_empty[pc % kDescs], ((pc / kDescs) & 1) ^ 1, p.status));
+            bool ok = __all_sync(kFull, wait_for(&desc_empty[pc % kDescs], ((pc / kDescs) & 1) ^ 1, p.status));
             if (!ok) break;
             if (lane == 0) {
                 int4* d = reinterpret_cast<int4*>(smem + L::kOffDesc) + 3 * (pc % kDescs);
                 d[0] = make_int4(s0, rows, kvh, table_of);
                 d[1] = make_int4(tile_hi, len, keys, (int)((own ? (long long)s * p.Hkv + kvh : item) + me));
-                d[2] = make_int4(own, jt == 0, jt + len == t1 - t0, 0);
+                d[2] = make_int4(own, jt == 0, jt + len == t1 - t0, warp0);
                 mbar_arrive(&desc_full[pc % kDescs]);
             }
             if (len == 0) break;
@@ -386,51 +440,46 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 return issues ? __ldg(table + min((tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
             };
             int page = page_of(0);
+#pragma unroll 1
             for (int j = 0; j < len; ++j) {
-                const int page_next = j + 1 < len ? page_of(j + 1) : 0;
                 const int row = (page * p.Hkv + kvh) * p.bs;                       // row of the [rows, D] view
-                const int live = min(slices, (keys - (tile_hi - j) * kTN + p.bs - 1) / p.bs);    // slices that hold keys
-                ok = __all_sync(kFull, mbar_wait(&k_empty[st], ph, p.status));
+                const int live = min(slices, (keys - (tile_hi - j) * kTN + p.bs - 1) >> p.bs_log2);    // slices that hold keys
+                page = j + 1 < len ? page_of(j + 1) : 0;
+                ok = __all_sync(kFull, wait_for(&k_empty[st], ph, p.status));
                 if (!ok) break;
                 // q and the cache may still be written, the workspace still read, by the preceding kernel
                 if (pc == 0 && j == 0) grid_dependency_wait();
                 if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)(live * p.bs * D * 2));
                 __syncwarp();
                 if (issues && sub < live) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st]);
-                page = page_next;
                 if (++st == kStages) st = 0, ph ^= 1;
                 if (j == 0) {               // Q behind the first K tile, which does not have to wait for the piece before
-                    if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
+                    if (pc > 0) ok = __all_sync(kFull, wait_for(q_empty, (pc - 1) & 1, p.status));
                     if (!ok) break;
                     if (lane == 0) {
                         // an own item's G rows alone: what the other rows of the tile hold reaches no live row
                         mbar_expect_tx(q_full, own ? (uint32_t)(G * D * 2) : (uint32_t)L::kQBytes);
-#pragma unroll
+#pragma unroll 1
                         for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_3d(smem + kOffQ + h * kQHalfBytes, own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, q_full);
+                            tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * (32 * 128), own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, q_full);
                     }
                 }
             }
+            if (!ok) break;
             // on to the next piece
-            pos += (long long)weight * len;
+            ++pc;
+            pos += own ? kOwnTile * (long long)len + kOwnItem : len;
             jt = 0;
+            if (pos >= hi) continue;
             if (own) {
-                pos += kOwnItem;
-                if (pos < hi && ++kvh == p.Hkv) {
+                if (++kvh == p.Hkv) {
                     kvh = 0;
                     ++s;
-                    enter_sequence();
-                    if (s >= p.B) pos = hi;
+                    walk = true;
                 }
-            } else if (pos < hi) {
+            } else {
                 ++item;
-                if (pos >= group_total) {
-                    pos += kOwnItem;
-                    kvh = 0;
-                    s = 0;
-                    enter_sequence();
-                    if (s >= p.B) pos = hi;
-                } else if (++mt == blocks) {
+                if (++mt == blocks) {
                     mt = 0;
                     if (++kvh == p.Hkv) {
                         kvh = 0;
@@ -444,14 +493,16 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
     } else {
         // what every other warp does first with the next piece; false at the end of the list
+        // before any wait with a limit: what the producers wait for may take as long as it likes
+        grid_dependency_wait();
         Piece d;
         auto next_piece = [&](int pc, bool& ok) -> bool {
-            ok = __all_sync(kFull, mbar_wait(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
+            ok = __all_sync(kFull, wait_for(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
             if (!ok) return false;
             const int4 *at = descs + 3 * (pc % kDescs), a = at[0], b = at[1], c = at[2];
             d.s0 = a.x, d.rows = a.y, d.kvh = a.z, d.table = a.w;
             d.tile_hi = b.x, d.len = b.y, d.n = b.z, d.piece = b.w;
-            d.own = c.x, d.opens = c.y, d.closes = c.z;
+            d.own = c.x, d.opens = c.y, d.closes = c.z, d.warp0 = c.w;
             __syncwarp();
             if (lane == 0) mbar_arrive(&desc_empty[pc % kDescs]);
             return d.len > 0;
@@ -460,7 +511,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         if (warp == 6) {
             // -------------------------------------------------------------- V
             // A box is all of a slice (the bs tokens of a page), half after half: see the issuing thread for the layout.
-            const int slices = kTN / p.bs, sub = lane % slices;
+            const int slices = kTN >> p.bs_log2, sub = lane & (slices - 1);
             const bool issues = lane < slices;
             char* ring = smem + kOffV + sub * p.bs * (D * 2);
             int st = 0;
@@ -471,17 +522,16 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     return issues ? __ldg(table + min((d.tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
                 };
                 int page = page_of(0);
-                if (pc == 0) grid_dependency_wait();
+#pragma unroll 1
                 for (int j = 0; j < d.len; ++j) {
-                    const int page_next = j + 1 < d.len ? page_of(j + 1) : 0;
                     const int row = (page * p.Hkv + d.kvh) * p.bs;
-                    const int live = min(slices, (d.n - (d.tile_hi - j) * kTN + p.bs - 1) / p.bs);
-                    ok = __all_sync(kFull, mbar_wait(&v_empty[st], ph, p.status));
+                    const int live = min(slices, (d.n - (d.tile_hi - j) * kTN + p.bs - 1) >> p.bs_log2);
+                    page = j + 1 < d.len ? page_of(j + 1) : 0;
+                    ok = __all_sync(kFull, wait_for(&v_empty[st], ph, p.status));
                     if (!ok) break;
                     if (lane == 0) mbar_expect_tx(&v_full[st], (uint32_t)(live * p.bs * D * 2));
                     __syncwarp();
                     if (issues && sub < live) tma_load_3d(ring + st * kTileBytes, &map_v, 0, row, 0, &v_full[st]);
-                    page = page_next;
                     if (++st == kStages) st = 0, ph ^= 1;
                 }
                 if (!ok) break;
@@ -501,8 +551,9 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (alibi) {
                     // The ALiBi step's operand for this KV head: slope / |scale| as a sum of three bf16 values, the rows a head
                     // each in turn.  Nothing reads the one before once that piece's last scores are there.
-                    if (pc > 0) ok = __all_sync(kFull, mbar_wait(q_empty, (pc - 1) & 1, p.status));
+                    if (pc > 0) ok = __all_sync(kFull, wait_for(q_empty, (pc - 1) & 1, p.status));
                     if (!ok) break;
+#pragma unroll 1
                     for (int r = lane; r < kRows; r += 32) {
                         const float a = p.slopes ? __ldg(p.slopes + d.kvh * G + r % G) / sabs : 0.f;
                         const __nv_bfloat16 a0 = __float2bfloat16_rn(a);
@@ -517,13 +568,14 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     __syncwarp();
                 }
                 if (lane == 0) {
-                    ok = mbar_wait(q_full, pc & 1, p.status);
+                    ok = wait_for(q_full, pc & 1, p.status);
+#pragma unroll 1
                     for (int j = 0; ok && j < d.len; ++j, ++it) {
                         const int sb = it & 1;
                         // the score buffer is free once the P V of the tile before the last one has read its weights there
                         // (kStages is 2: that tile's V stage is this tile's)
-                        if (it >= 2) ok = mbar_wait(&v_empty[st], ph ^ 1, p.status);
-                        ok = ok && mbar_wait(&k_full[st], ph, p.status);
+                        if (it >= 2) ok = wait_for(&v_empty[st], ph ^ 1, p.status);
+                        ok = ok && wait_for(&k_full[st], ph, p.status);
                         if (!ok) break;
                         tc_fence_after();
                         const uint64_t kd = desc_advance(k_desc0, st * kTileBytes);
@@ -550,18 +602,22 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
             constexpr uint32_t idesc_pv = instr_desc(true, D);
             const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
+            const uint32_t half_slice = p.bs == 16 ? 16 * D * 2 : 2048;     // from 16 keys to the next 16 of the same 32
             int it = 0, st = 0;
             uint32_t ph = 0;
+            uint32_t reading = 0, o_ph = 0;     // row warps that read the piece before; per row warp the parity of its next reading
             for (int pc = 0; next_piece(pc, ok); ++pc) {
+#pragma unroll 1
                 for (int j = 0; j < d.len; ++j, ++it) {
                     const int sb = it & 1, live = d.n - (d.tile_hi - j) * kTN;      // keys of the tile that exist
-                    ok = __all_sync(kFull, mbar_wait(&v_full[st], ph, p.status));
+                    ok = __all_sync(kFull, wait_for(&v_full[st], ph, p.status));
                     if (!ok) break;
                     if (live < kTN) {
                         // Rows past the sequence's end hold whatever the page held, or stale shared memory where no page
                         // exists: zero them, so that a weight of 0 times garbage cannot be NaN.
+#pragma unroll 1
                         for (int r = live + (lane >> 3); r < kTN; r += 4) {
-                            char* vrow = smem + kOffV + st * kTileBytes + (r / p.bs) * p.bs * (D * 2) + (r % p.bs) * 128 + (lane & 7) * 16;
+                            char* vrow = smem + kOffV + st * kTileBytes + (r >> p.bs_log2 << p.bs_log2) * (D * 2) + (r & (p.bs - 1)) * 128 + (lane & 7) * 16;
 #pragma unroll
                             for (int b = 0; b < L::kHalves; ++b)
                                 *reinterpret_cast<uint4*>(vrow + b * p.bs * 128) = make_uint4(0, 0, 0, 0);
@@ -570,15 +626,20 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         __syncwarp();
                     }
                     if (lane == 0) {
-                        ok = mbar_wait(&p_full[sb], (it >> 1) & 1, p.status) &&
-                             (j > 0 || pc == 0 || mbar_wait(o_empty, (pc - 1) & 1, p.status));    // O of the piece before is read
+                        ok = wait_for(&p_full[sb], (it >> 1) & 1, p.status);
+                        if (j == 0) {           // O of the piece before has been read
+#pragma unroll 1
+                            for (int w = 0; w < 4; ++w)
+                                if (reading >> w & 1) ok = ok && wait_for(&o_empty[w], o_ph >> w & 1, p.status);
+                            o_ph ^= reading;
+                        }
                         if (ok) {
                             tc_fence_after();
                             const uint64_t vd = desc_advance(v_desc0, st * kTileBytes);
                             const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
 #pragma unroll
                             for (int kk = 0; kk < kTN / 16; ++kk) {
-                                const uint32_t at = p.bs == 16 ? kk * 16 * (D * 2) : (kk >> 1) * 32 * (D * 2) + (kk & 1) * 2048;
+                                const uint32_t at = (kk >> 1) * 32 * (D * 2) + (kk & 1) * half_slice;
                                 umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, at), idesc_pv, j > 0 || kk > 0);
                             }
                             tc_commit(&v_empty[st]);
@@ -589,10 +650,11 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (++st == kStages) st = 0, ph ^= 1;
                 }
                 if (!ok) break;
+                reading = d.own ? 1u << d.warp0 : (1u << ((d.rows + 31) / 32)) - 1;
             }
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
-            const int r = threadIdx.x, hg = r % G;
+            const int r = threadIdx.x, hg = r % G;       // (32 is a multiple of G)
             const float qscale = sabs * kLog2e;
             const uint32_t lane_addr = tmem_base + ((uint32_t)(warp * 32) << 16);
             int it = 0, st = 0;                     // tile, and the stage and parity of its V
@@ -600,11 +662,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             // waits for the P V of the tile before this one
             auto prev_pv_done = [&]() {
                 const int ps = st == 0 ? kStages - 1 : st - 1;
-                return __all_sync(kFull, mbar_wait(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
+                return __all_sync(kFull, wait_for(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
             };
             for (int pc = 0; next_piece(pc, ok); ++pc) {
-                const int s = d.s0 + r / G;
-                const bool valid = r < d.rows;
+                const int rr = r - 32 * d.warp0;                    // row of the item
+                const int s = d.s0 + rr / G;
+                const bool valid = rr >= 0 && rr < d.rows;
                 const int n = valid ? __ldg(p.context_lens + s) : 0;
                 // keys the row sees: of a group's item whole tiles
                 const int e_row = !valid ? 0 : d.own ? n : shared_tokens(__ldg(p.prefix_lens + s), n);
@@ -616,7 +679,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 };
                 for (int j = 0; j < d.len; ++j, next_tile()) {
                     const int sb = it & 1, j0 = (d.tile_hi - j) * kTN;
-                    ok = __all_sync(kFull, mbar_wait(&s_full[sb], (it >> 1) & 1, p.status));
+                    ok = __all_sync(kFull, wait_for(&s_full[sb], (it >> 1) & 1, p.status));
                     if (!ok) break;
                     tc_fence_after();
                     const bool sees = j0 < e_row;
@@ -630,29 +693,22 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     const uint32_t s_addr = lane_addr + kColS + sb * kTN;
                     const float bias0 = slope2 * (float)(j0 - (n - 1));       // ALiBi term of the tile's first key
-                    float v[kTN / 32][32];
-                    {
-                        uint32_t raw[kTN / 32][32];
+                    // The scores are read twice, 32 at a time, and the loops over the two chunks stay loops (see wait_long).
+                    const int live = masked ? d.n - j0 : kTN;       // keys of the tile that exist
+                    auto read_chunk = [&](int c, float (&v)[32]) {
+                        tmem_ld32(s_addr + c * 32, v);
+                        if (masked) {
 #pragma unroll
-                        for (int c = 0; c < kTN / 32; ++c) tmem_ld32_issue(s_addr + c * 32, raw[c]);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int c = 0; c < kTN / 32; ++c) {
-                            tmem_pin(raw[c]);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[c][e] = __uint_as_float(raw[c][e]);
+                            for (int e = 0; e < 32; ++e) v[e] = c * 32 + e < live ? v[e] : -INFINITY;
                         }
-                    }
-                    if (masked) {
-                        // -inf in the place of what lies past the end: both passes then run as they are
-                        const int live = d.n - j0;
-#pragma unroll
-                        for (int e = 0; e < kTN; ++e)
-                            if (e >= live) v[e / 32][e % 32] = -INFINITY;
-                    }
+                    };
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int c = 0; c < kTN / 32; ++c) chunk_max<false>(v[c], 0, 0, 0, mx);
+#pragma unroll 1
+                    for (int c = 0; c < kTN / 32; ++c) {
+                        float v[32];
+                        read_chunk(c, v);
+                        chunk_max<false>(v, 0, 0, 0, mx);
+                    }
                     const float m_tile = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), qscale, bias0);
                     // the running maximum moves (and l and O are rescaled) only when it grew by more than the threshold,
                     // and at the row's first tile
@@ -680,22 +736,22 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const float bias_m = bias0 - m_sub;
                     // every weight of the tile is exactly zero (see prefill_umma.cu), or the row does not see it
                     const bool all_zero = __all_sync(kFull, !sees || m_tile - m_used < -127.f);
-                    if (all_zero) {
+                    float sum = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < kTN / 32; ++c) {
                         uint32_t w[16];
+                        if (all_zero) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) w[e] = 0u;
-#pragma unroll
-                        for (int c = 0; c < kTN / 32; ++c) tmem_st16(s_addr + c * 16, w);
-                    } else {
-                        float sum = 0.f;
-#pragma unroll
-                        for (int c = 0; c < kTN / 32; ++c) {
-                            uint32_t w[16];
-                            sum += chunk_exp<false>(v[c], qscale, bias_m, 0, 0, 0, w);
-                            tmem_st16(s_addr + c * 16, w);
+                            for (int e = 0; e < 16; ++e) w[e] = 0u;
+                        } else {
+                            float v[32];
+                            read_chunk(c, v);
+                            sum += chunk_exp<false>(v, qscale, bias_m, 0, 0, 0, w);
                         }
-                        if (sees) l += sum;
+                        // (chunk 0's weights lie over scores that have been read twice, chunk 1's likewise)
+                        tmem_st16(s_addr + c * 16, w);
                     }
+                    if (sees) l += sum;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&p_full[sb]);
@@ -703,10 +759,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (!ok) break;
 
                 // ---- the piece is complete once its last P V is: normalise, store, hand O back
-                ok = prev_pv_done();
-                if (!ok) break;
-                tc_fence_after();
                 if (__any_sync(kFull, valid)) {
+                    ok = prev_pv_done();
+                    if (!ok) break;
+                    tc_fence_after();
                     const float inv = 1.f / l;
                     const bool begun = (d.tile_hi - d.len + 1) * kTN < e_row;      // the row saw a tile of the piece
                     // a group's piece is [D][128 rows], so that 32 neighbouring rows are one line; an own piece [G][D]
@@ -714,8 +770,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     for (int c = 0; c < D / 32; ++c) {
                         float o[32];
                         tmem_ld32(lane_addr + kColO + c * 32, o);
+                        if (c == D / 32 - 1) {                      // the next piece may overwrite O
+                            tc_fence_before();
+                            mbar_arrive(&o_empty[warp]);
+                        }
                         if (begun && d.own) {
-                            float4* po = reinterpret_cast<float4*>(p.own_out + ((size_t)d.piece * G + r) * D + c * 32);
+                            float4* po = reinterpret_cast<float4*>(p.own_out + ((size_t)d.piece * G + rr) * D + c * 32);
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 po[e] = make_float4(o[4 * e] * inv, o[4 * e + 1] * inv, o[4 * e + 2] * inv, o[4 * e + 3] * inv);
@@ -737,10 +797,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     // a row that saw nothing of the piece: weight zero
                     if (valid)
-                        (d.own ? p.own_lse + (size_t)d.piece * G : p.group_lse + (size_t)d.piece * kRows)[r] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
+                        (d.own ? p.own_lse + (size_t)d.piece * G : p.group_lse + (size_t)d.piece * kRows)[rr] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
                 }
-                tc_fence_before();
-                mbar_arrive(o_empty);
             }
         }
     }
@@ -983,6 +1041,7 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     p.Hq = Hq;
     p.Hkv = Hkv;
     p.bs = bs;
+    p.bs_log2 = bs == 32 ? 5 : 4;
     p.lanes_log2 = 0;           // lanes that scan one group's sequences: about the mean size of a group
     while (p.lanes_log2 < 5 && ((long long)N << p.lanes_log2) < B) ++p.lanes_log2;
     MergeParams m;
