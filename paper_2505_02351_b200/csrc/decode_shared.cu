@@ -13,13 +13,11 @@
 // special-function unit and the tensor core, as the prefill is.
 //
 // The tiles of the groups' items, laid end to end, are cut into one contiguous range per worker (a CTA, two per SM), and so
-// are those of the sequences' own, so that one long prefix fills the GPU as well as many short ones, whatever the mix.  Each
-// worker gets of both: half of them, one of the two on each SM, begin with the groups' (bound by arithmetic, where they have
-// many rows), the others with the sequences' own (bound by memory), 256 sequences in 12 groups: 108 us with all groups' tiles
-// first.  A worker's part of an item is a piece: normalised partial rows and log-sum-exps in the workspace, merged by
-// merge_shared_kernel.  (The own contexts were first left to
-// decode_stream.cu, beside or behind the group pass: 113 against 70 us for 256 sequences in 12 groups; its mma.sync work
-// takes issue slots and tensor cycles from the group pass, and its workers drain between two 16-token tiles.)
+// are those of the sequences' own, as many workers for the one as for the other as their weights say, so that one long prefix
+// fills the GPU as well as many short ones, whatever the mix.  A worker's part of an item is a piece: normalised partial rows
+// and log-sum-exps in the workspace, merged by merge_shared_kernel.  (The own contexts were first left to decode_stream.cu:
+// its mma.sync work takes issue slots and tensor cycles from the group pass beside it, and its workers drain between two
+// 16-token tiles.  Workers that take of both lists make more pieces, 22.3 against 18.7 us for 32 sequences.)
 //
 // A sequence sees whole tiles of its group only: the first e_s = floor(min(prefix, n_s) / 64) * 64 tokens, the rest is its
 // own.  So no group tile is masked inside, and where sequences of a group differ in e_s (the tiles are taken from the last
@@ -59,9 +57,9 @@ constexpr int kQHalfBytes = kRows * 128;   // one 64-dim column half of the Q ti
 constexpr int kExtRowGroupBytes = 256;
 constexpr int kQxBytes = kRows / 8 * kExtRowGroupBytes;
 constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
-// barriers: q_full, q_empty, o_empty[4], k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
+// barriers: q_full[4], q_empty[4], o_empty[4], k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
 // desc_full[], desc_empty[]
-constexpr int kNumBars = 6 + 4 * kStages + 4 + 2 * kDescs;
+constexpr int kNumBars = 12 + 4 * kStages + 4 + 2 * kDescs;
 constexpr int kDescReaders = 7;            // warps that read a descriptor: all but the one that writes it
 
 template <int D>
@@ -127,10 +125,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     extern __shared__ char smem_raw[];
     char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
-    uint64_t* q_full = bars;
-    uint64_t* q_empty = bars + 1;
-    uint64_t* o_empty = bars + 2;               // [4], one per row warp
-    uint64_t* k_full = bars + 6;
+    uint64_t* q_full = bars;                    // [4], per quarter of Q: an own item's rows lie in one, a group's use the first
+    uint64_t* q_empty = bars + 4;
+    uint64_t* o_empty = bars + 8;               // [4], one per row warp
+    uint64_t* k_full = bars + 12;
     uint64_t* k_empty = k_full + kStages;
     uint64_t* v_full = k_empty + kStages;
     uint64_t* v_empty = v_full + kStages;
@@ -214,10 +212,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
     }
     if (threadIdx.x == 128) {
-        mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mbar_init(&o_empty[i], 32);
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+            mbar_init(&o_empty[i], 32);
+        }
 #pragma unroll
         for (int i = 0; i < kStages; ++i) {
             mbar_init(&k_full[i], 1);
@@ -298,24 +298,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             own_total *= p.Hkv;
             __syncwarp();
         }
-        // This worker's shares.  The groups' tiles go to the first `gw` workers evenly; a worker with such a share gets that
-        // much less of the own units, or none where little would be left.
-        const long long W = gridDim.x, me = blockIdx.x;
-        const long long gw = min(W, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
+        // This worker's share: as many workers as their units are worth take the groups' tiles (fewer where a share would have
+        // less than kMinGroupTiles), the others the own units (kMinOwnUnits each at least).
+        const long long W = gridDim.x, me = blockIdx.x, units = kGroupTile * group_total + own_total;
+        long long gw = units > 0 ? (kGroupTile * group_total * W + units / 2) / units : 0;
+        gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1ll : 0ll);
+        gw = min(gw, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
+        const long long o0 = W > 1 ? gw : 0, ow = max(min(W - o0, own_total / kMinOwnUnits), 1ll);
         const long long g_lo = me < gw ? group_total * me / gw : 0, g_hi = me < gw ? group_total * (me + 1) / gw : 0;
-        long long o_lo = 0, o_hi = 0;
-        {
-            const long long left = (kGroupTile * group_total + own_total) / W - (gw > 0 ? kGroupTile * group_total / gw : 0);
-            const bool both = left >= kMinOwnUnits && gw < W;           // workers with a group share get `left` own units
-            const long long before = both ? gw * left : 0, first = gw < W ? gw : 0;
-            const long long ow = both ? W - gw : max(min(W - first, own_total / kMinOwnUnits), 1ll);    // the other own workers
-            auto own_at = [&](long long i) {
-                if (both && i < gw) return left * i;
-                return before + (own_total - before) * min(max(i - first, 0ll), ow) / ow;
-            };
-            o_lo = own_at(me);
-            o_hi = own_at(me + 1);
-        }
+        const long long o_lo = own_total * min(max(me - o0, 0ll), ow) / ow, o_hi = own_total * min(max(me + 1 - o0, 0ll), ow) / ow;
         // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
         // at the same time and its tiles come from L2 after their first reading; then (sequence, KV head)
         int g = 0, kvh = 0, mt = 0, blocks = 1, s = 0, n = 0, jt = 0, t0 = 0, t1 = 0;    // the item's tiles t0 .. t1 - 1
@@ -362,10 +353,11 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
         int st = 0;
         uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
-        // The CTAs of a multiprocessor are numbers b and b + half the grid: one begins with the groups, the other with its own.
         // (One place for each of the steps below, for the sake of the instruction cache.)
-        bool own = me >= W / 2, open_list = true, walk = false, seek = false;
+        bool own = false, open_list = true, walk = false, seek = false;
         int lists = 0;                      // lists done
+        uint32_t q_used = 0, q_ph = 0;      // quarters of Q not yet seen free again, and the parity of their next release
+        bool q_group = false;               // the first of them stands for all of Q
         long long before = 0;
         for (int pc = 0;;) {
             if (open_list) {
@@ -453,15 +445,26 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 __syncwarp();
                 if (issues && sub < live) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st]);
                 if (++st == kStages) st = 0, ph ^= 1;
-                if (j == 0) {               // Q behind the first K tile, which does not have to wait for the piece before
-                    if (pc > 0) ok = __all_sync(kFull, wait_for(q_empty, (pc - 1) & 1, p.status));
+                if (j == 0) {
+                    // Q behind the first K tile.  Own items lie in different quarters, so that the next one's rows are fetched
+                    // while the piece before is still at work; a group's need all of Q.
+                    uint32_t wait = own && !q_group ? q_used & (1u << warp0) : q_used;
+                    q_used = own && !q_group ? q_used & ~wait : 0u;
+#pragma unroll 1
+                    for (int w = 0; wait; ++w, wait >>= 1)
+                        if (wait & 1) {
+                            ok = ok && __all_sync(kFull, wait_for(&q_empty[w], q_ph >> w & 1, p.status));
+                            q_ph ^= 1u << w;
+                        }
                     if (!ok) break;
+                    q_used |= 1u << warp0;
+                    q_group = !own;
                     if (lane == 0) {
                         // an own item's G rows alone: what the other rows of the tile hold reaches no live row
-                        mbar_expect_tx(q_full, own ? (uint32_t)(G * D * 2) : (uint32_t)L::kQBytes);
+                        mbar_expect_tx(&q_full[warp0], own ? (uint32_t)(G * D * 2) : (uint32_t)L::kQBytes);
 #pragma unroll 1
                         for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * (32 * 128), own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, q_full);
+                            tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * (32 * 128), own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, &q_full[warp0]);
                     }
                 }
             }
@@ -545,14 +548,18 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
             const uint64_t qx_desc = smem_desc_plain(smem_u32(smem + kOffQx), 128, kExtRowGroupBytes);
             const uint64_t kp_desc = smem_desc_plain(smem_u32(smem + kOffKp), 128, kExtRowGroupBytes);
-            int it = 0, st = 0;
-            uint32_t ph = 0;
+            int it = 0, st = 0, qx_kvh = -1;
+            uint32_t ph = 0, q_ph = 0;          // q_ph: per quarter of Q the parity of its next filling
+            uint64_t* last_q = nullptr;         // where the piece before says that its scores are done, and the parity of that
+            uint32_t last_ph = 0;
             for (int pc = 0; next_piece(pc, ok); ++pc) {
-                if (alibi) {
+                const int w0 = d.warp0;
+                if (alibi && d.kvh != qx_kvh) {
                     // The ALiBi step's operand for this KV head: slope / |scale| as a sum of three bf16 values, the rows a head
                     // each in turn.  Nothing reads the one before once that piece's last scores are there.
-                    if (pc > 0) ok = __all_sync(kFull, wait_for(q_empty, (pc - 1) & 1, p.status));
+                    if (pc > 0) ok = __all_sync(kFull, wait_for(last_q, last_ph, p.status));
                     if (!ok) break;
+                    qx_kvh = d.kvh;
 #pragma unroll 1
                     for (int r = lane; r < kRows; r += 32) {
                         const float a = p.slopes ? __ldg(p.slopes + d.kvh * G + r % G) / sabs : 0.f;
@@ -568,7 +575,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     __syncwarp();
                 }
                 if (lane == 0) {
-                    ok = wait_for(q_full, pc & 1, p.status);
+                    ok = wait_for(&q_full[w0], q_ph >> w0 & 1, p.status);
 #pragma unroll 1
                     for (int j = 0; ok && j < d.len; ++j, ++it) {
                         const int sb = it & 1;
@@ -589,12 +596,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         if (alibi) umma_ss(s_tmem, qx_desc, kp_desc, idesc_s, dots);
                         tc_commit(&s_full[sb]);
                         tc_commit(&k_empty[st]);
-                        if (j == d.len - 1) tc_commit(q_empty);
+                        if (j == d.len - 1) tc_commit(&q_empty[w0]);
                         if (++st == kStages) st = 0, ph ^= 1;
                     }
                 }
                 ok = __all_sync(kFull, ok);
                 if (!ok) break;
+                last_q = &q_empty[w0];
+                last_ph = q_ph >> w0 & 1;
+                q_ph ^= 1u << w0;
             }
         } else if (warp == 7) {
             // -------------------------------------------------------------- one thread issues O (+)= P V
@@ -693,22 +703,29 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     const uint32_t s_addr = lane_addr + kColS + sb * kTN;
                     const float bias0 = slope2 * (float)(j0 - (n - 1));       // ALiBi term of the tile's first key
-                    // The scores are read twice, 32 at a time, and the loops over the two chunks stay loops (see wait_long).
-                    const int live = masked ? d.n - j0 : kTN;       // keys of the tile that exist
-                    auto read_chunk = [&](int c, float (&v)[32]) {
-                        tmem_ld32(s_addr + c * 32, v);
-                        if (masked) {
+                    float v[kTN / 32][32];
+                    {
+                        uint32_t raw[kTN / 32][32];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = c * 32 + e < live ? v[e] : -INFINITY;
+                        for (int c = 0; c < kTN / 32; ++c) tmem_ld32_issue(s_addr + c * 32, raw[c]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) {
+                            tmem_pin(raw[c]);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[c][e] = __uint_as_float(raw[c][e]);
                         }
-                    };
-                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-                    for (int c = 0; c < kTN / 32; ++c) {
-                        float v[32];
-                        read_chunk(c, v);
-                        chunk_max<false>(v, 0, 0, 0, mx);
                     }
+                    if (masked) {
+                        // -inf in the place of what lies past the end: both passes then run as they are
+                        const int live = d.n - j0;
+#pragma unroll
+                        for (int e = 0; e < kTN; ++e)
+                            if (e >= live) v[e / 32][e % 32] = -INFINITY;
+                    }
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < kTN / 32; ++c) chunk_max<false>(v[c], 0, 0, 0, mx);
                     const float m_tile = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), qscale, bias0);
                     // the running maximum moves (and l and O are rescaled) only when it grew by more than the threshold,
                     // and at the row's first tile
@@ -736,22 +753,22 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     const float bias_m = bias0 - m_sub;
                     // every weight of the tile is exactly zero (see prefill_umma.cu), or the row does not see it
                     const bool all_zero = __all_sync(kFull, !sees || m_tile - m_used < -127.f);
-                    float sum = 0.f;
-#pragma unroll 1
-                    for (int c = 0; c < kTN / 32; ++c) {
+                    if (all_zero) {
                         uint32_t w[16];
-                        if (all_zero) {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) w[e] = 0u;
-                        } else {
-                            float v[32];
-                            read_chunk(c, v);
-                            sum += chunk_exp<false>(v, qscale, bias_m, 0, 0, 0, w);
+                        for (int e = 0; e < 16; ++e) w[e] = 0u;
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) tmem_st16(s_addr + c * 16, w);
+                    } else {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) {
+                            uint32_t w[16];
+                            sum += chunk_exp<false>(v[c], qscale, bias_m, 0, 0, 0, w);
+                            tmem_st16(s_addr + c * 16, w);
                         }
-                        // (chunk 0's weights lie over scores that have been read twice, chunk 1's likewise)
-                        tmem_st16(s_addr + c * 16, w);
+                        if (sees) l += sum;
                     }
-                    if (sees) l += sum;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&p_full[sb]);
