@@ -105,6 +105,11 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* st
     return mbar_try_wait(bar, parity) || wait_long(bar, parity, status);
 }
 
+// Where the share of worker i of W begins in a list of `total`: rounded down, so that the shares follow one another.
+__device__ __forceinline__ long long share_at(long long total, int i, int W) {
+    return total < (1 << 22) ? (long long)((unsigned)total * (unsigned)i / (unsigned)W) : total * i / W;      // (W < 512)
+}
+
 // What the other warps need to know of a piece.
 struct Piece {
     int s0, rows, kvh, table;       // first sequence, live rows, KV head, sequence whose page table is walked
@@ -300,13 +305,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         }
         // This worker's share: as many workers as their units are worth take the groups' tiles (fewer where a share would have
         // less than kMinGroupTiles), the others the own units (kMinOwnUnits each at least).
-        const long long W = gridDim.x, me = blockIdx.x, units = kGroupTile * group_total + own_total;
-        long long gw = units > 0 ? (kGroupTile * group_total * W + units / 2) / units : 0;
-        gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1ll : 0ll);
-        gw = min(gw, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
-        const long long o0 = W > 1 ? gw : 0, ow = max(min(W - o0, own_total / kMinOwnUnits), 1ll);
-        const long long g_lo = me < gw ? group_total * me / gw : 0, g_hi = me < gw ? group_total * (me + 1) / gw : 0;
-        const long long o_lo = own_total * min(max(me - o0, 0ll), ow) / ow, o_hi = own_total * min(max(me + 1 - o0, 0ll), ow) / ow;
+        const int W = gridDim.x, me = blockIdx.x;
+        const long long units = kGroupTile * group_total + own_total;
+        // (rounded in fp32: which way matters to nobody, all workers round alike)
+        int gw = units > 0 ? __float2int_rn(__ll2float_rn(kGroupTile * group_total) / __ll2float_rn(units) * W) : 0;
+        gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1 : 0);
+        gw = (int)min((long long)gw, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
+        const int o0 = W > 1 ? gw : 0, ow = (int)max(min((long long)(W - o0), own_total / kMinOwnUnits), 1ll), oi = min(max(me - o0, -1), ow);
+        const long long g_lo = me < gw ? share_at(group_total, me, gw) : 0, g_hi = me < gw ? share_at(group_total, me + 1, gw) : 0;
+        const long long o_lo = share_at(own_total, max(oi, 0), ow), o_hi = share_at(own_total, min(oi + 1, ow), ow);
         // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
         // at the same time and its tiles come from L2 after their first reading; then (sequence, KV head)
         int g = 0, kvh = 0, mt = 0, blocks = 1, s = 0, n = 0, jt = 0, t0 = 0, t1 = 0;    // the item's tiles t0 .. t1 - 1
@@ -331,7 +338,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             g = a;
             enter_group();
             const long long r = pos - g_tiles[g] * p.Hkv;
-            const int in_group = (int)(r / t1);
+            const int in_group = r < 0x7fffffff ? (int)r / t1 : (int)(r / t1);
             jt = (int)(r - (long long)in_group * t1);
             kvh = in_group / blocks;
             mt = in_group - kvh * blocks;
@@ -960,10 +967,17 @@ merge_shared_kernel(const MergeParams p) {
     }
     if (!active) return;
     const float inv = has1 || has2 ? 1.f / den : 0.f;           // an empty sequence gives a zero row
-    uint2* o = reinterpret_cast<uint2*>(p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0);
+    __nv_bfloat16* o = p.out + ((size_t)s * p.Hq + kvh * G + hh) * D + d0;
+    if constexpr (C % 8 == 0) {
 #pragma unroll
-    for (int c = 0; c < C / 4; ++c)
-        o[c] = make_uint2(pack2(num[4 * c] * inv, num[4 * c + 1] * inv), pack2(num[4 * c + 2] * inv, num[4 * c + 3] * inv));
+        for (int c = 0; c < C; c += 8)
+            *reinterpret_cast<uint4*>(o + c) = make_uint4(pack2(num[c] * inv, num[c + 1] * inv), pack2(num[c + 2] * inv, num[c + 3] * inv),
+                                                          pack2(num[c + 4] * inv, num[c + 5] * inv), pack2(num[c + 6] * inv, num[c + 7] * inv));
+    } else {
+#pragma unroll
+        for (int c = 0; c < C; c += 4)
+            *reinterpret_cast<uint2*>(o + c) = make_uint2(pack2(num[c] * inv, num[c + 1] * inv), pack2(num[c + 2] * inv, num[c + 3] * inv));
+    }
 }
 
 // ----------------------------------------------------------------------------- host
