@@ -21,6 +21,8 @@ def test_workspace_holds_every_piece_of_both_passes(lib):
     # and of at most two more pieces of either kind per multiprocessor, 32 bytes per (sequence, KV head), rounding
     assert rows * (D + 1) * 4 <= need
     assert need <= (rows + 2 * 148 * (128 + G)) * (D + 1) * 4 + B * Hkv * 32 + 4096
+    # the route of small batches (of up to 32 MB of cache) needs the balanced decode's
+    assert binding.shared_workspace_bytes(4, 32, 8, 128, 1, 110) >= (4 * 32 * 110 + 2048 * 4) * 129 * 4
     for bad in ((0, Hq, Hkv, D, N, P), (B, 63, Hkv, D, N, P), (B, Hq, Hkv, 96, N, P), (B, Hq, Hkv, D, 0, P),
                 (B, Hq, Hkv, D, 513, P), (B, Hq, Hkv, D, N, 0), (1 << 17, Hq, Hkv, D, N, P), (B, 48, 3, D, N, P)):
         assert binding.shared_workspace_bytes(*bad) == 0, bad

@@ -55,8 +55,12 @@ class Batch:
         self.prefix = i32(shared if told is None else told)
         self.slopes = torch.exp2(-8.0 * torch.arange(1, Hq + 1, device=DEV, dtype=torch.float32) / Hq) if slopes else None
 
-    def workspace(self, P):
+    def workspace(self, P, small=False):
+        """small: the bound on the contexts is tight, so that small batches take the route of small batches; otherwise it is
+        loose enough for the group pass to run."""
         parts = max(1, -(-max(self.n) // P))
+        if not small:
+            parts = max(parts, int(33e6 / (self.B * P * self.Hkv * self.q.shape[2] * 4)) + 1)
         need = binding.shared_workspace_bytes(self.B, self.q.shape[1], self.Hkv, self.q.shape[2], self.start.numel() - 1, parts)
         return torch.full((need // 4 + 1,), float("nan"), device=DEV).view(torch.uint8)[:need], parts
 
@@ -116,6 +120,15 @@ def test_lengths_of_the_prefix_and_behind_it(prefix, own):
     n = prefix + own
     b = Batch(16, 4, 128, 16, sizes=[6], prefix=[prefix], lens=[n] * 6, seed=n)
     b.check(P=64)
+
+
+@pytest.mark.parametrize("slopes", [False, True])
+def test_small_batches_and_tight_bounds(slopes):
+    """The same batches with a tight bound on the contexts: whichever route a call takes, the result is the definition's."""
+    for sizes, prefix, lens in (([4], [500], [501, 560, 512, 777]), ([2, 2], [64, 700], [0, 70, 701, 700]), ([3], [0], [1, 2, 0]),
+                                ([40], [600], [601 + 3 * i for i in range(40)])):
+        b = Batch(32, 8, 128, 16, sizes=sizes, prefix=prefix, lens=lens, slopes=slopes)
+        b.check(P=64, ws=b.workspace(64, small=True))
 
 
 def test_rows_without_tokens_give_zero_rows_and_disturb_nobody():
