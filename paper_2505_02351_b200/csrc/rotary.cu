@@ -15,8 +15,8 @@
 // A unit of work is P pairs of one row, two 16-byte vectors: vectors P u and R/2 + P u of the half layout, two
 // adjacent ones of the interleaved layout and of the dims past R, which pass through unchanged.  A thread requests
 // kBatch units before it uses the first; registers are held to five CTAs per multiprocessor (80 KB in flight; four
-// units per thread at two CTAs took 40 us where this takes 29).  Where R is no multiple of two vectors,
-// a unit is one pair of elements (P = 1).
+// units per thread at two CTAs took 40 us where this takes 29).  It asks for R / 2 to be whole vectors; for any other R
+// the rows go through shared memory, where a pair's elements are read one by one (rotary_staged_kernel).
 #include <math.h>
 
 #include "common.cuh"
@@ -45,7 +45,7 @@ struct RotaryParams {
     float cos_amp, sin_amp;            // amplitude, and with the direction's sign
 };
 
-// P adjacent elements as fp32; 16 bytes at once unless P is 1.
+// P adjacent elements, 16 bytes, as fp32.
 template <typename T, int P>
 struct Chunk {
     uint4 raw;
@@ -72,14 +72,46 @@ struct Chunk {
             raw = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
 };
-template <typename T>
-struct Chunk<T, 1> {
-    T raw;
-    __device__ __forceinline__ void load(const T* p) { raw = *p; }
-    __device__ __forceinline__ void store(T* p) const { *p = raw; }
-    __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = static_cast<float>(raw); }
-    __device__ __forceinline__ void set(const float (&f)[1]) { raw = static_cast<T>(f[0]); }
-};
+// cos and sin of the pairs of `tokens` tokens from t0 on, [tokens][D / 2], by all threads of the CTA.
+template <int D>
+__device__ __forceinline__ void angles(const RotaryParams& p, long long t0, int tokens, float* s_cos, float* s_sin) {
+    const int half = p.R / 2;
+    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
+        const int tok = i / half, pair = i - tok * half;
+        const uint64_t turn = (uint64_t)(int64_t)__ldg(p.positions + t0 + tok) * __ldg(p.freq + pair);
+        float s, c;
+        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);     // half turns, in [-1, 1]
+        s_cos[tok * (D / 2) + pair] = c * p.cos_amp;
+        s_sin[tok * (D / 2) + pair] = s * p.sin_amp;
+    }
+}
+
+// Row h of token t (queries, then keys, then values).
+template <typename T, int D>
+__device__ __forceinline__ const T* source_row(const RotaryParams& p, long long t, int h) {
+    return h < p.Hq          ? static_cast<const T*>(p.q) + t * p.q_stride + (long long)h * D
+           : h < p.Hq + p.Hk ? static_cast<const T*>(p.k) + t * p.k_stride + (long long)(h - p.Hq) * D
+                             : static_cast<const T*>(p.v) + t * p.v_stride + (long long)(h - p.Hq - p.Hk) * D;
+}
+
+// Calls store(destination row) for every place row h of token t goes to.
+template <typename T, int D, typename Store>
+__device__ __forceinline__ void for_destinations(const RotaryParams& p, long long t, int h, Store store) {
+    if (h < p.Hq) {
+        store(static_cast<T*>(p.q_out) + t * p.q_out_stride + (long long)h * D);
+        return;
+    }
+    const bool is_v = h >= p.Hq + p.Hk;
+    const int kh = is_v ? h - p.Hq - p.Hk : h - p.Hq;
+    if (!is_v && p.k_out) store(static_cast<T*>(p.k_out) + t * p.k_out_stride + (long long)kh * D);
+    if (p.k_cache) {
+        const long long slot = p.slots[t];
+        if (slot >= 0 && slot < p.num_slots) {
+            const long long page = slot >> p.bs_log2, off = slot & ((1 << p.bs_log2) - 1);
+            store(static_cast<T*>(is_v ? p.v_cache : p.k_cache) + (((page * p.Hk + kh) << p.bs_log2) + off) * D);
+        }
+    }
+}
 
 template <typename T, int D, int P, bool kInterleaved, int kTokens, int kBatch>
 __global__ void __launch_bounds__(kRotThreads, kRotCtas)
@@ -89,14 +121,7 @@ rotary_kernel(const RotaryParams p) {
     grid_dependency_launch();
     const long long t0 = (long long)blockIdx.x * kTokens;
     const int tokens = (int)min((long long)kTokens, p.T - t0), half = p.R / 2;
-    for (int i = threadIdx.x; i < tokens * half; i += kRotThreads) {
-        const int tok = i / half, pair = i - tok * half;
-        const uint64_t turn = (uint64_t)(int64_t)__ldg(p.positions + t0 + tok) * __ldg(p.freq + pair);
-        float s, c;
-        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &c);     // half turns, in [-1, 1]
-        s_cos[tok][pair] = c * p.cos_amp;
-        s_sin[tok][pair] = s * p.sin_amp;
-    }
+    angles<D>(p, t0, tokens, &s_cos[0][0], &s_sin[0][0]);
     __syncthreads();
     grid_dependency_wait();     // q, k, v may come from the preceding kernel, which may also still read what is written here
 
@@ -118,9 +143,7 @@ rotary_kernel(const RotaryParams p) {
                 const long long t = t0 + tok;
                 int e0, e1;
                 offsets(i % U, e0, e1);
-                const T* src = h < p.Hq             ? static_cast<const T*>(p.q) + t * p.q_stride + (long long)h * D
-                               : h < p.Hq + p.Hk    ? static_cast<const T*>(p.k) + t * p.k_stride + (long long)(h - p.Hq) * D
-                                                    : static_cast<const T*>(p.v) + t * p.v_stride + (long long)(h - p.Hq - p.Hk) * D;
+                const T* src = source_row<T, D>(p, t, h);
                 a[n].load(src + e0);
                 b[n].load(src + e1);
             }
@@ -139,7 +162,7 @@ rotary_kernel(const RotaryParams p) {
                     float x[P], y[P];
                     a[n].get(x);
                     b[n].get(y);
-                    if constexpr (kInterleaved && P > 1) {
+                    if constexpr (kInterleaved) {
                         // the P pairs are (2i, 2i + 1) of the 2 P adjacent elements x, y
 #pragma unroll
                         for (int e = 0; e < P / 2; ++e) {
@@ -160,31 +183,87 @@ rotary_kernel(const RotaryParams p) {
                     a[n].set(x);
                     b[n].set(y);
                 }
-                if (h < p.Hq) {
-                    T* dst = static_cast<T*>(p.q_out) + t * p.q_out_stride + (long long)h * D;
+                for_destinations<T, D>(p, t, h, [&](T* dst) {
                     a[n].store(dst + e0);
                     b[n].store(dst + e1);
-                    continue;
-                }
-                const bool is_v = h >= p.Hq + p.Hk;
-                const int kh = is_v ? h - p.Hq - p.Hk : h - p.Hq;
-                if (!is_v && p.k_out) {
-                    T* dst = static_cast<T*>(p.k_out) + t * p.k_out_stride + (long long)kh * D;
-                    a[n].store(dst + e0);
-                    b[n].store(dst + e1);
-                }
-                if (p.k_cache) {
-                    const long long slot = p.slots[t];
-                    if (slot >= 0 && slot < p.num_slots) {
-                        const long long page = slot >> p.bs_log2, off = slot & ((1 << p.bs_log2) - 1);
-                        T* dst = static_cast<T*>(is_v ? p.v_cache : p.k_cache) + (((page * p.Hk + kh) << p.bs_log2) + off) * D;
-                        a[n].store(dst + e0);
-                        b[n].store(dst + e1);
-                    }
-                }
+                });
             }
         }
     }
+}
+
+// Any even R: a warp brings kBatch times 512 bytes of rows into shared memory, 16 bytes a lane, its lanes rotate pair by pair
+// there, and the rows leave as they came; the next ones are requested before.  8192 tokens of 40 heads of 128, bf16, R 126:
+// 47.6 us of a floor of 26.0 (R 50: 40.2); bound by the two-byte passes through shared memory.  One row at a time 57.7, four 47.4
+// (R 50: 40.5, 64 wide 34.8 where two take 31.4); one pair per thread straight from memory 101.
+template <typename T, int D, bool kInterleaved, int kTokens, int kBatch>
+__global__ void __launch_bounds__(kRotThreads)
+rotary_staged_kernel(const RotaryParams p) {
+    constexpr int kVec = 16 / sizeof(T), kLanes = D / kVec, kRowsPer = 32 / kLanes, kWarps = kRotThreads / 32;
+    __shared__ float s_cos[kTokens * D / 2], s_sin[kTokens * D / 2];
+    __shared__ __align__(16) T s_rows[kWarps][kBatch * kRowsPer * D];
+    grid_dependency_launch();
+    const long long t0 = (long long)blockIdx.x * kTokens;
+    const int tokens = (int)min((long long)kTokens, p.T - t0), half = p.R / 2;
+    angles<D>(p, t0, tokens, s_cos, s_sin);
+    __syncthreads();
+    grid_dependency_wait();
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int H = p.Hq + p.Hk + p.Hv, rows = tokens * H, mine = lane / kLanes, e = lane % kLanes * kVec;
+    const int step = kWarps * kBatch * kRowsPer * gridDim.y;        // rows all warps take at a time
+    T* stage = s_rows[warp];
+    uint4 next[kBatch];
+    auto fetch = [&](int first) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int row = first + u * kRowsPer + mine;
+            if (row < rows) next[u] = *reinterpret_cast<const uint4*>(source_row<T, D>(p, t0 + row / H, row % H) + e);
+        }
+    };
+    int first = (blockIdx.y * kWarps + warp) * kBatch * kRowsPer;
+    fetch(first);
+    for (; first < rows; first += step) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) *reinterpret_cast<uint4*>(stage + (u * kRowsPer + mine) * D + e) = next[u];
+        __syncwarp();
+        fetch(first + step);
+#pragma unroll
+        for (int r = 0; r < kBatch * kRowsPer; ++r) {
+            const int row = first + r, tok = row / H;
+            if (row >= rows || row - tok * H >= p.Hq + p.Hk) continue;     // values are not rotated
+            const float *cs = s_cos + tok * (D / 2), *sn = s_sin + tok * (D / 2);
+            for (int i = lane; i < half; i += 32) {
+                T *a = stage + r * D + (kInterleaved ? 2 * i : i), *b = kInterleaved ? a + 1 : a + half;
+                const float x = static_cast<float>(*a), y = static_cast<float>(*b);
+                *a = static_cast<T>(x * cs[i] - y * sn[i]);
+                *b = static_cast<T>(y * cs[i] + x * sn[i]);
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int row = first + u * kRowsPer + mine;
+            if (row < rows) {
+                const uint4 out = *reinterpret_cast<const uint4*>(stage + (u * kRowsPer + mine) * D + e);
+                for_destinations<T, D>(p, t0 + row / H, row % H, [&](T* dst) { *reinterpret_cast<uint4*>(dst + e) = out; });
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <typename T, int D, bool kInterleaved>
+int launch_staged(const RotaryParams& p, cudaStream_t stream) {
+    constexpr int kStep = kRotThreads * 16 / (D * (int)sizeof(T));        // rows a CTA takes at a time
+    // as in launch_tokens: several CTAs per token of a few, four tokens per CTA of many
+    const int rounds = (p.Hq + p.Hk + p.Hv + kStep - 1) / kStep;
+    auto launch = [&](auto kernel, long long x, int y) {
+        return launch_dependent(kernel, dim3((unsigned)x, (unsigned)y), dim3(kRotThreads), 0, stream, p);
+    };
+    if (p.T <= 512) return launch(rotary_staged_kernel<T, D, kInterleaved, 1, 1>, p.T, rounds);
+    if (p.T >= 4096) return launch(rotary_staged_kernel<T, D, kInterleaved, 4, 2>, (p.T + 3ll) / 4, 1);
+    return launch(rotary_staged_kernel<T, D, kInterleaved, 1, 2>, p.T, 1);
 }
 
 template <typename T, int D, int P, bool kInterleaved>
@@ -212,8 +291,8 @@ int launch_typed(const RotaryParams& p, int layout, cudaStream_t stream) {
     // whole vectors on both sides of every pair: R / 2 elements are whole 16-byte vectors
     const bool wide = p.R % (2 * kVec) == 0;
     if (layout == OPT_GQA_ROTARY_INTERLEAVED)
-        return wide ? launch_tokens<T, D, kVec, true>(p, stream) : launch_tokens<T, D, 1, true>(p, stream);
-    return wide ? launch_tokens<T, D, kVec, false>(p, stream) : launch_tokens<T, D, 1, false>(p, stream);
+        return wide ? launch_tokens<T, D, kVec, true>(p, stream) : launch_staged<T, D, true>(p, stream);
+    return wide ? launch_tokens<T, D, kVec, false>(p, stream) : launch_staged<T, D, false>(p, stream);
 }
 
 }  // namespace
