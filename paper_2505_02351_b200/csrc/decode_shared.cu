@@ -152,7 +152,6 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     long long* c_units = reinterpret_cast<long long*>(smem + kOffK);
     long long* w_units = c_units + kThreads;
 
-    grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int N = p.num_groups;
     if (threadIdx.x == 192) {
@@ -265,6 +264,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_launch();           // not before this CTA has its tensor memory: a later grid's could take it and wait for this one
 
     if (warp == 4) {
         // ------------------------------------------------------------------ the list of pieces, Q and K

@@ -111,7 +111,6 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     uint64_t* p_full = s_full + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
 
-    grid_dependency_launch();
     const int kvh = blockIdx.y, s = blockIdx.z;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int qstart = p.q_start_loc[s];
@@ -188,6 +187,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_launch();   // not before this CTA has its tensor memory: a later grid's could take it and wait for this one
     grid_dependency_wait();     // the cache may still be receiving this step's appended tokens
 
     if (warp == 4) {
