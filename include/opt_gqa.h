@@ -23,9 +23,10 @@
  *  - Ordering inside a stream: the kernels are launched with programmatic stream
  *    serialisation and wait for the preceding kernel of the stream before they read
  *    anything it may write (q, k_new, v_new, the cache, the partials) or overwrite
- *    anything it may read (out, the workspace).  Two index arrays are the exception:
- *    block_tables and context_lens are read BEFORE that wait (the split of the work is
- *    computed from them while the preceding kernel drains).  They must therefore not be
+ *    anything it may read (out, the workspace).  Index arrays are the exception:
+ *    block_tables, context_lens, q_start_loc, group_start, prefix_lens, positions and
+ *    freq are read BEFORE that wait (the split of the work and the angles are computed
+ *    from them while the preceding kernel drains).  They must therefore not be
  *    produced by a kernel that signals its dependents early (griddepcontrol
  *    .launch_dependents / cudaTriggerProgrammaticLaunchCompletion); no kernel of this
  *    library writes them except the gather of opt_gqa_decode_step_host, which does not
@@ -239,10 +240,12 @@ int opt_gqa_paged_attention_decode_no_alloc(void* out, const void* q, const void
  *                and need not be multiples of a page; the shared pass takes whole tiles of 64 tokens,
  *                e_s = floor(min(prefix_lens[s], context_lens[s]) / 64) * 64, and only those have to agree.
  *                prefix_lens of a sequence of no group is not looked at.
+ *   num_blocks   num_blocks * Hkv * bs < 2^31
  *   num_groups   1 .. 512 (a group of one sequence gains nothing: leave it out of the groups)
  *   alibi_slopes, scale, partition_size, max_partitions  as in opt_gqa_paged_attention_decode_balanced: max_partitions *
- *                partition_size bounds every context.  Where it bounds the whole cache by 32 MB, every context is read for
- *                itself as in that call and its merge, and the groups are not looked at; beyond, it sizes the grid and the partitions play no part.
+ *                partition_size bounds every context.  Where that bounds the whole cache by 32 MB, every context is read
+ *                for itself as in that call and its merge, and the groups are not looked at; beyond, it sizes the grid
+ *                and the partitions play no part.
  *   workspace    opt_gqa_shared_workspace_bytes(...) bytes (host arithmetic; 0 for bad arguments), 16-byte aligned; contents
  *                need no initialisation.  Calls that can overlap on the GPU need a workspace each.
  * group_start and prefix_lens are read before the wait for the preceding kernel, like block_tables.
@@ -392,7 +395,8 @@ int opt_gqa_qkv_project_int4(void* q_out, void* k_out, void* v_out, void* k_cach
  *   PARTS   r = original_len f / 2pi turns over the original context, w = (r - low_turns) / (high_turns - low_turns)
  *           held in [0, 1]:  f (w + (1 - w) / factor)
  *   RAMP    with i(r) = R ln(original_len / (2pi r)) / (2 ln base), lo = max(floor i(high_turns), 0),
- *           hi = min(ceil i(low_turns), R - 1), w = 1 - (i - lo) / (hi - lo) held in [0, 1]:  f (w + (1 - w) / factor);
+ *           hi = min(ceil i(low_turns), R - 1), w = 1 - (i - lo) / max(hi - lo, 0.001) held in [0, 1]:
+ *           f (w + (1 - w) / factor);
  *           the amplitude that goes with it, 0.1 ln(factor) + 1, is the caller's to pass
  *   (arguments a scaling does not name are ignored; OPT_GQA_ERR_SHAPE for an odd R, base or factor <= 0, PARTS or RAMP
  *   with original_len <= 0 or not 0 < low_turns < high_turns, RAMP with base <= 1, or a frequency that is not finite).

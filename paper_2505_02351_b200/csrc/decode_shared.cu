@@ -435,8 +435,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             if (len == 0) break;
             const int32_t* table = p.block_tables + (size_t)table_of * p.max_blocks;
+            const int pages = min((keys + p.bs - 1) >> p.bs_log2, p.max_blocks);       // the table is not read past them
             auto page_of = [&](int j) {
-                return issues ? __ldg(table + min((tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
+                const int i = (tile_hi - j) * slices + sub;
+                return issues && i < pages ? __ldg(table + i) : 0;
             };
             int page = page_of(0);
 #pragma unroll 1
@@ -528,8 +530,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             uint32_t ph = 1;
             for (int pc = 0; next_piece(pc, ok); ++pc) {
                 const int32_t* table = p.block_tables + (size_t)d.table * p.max_blocks;
+                const int pages = min((d.n + p.bs - 1) >> p.bs_log2, p.max_blocks);
                 auto page_of = [&](int j) {
-                    return issues ? __ldg(table + min((d.tile_hi - j) * slices + sub, p.max_blocks - 1)) : 0;
+                    const int i = (d.tile_hi - j) * slices + sub;
+                    return issues && i < pages ? __ldg(table + i) : 0;
                 };
                 int page = page_of(0);
 #pragma unroll 1
