@@ -42,10 +42,12 @@ constexpr int kStages = 2;                 // of the K ring and of the V ring
 constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
 // What the cut counts, in units of about 270 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp), and
-// what an own item costs besides (Q, the wait for its last P V, storing the piece).
-constexpr int kGroupTile = 8, kOwnTile = 7, kOwnItem = 10;
-constexpr int kMinGroupTiles = 2;          // a worker's share of the groups' tiles at least (a piece of theirs is 64 KB)
-constexpr int kMinOwnUnits = 16;           // and of the own units: every share then holds a tile of each item it reaches into
+// what an item costs besides (the next one's Q, which takes the place of this one's, the wait for its last P V, storing the
+// piece).
+constexpr int kGroupTile = 8, kGroupItem = 24, kOwnTile = 7, kOwnItem = 13;
+// A worker's share of the groups' units at least (a piece of theirs is 64 KB), and of the own ones.  More than a tile's units:
+// a share that lies within an item behind its begin then holds a tile of it, and no piece of the item's run is missing.
+constexpr int kMinGroupUnits = 32, kMinOwnUnits = 16;
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
@@ -74,7 +76,7 @@ struct ShLayout {
     static constexpr int kOffKp = kOffQx + kQxBytes;
     static constexpr int kOffBar = kOffKp + kKpBytes;
     static constexpr int kOffDesc = kOffBar + kNumBars * 8 + 16;
-    static constexpr int kOffGroups = kOffDesc + kDescs * 48;           // tiles before (8 B), tiles, leader, items before (2 B)
+    static constexpr int kOffGroups = kOffDesc + kDescs * 48;           // units before (8 B), tiles, leader, items before (2 B)
     static constexpr int kSmemBytes = kOffGroups + kMaxGroups * 18 + 1024;
 };
 
@@ -143,8 +145,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* desc_empty = desc_full + kDescs;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
     const int4* descs = reinterpret_cast<const int4*>(smem + L::kOffDesc);
-    long long* g_tiles = reinterpret_cast<long long*>(smem + L::kOffGroups);     // exclusive sums over the groups, one head
-    int* g_kt = reinterpret_cast<int*>(g_tiles + kMaxGroups);
+    long long* g_units = reinterpret_cast<long long*>(smem + L::kOffGroups);     // of the groups before (one head)
+    int* g_kt = reinterpret_cast<int*>(g_units + kMaxGroups);
     int* g_lead = g_kt + kMaxGroups;
     uint16_t* g_items = reinterpret_cast<uint16_t*>(g_lead + kMaxGroups);        // at most kMaxGroups + 65535 * 8 / 128
     // units of the own items (one head) of the sequences before each thread's chunk, from its warp's first on, and of each
@@ -173,6 +175,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     };
     auto own_end = [&](int n) { return (max(n, 0) + kTN - 1) / kTN; };
     auto item_units = [&](int tiles) { return tiles > 0 ? kOwnItem + kOwnTile * (long long)tiles : 0ll; };
+    auto group_units = [&](int tiles) { return kGroupItem + kGroupTile * (long long)tiles; };
 
     // ------------------------------------------------------------------ the items (the index arrays are read before the
     // wait for the preceding kernel: see the ordering contract in the header)
@@ -284,14 +287,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (lane >= o) incl += v;
                 }
                 if (items + incl > most) b = 0, kt = 0;       // (items + incl only grows: all later ones too)
-                long long incl_t = (long long)b * kt;
+                const long long units = b * group_units(kt);
+                long long incl_t = units;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const long long v = __shfl_up_sync(kFull, incl_t, o);
                     if (lane >= o) incl_t += v;
                 }
                 if (g < N) {
-                    g_tiles[g] = group_total + incl_t - (long long)b * kt;
+                    g_units[g] = group_total + incl_t - units;
                     g_items[g] = (uint16_t)min(items + incl - b, most);
                     g_kt[g] = kt;
                 }
@@ -303,14 +307,14 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             own_total *= p.Hkv;
             __syncwarp();
         }
-        // This worker's share: as many workers as their units are worth take the groups' tiles (fewer where a share would have
-        // less than kMinGroupTiles), the others the own units (kMinOwnUnits each at least).
+        // This worker's share: as many workers as they are worth take the groups' units (fewer where a share would have less than
+        // kMinGroupUnits), the others the own ones (kMinOwnUnits each at least).
         const int W = gridDim.x, me = blockIdx.x;
-        const long long units = kGroupTile * group_total + own_total;
+        const long long units = group_total + own_total;
         // (rounded in fp32: which way matters to nobody, all workers round alike)
-        int gw = units > 0 ? __float2int_rn(__ll2float_rn(kGroupTile * group_total) / __ll2float_rn(units) * W) : 0;
+        int gw = units > 0 ? __float2int_rn(__ll2float_rn(group_total) / __ll2float_rn(units) * W) : 0;
         gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1 : 0);
-        gw = (int)min((long long)gw, (group_total + kMinGroupTiles - 1) / kMinGroupTiles);
+        gw = (int)min((long long)gw, (group_total + kMinGroupUnits - 1) / kMinGroupUnits);
         const int o0 = W > 1 ? gw : 0, ow = (int)max(min((long long)(W - o0), own_total / kMinOwnUnits), 1ll), oi = min(max(me - o0, -1), ow);
         const long long g_lo = me < gw ? share_at(group_total, me, gw) : 0, g_hi = me < gw ? share_at(group_total, me + 1, gw) : 0;
         const long long o_lo = share_at(own_total, max(oi, 0), ow), o_hi = share_at(own_total, min(oi + 1, ow), ow);
@@ -324,7 +328,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             blocks = blocks_of(g);
         };
         long long pos = 0, hi = 0;          // in the list at hand: the next tile's place and the end of the share
-        // a group's tile lies at its number in the groups' tiles
+        // a group item's tile j lies kGroupItem + kGroupTile * j units behind the item's begin
         auto locate_group = [&]() {
             pos = g_lo;
             hi = g_hi;
@@ -332,14 +336,16 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             int a = 0, b = N - 1;           // the last group that begins at or before it (and so one that has tiles)
             while (a < b) {
                 const int m = (a + b + 1) >> 1;
-                if (g_tiles[m] * p.Hkv <= pos) a = m;
+                if (g_units[m] * p.Hkv <= pos) a = m;
                 else b = m - 1;
             }
             g = a;
             enter_group();
-            const long long r = pos - g_tiles[g] * p.Hkv;
-            const int in_group = r < 0x7fffffff ? (int)r / t1 : (int)(r / t1);
-            jt = (int)(r - (long long)in_group * t1);
+            const long long u = group_units(t1), r = pos - g_units[g] * p.Hkv;
+            const int in_group = r < 0x7fffffff ? (int)r / (int)u : (int)(r / u);
+            const int in_item = (int)(r - in_group * u) - kGroupItem;
+            jt = in_item > 0 ? (in_item + kGroupTile - 1) / kGroupTile : 0;
+            pos += (long long)jt * kGroupTile - in_item;
             kvh = in_group / blocks;
             mt = in_group - kvh * blocks;
             item = (long long)g_items[g] * p.Hkv + in_group;
@@ -361,7 +367,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         int st = 0;
         uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
         // (One place for each of the steps below, for the sake of the instruction cache.)
-        bool own = false, open_list = true, walk = false, seek = false;
+        bool own = false, open_list = true, step = false, walk = false, seek = false;
         int lists = 0;                      // lists done
         uint32_t q_used = 0, q_ph = 0;      // quarters of Q not yet seen free again, and the parity of their next release
         bool q_group = false;               // the first of them stands for all of Q
@@ -378,6 +384,34 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                 } else {
                     locate_group();
+                    if (jt == t1) {         // (of an empty share too)
+                        jt = 0;
+                        pos += kGroupItem;
+                        step = true;
+                    }
+                }
+            }
+            if (step) {                     // to the next item, where there is one
+                step = false;
+                if (pos >= hi) {
+                } else if (own) {
+                    if (++kvh == p.Hkv) {
+                        kvh = 0;
+                        ++s;
+                        walk = true;
+                    }
+                } else {
+                    ++item;
+                    if (++mt == blocks) {
+                        mt = 0;
+                        if (++kvh == p.Hkv) {
+                            kvh = 0;
+                            do ++g;
+                            while (g < N - 1 && g_kt[g] == 0);
+                            enter_group();
+                            item = (long long)g_items[g] * p.Hkv;
+                        }
+                    }
                 }
             }
             if (walk) {                     // s, or the first one behind it that has tiles of its own -- or holds o_lo
@@ -402,12 +436,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (jt == t1 - t0) {    // the item is over: the next one
                         jt = 0;
                         pos += kOwnItem;
-                        if (++kvh == p.Hkv) {
-                            kvh = 0;
-                            ++s;
-                            walk = true;
-                            continue;
-                        }
+                        step = true;
+                        continue;
                     }
                 }
             }
@@ -417,7 +447,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 continue;
             }
             const unsigned room = (unsigned)max(min(hi - pos, (long long)0x3fffffff), 0ll);
-            const int len = (int)min((unsigned)(t1 - t0 - jt), own ? (room + kOwnTile - 1) / kOwnTile : room);    // 0: the end
+            const int len = (int)min((unsigned)(t1 - t0 - jt), own ? (room + kOwnTile - 1) / kOwnTile : (room + kGroupTile - 1) / kGroupTile);    // 0: the end
             const int s0 = own ? s : group_lo(g) + mt * TQ;
             const int rows = own ? G : min(kRows, (group_lo(g + 1) - s0) * G);
             // Own items take the row warps in turns: while one waits for its item's last P V and stores the piece, the next is
@@ -480,28 +510,9 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (!ok) break;
             // on to the next piece
             ++pc;
-            pos += own ? kOwnTile * (long long)len + kOwnItem : len;
+            pos += own ? kOwnTile * (long long)len + kOwnItem : kGroupTile * (long long)len + kGroupItem;
             jt = 0;
-            if (pos >= hi) continue;
-            if (own) {
-                if (++kvh == p.Hkv) {
-                    kvh = 0;
-                    ++s;
-                    walk = true;
-                }
-            } else {
-                ++item;
-                if (++mt == blocks) {
-                    mt = 0;
-                    if (++kvh == p.Hkv) {
-                        kvh = 0;
-                        do ++g;
-                        while (g < N - 1 && g_kt[g] == 0);
-                        enter_group();
-                        item = (long long)g_items[g] * p.Hkv;
-                    }
-                }
-            }
+            step = true;
         }
     } else {
         // what every other warp does first with the next piece; false at the end of the list
