@@ -41,13 +41,13 @@ constexpr int kTN = kSharedTile;
 constexpr int kStages = 2;                 // of the K ring and of the V ring
 constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
-// What the cut counts, in units of about 270 cycles of a CTA: a group's tile, a tile of a sequence's own (one live warp), and
-// what an item costs besides (the next one's Q, which takes the place of this one's, the wait for its last P V, storing the
-// piece).
-constexpr int kGroupTile = 8, kGroupItem = 24, kOwnTile = 7, kOwnItem = 13;
-// A worker's share of the groups' units at least (a piece of theirs is 64 KB), and of the own ones.  More than a tile's units:
-// a share that lies within an item behind its begin then holds a tile of it, and no piece of the item's run is missing.
-constexpr int kMinGroupUnits = 32, kMinOwnUnits = 16;
+// The cut counts tiles, and for an item besides (the next one's Q, which takes the place of this one's, the wait for its last
+// P V, storing the piece) as many of them as it costs time: fitted to the times of 296 workers with different numbers of
+// tiles and pieces, a group's tile and one of a sequence's own last alike (1.06 us, two CTAs per SM), a group's item 2.4 to 3.7
+// of them, an own item about one.
+constexpr int kGroupItem = 3, kOwnItem = 1;
+// A worker's share of the groups' list at least (a piece of theirs is 64 KB), and of the own one.
+constexpr int kMinGroupShare = 4, kMinOwnShare = 2;
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
@@ -174,8 +174,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         return s >= grouped_lo && s < grouped_hi ? e : 0;
     };
     auto own_end = [&](int n) { return (max(n, 0) + kTN - 1) / kTN; };
-    auto item_units = [&](int tiles) { return tiles > 0 ? kOwnItem + kOwnTile * (long long)tiles : 0ll; };
-    auto group_units = [&](int tiles) { return kGroupItem + kGroupTile * (long long)tiles; };
+    auto item_units = [&](int tiles) { return tiles > 0 ? tiles + kOwnItem : 0; };
 
     // ------------------------------------------------------------------ the items (the index arrays are read before the
     // wait for the preceding kernel: see the ordering contract in the header)
@@ -287,7 +286,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (lane >= o) incl += v;
                 }
                 if (items + incl > most) b = 0, kt = 0;       // (items + incl only grows: all later ones too)
-                const long long units = b * group_units(kt);
+                const long long units = b * (long long)(kt + kGroupItem);
                 long long incl_t = units;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -308,14 +307,14 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             __syncwarp();
         }
         // This worker's share: as many workers as they are worth take the groups' units (fewer where a share would have less than
-        // kMinGroupUnits), the others the own ones (kMinOwnUnits each at least).
+        // kMinGroupShare), the others the own ones (kMinOwnShare each at least).
         const int W = gridDim.x, me = blockIdx.x;
         const long long units = group_total + own_total;
         // (rounded in fp32: which way matters to nobody, all workers round alike)
         int gw = units > 0 ? __float2int_rn(__ll2float_rn(group_total) / __ll2float_rn(units) * W) : 0;
         gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1 : 0);
-        gw = (int)min((long long)gw, (group_total + kMinGroupUnits - 1) / kMinGroupUnits);
-        const int o0 = W > 1 ? gw : 0, ow = (int)max(min((long long)(W - o0), own_total / kMinOwnUnits), 1ll), oi = min(max(me - o0, -1), ow);
+        gw = (int)min((long long)gw, (group_total + kMinGroupShare - 1) / kMinGroupShare);
+        const int o0 = W > 1 ? gw : 0, ow = (int)max(min((long long)(W - o0), own_total / kMinOwnShare), 1ll), oi = min(max(me - o0, -1), ow);
         const long long g_lo = me < gw ? share_at(group_total, me, gw) : 0, g_hi = me < gw ? share_at(group_total, me + 1, gw) : 0;
         const long long o_lo = share_at(own_total, max(oi, 0), ow), o_hi = share_at(own_total, min(oi + 1, ow), ow);
         // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
@@ -328,7 +327,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             blocks = blocks_of(g);
         };
         long long pos = 0, hi = 0;          // in the list at hand: the next tile's place and the end of the share
-        // a group item's tile j lies kGroupItem + kGroupTile * j units behind the item's begin
+        // a group item's tile j lies kGroupItem + j behind the item's begin
         auto locate_group = [&]() {
             pos = g_lo;
             hi = g_hi;
@@ -341,16 +340,17 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             g = a;
             enter_group();
-            const long long u = group_units(t1), r = pos - g_units[g] * p.Hkv;
-            const int in_group = r < 0x7fffffff ? (int)r / (int)u : (int)(r / u);
-            const int in_item = (int)(r - in_group * u) - kGroupItem;
-            jt = in_item > 0 ? (in_item + kGroupTile - 1) / kGroupTile : 0;
-            pos += (long long)jt * kGroupTile - in_item;
+            const int u = t1 + kGroupItem;
+            const long long r = pos - g_units[g] * p.Hkv;
+            const int in_group = r < 0x7fffffff ? (int)r / u : (int)(r / u);
+            const int in_item = (int)(r - (long long)in_group * u) - kGroupItem;
+            jt = max(in_item, 0);
+            pos += jt - in_item;
             kvh = in_group / blocks;
             mt = in_group - kvh * blocks;
             item = (long long)g_items[g] * p.Hkv + in_group;
         };
-        // tile j of an own item lies kOwnItem + kOwnTile * j units behind the item's begin
+        // an own item's tile j lies kOwnItem + j behind the item's begin
         int own_chunk = 0;                  // the last thread's chunk that begins at or before o_lo, and its begin
         long long chunk_begin = 0;
         if (o_lo < o_hi) {
@@ -384,11 +384,6 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                 } else {
                     locate_group();
-                    if (jt == t1) {         // (of an empty share too)
-                        jt = 0;
-                        pos += kGroupItem;
-                        step = true;
-                    }
                 }
             }
             if (step) {                     // to the next item, where there is one
@@ -421,24 +416,19 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     t0 = own_begin(s, n);
                     t1 = own_end(n);
                     if (t1 <= t0) continue;
-                    if (!seek || before + item_units(t1 - t0) * p.Hkv > o_lo) break;
-                    before += item_units(t1 - t0) * p.Hkv;
+                    if (!seek || before + item_units(t1 - t0) * (long long)p.Hkv > o_lo) break;
+                    before += item_units(t1 - t0) * (long long)p.Hkv;
                 }
                 if (s >= p.B) {
                     pos = hi;               // cannot happen: the shares end where the items do
                 } else if (seek) {
-                    // tile j of an item lies kOwnItem + kOwnTile * j units behind the item's begin
                     seek = false;
-                    kvh = (int)((o_lo - before) / item_units(t1 - t0));
-                    const int r = (int)(o_lo - before - kvh * item_units(t1 - t0)) - kOwnItem;
-                    jt = r > 0 ? (r + kOwnTile - 1) / kOwnTile : 0;
-                    pos = o_lo - r + (long long)jt * kOwnTile;
-                    if (jt == t1 - t0) {    // the item is over: the next one
-                        jt = 0;
-                        pos += kOwnItem;
-                        step = true;
-                        continue;
-                    }
+                    const long long r = o_lo - before;
+                    const int u = item_units(t1 - t0);
+                    kvh = r < 0x7fffffff ? (int)r / u : (int)(r / u);
+                    const int in_item = (int)(r - (long long)kvh * u) - kOwnItem;
+                    jt = max(in_item, 0);
+                    pos = o_lo + jt - in_item;
                 }
             }
             if (pos >= hi && ++lists < 2) {
@@ -447,7 +437,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 continue;
             }
             const unsigned room = (unsigned)max(min(hi - pos, (long long)0x3fffffff), 0ll);
-            const int len = (int)min((unsigned)(t1 - t0 - jt), own ? (room + kOwnTile - 1) / kOwnTile : (room + kGroupTile - 1) / kGroupTile);    // 0: the end
+            const int len = (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
             const int s0 = own ? s : group_lo(g) + mt * TQ;
             const int rows = own ? G : min(kRows, (group_lo(g + 1) - s0) * G);
             // Own items take the row warps in turns: while one waits for its item's last P V and stores the piece, the next is
@@ -510,7 +500,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (!ok) break;
             // on to the next piece
             ++pc;
-            pos += own ? kOwnTile * (long long)len + kOwnItem : kGroupTile * (long long)len + kGroupItem;
+            pos += len + (own ? kOwnItem : kGroupItem);
             jt = 0;
             step = true;
         }
