@@ -194,10 +194,10 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         c_units[threadIdx.x] = incl - sum;
         if (lane == 31) w_units[warp] = incl;
     }
-    if (warp < 4) {
-        // of each group the longest shared run, and whose it is: 2^lanes_log2 lanes per group
+    {
+        // of each group the longest shared run, whose it is, and the row blocks: 2^lanes_log2 lanes per group
         const int lanes = 1 << p.lanes_log2, sub = lane & (lanes - 1), per_warp = 32 >> p.lanes_log2;
-        for (int g0 = warp * per_warp; g0 < N; g0 += 4 * per_warp) {
+        for (int g0 = warp * per_warp; g0 < N; g0 += kThreads / 32 * per_warp) {
             const int g = g0 + (lane >> p.lanes_log2);
             int best = 0, lead = 0;
             if (g < N) {
@@ -214,6 +214,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             if (g < N && sub == 0) {
                 g_kt[g] = best / kTN;
                 g_lead[g] = lead;
+                g_items[g] = best > 0 ? (uint16_t)blocks_of(g) : 0;     // (at most 65535 * 8 / 128)
             }
         }
     }
@@ -278,7 +279,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const int most = N + (int)((long long)p.B * G / kRows);
             for (int g0 = 0; g0 < N; g0 += 32) {
                 const int g = g0 + lane;
-                int b = g < N && g_kt[g] > 0 ? blocks_of(g) : 0, kt = g < N ? g_kt[g] : 0;
+                int b = g < N ? g_items[g] : 0, kt = g < N ? g_kt[g] : 0;
                 int incl = b;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
