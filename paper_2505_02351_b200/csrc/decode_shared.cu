@@ -367,6 +367,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
         int st = 0;
         uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
+        // a sequence's own tiles are read once, a group's by all its row blocks
+        const uint64_t read_once = l2_policy_evict_first(), read_again = l2_policy_evict_normal();
         // (One place for each of the steps below, for the sake of the instruction cache.)
         bool own = false, open_list = true, step = false, walk = false, seek = false;
         int lists = 0;                      // lists done
@@ -473,7 +475,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (pc == 0 && j == 0) grid_dependency_wait();
                 if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)(live * p.bs * D * 2));
                 __syncwarp();
-                if (issues && sub < live) tma_load_2d(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st]);
+                if (issues && sub < live) tma_load_2d_hint(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st], own ? read_once : read_again);
                 if (++st == kStages) st = 0, ph ^= 1;
                 if (j == 0) {
                     // Q behind the first K tile.  Own items lie in different quarters, so that the next one's rows are fetched
@@ -531,6 +533,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             int st = 0;
             uint32_t ph = 1;
             for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const uint64_t policy = d.own ? l2_policy_evict_first() : l2_policy_evict_normal();
                 const int32_t* table = p.block_tables + (size_t)d.table * p.max_blocks;
                 const int pages = min((d.n + p.bs - 1) >> p.bs_log2, p.max_blocks);
                 auto page_of = [&](int j) {
@@ -547,7 +550,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (!ok) break;
                     if (lane == 0) mbar_expect_tx(&v_full[st], (uint32_t)(live * p.bs * D * 2));
                     __syncwarp();
-                    if (issues && sub < live) tma_load_3d(ring + st * kTileBytes, &map_v, 0, row, 0, &v_full[st]);
+                    if (issues && sub < live) tma_load_3d_hint(ring + st * kTileBytes, &map_v, 0, row, 0, &v_full[st], policy);
                     if (++st == kStages) st = 0, ph ^= 1;
                 }
                 if (!ok) break;
