@@ -28,8 +28,6 @@
 // issue S = Q K^T and O += P V.  (One producer was what everything waited for: a copy of 16 rows costs its warp about 90
 // cycles, 16 of them a tile; and one issuing thread adds the waits for K, V and P up, 1690 cycles a tile.)  Every wait is a
 // bounded mbarrier wait.
-#include <type_traits>
-
 #include "umma.cuh"
 
 namespace optgqa {
@@ -902,55 +900,50 @@ merge_shared_kernel(const MergeParams p) {
     float M = -INFINITY, den = 0.f, num[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) num[c] = 0.f;
-    // R pieces of `rows` rows each, log-sum-exps `rows` apart
-    auto sweep = [&](auto is_own, int R, int rows, const float* lse, const float* po) {
-        for (int i = wp; i < R; i += kWP * kBatch) {
-            float lw[kBatch];
-            __align__(16) float x[kBatch][C];
+    // the two runs as one, so that a group's pieces and the own ones are requested together
+    const int R1 = has1 ? i0.z - i0.x + 1 : 0, R = R1 + (has2 ? i1.y - i1.x + 1 : 0);
+    const float* lse1 = p.group_lse + (size_t)i0.x * kRows + i0.y + hh;
+    const float* out1 = p.group_out + ((size_t)i0.x * D + d0) * kRows + i0.y + hh;
+    const float* lse2 = p.own_lse + (size_t)i1.x * G + hh;
+    const float* out2 = p.own_out + ((size_t)i1.x * G + hh) * D + d0;
+    for (int i = wp; i < R; i += kWP * kBatch) {
+        float lw[kBatch];
+        __align__(16) float x[kBatch][C];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int k = i + u * kWP;
-                lw[u] = -INFINITY;
-                if (k < R) {
-                    lw[u] = lse[(size_t)k * rows];
+        for (int u = 0; u < kBatch; ++u) {
+            const int k = i + u * kWP, k2 = k - R1;
+            lw[u] = -INFINITY;
+            if (k < R1) {                                               // [D][rows]
+                lw[u] = lse1[(size_t)k * kRows];
 #pragma unroll
-                    for (int c = 0; c < C; c += 4) {
-                        if constexpr (decltype(is_own)::value) {        // [rows][D]
-                            *reinterpret_cast<float4*>(&x[u][c]) = *reinterpret_cast<const float4*>(po + (size_t)k * rows * D + c);
-                        } else {                                        // [D][rows]
+                for (int c = 0; c < C; ++c) x[u][c] = out1[((size_t)k * D + c) * kRows];
+            } else if (k < R) {                                         // [G][D]
+                lw[u] = lse2[(size_t)k2 * G];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) x[u][c + e] = po[((size_t)k * D + c + e) * rows];
-                        }
-                    }
-                }
-            }
-            float top = M;
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u]);
-            if (top > M) {
-                const float f = ex2((M - top) * kLog2e);        // 0 the first time
-                den *= f;
-#pragma unroll
-                for (int c = 0; c < C; ++c) num[c] *= f;
-                M = top;
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                // -inf: no piece, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
-                const bool holds = lw[u] != -INFINITY;
-                const float w = holds ? ex2((lw[u] - M) * kLog2e) : 0.f;
-                den += w;
-#pragma unroll
-                for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? x[u][c] : 0.f, num[c]);
+                for (int c = 0; c < C; c += 4)
+                    *reinterpret_cast<float4*>(&x[u][c]) = *reinterpret_cast<const float4*>(out2 + (size_t)k2 * G * D + c);
             }
         }
-    };
-    if (has1)
-        sweep(std::false_type(), i0.z - i0.x + 1, kRows, p.group_lse + (size_t)i0.x * kRows + i0.y + hh,
-              p.group_out + ((size_t)i0.x * D + d0) * kRows + i0.y + hh);
-    if (has2)
-        sweep(std::true_type(), i1.y - i1.x + 1, G, p.own_lse + (size_t)i1.x * G + hh,
-              p.own_out + ((size_t)i1.x * G + hh) * D + d0);
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u]);
+        if (top > M) {
+            const float f = ex2((M - top) * kLog2e);        // 0 the first time
+            den *= f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c] *= f;
+            M = top;
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            // -inf: no piece, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
+            const bool holds = lw[u] != -INFINITY;
+            const float w = holds ? ex2((lw[u] - M) * kLog2e) : 0.f;
+            den += w;
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? x[u][c] : 0.f, num[c]);
+        }
+    }
     if constexpr (kWP > 1) {
         s_max[warp][lane] = M;
         s_den[warp][lane] = den;
