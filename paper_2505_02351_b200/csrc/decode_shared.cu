@@ -46,6 +46,7 @@ constexpr int kThreads = 256;
 constexpr int kGroupItem = 3, kOwnItem = 1;
 // A worker's share of the groups' list at least (a piece of theirs is 64 KB), and of the own one.
 constexpr int kMinGroupShare = 4, kMinOwnShare = 2;
+constexpr int kOwnRows = 64;              // M of an own item's products: row 16 w + h lies in lane 32 w + h of tensor memory
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
@@ -494,7 +495,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         mbar_expect_tx(&q_full[warp0], own ? (uint32_t)(G * D * 2) : (uint32_t)L::kQBytes);
 #pragma unroll 1
                         for (int h = 0; h < L::kHalves; ++h)
-                            tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * (32 * 128), own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, &q_full[warp0]);
+                            tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * (kOwnRows / 4 * 128), own ? &map_q1 : &map_q, 64 * h, kvh * G, s0, &q_full[warp0]);
                     }
                 }
             }
@@ -555,8 +556,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
         } else if (warp == 5) {
             // -------------------------------------------------------------- one thread issues S = Q K^T
-            constexpr uint32_t idesc_s = instr_desc(false, kTN);
-            const uint32_t idesc_qk = p.scale < 0.f ? instr_desc(false, kTN, true) : idesc_s;
+            const bool negate = p.scale < 0.f;
             const bool dots = p.scale != 0.f;
             const uint64_t q_desc0 = smem_desc(smem_u32(smem + kOffQ), 16, 1024);
             const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
@@ -588,6 +588,8 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     fence_proxy_async();
                     __syncwarp();
                 }
+                const uint32_t idesc_s = d.own ? instr_desc(false, kTN, false, kOwnRows) : instr_desc(false, kTN);
+                const uint32_t idesc_qk = idesc_s | (negate ? instr_desc(false, kTN, true) ^ instr_desc(false, kTN) : 0u);
                 if (lane == 0) {
                     ok = wait_for(&q_full[w0], q_ph >> w0 & 1, p.status);
 #pragma unroll 1
@@ -624,13 +626,13 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             // -------------------------------------------------------------- one thread issues O (+)= P V
             // V is MN-major, in slices of bs keys with the 64-dim halves of a slice side by side: halves bs * 128 bytes
             // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
-            constexpr uint32_t idesc_pv = instr_desc(true, D);
             const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
             const uint32_t half_slice = p.bs == 16 ? 16 * D * 2 : 2048;     // from 16 keys to the next 16 of the same 32
             int it = 0, st = 0;
             uint32_t ph = 0;
             uint32_t reading = 0, o_ph = 0;     // row warps that read the piece before; per row warp the parity of its next reading
             for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const uint32_t idesc_pv = d.own ? instr_desc(true, D, false, kOwnRows) : instr_desc(true, D);
 #pragma unroll 1
                 for (int j = 0; j < d.len; ++j, ++it) {
                     const int sb = it & 1, live = d.n - (d.tile_hi - j) * kTN;      // keys of the tile that exist

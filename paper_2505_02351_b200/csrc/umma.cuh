@@ -36,11 +36,11 @@ __device__ __forceinline__ uint64_t desc_advance(uint64_t desc, uint32_t bytes) 
     return (desc & 0xFFFFFFFF00000000ull) | (uint32_t)((uint32_t)desc + (bytes >> 4));
 }
 
-// Instruction descriptor, kind::f16: bf16 x bf16 -> fp32, M = 128, N = n, A K-major (optionally negated), B K-major
+// Instruction descriptor, kind::f16: bf16 x bf16 -> fp32, M = m, N = n, A K-major (optionally negated), B K-major
 // or MN-major.
-__host__ __device__ constexpr uint32_t instr_desc(bool b_mn_major, uint32_t n, bool negate_a = false) {
+__host__ __device__ constexpr uint32_t instr_desc(bool b_mn_major, uint32_t n, bool negate_a = false, uint32_t m = 128) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((negate_a ? 1u : 0u) << 13) | ((b_mn_major ? 1u : 0u) << 16) |
-           ((n >> 3) << 17) | ((128u >> 4) << 24);
+           ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
 // D[tmem] (+)= A[smem] * B[smem]
