@@ -6,18 +6,29 @@
 // P the keys a sequence shares, S its own.  Both are items of one kernel: over the shared keys of a group the n_g sequences
 // times the G query heads of a KV head are the rows (in blocks of 128), a real matrix product with 2 n_g G flops per byte
 // of the cache; over a sequence's own keys the G heads are the rows.  Per item S = Q K^T and O += P V run on tcgen05 over
-// 64-key tiles, accumulators in tensor memory, as a query block of the chunked prefill does.  For an own item most of a
-// 128-row tile is idle, and that costs nothing that counts: a 32 KB tile takes an SM's share of the memory bandwidth 1480
-// cycles, and the two resident CTAs need fewer for its arithmetic, idle rows or not (warps none of whose rows are live skip
-// the softmax).  So own contexts and prefixes of up to 128 rows are bound by reading the cache; prefixes of more rows by the
-// special-function unit and the tensor core, as the prefill is.
+// 64-key tiles, accumulators in tensor memory, as a query block of the chunked prefill does.  For an own item most of the
+// rows of a product (64, the fewest the instruction has) are idle, and that costs little that counts: a 32 KB tile takes an
+// SM's share of the memory bandwidth 1480 cycles, and the two resident CTAs need 1000 for its arithmetic, idle rows or not
+// (warps none of whose rows are live skip the softmax).  So own contexts and prefixes of up to 128 rows are bound by reading the
+// cache; prefixes of more rows by the special-function unit and the tensor core, as the prefill is (1.07 PFLOP/s).
+// (Products with the keys as rows and the G heads as columns, S^T = K Q^T and O^T = V^T P, waste nothing and spread the
+// exponentials over all warps, but take 80 cycles an instruction and, V^T being transposed, 160: 256 sequences in 12 groups
+// 119.6 us against 94.  128 rows instead of 64 cost power: 108.7 us against 104.3 when run without a pause.)
 //
 // The tiles of the groups' items, laid end to end, are cut into one contiguous range per worker (a CTA, two per SM), and so
-// are those of the sequences' own, as many workers for the one as for the other as their weights say, so that one long prefix
+// are those of the sequences' own, as many workers for the one as for the other as they are worth, so that one long prefix
 // fills the GPU as well as many short ones, whatever the mix.  A worker's part of an item is a piece: normalised partial rows
 // and log-sum-exps in the workspace, merged by merge_shared_kernel.  (The own contexts were first left to decode_stream.cu:
 // its mma.sync work takes issue slots and tensor cycles from the group pass beside it, and its workers drain between two
-// 16-token tiles.  Workers that take of both lists make more pieces, 22.3 against 18.7 us for 32 sequences.)
+// 16-token tiles: 28.6 us for 32 sequences behind 1500 tokens, where this took 19.3.  Workers that take of both lists make more
+// pieces: 22.3.)
+//
+// 32/8 heads, 32 sequences of 64 to 548 tokens behind 1500 shared ones: 18.5 us (37 MB: 5.7 us of copy bandwidth); 32/4
+// heads, 8 behind 32768: 24.6 us (78 MB, 12.1); 64/8 heads, 256 in 12 groups: 92 us (383 MB, 59; DRAM reads 420 MB; 103 where
+// it runs without a pause and the power limit takes the clock down to 1.75 GHz); 32/8 heads, 128 behind 16384: 62 to 68 us
+// (34.5 GFLOP, 20 at the burst rate, 24 at the sustained one).  Besides the main phase each has 5 to 7 us from the launch to the
+// first copy (the list is computed from cold memory and cold code), 3 to 5 us between a worker's mean end and the last one's,
+// 1.5 to 2.5 us until the merge may read, and 3 to 10 us of merge.
 //
 // A sequence sees whole tiles of its group only: the first e_s = floor(min(prefix, n_s) / 64) * 64 tokens, the rest is its
 // own.  So no group tile is masked inside, and where sequences of a group differ in e_s (the tiles are taken from the last
