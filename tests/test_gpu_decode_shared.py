@@ -282,3 +282,62 @@ def test_rotation_append_and_shared_decode_together():
         b.n = grown
         b.lens.copy_(torch.tensor(grown, dtype=torch.int32, device=DEV))
     assert binding.device_status() == 0
+
+
+def test_pages_past_32_bit_offsets():
+    """The same batch with its pages at the end of a pool of 2^33 bytes: element and byte offsets pass 32 bits."""
+    b = Batch(8, 2, 128, 16, sizes=[3], prefix=[200], lens=[201, 260, 330], loose=0, slopes=True)
+    want = b.check()
+    pool, used = 2 ** 33 // (2 * 16 * 128 * 2), b.k.shape[0]
+    for name in ("k", "v"):
+        big = torch.empty(pool, 2, 16, 128, dtype=torch.bfloat16, device=DEV)
+        big[pool - used:] = getattr(b, name)
+        setattr(b, name, big)
+    b.table.copy_(torch.where(b.table >= 0, b.table + (pool - used), b.table))
+    assert torch.equal(b.run(128 ** -0.5), want)
+
+
+def test_a_page_named_more_than_once():
+    """A page that a sequence names twice, and that two groups and a sequence of none have in common."""
+    b = Batch(16, 4, 64, 16, sizes=[3, 2], prefix=[256, 192], lens=[300, 310, 320, 200, 210, 150], loose=1)
+    b.table[:3, 5] = b.table[0, 2]
+    b.table[3:5, 1] = b.table[0, 2]
+    b.table[5, :2] = b.table[0, 2]
+    b.table[4, 12] = b.table[0, 17]
+    b.check()
+
+
+@pytest.mark.parametrize("slopes", [False, True])
+def test_infinite_scores_reach_the_rows_that_see_them_alone(slopes):
+    """An infinite key: a head whose score is -inf gives it no weight, one whose score is +inf has no value, and a row that
+    does not see it is not touched."""
+    b = Batch(16, 4, 128, 16, sizes=[4], prefix=[200], lens=[60, 190, 260, 300], slopes=slopes, told=[0, 190, 200, 200])
+    before = b.check()
+    shared, own = int(b.table[1, 6]), int(b.table[3, 17])
+    b.k[shared, 1, 3, 0] = float("inf")
+    b.k[own, 2, 9, 5] = float("-inf")
+    got = b.run(128 ** -0.5)
+    want, size = b.wanted(128 ** -0.5)
+    bad = torch.isnan(want)
+    assert bad.any() and not bad[0].any() and torch.equal(torch.isnan(got), bad)
+    bound = (2 * 2.0 ** -8 + 2.0 ** -12) * size + 2.0 ** -8 * want.abs() + 1e-30
+    assert bool(((got.double() - want).abs() <= bound)[~bad].all())
+    assert torch.equal(got[0], before[0])
+
+
+def test_two_graphs_with_one_workspace():
+    """Two batches captured with the same workspace, replayed one behind the other on one stream."""
+    b = Batch(32, 8, 128, 16, sizes=[6], prefix=[800], lens=[801 + 13 * i for i in range(6)], seed=4)
+    c = Batch(32, 8, 128, 16, sizes=[2, 4], prefix=[300, 1000], lens=[301, 340, 1000, 1010, 1100, 1200], slopes=True, seed=5)
+    wants = [x.check() for x in (b, c)]
+    ws, parts = max((x.workspace(512) for x in (b, c)), key=lambda t: t[0].numel())
+    outs, graphs = [torch.empty_like(x.q) for x in (b, c)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for x, out, graph in zip((b, c), outs, graphs):
+        with torch.cuda.graph(graph):
+            x.run(128 ** -0.5, ws=(ws, parts), out=out)
+    for _ in range(4):
+        for out, graph in zip(outs, graphs):
+            out.fill_(float("nan"))
+            graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], wants[0]) and torch.equal(outs[1], wants[1])
