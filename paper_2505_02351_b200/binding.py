@@ -111,12 +111,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 # The current stream's handle without building a Stream object (0.3 us per call against 3.3).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# And the current device's number once CUDA is up (0.1 us against 0.4).
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
     if stream is not None:
         return stream.cuda_stream
-    device = torch.cuda.current_device()
+    if device is None:
+        device = torch.cuda.current_device()
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
@@ -353,7 +356,7 @@ def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
 def _current_device(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
-    return torch.cuda.current_device()
+    return _raw_device()            # CUDA is up: the tensor lives there
 
 
 def rotary(q_out, q, positions, freq, layout: int, k_out=None, k=None, amplitude: float = 1.0, inverse: bool = False,
@@ -371,7 +374,7 @@ def rotary(q_out, q, positions, freq, layout: int, k_out=None, k=None, amplitude
     _check(load().opt_gqa_rotary(
         qop, qp, kop, kp, _index("positions", positions, torch.int32, T, dev), _index("freq", freq, torch.int64, -1, dev),
         2 * freq.numel(), layout, amplitude, inverse, T, Hq, Hkv, D, qos, qs, kos, ks, _DTYPE_CODE[dtype],
-        _stream(stream)), "opt_gqa_rotary")
+        _stream(stream, dev)), "opt_gqa_rotary")
 
 
 def rotary_append(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, freq, layout: int, amplitude: float = 1.0,
@@ -402,7 +405,7 @@ def rotary_append(q_out, q, k, v, k_cache, v_cache, slot_mapping, positions, fre
         qop, qp, kop, kp, vp, kcp, vcp, _index("slot_mapping", slot_mapping, torch.int64, T, dev),
         _index("positions", positions, torch.int32, T, dev), _index("freq", freq, torch.int64, -1, dev),
         2 * freq.numel(), layout, amplitude, T, Hq, Hkv, D, qs, ks, vs, bs, num_blocks, _DTYPE_CODE[dtype],
-        _stream(stream)), "opt_gqa_rotary_append")
+        _stream(stream, dev)), "opt_gqa_rotary_append")
 
 
 def shared_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, num_groups: int, max_partitions: int) -> int:
@@ -428,7 +431,7 @@ def paged_attention_decode_shared(out, q, k_cache, v_cache, block_tables, contex
         _index("group_start", group_start, torch.int32, -1, dev), _index("prefix_lens", prefix_lens, torch.int32, B, dev),
         num_groups, None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale,
         B, Hq, Hkv, D, bs, num_blocks, partition_size, _ptr(workspace), _nbytes(workspace), max_partitions,
-        _DTYPE_CODE[dtype], _stream(stream)), "opt_gqa_paged_attention_decode_shared")
+        _DTYPE_CODE[dtype], _stream(stream, dev)), "opt_gqa_paged_attention_decode_shared")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:
