@@ -244,8 +244,9 @@ int opt_gqa_paged_attention_decode_no_alloc(void* out, const void* q, const void
  *   num_groups   1 .. 512 (a group of one sequence gains nothing: leave it out of the groups)
  *   alibi_slopes, scale, partition_size, max_partitions  as in opt_gqa_paged_attention_decode_balanced: max_partitions *
  *                partition_size bounds every context.  Where that bounds the whole cache by 32 MB, every context is read
- *                for itself as in that call and its merge, and the groups are not looked at; beyond, it sizes the grid
- *                and the partitions play no part.
+ *                for itself as in that call and its merge (up to 1024 tokens: as in the single pass of
+ *                opt_gqa_paged_attention_decode) and the groups are not looked at; beyond, it sizes the grid and the
+ *                partitions play no part.
  *   workspace    opt_gqa_shared_workspace_bytes(...) bytes (host arithmetic; 0 for bad arguments), 16-byte aligned; contents
  *                need no initialisation.  Calls that can overlap on the GPU need a workspace each.
  * group_start and prefix_lens are read before the wait for the preceding kernel, like block_tables.

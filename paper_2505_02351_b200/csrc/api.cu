@@ -215,10 +215,13 @@ int opt_gqa_paged_attention_decode_local(void* out, const void* q, const void* k
                                    max_partitions, window, dtype, stream);
 }
 
-// Up to this many bytes of cache (as the host can bound them) every sequence's context is read for itself, by the balanced
-// decode and its merge: so few bytes pass through L2 in less time than the group pass needs to set out (4 sequences of 540
-// tokens behind 512 shared ones, 8 KV heads: 6.8 us against 9.6; 32 of 1770 behind 1500, 268 MB: 33 us against 19).
+// Up to this many bytes of cache (as the host can bound them) every sequence's context is read for itself: so few bytes pass
+// through L2 in less time than the group pass needs to set out (4 sequences of 540 tokens behind 512 shared ones, 8 KV heads:
+// 6.8 us against 9.6; 32 of 1770 behind 1500, 268 MB: 33 us against 19).  With contexts of up to kSharedSingleTokens by the
+// single pass, one launch; beyond by the balanced decode and its merge (32/8 heads, us: 4 sequences of 64 tokens 4.0 against 6.3,
+// of 576 6.3 against 7.1, of 1024 9.2 against 8.4, of 1900 13.7 against 12.3; a launch fewer also takes 2 us off the call).
 static constexpr double kSharedMinBytes = 32e6;
+static constexpr int64_t kSharedSingleTokens = 1024;
 
 static size_t shared_workspace_need(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
     size_t need = shared_layout(B, Hq, Hkv, D, num_groups).total;
@@ -259,6 +262,9 @@ int opt_gqa_paged_attention_decode_shared(void* out, const void* q, const void* 
     if (!status) return OPT_GQA_ERR_CUDA;
     const int64_t max_context = (int64_t)max_partitions * partition_size;
     if ((double)B * (double)max_context * Hkv * D * 4 <= kSharedMinBytes) {
+        if (max_context <= kSharedSingleTokens)
+            return decode_checked(true, 0, out, q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, alibi_slopes,
+                                  scale, B, Hq, Hkv, D, bs, num_blocks, 0, nullptr, nullptr, 0, dtype, stream);
         const int rc = decode_balanced_checked(q, k_cache, v_cache, block_tables, max_blocks_per_seq, context_lens, alibi_slopes,
                                                scale, B, Hq, Hkv, D, bs, num_blocks, partition_size, workspace, workspace_bytes,
                                                max_partitions, 0, dtype, stream);

@@ -126,7 +126,7 @@ def test_lengths_of_the_prefix_and_behind_it(prefix, own):
 def test_small_batches_and_tight_bounds(slopes):
     """The same batches with a tight bound on the contexts: whichever route a call takes, the result is the definition's."""
     for sizes, prefix, lens in (([4], [500], [501, 560, 512, 777]), ([2, 2], [64, 700], [0, 70, 701, 700]), ([3], [0], [1, 2, 0]),
-                                ([40], [600], [601 + 3 * i for i in range(40)])):
+                                ([4], [1000], [1001, 1100, 1500, 0]), ([40], [600], [601 + 3 * i for i in range(40)])):
         b = Batch(32, 8, 128, 16, sizes=sizes, prefix=prefix, lens=lens, slopes=slopes)
         b.check(P=64, ws=b.workspace(64, small=True))
 
