@@ -326,8 +326,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         gw = max(min(gw, own_total > 0 && W > 1 ? W - 1 : W), group_total > 0 ? 1 : 0);
         gw = (int)min((long long)gw, (group_total + kMinGroupShare - 1) / kMinGroupShare);
         const int o0 = W > 1 ? gw : 0, ow = (int)max(min((long long)(W - o0), own_total / kMinOwnShare), 1ll), oi = min(max(me - o0, -1), ow);
-        const long long g_lo = me < gw ? share_at(group_total, me, gw) : 0, g_hi = me < gw ? share_at(group_total, me + 1, gw) : 0;
-        const long long o_lo = share_at(own_total, max(oi, 0), ow), o_hi = share_at(own_total, min(oi + 1, ow), ow);
+        // four lanes one bound each: the groups' share's begin and end, the own one's
+        const bool of_own = lane & 2;
+        const int at = of_own ? min(max(oi + (lane & 1), 0), ow) : min(me + (lane & 1), gw);
+        const long long bound = share_at(of_own ? own_total : group_total, at, of_own ? ow : max(gw, 1));
+        const long long g_lo = __shfl_sync(kFull, bound, 0), g_hi = __shfl_sync(kFull, bound, 1);
+        const long long o_lo = __shfl_sync(kFull, bound, 2), o_hi = __shfl_sync(kFull, bound, 3);
         // the place in the list: (group, KV head, row block), row block fastest, so that the blocks of one prefix are worked on
         // at the same time and its tiles come from L2 after their first reading; then (sequence, KV head)
         int g = 0, kvh = 0, mt = 0, blocks = 1, s = 0, n = 0, jt = 0, t0 = 0, t1 = 0;    // the item's tiles t0 .. t1 - 1
