@@ -154,7 +154,6 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     uint64_t* desc_full = p_full + 2;
     uint64_t* desc_empty = desc_full + kDescs;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
-    const int4* descs = reinterpret_cast<const int4*>(smem + L::kOffDesc);
     long long* g_units = reinterpret_cast<long long*>(smem + L::kOffGroups);     // of the groups before (one head)
     int* g_kt = reinterpret_cast<int*>(g_units + kMaxGroups);
     int* g_lead = g_kt + kMaxGroups;
@@ -526,15 +525,24 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         // before any wait with a limit: what the producers wait for may take as long as it likes
         grid_dependency_wait();
         Piece d;
-        auto next_piece = [&](int pc, bool& ok) -> bool {
-            ok = __all_sync(kFull, wait_for(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
-            if (!ok) return false;
-            const int4 *at = descs + 3 * (pc % kDescs), a = at[0], b = at[1], c = at[2];
-            d.s0 = a.x, d.rows = a.y, d.kvh = a.z, d.table = a.w;
-            d.tile_hi = b.x, d.len = b.y, d.n = b.z, d.piece = b.w;
-            d.own = c.x, d.opens = c.y, d.closes = c.z, d.warp0 = c.w;
+        auto read_piece = [&](int pc) {
+            const uint32_t at = smem_u32(smem + L::kOffDesc) + 48 * (pc % kDescs);
+            auto load = [&](uint32_t from, int& x, int& y, int& z, int& w) {
+                asm volatile("ld.volatile.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(from));
+            };
+            load(at, d.s0, d.rows, d.kvh, d.table);
+            load(at + 16, d.tile_hi, d.len, d.n, d.piece);
+            load(at + 32, d.own, d.opens, d.closes, d.warp0);
+        };
+        auto release_piece = [&](int pc) {
             __syncwarp();
             if (lane == 0) mbar_arrive(&desc_empty[pc % kDescs]);
+        };
+        auto next_piece = [&](int pc, bool& ok, bool keep = false) -> bool {
+            ok = __all_sync(kFull, wait_for(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
+            if (!ok) return false;
+            read_piece(pc);
+            if (!keep) release_piece(pc);
             return d.len > 0;
         };
         bool ok = true;
@@ -705,13 +713,15 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const int ps = st == 0 ? kStages - 1 : st - 1;
                 return __all_sync(kFull, wait_for(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
             };
-            for (int pc = 0; next_piece(pc, ok); ++pc) {
-                const int rr = r - 32 * d.warp0;                    // row of the item
-                const int s = d.s0 + rr / G;
-                const bool valid = rr >= 0 && rr < d.rows;
-                const int n = valid ? __ldg(p.context_lens + s) : 0;
-                // keys the row sees: of a group's item whole tiles
-                const int e_row = !valid ? 0 : d.own ? n : shared_tokens(__ldg(p.prefix_lens + s), n);
+            for (int pc = 0; next_piece(pc, ok, true); ++pc) {
+                int n = 0, e_row = 0;       // the row's context, and of that what it sees: of a group's item whole tiles
+                {
+                    const int rr = r - 32 * d.warp0, s = d.s0 + rr / G;     // row of the item
+                    if (rr >= 0 && rr < d.rows) {
+                        n = __ldg(p.context_lens + s);
+                        e_row = d.own ? n : shared_tokens(__ldg(p.prefix_lens + s), n);
+                    }
+                }
                 const float slope2 = p.slopes ? __ldg(p.slopes + d.kvh * G + hg) * kLog2e : 0.f;
                 float m_used = -INFINITY, l = 0.f;
                 auto next_tile = [&]() {
@@ -807,6 +817,9 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 if (!ok) break;
 
                 // ---- the piece is complete once its last P V is: normalise, store, hand O back
+                read_piece(pc);             // (again, rather than in registers meanwhile)
+                const int rr = r - 32 * d.warp0, s = d.s0 + rr / G;
+                const bool valid = rr >= 0 && rr < d.rows;
                 if (__any_sync(kFull, valid)) {
                     ok = prev_pv_done();
                     if (!ok) break;
@@ -847,6 +860,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (valid)
                         (d.own ? p.own_lse + (size_t)d.piece * G : p.group_lse + (size_t)d.piece * kRows)[rr] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
                 }
+                release_piece(pc);
             }
         }
     }
