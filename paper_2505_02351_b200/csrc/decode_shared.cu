@@ -23,12 +23,13 @@
 // 16-token tiles: 28.6 us for 32 sequences behind 1500 tokens, where this took 19.3.  Workers that take of both lists make more
 // pieces: 22.3.)
 //
-// 32/8 heads, 32 sequences of 64 to 548 tokens behind 1500 shared ones: 18.5 us (37 MB: 5.7 us of copy bandwidth); 32/4
-// heads, 8 behind 32768: 24.6 us (78 MB, 12.1); 64/8 heads, 256 in 12 groups: 92 us (383 MB, 59; DRAM reads 420 MB; 103 where
-// it runs without a pause and the power limit takes the clock down to 1.75 GHz); 32/8 heads, 128 behind 16384: 62 to 68 us
-// (34.5 GFLOP, 20 at the burst rate, 24 at the sustained one).  Besides the main phase each has 5 to 7 us from the launch to the
-// first copy (the list is computed from cold memory and cold code), 3 to 5 us between a worker's mean end and the last one's,
-// 1.5 to 2.5 us until the merge may read, and 3 to 10 us of merge.
+// 32/8 heads, 32 sequences of 64 to 548 tokens behind 1500 shared ones: 17.8 us (37 MB: 5.7 us of copy bandwidth); 32/4
+// heads, 8 behind 32768: 23.9 us (78 MB, 12.1); 64/8 heads, 256 in 12 groups: 88 us (383 MB, 59; DRAM reads 419 MB; 100 to 103
+// where it runs without a pause and the power limit takes the clock down to 1.75 GHz); 32/8 heads, 128 behind 16384: 61 to 66
+// us (34.5 GFLOP, 20 at the burst rate, 24 at the sustained one).  Besides the main phase each has 5 to 7 us from the launch to
+// the first copy (the list is computed from cold memory and cold code; one CTA per SM does that while a preceding call's merge
+// runs, the other behind it), 3 to 5 us between a worker's mean end and the last one's, 1.5 to 2.5 us until the merge may read,
+// and 3 to 10 us of merge.  The row warps' loop fills their 128 registers: 24 bytes spilled cost 4 %.
 //
 // A sequence sees whole tiles of its group only: the first e_s = floor(min(prefix, n_s) / 64) * 64 tokens, the rest is its
 // own.  So no group tile is masked inside, and where sequences of a group differ in e_s (the tiles are taken from the last
