@@ -765,10 +765,12 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         for (int e = 0; e < kTN; ++e)
                             if (e >= live) v[e / 32][e % 32] = -INFINITY;
                     }
+                    // (NaN where a score is, so that such a tile is never taken for one whose weights are all zero: its sum
+                    // is NaN, and with it the row)
                     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int c = 0; c < kTN / 32; ++c) chunk_max<false>(v[c], 0, 0, 0, mx);
-                    const float m_tile = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), qscale, bias0);
+                    for (int c = 0; c < kTN / 32; ++c) chunk_max<false, true>(v[c], 0, 0, 0, mx);
+                    const float m_tile = fmaf(max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]), qscale, bias0);
                     // the running maximum moves (and l and O are rescaled) only when it grew by more than the threshold,
                     // and at the row's first tile
                     const bool begins = sees && m_used == -INFINITY;

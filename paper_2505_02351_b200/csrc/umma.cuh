@@ -130,6 +130,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// the same, NaN where one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -138,8 +145,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // Pass 1 over one 32-key chunk of a row's raw scores s = q.k + (slope/scale)*(key index in the tile): running
 // maxima.  The map to log2 units, t = s*qscale + (tile constant), is increasing, so it is applied to the maximum
 // afterwards.  kMasked adds the select of the visible keys, lo < key <= pos (causal bound pos; lo = pos - window,
-// or -1); tiles strictly inside that range skip it.
-template <bool kMasked>
+// or -1); tiles strictly inside that range skip it.  kNan: a score that is NaN makes its maximum NaN.
+template <bool kMasked, bool kNan = false>
 __device__ __forceinline__ void chunk_max(const float (&v)[32], int key0, int pos, int lo, float (&mx)[4]) {
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
@@ -148,7 +155,7 @@ __device__ __forceinline__ void chunk_max(const float (&v)[32], int key0, int po
             s0 = (key0 + e <= pos && key0 + e > lo) ? s0 : -INFINITY;
             s1 = (key0 + e + 1 <= pos && key0 + e + 1 > lo) ? s1 : -INFINITY;
         }
-        mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], s0, s1);
+        mx[(e >> 1) & 3] = kNan ? max3_nan(mx[(e >> 1) & 3], s0, s1) : max3(mx[(e >> 1) & 3], s0, s1);
     }
 }
 
