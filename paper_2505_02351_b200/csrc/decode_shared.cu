@@ -808,7 +808,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                         for (int c = 0; c < kTN / 32; ++c) {
                             uint32_t w[16];
-                            sum += chunk_exp<false>(v[c], qscale, bias_m, 0, 0, 0, w);
+                            sum += chunk_exp<false, true>(v[c], qscale, bias_m, 0, 0, 0, w);
                             tmem_st16(s_addr + c * 16, w);
                         }
                         if (sees) l += sum;

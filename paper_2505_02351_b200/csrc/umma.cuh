@@ -180,8 +180,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 
 // Pass 2 over one chunk: p = 2^(s*qscale + bias) with the tile's ALiBi constant and the row maximum folded into
-// bias; bf16 pairs for the tensor core; returns the chunk's sum of p.
-template <bool kMasked>
+// bias; bf16 pairs for the tensor core; returns the chunk's sum of p (kRounded: of the bf16 values, so that numerator and
+// denominator round alike).
+template <bool kMasked, bool kRounded = false>
 __device__ __forceinline__ float chunk_exp(const float (&v)[32], float qscale, float bias, int key0, int pos, int lo,
                                            uint32_t (&w)[16]) {
     if (kMasked) {
@@ -193,8 +194,9 @@ __device__ __forceinline__ float chunk_exp(const float (&v)[32], float qscale, f
             t0 = (key0 + 2 * e <= pos && key0 + 2 * e > lo) ? t0 : -INFINITY;
             t1 = (key0 + 2 * e + 1 <= pos && key0 + 2 * e + 1 > lo) ? t1 : -INFINITY;
             const float p0 = ex2(t0), p1 = ex2(t1);
-            sm[e & 3] += p0 + p1;
             w[e] = pack2(p0, p1);
+            const float2 sum = kRounded ? bf16x2_to_float2(w[e]) : make_float2(p0, p1);
+            sm[e & 3] += sum.x + sum.y;
         }
         return (sm[0] + sm[1]) + (sm[2] + sm[3]);
     }
@@ -206,8 +208,9 @@ __device__ __forceinline__ float chunk_exp(const float (&v)[32], float qscale, f
         float t0, t1;
         unpack_f2(t2, t0, t1);
         const float p0 = ex2(t0), p1 = ex2(t1);
-        sm2[e & 1] = add2(sm2[e & 1], pack_f2(p0, p1));
         w[e] = pack2(p0, p1);
+        const float2 sum = kRounded ? bf16x2_to_float2(w[e]) : make_float2(p0, p1);
+        sm2[e & 1] = add2(sm2[e & 1], pack_f2(sum.x, sum.y));
     }
     float s0, s1;
     unpack_f2(add2(sm2[0], sm2[1]), s0, s1);
