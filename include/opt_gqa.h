@@ -248,7 +248,8 @@ int opt_gqa_paged_attention_decode_no_alloc(void* out, const void* q, const void
  *                opt_gqa_paged_attention_decode) and the groups are not looked at; beyond, it sizes the grid and the
  *                partitions play no part.
  *   workspace    opt_gqa_shared_workspace_bytes(...) bytes (host arithmetic; 0 for bad arguments), 16-byte aligned; contents
- *                need no initialisation.  Calls that can overlap on the GPU need a workspace each.
+ *                need no initialisation.  The size never falls as B, num_groups or max_partitions grow: the largest call's serves
+ *                all others of the same heads.  Calls that can overlap on the GPU need a workspace each.
  * group_start and prefix_lens are read before the wait for the preceding kernel, like block_tables.
  * context_lens[s] == 0 gives a zero row.  bf16 only.  What a sequence does not see never reaches its row, whatever it holds.
  */

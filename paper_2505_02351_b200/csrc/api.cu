@@ -223,13 +223,13 @@ int opt_gqa_paged_attention_decode_local(void* out, const void* q, const void* k
 static constexpr double kSharedMinBytes = 32e6;
 static constexpr int64_t kSharedSingleTokens = 1024;
 
+// What the routes need, the balanced one with as many partitions (of 16 tokens at least) as it can be taken with: a size that
+// never falls as B, num_groups or max_partitions grow, so that the workspace of the largest call serves all others.
 static size_t shared_workspace_need(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {
-    size_t need = shared_layout(B, Hq, Hkv, D, num_groups).total;
-    if ((double)B * max_partitions * 16 * Hkv * D * 4 <= kSharedMinBytes) {       // partitions have 16 tokens at least
-        const size_t own = balanced_layout(B, Hq, Hkv, D, max_partitions).total;
-        need = need > own ? need : own;
-    }
-    return need;
+    const size_t need = shared_layout(B, Hq, Hkv, D, num_groups).total;
+    const long long most = (long long)(kSharedMinBytes / (16.0 * Hkv * D * 4)), partitions = (long long)B * max_partitions;
+    const size_t own = balanced_layout_of(B, Hq, Hkv, D, (unsigned long long)(partitions < most ? partitions : most)).total;
+    return need > own ? need : own;
 }
 
 size_t opt_gqa_shared_workspace_bytes(int B, int Hq, int Hkv, int D, int num_groups, int max_partitions) {

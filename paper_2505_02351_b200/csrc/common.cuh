@@ -226,16 +226,20 @@ struct BalancedLayout {
     unsigned long long rows;      // rows of partial_lse / partial_out
 };
 inline size_t round_up_256(size_t x) { return (x + 255) & ~(size_t)255; }
-inline BalancedLayout balanced_layout(int B, int Hq, int Hkv, int D, int max_partitions) {
+// partitions: of all sequences together
+inline BalancedLayout balanced_layout_of(int B, int Hq, int Hkv, int D, unsigned long long partitions) {
     BalancedLayout L;
     const unsigned long long G = (unsigned long long)(Hq / Hkv);
-    L.rows = ((unsigned long long)B * Hkv * max_partitions + kBalancedMaxWorkers) * G;
+    L.rows = (partitions * Hkv + kBalancedMaxWorkers) * G;
     L.header = 0;
     L.seq_info = 256;
     L.lse = L.seq_info + round_up_256((size_t)B * 16);
     L.out = L.lse + round_up_256((size_t)L.rows * 4);
     L.total = L.out + (size_t)L.rows * D * 4;
     return L;
+}
+inline BalancedLayout balanced_layout(int B, int Hq, int Hkv, int D, int max_partitions) {
+    return balanced_layout_of(B, Hq, Hkv, D, (unsigned long long)B * max_partitions);
 }
 
 // The step's new K/V rows for the streaming kernel to store itself (Algorithm 2, "Store reshaped K, V into C_K,
