@@ -217,9 +217,12 @@ int opt_gqa_paged_attention_decode_local(void* out, const void* q, const void* k
 
 // Up to this many bytes of cache (as the host can bound them) every sequence's context is read for itself: so few bytes pass
 // through L2 in less time than the group pass needs to set out (4 sequences of 540 tokens behind 512 shared ones, 8 KV heads:
-// 6.8 us against 9.6; 32 of 1770 behind 1500, 268 MB: 33 us against 19).  With contexts of up to kSharedSingleTokens by the
-// single pass, one launch; beyond by the balanced decode and its merge (32/8 heads, us: 4 sequences of 64 tokens 4.0 against 6.3,
-// of 576 6.3 against 7.1, of 1024 9.2 against 8.4, of 1900 13.7 against 12.3; a launch fewer also takes 2 us off the call).
+// 6.3 us against 9.6; 32 of 1770 behind 1500, 268 MB: 33 us against 18).  With contexts of up to kSharedSingleTokens by the
+// single pass, one launch; beyond by the balanced decode and its merge.  In a graph (us, single pass against balanced, contexts
+// of 64, 512, 800, 1024 and 1100 tokens) 7 sequences, 32/8 heads of 128: 3.3 6.1 8.1 9.5 9.7 against 6.3 9.0 10.1 11.1 11.7; 4:
+// 3.2 6.1 8.1 9.2 9.5 against 6.1 6.9 8.0 8.4 9.5; one: 3.2 5.9 7.8 8.9 9.2 against 5.6 5.9 6.3 6.5 6.6; 4, 64/8: 4.0 7.6 9.8
+// 11.0 11.2 against 6.5 7.9 8.6 9.2 10.0; 4, 8/8 of 64: 2.1 4.1 5.5 6.2 6.4 against 5.3 6.0 6.1 6.2 6.9.  The two cross between
+// 512 tokens and past 1100, the later the more sequences; a call made from the host is 2 us shorter with the one launch.
 static constexpr double kSharedMinBytes = 32e6;
 static constexpr int64_t kSharedSingleTokens = 1024;
 

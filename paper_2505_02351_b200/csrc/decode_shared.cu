@@ -108,7 +108,7 @@ struct SharedParams {
     float* own_out;
     int* status;
     float scale;
-    int num_groups, B, max_blocks, Hq, Hkv, bs, bs_log2, lanes_log2;
+    int num_groups, B, max_blocks, Hkv, bs, bs_log2, lanes_log2;
 };
 
 // mbar_wait with its waiting loop in one place: this kernel waits at some twenty, its warps run all over it, and its time
@@ -522,7 +522,6 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             step = true;
         }
     } else {
-        // what every other warp does first with the next piece; false at the end of the list
         // before any wait with a limit: what the producers wait for may take as long as it likes
         grid_dependency_wait();
         Piece d;
@@ -539,6 +538,7 @@ decode_shared_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(&desc_empty[pc % kDescs]);
         };
+        // what every other warp does first with the next piece; false at the end of the list
         auto next_piece = [&](int pc, bool& ok, bool keep = false) -> bool {
             ok = __all_sync(kFull, wait_for(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
             if (!ok) return false;
@@ -1105,7 +1105,6 @@ int launch_decode_shared(void* out, const void* q, const void* k_cache, const vo
     p.num_groups = N;
     p.B = B;
     p.max_blocks = max_blocks_per_seq;
-    p.Hq = Hq;
     p.Hkv = Hkv;
     p.bs = bs;
     p.bs_log2 = bs == 32 ? 5 : 4;
