@@ -23,10 +23,12 @@
 // 16-token tiles: 28.6 us for 32 sequences behind 1500 tokens, where this took 19.3.  Workers that take of both lists make more
 // pieces: 22.3.)
 //
-// 32/8 heads, 32 sequences of 64 to 548 tokens behind 1500 shared ones: 17.8 us (37 MB: 5.7 us of copy bandwidth); 32/4
-// heads, 8 behind 32768: 23.9 us (78 MB, 12.1); 64/8 heads, 256 in 12 groups: 88 us (383 MB, 59; DRAM reads 419 MB; 100 to 103
-// where it runs without a pause and the power limit takes the clock down to 1.75 GHz); 32/8 heads, 128 behind 16384: 61 to 66
-// us (34.5 GFLOP, 20 at the burst rate, 24 at the sustained one).  Besides the main phase each has 5 to 7 us from the launch to
+// 32/8 heads, 32 sequences of 64 to 548 tokens behind 1500 shared ones: 18.3 us (37 MB: 5.7 us of copy bandwidth); 32/4
+// heads, 8 behind 32768: 23.9 us (78 MB, 12.1); 64/8 heads, 256 in 12 groups: 89 us (383 MB, 59; DRAM reads 419 MB; 100 to 104
+// where it runs without a pause and the power limit takes the clock down to 1.75 GHz); 32/8 heads, 128 behind 16384: 61 to 68
+// us (34.5 GFLOP, 20 at the burst rate, 24 at the sustained one).  The weights are rounded to bf16 for P V, as in the other
+// decode kernels, and the denominator sums the rounded ones: 0.2 to 2 us of that (18.1, 24.1, 89.2, 61.0 against 17.7, 23.9,
+// 87.9, 59.5), for a value that all keys have to come out as it went in.  Besides the main phase each has 5 to 7 us from the launch to
 // the first copy (the list is computed from cold memory and cold code; one CTA per SM does that while a preceding call's merge
 // runs, the other behind it), 3 to 5 us between a worker's mean end and the last one's, 1.5 to 2.5 us until the merge may read,
 // and 3 to 10 us of merge.  The row warps' loop fills their 128 registers: 24 bytes spilled cost 4 %.

@@ -256,7 +256,8 @@ rotary_staged_kernel(const RotaryParams p) {
 template <typename T, int D, bool kInterleaved>
 int launch_staged(const RotaryParams& p, cudaStream_t stream) {
     constexpr int kStep = kRotThreads * 16 / (D * (int)sizeof(T));        // rows a CTA takes at a time
-    // as in launch_tokens: several CTAs per token of a few, four tokens per CTA of many
+    // as in launch_tokens: several CTAs per token of a few, four tokens per CTA of many (us with four against one, bf16 of 128,
+    // R 50, 24 / 40 / 80 heads: 2048 tokens 11.6 18.3 34.8 against 9.7 14.7 22.1, 4096 15.5 22.3 41.5 against 17.5 25.8 41.4)
     const int rounds = (p.Hq + p.Hk + p.Hv + kStep - 1) / kStep;
     auto launch = [&](auto kernel, long long x, int y) {
         return launch_dependent(kernel, dim3((unsigned)x, (unsigned)y), dim3(kRotThreads), 0, stream, p);
@@ -278,8 +279,11 @@ int launch_tokens(const RotaryParams& p, cudaStream_t stream) {
     if (p.T <= 512)
         return launch(rotary_kernel<T, D, P, kInterleaved, 1, 1>, p.T, (units + kRotThreads - 1) / kRotThreads);
     // Many tokens whose rows do not fill a CTA's two units per thread: four per CTA (8192 tokens of 40 heads, bf16: 28.7
-    // us against 40 with one); but not where one token fills it (4095 tokens of 72 heads, fp32: 47 us against 63 with four),
-    // nor where the grid would end up below a few CTAs per multiprocessor (1999 tokens of 24 heads: 5.6 against 6.4).
+    // us against 35 to 40 with one); but not where one token fills it (4095 tokens of 72 heads, fp32: 47 us against 63 with
+    // four).  Below, few CTAs per multiprocessor are left of a quarter of the tokens (1024 of 24 heads of 128, bf16: 5.0 us
+    // with four against 3.7, of 40: 8.0 against 5.5; 1999 of 24 of 64, fp32: 6.4 against 5.6).  The two cross near 2048 tokens
+    // already (us with four against one, bf16, 2048 / 3000 / 4095 tokens: 24 heads of 128 6.6 9.5 11.2 against 7.4 10.8 14.3;
+    // 40 of 128 9.8 14.1 16.4 against 10.3 14.4 18.8; 40 of 64 5.7 8.7 10.2 against 6.1 9.9 12.9).
     if (p.T >= 4096 && units <= 2 * kRotThreads)
         return launch(rotary_kernel<T, D, P, kInterleaved, 4, 2>, (p.T + 3ll) / 4, 1);
     return launch(rotary_kernel<T, D, P, kInterleaved, 1, 2>, p.T, 1);
