@@ -83,6 +83,9 @@ extern "C" {
 #define OPT_GQA_ROTARY_PARTS 3
 #define OPT_GQA_ROTARY_RAMP 4
 
+/* Most pools one call of the page operators takes (K and V of every layer). */
+#define OPT_GQA_MAX_POOLS 256
+
 /* Size of the scratch array built into the library for opt_gqa_paged_attention_decode_no_alloc. */
 #define OPT_GQA_STATIC_SCRATCH_BYTES (8u << 20)
 
@@ -438,6 +441,69 @@ int opt_gqa_rotary_append(void* q_out, const void* q, void* k_out, const void* k
                           void* v_cache, const int64_t* slot_mapping, const int32_t* positions, const uint64_t* freq,
                           int rot_dim, int layout, float amplitude, int T, int Hq, int Hkv, int D, int64_t q_stride,
                           int64_t k_stride, int64_t v_stride, int bs, int64_t num_blocks, int dtype, void* stream);
+
+/*
+ * The pages of the cache and whose they are (the paper's "Memory Allocation and Management Optimization" names paged memory and
+ * gives no operations; no counterpart there).  Everything lives in device memory, so that a step which forks, grows or ends
+ * sequences runs without the host seeing a page number, in a captured graph too:
+ *
+ *   pools         HOST array of num_pools (1 .. OPT_GQA_MAX_POOLS) DEVICE pointers: the pools [num_blocks, Hkv, bs, D] whose pages
+ *                 are numbered alike -- k_cache and v_cache of every layer.  Read during the call, not kept.
+ *   block_tables  [num_seqs, max_blocks_per_seq] int32, context_lens [num_seqs] int32, as the attention calls take them
+ *   ref_counts    [num_blocks] int32, 16-byte aligned: how many tables hold a page (and whoever else keeps one: a cache of prompts,
+ *                 say); a page is free where it is 0.  Before the first call: 0, and context_lens 0.
+ *   workspace     opt_gqa_pages_workspace_bytes(n, num_blocks) bytes (host arithmetic; n = 1 for the compaction; 0 for bad
+ *                 arguments), 16-byte aligned; contents need no initialisation, and the size grows with n and num_blocks.  Calls
+ *                 that can overlap on the GPU need a workspace each.
+ *   done          [n] int32 out: 1 where request i was carried out, else 0
+ *
+ * Free pages are handed out lowest number first, in the order of the requests, and a request is carried out where as many are
+ * free as it and all requests before it ask for: one whose pages are not there is left out, and so are those behind it that ask
+ * for any.  Results are the same in every run.  num_seqs rows, n <= 65535, max_blocks_per_seq * 32 and context lengths below 2^31,
+ * num_blocks <= 2^28; fp32 or bf16 pools.  The calls read their arrays behind the wait for the preceding kernel and let no later kernel
+ * start before they have ended, so that attention calls may follow on the same stream.
+ *
+ * opt_gqa_cache_copy_pages: page dst_pages[i] becomes a copy of page src_pages[i] in every pool, n pairs in one launch; a pair
+ *   with a number outside the pool (-1, say) is skipped.  The pages written are distinct and none of them is read by the same call.
+ * opt_gqa_cache_fork: row children[i] becomes a continuation of row parents[i]: what the child held is dropped, the parent's full
+ *   pages are shared (their counts grow), a part-full last page is copied to a page of the child's own, as far as it is full.
+ *   Children are distinct and none of them is a parent in the same call; several may have one parent (cheapest where they are
+ *   neighbours in the list).  A request with a row outside 0 .. num_seqs - 1 (-1, say) is void: done 0, nothing changes.  Where the
+ *   page is not there the child is left empty (length 0).
+ * opt_gqa_cache_resize: row seqs[i] gets length new_lens[i].  Shorter: the pages past it are dropped (0 frees the sequence; first
+ *   for all requests, so that others of the same call can have them).  Longer: pages are given; if its last page is part full and
+ *   another table holds it too, the row first gets a copy of its own (and all that grow do, if several hold one).  The tokens
+ *   themselves are the caller's to store.  Rows are distinct.  A row outside, a negative length or one past the table is void.
+ *   A row whose pages are not there keeps its length.
+ * opt_gqa_cache_compact: with U the number of pages in use, the k-th of those numbered U or more moves to the k-th free page
+ *   below U, in every pool; then the pages from U on are free.  used_out [1] gets U, page_map [num_blocks] every page's new
+ *   number (-1 of a free one), block_tables_out and ref_counts_out the tables (entries that hold no token as they were) and counts,
+ *   which may be the inputs.  What a page held stays in it until the page is given away: a caller that keeps the old tables can
+ *   still attend through them.
+ *
+ * Table entries whose page was dropped and that get no other become -1; others past a row's length are left as they are.  Contract (not
+ * checked on the device): entries below a row's length are its pages, counted in ref_counts.  A number that breaks it makes
+ * wrong tables, never an access outside the arrays.
+ */
+size_t opt_gqa_pages_workspace_bytes(int n, int64_t num_blocks);
+
+int opt_gqa_cache_copy_pages(void* const* pools, int num_pools, const int32_t* src_pages, const int32_t* dst_pages, int n, int Hkv,
+                             int D, int bs, int64_t num_blocks, int dtype, void* stream);
+
+int opt_gqa_cache_fork(void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
+                       int32_t* ref_counts, const int32_t* parents, const int32_t* children, int n, int32_t* done, int num_seqs,
+                       int Hkv, int D, int bs, int64_t num_blocks, void* workspace, size_t workspace_bytes, int dtype,
+                       void* stream);
+
+int opt_gqa_cache_resize(void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
+                         int32_t* ref_counts, const int32_t* seqs, const int32_t* new_lens, int n, int32_t* done, int num_seqs,
+                         int Hkv, int D, int bs, int64_t num_blocks, void* workspace, size_t workspace_bytes, int dtype,
+                         void* stream);
+
+int opt_gqa_cache_compact(void* const* pools, int num_pools, const int32_t* block_tables, int32_t* block_tables_out,
+                          int max_blocks_per_seq, const int32_t* context_lens, const int32_t* ref_counts, int32_t* ref_counts_out,
+                          int32_t* page_map, int32_t* used_out, int num_seqs, int Hkv, int D, int bs, int64_t num_blocks,
+                          void* workspace, size_t workspace_bytes, int dtype, void* stream);
 
 /*
  * One decode step of the attention layer, Algorithm 2 from "Store reshaped K, V

@@ -60,6 +60,11 @@ SIGNATURES = {
                             _vp]),
     "opt_gqa_rotary_append": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _f, _i, _i, _i, _i, _i64,
                                    _i64, _i64, _i, _i64, _i, _vp]),
+    "opt_gqa_pages_workspace_bytes": (_c.c_size_t, [_i, _i64]),
+    "opt_gqa_cache_copy_pages": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i64, _i, _vp]),
+    "opt_gqa_cache_fork": (_i, [_vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
+    "opt_gqa_cache_resize": (_i, [_vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
+    "opt_gqa_cache_compact": (_i, [_vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
     "opt_gqa_decode_step": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i, _i, _i, _i64,
                                  _i, _vp, _sz, _i, _i, _vp]),
     "opt_gqa_decode_step_host": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _f, _i, _i, _i, _i,
@@ -432,6 +437,95 @@ def paged_attention_decode_shared(out, q, k_cache, v_cache, block_tables, contex
         num_groups, None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale,
         B, Hq, Hkv, D, bs, num_blocks, partition_size, _ptr(workspace), _nbytes(workspace), max_partitions,
         _DTYPE_CODE[dtype], _stream(stream, dev)), "opt_gqa_paged_attention_decode_shared")
+
+
+class PagePools:
+    """The pools of a cache whose pages are numbered alike (K and V of every layer), looked up once: see page_pools."""
+
+    def __init__(self, pools):
+        if not pools:
+            raise ValueError("pools: expected at least one tensor [blocks, heads, block size, dims]")
+        first = pools[0]
+        self.device = _current_device(first)
+        if first.dim() != 4 or first.dtype not in _DTYPE_CODE:
+            raise ValueError("pools: expected fp32 or bf16 tensors [blocks, heads, block size, dims]")
+        self.shape, self.dtype = first.shape, first.dtype
+        for t in pools:
+            if t.shape != first.shape or t.dtype != first.dtype or not t.is_contiguous() or t.get_device() != self.device:
+                raise ValueError("pools: expected contiguous tensors of one shape and type on the current CUDA device")
+        self.tensors = tuple(pools)                   # keeps them alive
+        self.num_blocks, self.Hkv, self.bs, self.D = first.shape
+        self.count = len(pools)
+        self.pointers = (_vp * self.count)(*[t.data_ptr() for t in pools])
+        self.address = _c.addressof(self.pointers)
+        self.code = _DTYPE_CODE[first.dtype]
+
+
+def page_pools(pools) -> PagePools:
+    """Handle of the pools for the page operators: k_cache and v_cache of every layer, all [blocks, heads, block size, dims]."""
+    return PagePools(pools)
+
+
+def pages_workspace_bytes(n: int, num_blocks: int) -> int:
+    return int(load().opt_gqa_pages_workspace_bytes(n, num_blocks))
+
+
+def _pools_device(pools: PagePools) -> int:
+    dev = _raw_device()
+    if dev != pools.device:
+        raise ValueError("expected pools on the current CUDA device")
+    return dev
+
+
+def _table(block_tables, context_lens, dev: int):
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables: expected a row per sequence")
+    S, W = block_tables.shape
+    return (_index("block_tables", block_tables, torch.int32, -1, dev), S, W,
+            _index("context_lens", context_lens, torch.int32, S, dev))
+
+
+def cache_copy_pages(pools: PagePools, src_pages, dst_pages, stream=None) -> None:
+    """Page dst_pages[i] becomes a copy of page src_pages[i] in every pool (int32; a pair with a number outside is skipped)."""
+    dev, n = _pools_device(pools), src_pages.numel()
+    _check(load().opt_gqa_cache_copy_pages(
+        pools.address, pools.count, _index("src_pages", src_pages, torch.int32, n, dev),
+        _index("dst_pages", dst_pages, torch.int32, n, dev), n, pools.Hkv, pools.D, pools.bs, pools.num_blocks, pools.code,
+        _stream(stream, dev)), "opt_gqa_cache_copy_pages")
+
+
+def _pages(entry: str, pools, block_tables, context_lens, ref_counts, a, b, done, workspace, stream) -> None:
+    dev, n = _pools_device(pools), a.numel()
+    bt, S, W, lens = _table(block_tables, context_lens, dev)
+    _check(getattr(load(), entry)(
+        pools.address, pools.count, bt, W, lens, _index("ref_counts", ref_counts, torch.int32, pools.num_blocks, dev),
+        _index("requests", a, torch.int32, n, dev), _index("requests", b, torch.int32, n, dev), n,
+        _index("done", done, torch.int32, n, dev), S, pools.Hkv, pools.D, pools.bs, pools.num_blocks, _ptr(workspace),
+        _nbytes(workspace), pools.code, _stream(stream, dev)), entry)
+
+
+def cache_fork(pools: PagePools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream=None) -> None:
+    """Rows `children` continue rows `parents`: full pages shared, a part-full last page copied.  done [n] int32: 1 where it was."""
+    _pages("opt_gqa_cache_fork", pools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream)
+
+
+def cache_resize(pools: PagePools, block_tables, context_lens, ref_counts, seqs, new_lens, done, workspace, stream=None) -> None:
+    """Rows `seqs` get the lengths `new_lens`: pages dropped (0 frees a sequence) or given.  done [n] int32: 1 where it was."""
+    _pages("opt_gqa_cache_resize", pools, block_tables, context_lens, ref_counts, seqs, new_lens, done, workspace, stream)
+
+
+def cache_compact(pools: PagePools, block_tables, context_lens, ref_counts, block_tables_out, ref_counts_out, page_map, used_out,
+                  workspace, stream=None) -> None:
+    """The pages in use move to the front of the pools; outputs may be their inputs.  page_map: old number -> new one or -1."""
+    dev, nb = _pools_device(pools), pools.num_blocks
+    bt, S, W, lens = _table(block_tables, context_lens, dev)
+    if block_tables_out.shape != block_tables.shape:
+        raise ValueError("block_tables_out: expected the shape of block_tables")
+    _check(load().opt_gqa_cache_compact(
+        pools.address, pools.count, bt, _index("block_tables_out", block_tables_out, torch.int32, -1, dev), W, lens,
+        _index("ref_counts", ref_counts, torch.int32, nb, dev), _index("ref_counts_out", ref_counts_out, torch.int32, nb, dev),
+        _index("page_map", page_map, torch.int32, nb, dev), _index("used_out", used_out, torch.int32, 1, dev), S, pools.Hkv,
+        pools.D, pools.bs, nb, _ptr(workspace), _nbytes(workspace), pools.code, _stream(stream, dev)), "opt_gqa_cache_compact")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

@@ -438,6 +438,99 @@ int opt_gqa_rotary_append(void* q_out, const void* q, void* k_out, const void* k
     return rotary_checked(a, stream);
 }
 
+// The checks the page calls share.  num_blocks and the tables' width bound every index that the kernels form.
+static int pools_checked(void* const* pools, int num_pools, int Hkv, int D, int bs, int64_t num_blocks, int dtype, PoolSet* set, PageShape* sh) {
+    if (!dtype_ok(dtype)) return OPT_GQA_ERR_DTYPE;
+    if (num_pools <= 0 || num_pools > OPT_GQA_MAX_POOLS || Hkv <= 0 || Hkv > 65535 || (D != 64 && D != 128) || (bs != 16 && bs != 32) ||
+        num_blocks <= 0 || num_blocks > (1 << 28))
+        return OPT_GQA_ERR_SHAPE;
+    if (!pools) return OPT_GQA_ERR_NULL;
+    for (int i = 0; i < num_pools; ++i)
+        if (!pools[i]) return OPT_GQA_ERR_NULL;
+    for (int i = 0; i < num_pools; ++i) {
+        if (!aligned16(pools[i])) return OPT_GQA_ERR_ALIGN;
+        set->p[i] = static_cast<char*>(pools[i]);
+    }
+    sh->num_pools = num_pools, sh->num_blocks = (int)num_blocks;
+    sh->row_bytes = (unsigned)D * (dtype == OPT_GQA_FP32 ? 4 : 2);
+    sh->head_bytes = sh->row_bytes * (unsigned)bs;
+    sh->page_bytes = sh->head_bytes * (unsigned)Hkv;
+    return OPT_GQA_OK;
+}
+
+// num_seqs rows of max_blocks entries; every length that fits them is an int
+static bool tables_ok(int num_seqs, int max_blocks) { return num_seqs > 0 && max_blocks > 0 && max_blocks <= INT32_MAX / 32; }
+
+size_t opt_gqa_pages_workspace_bytes(int n, int64_t num_blocks) {
+    if (n <= 0 || n > 65535 || num_blocks <= 0 || num_blocks > (1 << 28)) return 0;
+    return page_work_layout(n, (int)num_blocks, nullptr, nullptr);
+}
+
+int opt_gqa_cache_copy_pages(void* const* pools, int num_pools, const int32_t* src_pages, const int32_t* dst_pages, int n, int Hkv, int D,
+                             int bs, int64_t num_blocks, int dtype, void* stream) {
+    PoolSet set;
+    PageShape sh;
+    if (n < 0) return OPT_GQA_ERR_SHAPE;
+    const int rc = pools_checked(pools, num_pools, Hkv, D, bs, num_blocks, dtype, &set, &sh);
+    if (rc != OPT_GQA_OK) return rc;
+    if (n == 0) return OPT_GQA_OK;
+    if (!src_pages || !dst_pages) return OPT_GQA_ERR_NULL;
+    return launch_copy_pages(set, sh, src_pages, dst_pages, n, static_cast<cudaStream_t>(stream));
+}
+
+static int requests_checked(bool fork, void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
+                            int32_t* ref_counts, const int32_t* a, const int32_t* b, int n, int32_t* done, int num_seqs, int Hkv, int D,
+                            int bs, int64_t num_blocks, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+    PoolSet set;
+    PageShape sh;
+    if (n < 0 || n > 65535 || !tables_ok(num_seqs, max_blocks_per_seq)) return OPT_GQA_ERR_SHAPE;
+    const int rc = pools_checked(pools, num_pools, Hkv, D, bs, num_blocks, dtype, &set, &sh);
+    if (rc != OPT_GQA_OK) return rc;
+    if (n == 0) return OPT_GQA_OK;
+    if (!block_tables || !context_lens || !ref_counts || !a || !b || !done || !workspace) return OPT_GQA_ERR_NULL;
+    if (workspace_bytes < page_work_layout(n, (int)num_blocks, nullptr, nullptr)) return OPT_GQA_ERR_SHAPE;
+    if (!aligned16(ref_counts) || !aligned16(workspace)) return OPT_GQA_ERR_ALIGN;
+    PageWork w;
+    page_work_layout(n, (int)num_blocks, static_cast<char*>(workspace), &w);
+    const PageTables t = {block_tables, context_lens, ref_counts, num_seqs, max_blocks_per_seq, bs, (int)num_blocks};
+    const PageRequests r = {a, b, done, n};
+    return fork ? launch_fork(set, sh, t, r, w, static_cast<cudaStream_t>(stream)) : launch_resize(set, sh, t, r, w, static_cast<cudaStream_t>(stream));
+}
+
+int opt_gqa_cache_fork(void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
+                       int32_t* ref_counts, const int32_t* parents, const int32_t* children, int n, int32_t* done, int num_seqs, int Hkv,
+                       int D, int bs, int64_t num_blocks, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+    return requests_checked(true, pools, num_pools, block_tables, max_blocks_per_seq, context_lens, ref_counts, parents, children, n, done,
+                            num_seqs, Hkv, D, bs, num_blocks, workspace, workspace_bytes, dtype, stream);
+}
+
+int opt_gqa_cache_resize(void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
+                         int32_t* ref_counts, const int32_t* seqs, const int32_t* new_lens, int n, int32_t* done, int num_seqs, int Hkv,
+                         int D, int bs, int64_t num_blocks, void* workspace, size_t workspace_bytes, int dtype, void* stream) {
+    return requests_checked(false, pools, num_pools, block_tables, max_blocks_per_seq, context_lens, ref_counts, seqs, new_lens, n, done,
+                            num_seqs, Hkv, D, bs, num_blocks, workspace, workspace_bytes, dtype, stream);
+}
+
+int opt_gqa_cache_compact(void* const* pools, int num_pools, const int32_t* block_tables, int32_t* block_tables_out, int max_blocks_per_seq,
+                          const int32_t* context_lens, const int32_t* ref_counts, int32_t* ref_counts_out, int32_t* page_map,
+                          int32_t* used_out, int num_seqs, int Hkv, int D, int bs, int64_t num_blocks, void* workspace,
+                          size_t workspace_bytes, int dtype, void* stream) {
+    PoolSet set;
+    PageShape sh;
+    if (!tables_ok(num_seqs, max_blocks_per_seq)) return OPT_GQA_ERR_SHAPE;
+    const int rc = pools_checked(pools, num_pools, Hkv, D, bs, num_blocks, dtype, &set, &sh);
+    if (rc != OPT_GQA_OK) return rc;
+    if (!block_tables || !block_tables_out || !context_lens || !ref_counts || !ref_counts_out || !page_map || !used_out || !workspace)
+        return OPT_GQA_ERR_NULL;
+    if (workspace_bytes < page_work_layout(1, (int)num_blocks, nullptr, nullptr)) return OPT_GQA_ERR_SHAPE;
+    if (!aligned16(ref_counts) || !aligned16(workspace)) return OPT_GQA_ERR_ALIGN;
+    PageWork w;
+    page_work_layout(1, (int)num_blocks, static_cast<char*>(workspace), &w);
+    const PageTables t = {const_cast<int32_t*>(block_tables), const_cast<int32_t*>(context_lens), const_cast<int32_t*>(ref_counts),
+                          num_seqs, max_blocks_per_seq, bs, (int)num_blocks};
+    return launch_compact(set, sh, t, block_tables_out, ref_counts_out, page_map, used_out, w, static_cast<cudaStream_t>(stream));
+}
+
 // Bytes of `workspace` a decode step of these sizes uses: the balanced split's layout for bf16 caches, one
 // (D + 1)-float row per (sequence, head, partition) for fp32 caches, nothing for a single pass.
 static size_t step_workspace_need(int B, int Hq, int Hkv, int D, int partition_size, int max_partitions, int dtype) {

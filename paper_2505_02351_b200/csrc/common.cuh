@@ -340,4 +340,54 @@ int launch_prompt_umma(void* out, const void* q, const void* k, const void* v, c
                        int total_q_tokens, int max_q_len, const float* alibi_slopes, float scale, int B, int Hq,
                        int Hkv, int D, int* device_status, cudaStream_t stream);
 
+// The pools of a cache whose pages are numbered alike (K and V of every layer), by value in a kernel's arguments.
+struct PoolSet {
+    char* p[OPT_GQA_MAX_POOLS];
+};
+struct PageShape {
+    int num_pools, num_blocks;
+    unsigned page_bytes, head_bytes, row_bytes;     // of a page in one pool, of one head's rows in it, of one row
+};
+struct PageTables {
+    int *tables, *lens, *refs;                      // [rows, width], [rows], [num_blocks]
+    int rows, width, bs, num_blocks;
+};
+// n requests: (parent, child) or (sequence, new length)
+struct PageRequests {
+    const int *a, *b;
+    int* done;
+    int n;
+};
+// Workspace of the page calls.  Per request: pages asked (-1: void), the table entry they begin at, rows of a part-full page to
+// copy, from which page to which, pages asked before it (in its CTA's share of the list); and the free pages to hand out.  The
+// compaction keeps the pages it moves (from, to, count) in src, dst and rows, and how many in first[0].
+struct PageWork {
+    int *need, *first, *rows, *src, *dst, *free_list;
+    long long* before;
+};
+inline size_t page_work_layout(int n, int num_blocks, char* base, PageWork* w) {
+    const size_t requests = n > num_blocks / 2 + 1 ? (size_t)n : (size_t)num_blocks / 2 + 1;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char* p = base + off;
+        off += round_up_256(bytes);
+        return p;
+    };
+    PageWork l;
+    l.before = reinterpret_cast<long long*>(take((size_t)(n > 0 ? n : 1) * 8));
+    l.need = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
+    l.first = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
+    l.rows = reinterpret_cast<int*>(take(requests * 4));
+    l.src = reinterpret_cast<int*>(take(requests * 4));
+    l.dst = reinterpret_cast<int*>(take(requests * 4));
+    l.free_list = reinterpret_cast<int*>(take((size_t)num_blocks * 4));
+    if (w) *w = l;
+    return off;
+}
+int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, int n, cudaStream_t stream);
+int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream);
+int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream);
+int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& t, int* tables_out, int* refs_out, int* page_map, int* used,
+                   const PageWork& w, cudaStream_t stream);
+
 }  // namespace optgqa
