@@ -330,6 +330,36 @@ int opt_gqa_paged_attention_prefill_local(void* out, const void* q, const int32_
                                           void* stream);
 
 /*
+ * Multi-token attention over the paged cache for any mix of chunks: the operation of opt_gqa_paged_attention_prefill (and, with
+ * window > 0, of _prefill_local), with the work split along the contexts as well as over the rows.  One call serves sequences
+ * with one new token (decode rows), with a few (drafts to verify) and with many (a prompt's chunk); few new tokens behind
+ * long contexts fill the GPU (the prefill gives a block of rows to one CTA).
+ *
+ *   out           [total_q_tokens, Hq, D]  bf16; rows no sequence has (behind q_start_loc[B], say) are left as they are
+ *   q             bf16 rows of Hq * D values, q_stride (a HOST value, elements, a multiple of 8, >= Hq * D) from token to token,
+ *                 so that q may be a slice of the fused projection's rows
+ *   q_start_loc   [B+1] int32, total_q_tokens, max_q_len, block_tables, context_lens  as in opt_gqa_paged_attention_prefill: new
+ *                 token i of sequence s sits at position pos = n_s - q_len_s + i, its K/V are in the cache already.  A sequence
+ *                 may have none.  Where q_len_s > n_s (padding: n_s = 0, say) the tokens before position 0 give zero rows.
+ *   alibi_slopes  [Hq] fp32 or NULL;  scale  any
+ *   window        0: none; > 0: keys pos - window < j <= pos
+ *   num_blocks    num_blocks * Hkv * bs < 2^31
+ *   workspace     opt_gqa_chunk_workspace_bytes(Hq, Hkv, D, max_q_len) bytes (host arithmetic; 0 for bad arguments), 16-byte aligned;
+ *                 contents need no initialisation.  The size grows with max_q_len up to 128 / G tokens and not with the batch:
+ *                 the one for 128 tokens serves all calls of the same heads.  Calls that can overlap on the GPU need one each.
+ * bf16 only.  Weights are rounded to bf16 for the product with V and the denominator sums the rounded ones.  Keys and values past
+ * a sequence's end never reach a row, whatever they hold; new tokens of one sequence share tiles, so a V row that is not
+ * finite can reach those of them that do not see its key.
+ */
+int opt_gqa_paged_attention_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_start_loc, int total_q_tokens,
+                                  int max_q_len, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                                  int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale, int B,
+                                  int Hq, int Hkv, int D, int bs, int64_t num_blocks, int window, void* workspace,
+                                  size_t workspace_bytes, int dtype, void* stream);
+
+size_t opt_gqa_chunk_workspace_bytes(int Hq, int Hkv, int D, int max_q_len);
+
+/*
  * The prompt branch with empty caches (Algorithms 1 and 2: "Caches are empty" -> "Adjust Q, K, V
  * for GQA grouping", "Create ALiBi bias", then Eq. 3-5): every sequence attends causally to its own
  * new tokens, read from contiguous tensors instead of the paged cache.  Token i of sequence s

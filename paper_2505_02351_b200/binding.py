@@ -50,6 +50,9 @@ SIGNATURES = {
                                                   _i, _vp, _sz, _i, _i, _i, _vp]),
     "opt_gqa_paged_attention_prefill_local": (_i, [_vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i,
                                                    _i, _i, _i64, _i, _i, _vp]),
+    "opt_gqa_paged_attention_chunk": (_i, [_vp, _vp, _i64, _vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i, _i, _i,
+                                           _i64, _i, _vp, _sz, _i, _vp]),
+    "opt_gqa_chunk_workspace_bytes": (_c.c_size_t, [_i, _i, _i, _i]),
     "opt_gqa_prompt_attention": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _f, _i, _i, _i, _i, _i, _vp]),
     "opt_gqa_paged_attention_decode_shared": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _f, _i, _i, _i, _i,
                                                    _i, _i64, _i, _vp, _sz, _i, _i, _vp]),
@@ -437,6 +440,32 @@ def paged_attention_decode_shared(out, q, k_cache, v_cache, block_tables, contex
         num_groups, None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale,
         B, Hq, Hkv, D, bs, num_blocks, partition_size, _ptr(workspace), _nbytes(workspace), max_partitions,
         _DTYPE_CODE[dtype], _stream(stream, dev)), "opt_gqa_paged_attention_decode_shared")
+
+
+def chunk_workspace_bytes(Hq: int, Hkv: int, D: int, max_q_len: int) -> int:
+    return int(load().opt_gqa_chunk_workspace_bytes(Hq, Hkv, D, max_q_len))
+
+
+def paged_attention_chunk(out, q, q_start_loc, max_q_len: int, k_cache, v_cache, block_tables, context_lens, alibi_slopes,
+                          scale: float, workspace, window: int = 0, stream=None) -> None:
+    """Causal attention of any mix of new tokens per sequence over the paged cache; q may be a slice of wider rows."""
+    shape, pool, dtype, dev = q.shape, k_cache.shape, q.dtype, _current_device(q)
+    T, Hq, D = shape
+    num_blocks, Hkv, bs, _ = pool
+    B = context_lens.numel()
+    if out.shape != shape or pool != (num_blocks, Hkv, bs, D) or v_cache.shape != pool:
+        raise ValueError("expected out like q and k_cache, v_cache [blocks, heads, block size, dims of q]")
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError("block_tables: expected a row per sequence")
+    qp, qs = _rows("q", q, shape, dtype, dev)
+    _check(load().opt_gqa_paged_attention_chunk(
+        _index("out", out, dtype, -1, dev), qp, qs, _index("q_start_loc", q_start_loc, torch.int32, B + 1, dev), T, max_q_len,
+        _index("k_cache", k_cache, dtype, -1, dev), _index("v_cache", v_cache, dtype, -1, dev),
+        _index("block_tables", block_tables, torch.int32, -1, dev), block_tables.shape[1],
+        _index("context_lens", context_lens, torch.int32, B, dev),
+        None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, B, Hq, Hkv, D, bs,
+        num_blocks, window, _ptr(workspace), _nbytes(workspace), _DTYPE_CODE[dtype], _stream(stream, dev)),
+        "opt_gqa_paged_attention_chunk")
 
 
 class PagePools:

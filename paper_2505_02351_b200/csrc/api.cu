@@ -337,6 +337,34 @@ int opt_gqa_paged_attention_prefill_local(void* out, const void* q, const int32_
                            stream);
 }
 
+size_t opt_gqa_chunk_workspace_bytes(int Hq, int Hkv, int D, int max_q_len) {
+    if (!shape_ok(Hq, Hkv, D, 16) || max_q_len <= 0) return 0;
+    return chunk_layout(Hq, Hkv, D, max_q_len).total;
+}
+
+int opt_gqa_paged_attention_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_start_loc, int total_q_tokens,
+                                  int max_q_len, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                                  int max_blocks_per_seq, const int32_t* context_lens, const float* alibi_slopes, float scale, int B,
+                                  int Hq, int Hkv, int D, int bs, int64_t num_blocks, int window, void* workspace,
+                                  size_t workspace_bytes, int dtype, void* stream) {
+    if (dtype != OPT_GQA_BF16) return OPT_GQA_ERR_DTYPE;
+    if (B < 0 || B > 65535 || max_q_len < 0 || total_q_tokens < 0 || !shape_ok(Hq, Hkv, D, bs) || Hkv > 65535 ||
+        max_blocks_per_seq < 0 || num_blocks < 0 || window < 0)
+        return OPT_GQA_ERR_SHAPE;
+    if (B == 0 || max_q_len == 0 || total_q_tokens == 0) return OPT_GQA_OK;
+    if (num_blocks == 0 || max_blocks_per_seq == 0) return OPT_GQA_ERR_SHAPE;
+    if (q_stride < (int64_t)Hq * D || q_stride >= (int64_t)1 << 38) return OPT_GQA_ERR_SHAPE;      // (what a tensor map holds, in bytes: 2^40)
+    if (!out || !q || !q_start_loc || !k_cache || !v_cache || !block_tables || !context_lens || !workspace) return OPT_GQA_ERR_NULL;
+    if (workspace_bytes < chunk_layout(Hq, Hkv, D, max_q_len).total) return OPT_GQA_ERR_SHAPE;
+    if (!aligned16(out) || !aligned16(q) || q_stride % 8 != 0 || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace))
+        return OPT_GQA_ERR_ALIGN;
+    int* status = device_status_ptr();
+    if (!status) return OPT_GQA_ERR_CUDA;
+    return launch_chunk(out, q, q_stride, q_start_loc, total_q_tokens, max_q_len, k_cache, v_cache, block_tables, max_blocks_per_seq,
+                        context_lens, alibi_slopes, scale, B, Hq, Hkv, D, bs, num_blocks, window, workspace, status,
+                        static_cast<cudaStream_t>(stream));
+}
+
 int opt_gqa_prompt_attention(void* out, const void* q, const void* k, const void* v, const int32_t* q_start_loc,
                              int total_q_tokens, int max_q_len, const float* alibi_slopes, float scale, int B, int Hq,
                              int Hkv, int D, int dtype, void* stream) {

@@ -1,0 +1,917 @@
+// Attention of a chunk of new tokens per sequence over the paged cache, causal, with ALiBi and a local window where asked: one
+// token (a decode row), a few (drafts to verify) or many (a prompt's chunk), in one batch.
+//
+//     out[t, h] = sum_j softmax_j(scale <q_t, k_j> - slope_h (pos_t - j)) v_j,   max(0, pos_t - window + 1) <= j <= pos_t
+//
+// An item is (sequence, KV head, block of up to 128 rows), a row being (new token, head of the group), over the 64-key tiles
+// that some row of the block sees; S = Q K^T and O += P V run on tcgen05 with accumulators in tensor memory, softmax with a
+// running maximum by one thread per row.  The items' tiles, laid end to end, are cut into one contiguous range per worker (a CTA,
+// two per SM), so that one long context fills the GPU as well as a large ragged batch.  A range covers whole items, written
+// out at once, and at its two ends parts of items: normalised partial rows and log-sum-exps in the workspace, two places a worker,
+// merged by chunk_merge_kernel.  (The chunked prefill gives a block of rows to one CTA whatever the context: with few new tokens
+// most of the GPU is idle.)
+//
+// Blocks of up to 32 rows lie in the lanes of one row warp, those of up to 64 in two: items take the warps in turns, so that one
+// block's last product and its storing overlap the next one's first scores.  Warps none of whose rows see a tile skip its softmax.
+//
+// Bound: few rows per sequence, the reading of the cache (2 q G flop per byte); blocks of 128 rows, tensor core and
+// special-function unit, as in the prefill.
+//
+// Eight warps: 0-3 one thread per row (softmax), 4 the list of pieces and the TMA copies of Q and K, 6 those of V, 5 and 7
+// issue S = Q K^T and O += P V.  Every wait is a bounded mbarrier wait.
+#include "umma.cuh"
+
+namespace optgqa {
+
+namespace {
+
+constexpr int kRows = kChunkRows;
+constexpr int kTN = 64;                    // keys per tile
+constexpr int kStages = 2;                 // of the K ring and of the V ring
+constexpr int kCtasPerSm = 2;
+constexpr int kThreads = 256;
+// The cut counts tiles, and for an item besides (the next one's Q, the wait for its last P V, storing the rows) about as many of
+// them as it costs time: a block of more than 32 rows occupies the row warps all together.
+constexpr int kFullItem = 3, kSmallItem = 1;
+constexpr int kMinShare = 2;               // a worker's share at least
+constexpr int kNarrowRows = 16;            // up to which the products take 64 rows: row 16 w + i lies in lane 32 w + i
+constexpr int kDescs = 4;                  // pieces described ahead
+constexpr int kDescBytes = 64;
+constexpr unsigned kFull = 0xffffffffu;
+constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
+
+constexpr int kHalfBytes = kTN * 128;      // one 64-dim column half of a K tile
+constexpr int kQHalfBytes = kRows * 128;   // one 64-dim column half of the Q tile
+constexpr int kQuarterBytes = 32 * 128;    // a row warp's rows in it
+// The ALiBi term inside a tile rides on the tensor core as one more k-step (see prefill_umma.cu): slope / |scale| as
+// three bf16 values against the key's index in the tile.
+constexpr int kExtRowGroupBytes = 256;
+constexpr int kQxBytes = kRows / 8 * kExtRowGroupBytes;
+constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
+// barriers: q_full[4], q_empty[4], o_empty[4], k_full[], k_empty[], v_full[], v_empty[], s_full[2], p_full[2],
+// desc_full[], desc_empty[]
+constexpr int kNumBars = 12 + 4 * kStages + 4 + 2 * kDescs;
+constexpr int kDescReaders = 7;            // warps that read a descriptor: all but the one that writes it
+
+template <int D>
+struct ChLayout {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;
+    static constexpr int kQBytes = kHalves * kQHalfBytes;
+    static constexpr int kOffQ = 0;
+    static constexpr int kOffK = kQBytes;
+    static constexpr int kOffV = kOffK + kStages * kTileBytes;
+    static constexpr int kOffQx = kOffV + kStages * kTileBytes;
+    static constexpr int kOffKp = kOffQx + kQxBytes;
+    static constexpr int kOffBar = kOffKp + kKpBytes;
+    static constexpr int kOffDesc = kOffBar + kNumBars * 8 + 16;
+    static constexpr int kSmemBytes = kOffDesc + kDescs * kDescBytes + 1024;
+};
+
+constexpr uint32_t kColS = 0;              // S buffers at 0 and kTN, P over the first half of its S
+constexpr uint32_t kColO = 2 * kTN;
+constexpr uint32_t kTmemCols = 256;
+
+struct ChunkParams {
+    __nv_bfloat16* out;
+    const int32_t* q_start_loc;
+    const int32_t* block_tables;
+    const int32_t* context_lens;
+    const float* slopes;
+    int32_t* info;              // see ChunkLayout, as the pieces below
+    float* lse;
+    float* part;
+    int* status;
+    float scale;
+    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows;
+};
+
+// A sequence of the batch: its rows of q, context, position of its first new token, and its blocks first .. blocks - 1 that see a key.
+struct Seq {
+    int q0, q, n, pos0, first, blocks;
+};
+
+template <int TQ>
+__device__ __forceinline__ Seq sequence(const ChunkParams& p, int s) {
+    Seq x;
+    // (inside the rows and the promised length, whatever the arrays hold)
+    x.q0 = min(max(__ldg(p.q_start_loc + s), 0), p.total_q);
+    x.q = min(max(min(__ldg(p.q_start_loc + s + 1), p.total_q) - x.q0, 0), p.max_q);
+    x.n = max(__ldg(p.context_lens + s), 0);
+    x.pos0 = x.n - x.q;
+    x.blocks = x.n > 0 ? (x.q + TQ - 1) / TQ : 0;
+    x.first = x.pos0 < 0 ? min(-x.pos0 / TQ, x.blocks) : 0;
+    return x;
+}
+
+// The tiles lo .. hi - 1 that the rows of block mt see.
+template <int TQ>
+__device__ __forceinline__ void block_tiles(const Seq& x, int mt, int window, int& lo, int& hi) {
+    hi = (x.pos0 + min((mt + 1) * TQ, x.q) - 1) / kTN + 1;
+    lo = window > 0 ? max(0, x.pos0 + mt * TQ - window + 1) / kTN : 0;
+}
+
+// What the other warps need to know of a piece.
+struct Piece {
+    int q0, rows, kvh, s;           // row of q of the block's first token, rows, KV head, sequence
+    int tile_hi, len, n, slot;      // last tile and how many, context, place in the workspace (-1: the whole item, rows to out)
+    int pos0, warp0, once, pad;     // position of the block's first token; the row warp whose lanes are the first rows;
+                                    // whether the tiles are read for this block alone
+};
+
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant__ CUtensorMap map_q16,
+             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const ChunkParams p) {
+    using L = ChLayout<D>;
+    constexpr int kTileBytes = L::kTileBytes, kOffQ = L::kOffQ, kOffK = L::kOffK, kOffV = L::kOffV, kOffQx = L::kOffQx,
+                  kOffKp = L::kOffKp;
+    constexpr int TQ = kRows / G;          // tokens per block
+    extern __shared__ char smem_raw[];
+    char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kOffBar);
+    uint64_t* q_full = bars;                    // [4], by the block's first row warp
+    uint64_t* q_empty = bars + 4;
+    uint64_t* o_empty = bars + 8;               // [4], one per row warp
+    uint64_t* k_full = bars + 12;
+    uint64_t* k_empty = k_full + kStages;
+    uint64_t* v_full = k_empty + kStages;
+    uint64_t* v_empty = v_full + kStages;
+    uint64_t* s_full = v_empty + kStages;
+    uint64_t* p_full = s_full + 2;
+    uint64_t* desc_full = p_full + 2;
+    uint64_t* desc_empty = desc_full + kDescs;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
+    // units (one head) of the sequences before each thread's chunk, from its warp's first on, and of each warp's chunks; gone
+    // once the K ring is in use
+    long long* c_units = reinterpret_cast<long long*>(smem + kOffK);
+    long long* w_units = c_units + kThreads;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 192) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q32) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q16) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
+    auto item_cost = [&](const Seq& x) { return x.q * G > 32 ? kFullItem : kSmallItem; };
+    auto seq_units = [&](const Seq& x) {
+        int sum = 0;
+        for (int mt = x.first; mt < x.blocks; ++mt) {
+            int lo, hi;
+            block_tiles<TQ>(x, mt, p.window, lo, hi);
+            sum += hi - lo;
+        }
+        return sum + (x.blocks - x.first) * item_cost(x);
+    };
+
+    // ------------------------------------------------------------------ the items (the index arrays are read before the
+    // wait for the preceding kernel: see the ordering contract in the header)
+    const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
+    {
+        long long sum = 0;
+        for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) sum += seq_units(sequence<TQ>(p, s));
+        long long incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += v;
+        }
+        c_units[threadIdx.x] = incl - sum;
+        if (lane == 31) w_units[warp] = incl;
+    }
+    if (threadIdx.x == 128) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&q_full[i], 1);
+            mbar_init(&q_empty[i], 1);
+            mbar_init(&o_empty[i], 32);
+        }
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&k_full[i], 1);
+            mbar_init(&k_empty[i], 1);
+            mbar_init(&v_full[i], 1);
+            mbar_init(&v_empty[i], 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], kRows);
+        }
+#pragma unroll
+        for (int i = 0; i < kDescs; ++i) {
+            mbar_init(&desc_full[i], 1);
+            mbar_init(&desc_empty[i], kDescReaders);
+        }
+        tmem_slot[1] = 0;
+        fence_barrier_init();
+    }
+    // The scale may have any sign (see prefill_umma.cu).
+    const float sabs = p.scale == 0.f ? 1.f : fabsf(p.scale);
+    const bool alibi = p.slopes != nullptr || p.scale == 0.f;
+    if (alibi && threadIdx.x >= kThreads - kTN) {
+        const int e = threadIdx.x - (kThreads - kTN);
+        const uint32_t eb = __bfloat16_as_ushort(__float2bfloat16_rn((float)e));      // exact: e < 256
+        char* row = smem + kOffKp + (e >> 3) * kExtRowGroupBytes + (e & 7) * 16;
+        *reinterpret_cast<uint4*>(row) = make_uint4(eb | (eb << 16), eb, 0u, 0u);
+        *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async();
+    }
+    if (warp == 5) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                     "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_proxy_async();                // c_units lies where the copies of K will land
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_launch();           // not before this CTA has its tensor memory: a later grid's could take it and wait for this one
+
+    if (warp == 4) {
+        // ------------------------------------------------------------------ the list of pieces, Q and K
+        long long total = 0;
+        for (int w = 0; w < kThreads / 32; ++w) total += w_units[w];
+        total *= p.Hkv;
+        const int me = blockIdx.x, W = (int)max(min((long long)gridDim.x, total / kMinShare), 1ll);
+        // this worker's share of the list
+        const long long begin = share_at(total, min(me, W), W), end = share_at(total, min(me + 1, W), W);
+        Seq x = {};
+        int s = 0, kvh = 0, mt = 0, jt = 0, t0 = 0, t1 = 0;        // the item's tiles t0 .. t1 - 1, jt of them done
+        long long pos = end;                                        // in the list: the next tile's place
+        if (begin < end) {
+            // the last thread's chunk that begins at or before the share, and its begin
+            int at = 0;
+            long long before = 0;
+            while (at < kThreads / 32 - 1 && before + w_units[at] * p.Hkv <= begin) before += w_units[at++] * p.Hkv;
+            at = at * 32 + __popc(__ballot_sync(kFull, before + c_units[at * 32 + lane] * p.Hkv <= begin)) - 1;
+            before += c_units[at] * p.Hkv;
+            int units = 0;
+            for (s = at * chunk; s < p.B; ++s) {
+                x = sequence<TQ>(p, s);
+                units = seq_units(x);
+                if (before + units * (long long)p.Hkv > begin) break;
+                before += units * (long long)p.Hkv;
+            }
+            if (s < p.B) {                                          // (always so: the shares end where the items do)
+                const long long r = begin - before;
+                kvh = r < 0x7fffffff ? (int)r / units : (int)(r / units);
+                int in_item = (int)(r - (long long)kvh * units) - item_cost(x);
+                for (mt = x.first;; ++mt) {                         // an item's tile j lies its cost + j behind its begin
+                    block_tiles<TQ>(x, mt, p.window, t0, t1);
+                    if (in_item < t1 - t0 || mt == x.blocks - 1) break;
+                    in_item -= t1 - t0 + item_cost(x);
+                }
+                jt = max(in_item, 0);
+                pos = begin + jt - in_item;
+            }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        const int slices = kTN >> p.bs_log2, sub = lane & (slices - 1), hf = lane >> (6 - p.bs_log2);
+        const bool issues = lane < slices * L::kHalves;
+        char* ring = smem + kOffK + hf * kHalfBytes + sub * p.bs * 128;
+        int st = 0;
+        uint32_t ph = 1;                    // parity of a stage's last release (none yet: passes)
+        const uint64_t read_once = l2_policy_evict_first(), read_again = l2_policy_evict_normal();
+        uint32_t owner = 0xffff, q_ph = 0;  // per quarter of Q (4 bits) whose block it holds (by its first row warp; f: none that
+                                            // has not been seen done), and the parity of that barrier's next release
+        int next_warp = 0;
+        // what the merge needs to know: the part of an item at the share's end that others continue, and at its begin
+        int4 open_a = make_int4(0, 0, 0, 0), open_b = make_int4(0, 0, 0, 0);
+        bool waited = false;
+        for (int pc = 0;; ++pc) {
+            const unsigned room = (unsigned)max(min(end - pos, (long long)0x3fffffff), 0ll);
+            const int len = (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
+            const int rows = min(TQ, x.q - mt * TQ) * G, wide = rows > 64 ? 4 : rows > 32 ? 2 : 1;
+            const bool opens = jt == 0, closes = jt + len == t1 - t0, once = x.blocks - x.first <= 1;
+            const int tile_hi = t0 + jt + len - 1, q0 = x.q0 + mt * TQ, pos0 = x.pos0 + mt * TQ;
+            // the row warps in turns
+            const int warp0 = ((next_warp + wide - 1) & ~(wide - 1)) & 3;
+            next_warp = warp0 + wide;
+            bool ok = __all_sync(kFull, wait_for(&desc_empty[pc % kDescs], ((pc / kDescs) & 1) ^ 1, p.status));
+            if (!ok) break;
+            const int slot = opens && closes ? -1 : 2 * me + (opens ? 1 : 0);
+            if (lane == 0) {
+                int4* d = reinterpret_cast<int4*>(smem + L::kOffDesc + kDescBytes * (pc % kDescs));
+                d[0] = make_int4(q0, rows, kvh, s);
+                d[1] = make_int4(tile_hi, len, x.n, slot);
+                d[2] = make_int4(pos0, warp0, once, 0);
+                mbar_arrive(&desc_full[pc % kDescs]);
+            }
+            if (len == 0) break;
+            if (!opens) open_b.x = closes ? 2 : 1;
+            else if (!closes) open_a = make_int4(1, q0, rows, kvh), open_b.y = pos0;
+            const int32_t* table = p.block_tables + (size_t)s * p.max_blocks;
+            const int pages = min((x.n + p.bs - 1) >> p.bs_log2, p.max_blocks);       // the table is not read past them
+            auto page_of = [&](int j) {
+                const int i = (tile_hi - j) * slices + sub;
+                return issues && i < pages ? __ldg(table + i) : 0;
+            };
+            int page = page_of(0);
+#pragma unroll 1
+            for (int j = 0; j < len; ++j) {
+                const int row = (page * p.Hkv + kvh) * p.bs;                       // row of the [rows, D] view
+                const int live = min(slices, (x.n - (tile_hi - j) * kTN + p.bs - 1) >> p.bs_log2);    // slices that hold keys
+                page = j + 1 < len ? page_of(j + 1) : 0;
+                ok = __all_sync(kFull, wait_for(&k_empty[st], ph, p.status));
+                if (!ok) break;
+                // q and the cache may still be written, the workspace still read, by the preceding kernel
+                if (!waited) grid_dependency_wait();
+                waited = true;
+                if (lane == 0) mbar_expect_tx(&k_full[st], (uint32_t)(live * p.bs * D * 2));
+                __syncwarp();
+                if (issues && sub < live) tma_load_2d_hint(ring + st * kTileBytes, &map_k, 64 * hf, row, &k_full[st], once ? read_once : read_again);
+                if (++st == kStages) st = 0, ph ^= 1;
+                if (j == 0) {
+                    // Q behind the first K tile, once the scores of the blocks whose rows lie there are done
+#pragma unroll 1
+                    for (int w = warp0; w < warp0 + wide; ++w) {
+                        const uint32_t o = owner >> (4 * w) & 15;
+                        if (o == 15) continue;
+                        ok = ok && __all_sync(kFull, wait_for(&q_empty[o], q_ph >> o & 1, p.status));
+                        q_ph ^= 1u << o;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if ((owner >> (4 * i) & 15) == o) owner |= 15u << (4 * i);
+                    }
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int w = warp0; w < warp0 + wide; ++w) owner = (owner & ~(15u << (4 * w))) | (uint32_t)warp0 << (4 * w);
+                    if (lane == 0) {
+                        // whole quarters of 32 rows (or 16): rows past the block's are others' or zeros and reach no live row
+                        const bool narrow = rows <= kNarrowRows;
+                        mbar_expect_tx(&q_full[warp0], (uint32_t)(narrow ? kNarrowRows * D * 2 : wide * 32 * D * 2));
+#pragma unroll 1
+                        for (int w = 0; w < wide; ++w)
+#pragma unroll
+                            for (int h = 0; h < L::kHalves; ++h)
+                                tma_load_3d(smem + kOffQ + h * kQHalfBytes + (warp0 + w) * kQuarterBytes, narrow ? &map_q16 : &map_q32, 64 * h,
+                                            kvh * G, q0 + w * (32 / G), &q_full[warp0]);
+                    }
+                }
+            }
+            if (!ok) break;
+            // on to the next item, where there is one
+            pos += len;
+            jt = 0;
+            if (pos < end) {
+                if (++mt == x.blocks) {
+                    if (++kvh == p.Hkv) {
+                        kvh = 0;
+                        for (++s; s < p.B; ++s) {
+                            x = sequence<TQ>(p, s);
+                            if (x.first < x.blocks) break;
+                        }
+                        if (s == p.B) pos = end;        // cannot happen: the shares end where the items do
+                    }
+                    mt = x.first;
+                }
+                block_tiles<TQ>(x, mt, p.window, t0, t1);
+                pos += item_cost(x);
+            }
+        }
+        if (!waited) grid_dependency_wait();
+        if (lane == 0) {
+            int4* info = reinterpret_cast<int4*>(p.info + kChunkInfoWords * me);
+            info[0] = open_a;
+            info[1] = open_b;
+        }
+    } else {
+        // before any wait with a limit: what the producers wait for may take as long as it likes
+        grid_dependency_wait();
+        Piece d;
+        auto read_piece = [&](int pc) {
+            const uint32_t at = smem_u32(smem + L::kOffDesc) + kDescBytes * (pc % kDescs);
+            auto load = [&](uint32_t from, int& x, int& y, int& z, int& w) {
+                asm volatile("ld.volatile.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(x), "=r"(y), "=r"(z), "=r"(w) : "r"(from));
+            };
+            load(at, d.q0, d.rows, d.kvh, d.s);
+            load(at + 16, d.tile_hi, d.len, d.n, d.slot);
+            load(at + 32, d.pos0, d.warp0, d.once, d.pad);
+        };
+        auto release_piece = [&](int pc) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&desc_empty[pc % kDescs]);
+        };
+        // what every other warp does first with the next piece; false at the end of the list
+        auto next_piece = [&](int pc, bool& ok, bool keep = false) -> bool {
+            ok = __all_sync(kFull, wait_for(&desc_full[pc % kDescs], (pc / kDescs) & 1, p.status));
+            if (!ok) return false;
+            read_piece(pc);
+            if (!keep) release_piece(pc);
+            return d.len > 0;
+        };
+        bool ok = true;
+        if (warp == 6) {
+            // -------------------------------------------------------------- V
+            // A box is all of a slice (the bs tokens of a page), half after half: see the issuing thread for the layout.
+            const int slices = kTN >> p.bs_log2, sub = lane & (slices - 1);
+            const bool issues = lane < slices;
+            char* ring = smem + kOffV + sub * p.bs * (D * 2);
+            int st = 0;
+            uint32_t ph = 1;
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const uint64_t policy = d.once ? l2_policy_evict_first() : l2_policy_evict_normal();
+                const int32_t* table = p.block_tables + (size_t)d.s * p.max_blocks;
+                const int pages = min((d.n + p.bs - 1) >> p.bs_log2, p.max_blocks);
+                auto page_of = [&](int j) {
+                    const int i = (d.tile_hi - j) * slices + sub;
+                    return issues && i < pages ? __ldg(table + i) : 0;
+                };
+                int page = page_of(0);
+#pragma unroll 1
+                for (int j = 0; j < d.len; ++j) {
+                    const int row = (page * p.Hkv + d.kvh) * p.bs;
+                    const int live = min(slices, (d.n - (d.tile_hi - j) * kTN + p.bs - 1) >> p.bs_log2);
+                    page = j + 1 < d.len ? page_of(j + 1) : 0;
+                    ok = __all_sync(kFull, wait_for(&v_empty[st], ph, p.status));
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(&v_full[st], (uint32_t)(live * p.bs * D * 2));
+                    __syncwarp();
+                    if (issues && sub < live) tma_load_3d_hint(ring + st * kTileBytes, &map_v, 0, row, 0, &v_full[st], policy);
+                    if (++st == kStages) st = 0, ph ^= 1;
+                }
+                if (!ok) break;
+            }
+        } else if (warp == 5) {
+            // -------------------------------------------------------------- one thread issues S = Q K^T
+            const bool negate = p.scale < 0.f;
+            const bool dots = p.scale != 0.f;
+            const uint64_t q_desc0 = smem_desc(smem_u32(smem + kOffQ), 16, 1024);
+            const uint64_t k_desc0 = smem_desc(smem_u32(smem + kOffK), 16, 1024);
+            const uint64_t qx_desc = smem_desc_plain(smem_u32(smem + kOffQx), 128, kExtRowGroupBytes);
+            const uint64_t kp_desc = smem_desc_plain(smem_u32(smem + kOffKp), 128, kExtRowGroupBytes);
+            int it = 0, st = 0, qx_kvh = -1;
+            uint32_t ph = 0, q_ph = 0;          // q_ph: per quarter of Q the parity of its next filling
+            uint64_t* last_q = nullptr;         // where the piece before says that its scores are done, and the parity of that
+            uint32_t last_ph = 0;
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const int w0 = d.warp0;
+                if (alibi && d.kvh != qx_kvh) {
+                    // The ALiBi step's operand for this KV head: slope / |scale| as a sum of three bf16 values, the rows a head
+                    // each in turn.  Nothing reads the one before once that piece's last scores are there.
+                    if (pc > 0) ok = __all_sync(kFull, wait_for(last_q, last_ph, p.status));
+                    if (!ok) break;
+                    qx_kvh = d.kvh;
+#pragma unroll 1
+                    for (int r = lane; r < kRows; r += 32) {
+                        const float a = p.slopes ? __ldg(p.slopes + d.kvh * G + r % G) / sabs : 0.f;
+                        const __nv_bfloat16 a0 = __float2bfloat16_rn(a);
+                        const __nv_bfloat16 a1 = __float2bfloat16_rn(a - __bfloat162float(a0));
+                        const __nv_bfloat16 a2 = __float2bfloat16_rn(a - __bfloat162float(a0) - __bfloat162float(a1));
+                        char* row = smem + kOffQx + (r >> 3) * kExtRowGroupBytes + (r & 7) * 16;
+                        *reinterpret_cast<uint4*>(row) = make_uint4((uint32_t)__bfloat16_as_ushort(a0) | ((uint32_t)__bfloat16_as_ushort(a1) << 16),
+                                                                    (uint32_t)__bfloat16_as_ushort(a2), 0u, 0u);
+                        *reinterpret_cast<uint4*>(row + 128) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                // products of 64 rows: Q begins so that their rows 16 w0 .. 16 w0 + 15 are the quarter's first
+                const bool narrow = d.rows <= kNarrowRows;
+                const uint64_t qd = desc_advance(q_desc0, narrow ? w0 * (kQuarterBytes - kNarrowRows * 128) : 0);
+                const uint32_t idesc_s = narrow ? instr_desc(false, kTN, false, 64) : instr_desc(false, kTN);
+                const uint32_t idesc_qk = idesc_s | (negate ? instr_desc(false, kTN, true) ^ instr_desc(false, kTN) : 0u);
+                if (lane == 0) {
+                    ok = wait_for(&q_full[w0], q_ph >> w0 & 1, p.status);
+#pragma unroll 1
+                    for (int j = 0; ok && j < d.len; ++j, ++it) {
+                        const int sb = it & 1;
+                        // the score buffer is free once the P V of the tile before the last one has read its weights there
+                        // (kStages is 2: that tile's V stage is this tile's)
+                        if (it >= 2) ok = wait_for(&v_empty[st], ph ^ 1, p.status);
+                        ok = ok && wait_for(&k_full[st], ph, p.status);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t kd = desc_advance(k_desc0, st * kTileBytes);
+                        const uint32_t s_tmem = tmem_base + kColS + sb * kTN;
+                        if (dots) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                umma_ss(s_tmem, desc_advance(qd, (ks >> 2) * kQHalfBytes + (ks & 3) * 32),
+                                        desc_advance(kd, (ks >> 2) * kHalfBytes + (ks & 3) * 32), idesc_qk, ks > 0);
+                        }
+                        if (alibi) umma_ss(s_tmem, qx_desc, kp_desc, idesc_s, dots);
+                        tc_commit(&s_full[sb]);
+                        tc_commit(&k_empty[st]);
+                        if (j == d.len - 1) tc_commit(&q_empty[w0]);
+                        if (++st == kStages) st = 0, ph ^= 1;
+                    }
+                }
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                last_q = &q_empty[w0];
+                last_ph = q_ph >> w0 & 1;
+                q_ph ^= 1u << w0;
+            }
+        } else if (warp == 7) {
+            // -------------------------------------------------------------- one thread issues O (+)= P V
+            // V is MN-major, in slices of bs keys with the 64-dim halves of a slice side by side: halves bs * 128 bytes
+            // apart (leading offset), groups of 8 keys 1 KiB apart (stride offset), slices bs * D * 2 bytes.
+            const uint64_t v_desc0 = smem_desc(smem_u32(smem + kOffV), p.bs * 128, 1024);
+            const uint32_t half_slice = p.bs == 16 ? 16 * D * 2 : 2048;     // from 16 keys to the next 16 of the same 32
+            int it = 0, st = 0;
+            uint32_t ph = 0;
+            uint32_t reading = 0, o_ph = 0;     // row warps that read the piece before; per row warp the parity of its next reading
+            for (int pc = 0; next_piece(pc, ok); ++pc) {
+                const uint32_t idesc_pv = d.rows <= kNarrowRows ? instr_desc(true, D, false, 64) : instr_desc(true, D);
+#pragma unroll 1
+                for (int j = 0; j < d.len; ++j, ++it) {
+                    const int sb = it & 1, live = d.n - (d.tile_hi - j) * kTN;      // keys of the tile that exist
+                    ok = __all_sync(kFull, wait_for(&v_full[st], ph, p.status));
+                    if (!ok) break;
+                    if (live < kTN) {
+                        // Rows past the sequence's end hold whatever the page held, or stale shared memory where no page
+                        // exists: zero them, so that a weight of 0 times garbage cannot be NaN.
+#pragma unroll 1
+                        for (int r = live + (lane >> 3); r < kTN; r += 4) {
+                            char* vrow = smem + kOffV + st * kTileBytes + (r >> p.bs_log2 << p.bs_log2) * (D * 2) + (r & (p.bs - 1)) * 128 + (lane & 7) * 16;
+#pragma unroll
+                            for (int b = 0; b < L::kHalves; ++b)
+                                *reinterpret_cast<uint4*>(vrow + b * p.bs * 128) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_proxy_async();
+                        __syncwarp();
+                    }
+                    if (lane == 0) {
+                        ok = wait_for(&p_full[sb], (it >> 1) & 1, p.status);
+                        if (j == 0) {           // O of the piece before has been read
+#pragma unroll 1
+                            for (int w = 0; w < 4; ++w)
+                                if (reading >> w & 1) ok = ok && wait_for(&o_empty[w], o_ph >> w & 1, p.status);
+                            o_ph ^= reading;
+                        }
+                        if (ok) {
+                            tc_fence_after();
+                            const uint64_t vd = desc_advance(v_desc0, st * kTileBytes);
+                            const uint32_t p_tmem = tmem_base + kColS + sb * kTN;
+#pragma unroll
+                            for (int kk = 0; kk < kTN / 16; ++kk) {
+                                const uint32_t at = (kk >> 1) * 32 * (D * 2) + (kk & 1) * half_slice;
+                                umma_ts(tmem_base + kColO, p_tmem + kk * 8, desc_advance(vd, at), idesc_pv, j > 0 || kk > 0);
+                            }
+                            tc_commit(&v_empty[st]);
+                        }
+                    }
+                    ok = __all_sync(kFull, ok);
+                    if (!ok) break;
+                    if (++st == kStages) st = 0, ph ^= 1;
+                }
+                if (!ok) break;
+                reading = ((1u << ((d.rows + 31) / 32)) - 1) << d.warp0;
+            }
+        } else {
+            // -------------------------------------------------------------- one thread per row: softmax, rescale, store
+            const int r = threadIdx.x, hg = r % G;       // (32 is a multiple of G)
+            // rows before position 0 (more new tokens than context: padding) see nothing and are zero
+            for (int s = blockIdx.x * 4 + warp; s < p.B; s += gridDim.x * 4) {
+                const Seq x = sequence<TQ>(p, s);
+                const int none = min(x.q, -x.pos0);
+                uint4* o = reinterpret_cast<uint4*>(p.out + (size_t)x.q0 * p.Hq * D);
+                for (long long i = lane; i < (long long)none * p.Hq * (D / 8); i += 32) o[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            const float qscale = sabs * kLog2e;
+            const uint32_t lane_addr = tmem_base + ((uint32_t)(warp * 32) << 16);
+            int it = 0, st = 0;                     // tile, and the stage and parity of its V
+            uint32_t ph = 0;
+            // waits for the P V of the tile before this one
+            auto prev_pv_done = [&]() {
+                const int ps = st == 0 ? kStages - 1 : st - 1;
+                return __all_sync(kFull, wait_for(&v_empty[ps], st == 0 ? ph ^ 1 : ph, p.status));
+            };
+            for (int pc = 0; next_piece(pc, ok, true); ++pc) {
+                // the row's position, and the last key before those it sees; a row that is not there sees none
+                int pos = -1, lo = -1;
+                {
+                    const int rr = r - 32 * d.warp0;
+                    if (rr >= 0 && rr < d.rows) {
+                        pos = d.pos0 + rr / G;
+                        if (p.window > 0) lo = pos - p.window;
+                    }
+                }
+                const float slope2 = p.slopes ? __ldg(p.slopes + d.kvh * G + hg) * kLog2e : 0.f;
+                float m_used = -INFINITY, l = 0.f;
+                bool begun = false;                 // the row saw a tile of the piece
+                auto next_tile = [&]() {
+                    ++it;
+                    if (++st == kStages) st = 0, ph ^= 1;
+                };
+                for (int j = 0; j < d.len; ++j, next_tile()) {
+                    const int sb = it & 1, j0 = (d.tile_hi - j) * kTN;
+                    ok = __all_sync(kFull, wait_for(&s_full[sb], (it >> 1) & 1, p.status));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const bool sees = j0 <= pos && j0 + kTN - 1 > lo;
+                    if (!__any_sync(kFull, sees || begun)) {
+                        // no row of the warp has begun: what the tensor core adds to their O from this tile's scores,
+                        // read as if they were weights, is discarded when they do
+                        tc_fence_before();
+                        mbar_arrive(&p_full[sb]);
+                        continue;
+                    }
+                    const uint32_t s_addr = lane_addr + kColS + sb * kTN;
+                    const float bias0 = slope2 * (float)(j0 - pos);       // ALiBi term of the tile's first key
+                    float v[kTN / 32][32];
+                    {
+                        uint32_t raw[kTN / 32][32];
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) tmem_ld32_issue(s_addr + c * 32, raw[c]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) {
+                            tmem_pin(raw[c]);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[c][e] = __uint_as_float(raw[c][e]);
+                        }
+                    }
+                    if (__any_sync(kFull, j0 + kTN - 1 > pos || j0 <= lo)) {
+                        // -inf in the place of what the row does not see: both passes then run as they are
+                        const int top = pos - j0, bottom = lo - j0;
+#pragma unroll
+                        for (int e = 0; e < kTN; ++e)
+                            if (e > top || e <= bottom) v[e / 32][e % 32] = -INFINITY;
+                    }
+                    // (NaN where a score is, so that such a tile is never taken for one whose weights are all zero: its sum
+                    // is NaN, and with it the row)
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < kTN / 32; ++c) chunk_max<false, true>(v[c], 0, 0, 0, mx);
+                    const float m_tile = fmaf(max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]), qscale, bias0);
+                    // the running maximum moves (and l and O are rescaled) only when it grew by more than the threshold,
+                    // and at the row's first tile
+                    const bool begins = sees && m_used == -INFINITY;
+                    const bool need = sees && m_tile > m_used + kRescaleThreshold;
+                    const float m_new = need ? m_tile : m_used;
+                    const float f = need ? ex2(m_used - m_new) : 1.f;
+                    if (j > 0 && __any_sync(kFull, need || begins)) {
+                        ok = prev_pv_done();
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            float o[32];
+                            uint32_t w[32];
+                            tmem_ld32(lane_addr + kColO + c * 32, o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) w[e] = begins ? 0u : __float_as_uint(o[e] * f);
+                            tmem_st32(lane_addr + kColO + c * 32, w);
+                        }
+                    }
+                    begun |= sees;
+                    m_used = m_new;
+                    l *= f;
+                    const float m_sub = m_used == -INFINITY ? 0.f : m_used;
+                    const float bias_m = bias0 - m_sub;
+                    // every weight of the tile is exactly zero (see prefill_umma.cu), or the row does not see it
+                    const bool all_zero = __all_sync(kFull, !sees || m_tile - m_used < -127.f);
+                    if (all_zero) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) w[e] = 0u;
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) tmem_st16(s_addr + c * 16, w);
+                    } else {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int c = 0; c < kTN / 32; ++c) {
+                            uint32_t w[16];
+                            sum += chunk_exp<false, true>(v[c], qscale, bias_m, 0, 0, 0, w);
+                            tmem_st16(s_addr + c * 16, w);
+                        }
+                        if (sees) l += sum;
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&p_full[sb]);
+                }
+                if (!ok) break;
+
+                // ---- the piece is complete once its last P V is: normalise, store, hand O back
+                read_piece(pc);             // (again, rather than in registers meanwhile)
+                const int rr = r - 32 * d.warp0;
+                const bool valid = rr >= 0 && rr < d.rows;
+                if (__any_sync(kFull, valid)) {
+                    ok = prev_pv_done();
+                    if (!ok) break;
+                    tc_fence_after();
+                    const float inv = 1.f / l;
+                    __nv_bfloat16* orow = p.out + ((size_t)(d.q0 + rr / G) * p.Hq + d.kvh * G + hg) * D;
+                    // a part is [D][rows], so that 32 neighbouring rows are one line
+                    float* part = p.part + (size_t)d.slot * D * p.slot_rows + rr;
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        float o[32];
+                        tmem_ld32(lane_addr + kColO + c * 32, o);
+                        if (c == D / 32 - 1) {                      // the next piece may overwrite O
+                            tc_fence_before();
+                            mbar_arrive(&o_empty[warp]);
+                        }
+                        if (begun && d.slot < 0) {
+                            uint4* po = reinterpret_cast<uint4*>(orow + c * 32);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                po[e] = make_uint4(pack2(o[8 * e] * inv, o[8 * e + 1] * inv), pack2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                                   pack2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                        } else if (begun) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) part[(size_t)(c * 32 + e) * p.slot_rows] = o[e] * inv;
+                        }
+                    }
+                    // a row that saw nothing of the piece: weight zero
+                    if (valid && d.slot >= 0) p.lse[(size_t)d.slot * p.slot_rows + rr] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
+                }
+                release_piece(pc);
+            }
+        }
+    }
+
+    // ---- every role is done with tensor memory: give it back (after a wait that gave up, let what is in flight drain)
+    if (*reinterpret_cast<volatile int*>(p.status) != 0) tmem_slot[1] = 1;
+    tc_fence_before();
+    __syncthreads();
+    if (tmem_slot[1]) {
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == 5) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+    }
+}
+
+// ----------------------------------------------------------------------------- merge
+// blockIdx.x: a worker whose last piece others continue; its parts are that one and the first ones of the workers behind it up
+// to the one that closes the item.  A CTA merges 32 rows of it, a lane per row, its eight warps C columns each.
+constexpr int kMergeWarps = 8;
+
+struct ChunkMergeParams {
+    __nv_bfloat16* out;
+    const int32_t* info;
+    const float* lse;
+    const float* part;
+    int W, Hq, total_q, slot_rows;
+};
+
+template <int D, int G, int C>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+chunk_merge_kernel(const ChunkMergeParams p) {
+    constexpr int kBatch = 32 / C;
+    grid_dependency_launch();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = blockIdx.x;
+    grid_dependency_wait();
+    const int4 open = *reinterpret_cast<const int4*>(p.info + kChunkInfoWords * me);
+    const int row = blockIdx.y * 32 + lane;
+    if (open.x != 1 || (int)blockIdx.y * 32 >= open.z) return;
+    const int pos0 = p.info[kChunkInfoWords * me + 5];
+    int parts = 1;                                          // workers behind this one that go on with its item
+    for (int at = me + 1;; at += 32) {
+        const bool more = at + lane < p.W && p.info[kChunkInfoWords * (at + lane) + 4] == 1;
+        const unsigned run = __ballot_sync(kFull, more);
+        if (run != kFull) {
+            parts += __ffs(~run);                           // and the one that closes it
+            break;
+        }
+        parts += 32;
+    }
+    parts = min(parts, p.W - me);
+    const int d0 = (blockIdx.z * kMergeWarps + warp) * C;
+    float M = -INFINITY, den = 0.f, num[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) num[c] = 0.f;
+    for (int i = 0; i < parts; i += kBatch) {
+        float lw[kBatch], x[kBatch][C];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            lw[u] = -INFINITY;
+            if (i + u < parts && row < open.z) {
+                const size_t slot = i + u == 0 ? 2 * (size_t)me + 1 : 2 * (size_t)(me + i + u);
+                lw[u] = p.lse[slot * p.slot_rows + row];
+#pragma unroll
+                for (int c = 0; c < C; ++c) x[u][c] = p.part[(slot * D + d0 + c) * p.slot_rows + row];
+            }
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u]);
+        if (top > M) {
+            const float f = ex2((M - top) * kLog2e);        // 0 the first time
+            den *= f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c] *= f;
+            M = top;
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            // -inf: no part, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
+            const bool holds = lw[u] != -INFINITY;
+            const float w = holds ? ex2((lw[u] - M) * kLog2e) : 0.f;
+            den += w;
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? x[u][c] : 0.f, num[c]);
+        }
+    }
+    const int t = open.y + row / G;
+    if (row >= open.z || pos0 + row / G < 0 || (unsigned)t >= (unsigned)p.total_q) return;
+    const float inv = 1.f / den;
+    __nv_bfloat16* o = p.out + ((size_t)t * p.Hq + open.w * G + row % G) * D + d0;
+#pragma unroll
+    for (int c = 0; c < C; c += 4)
+        *reinterpret_cast<uint2*>(o + c) = make_uint2(pack2(num[c] * inv, num[c + 1] * inv), pack2(num[c + 2] * inv, num[c + 3] * inv));
+}
+
+// ----------------------------------------------------------------------------- host
+// q [tokens, Hq, D] as a 3-D tensor; a box is 64 dims x the G heads of a group x `box` tokens.
+bool make_q_map(CUtensorMap* map, const void* q, int64_t stride, int tokens, int Hq, int G, int D, int box_tokens) {
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)box_tokens};
+    return make_bf16_map(map, q, 3, dims, strides, box);
+}
+
+struct Maps {
+    CUtensorMap q32, q16, k, v;
+};
+
+template <int D, int G>
+int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, cudaStream_t stream) {
+    static std::atomic<bool> configured[kMaxDevices];
+    if (!ensure_smem_limit(chunk_kernel<D, G>, ChLayout<D>::kSmemBytes, configured)) return OPT_GQA_ERR_CUDA;
+    const int rc = launch_dependent(chunk_kernel<D, G>, dim3((unsigned)m.W), dim3(kThreads), ChLayout<D>::kSmemBytes, stream,
+                                    maps.q32, maps.q16, maps.k, maps.v, p);
+    if (rc != OPT_GQA_OK || m.W == 1) return rc;            // (one worker has nothing to merge)
+    const unsigned slabs = (unsigned)((m.slot_rows + 31) / 32);
+    return launch_dependent(chunk_merge_kernel<D, G, 4>, dim3((unsigned)m.W - 1, slabs, D / 32), dim3(kMergeWarps * 32), 0, stream, m);
+}
+
+template <int D>
+int launch_g(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, int G, cudaStream_t stream) {
+    switch (G) {
+        case 1: return launch_both<D, 1>(maps, p, m, stream);
+        case 2: return launch_both<D, 2>(maps, p, m, stream);
+        case 4: return launch_both<D, 4>(maps, p, m, stream);
+        case 8: return launch_both<D, 8>(maps, p, m, stream);
+    }
+    return OPT_GQA_ERR_SHAPE;
+}
+
+}  // namespace
+
+int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_start_loc, int total_q_tokens, int max_q_len,
+                 const void* k_cache, const void* v_cache, const int32_t* block_tables, int max_blocks_per_seq,
+                 const int32_t* context_lens, const float* alibi_slopes, float scale, int B, int Hq, int Hkv, int D, int bs,
+                 int64_t num_blocks, int window, void* workspace, int* device_status, cudaStream_t stream) {
+    const uint64_t rows = (uint64_t)num_blocks * (uint64_t)Hkv * (uint64_t)bs;
+    if (rows == 0 || rows > 0x7fffffffull) return OPT_GQA_ERR_SHAPE;
+    const int G = Hq / Hkv, sms = sm_count();
+    if (sms <= 0) return OPT_GQA_ERR_CUDA;
+    Maps maps;
+    if (!make_q_map(&maps.q32, q, q_stride, total_q_tokens, Hq, G, D, 32 / G) ||
+        !make_q_map(&maps.q16, q, q_stride, total_q_tokens, Hq, G, D, kNarrowRows / G) || !make_cache_map(&maps.k, k_cache, rows, D, bs) ||
+        !make_slice_map(&maps.v, v_cache, rows, D, bs))
+        return OPT_GQA_ERR_CUDA;
+    const ChunkLayout L = chunk_layout(Hq, Hkv, D, max_q_len);
+    char* ws = static_cast<char*>(workspace);
+    ChunkParams p;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.q_start_loc = q_start_loc;
+    p.block_tables = block_tables;
+    p.context_lens = context_lens;
+    p.slopes = alibi_slopes;
+    p.info = reinterpret_cast<int32_t*>(ws + L.info);
+    p.lse = reinterpret_cast<float*>(ws + L.lse);
+    p.part = reinterpret_cast<float*>(ws + L.part);
+    p.status = device_status;
+    p.scale = scale;
+    p.B = B;
+    p.total_q = total_q_tokens;
+    p.max_q = max_q_len;
+    p.max_blocks = max_blocks_per_seq;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.bs = bs;
+    p.bs_log2 = bs == 32 ? 5 : 4;
+    p.window = window;
+    p.slot_rows = L.slot_rows;
+    ChunkMergeParams m;
+    m.out = p.out;
+    m.info = p.info;
+    m.lse = p.lse;
+    m.part = p.part;
+    m.Hq = Hq;
+    m.total_q = total_q_tokens;
+    m.slot_rows = L.slot_rows;
+    // one resident wave, and no more workers than there can be tiles
+    const long long blocks = (long long)Hkv * ((long long)total_q_tokens * G / kRows + B);
+    const long long most = blocks * ((long long)max_blocks_per_seq * bs / kTN + 1);
+    long long ctas = (long long)sms * kCtasPerSm;
+    if (ctas > kChunkMaxWorkers) ctas = kChunkMaxWorkers;
+    if (ctas > most) ctas = most;
+    m.W = (int)ctas;
+    return D == 128 ? launch_g<128>(maps, p, m, G, stream) : launch_g<64>(maps, p, m, G, stream);
+}
+
+}  // namespace optgqa

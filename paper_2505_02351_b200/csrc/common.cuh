@@ -340,6 +340,34 @@ int launch_prompt_umma(void* out, const void* q, const void* k, const void* v, c
                        int total_q_tokens, int max_q_len, const float* alibi_slopes, float scale, int B, int Hq,
                        int Hkv, int D, int* device_status, cudaStream_t stream);
 
+// Workspace of the chunk attention.  Per worker: what the merge needs to know {1 where its last piece is one that others continue,
+// that item's first row of q, rows, KV head; 1 / 2 where its first piece continues / closes an item that others began, position of
+// the last piece's first token}, and two places for parts of items -- its first piece and its last -- of slot_rows rows: log-sum-exps
+// lse[2 w + i][rows], normalised partial results part[2 w + i][D][rows].
+constexpr int kChunkRows = 128;
+constexpr int kChunkMaxWorkers = 296;
+constexpr int kChunkInfoWords = 8;
+struct ChunkLayout {
+    size_t info, lse, part, total;
+    int slot_rows;
+};
+inline ChunkLayout chunk_layout(int Hq, int Hkv, int D, int max_q_len) {
+    ChunkLayout L;
+    const long long rows = (long long)max_q_len * (Hq / Hkv);
+    L.slot_rows = rows >= kChunkRows ? kChunkRows : (int)(rows + 31) / 32 * 32;
+    L.info = 0;
+    L.lse = round_up_256((size_t)kChunkMaxWorkers * kChunkInfoWords * 4);
+    L.part = L.lse + round_up_256((size_t)kChunkMaxWorkers * 2 * L.slot_rows * 4);
+    L.total = L.part + (size_t)kChunkMaxWorkers * 2 * L.slot_rows * D * 4;
+    return L;
+}
+
+// bf16: chunk.cu.  window > 0 adds the local mask.
+int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_start_loc, int total_q_tokens, int max_q_len,
+                 const void* k_cache, const void* v_cache, const int32_t* block_tables, int max_blocks_per_seq,
+                 const int32_t* context_lens, const float* alibi_slopes, float scale, int B, int Hq, int Hkv, int D, int bs,
+                 int64_t num_blocks, int window, void* workspace, int* device_status, cudaStream_t stream);
+
 // The pools of a cache whose pages are numbered alike (K and V of every layer), by value in a kernel's arguments.
 struct PoolSet {
     char* p[OPT_GQA_MAX_POOLS];

@@ -113,18 +113,6 @@ struct SharedParams {
     int num_groups, B, max_blocks, Hkv, bs, bs_log2, lanes_log2;
 };
 
-// mbar_wait with its waiting loop in one place: this kernel waits at some twenty, its warps run all over it, and its time
-// goes with the instruction cache's misses (as inlined: 86 KB, the caches' shared port busy 74 % of the time).
-__noinline__ __device__ bool wait_long(uint64_t* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* status) {
-    return mbar_try_wait(bar, parity) || wait_long(bar, parity, status);
-}
-
-// Where the share of worker i of W begins in a list of `total`: rounded down, so that the shares follow one another.
-__device__ __forceinline__ long long share_at(long long total, int i, int W) {
-    return total < (1 << 22) ? (long long)((unsigned)total * (unsigned)i / (unsigned)W) : total * i / W;      // (W < 512)
-}
-
 // What the other warps need to know of a piece.
 struct Piece {
     int s0, rows, kvh, table;       // first sequence, live rows, KV head, sequence whose page table is walked
@@ -1025,14 +1013,6 @@ bool make_q_map(CUtensorMap* map, const void* q, int B, int Hq, int G, int D, in
     const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)Hq * D * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)seqs};
     return make_bf16_map(map, q, 3, dims, strides, box);
-}
-
-// The cache as a 3-D tensor [64-dim halves, rows, 64]; a box is the bs token rows of a page, half after half.
-bool make_slice_map(CUtensorMap* map, const void* cache, uint64_t rows, int D, int bs) {
-    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(D / 64)};
-    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, 128};
-    const cuuint32_t box[3] = {64, (cuuint32_t)bs, (cuuint32_t)(D / 64)};
-    return make_bf16_map(map, cache, 3, dims, strides, box);
 }
 
 struct Maps {

@@ -128,4 +128,12 @@ inline bool make_cache_map(CUtensorMap* map, const void* cache, uint64_t rows, i
     return make_bf16_map(map, cache, 2, dims, strides, box);
 }
 
+// The cache as a 3-D tensor [64-dim halves, rows, 64]; a box is the bs token rows of a page, half after half.
+inline bool make_slice_map(CUtensorMap* map, const void* cache, uint64_t rows, int D, int bs) {
+    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(D / 64)};
+    const cuuint64_t strides[2] = {(cuuint64_t)D * 2, 128};
+    const cuuint32_t box[3] = {64, (cuuint32_t)bs, (cuuint32_t)(D / 64)};
+    return make_bf16_map(map, cache, 3, dims, strides, box);
+}
+
 }  // namespace optgqa

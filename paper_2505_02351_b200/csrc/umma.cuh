@@ -1,4 +1,4 @@
-// Shared by the kernels on tcgen05 (prefill_umma.cu, decode_shared.cu): instruction wrappers, descriptors, and the two
+// Shared by the kernels on tcgen05 (prefill_umma.cu, decode_shared.cu, chunk.cu): instruction wrappers, descriptors, and the two
 // passes of a row thread over a chunk of its scores.
 #pragma once
 
@@ -157,6 +157,19 @@ __device__ __forceinline__ void chunk_max(const float (&v)[32], int key0, int po
         }
         mx[(e >> 1) & 3] = kNan ? max3_nan(mx[(e >> 1) & 3], s0, s1) : max3(mx[(e >> 1) & 3], s0, s1);
     }
+}
+
+// mbar_wait with its waiting loop in one place: the kernels that work through a list of items wait at some twenty, their
+// warps run all over them, and their time goes with the instruction cache's misses (the shared-prefix decode as inlined:
+// 86 KB, the caches' shared port busy 74 % of the time).
+inline __noinline__ __device__ bool wait_long(uint64_t* bar, uint32_t parity, int* status) { return mbar_wait(bar, parity, status); }
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* status) {
+    return mbar_try_wait(bar, parity) || wait_long(bar, parity, status);
+}
+
+// Where the share of worker i of W begins in a list of `total`: rounded down, so that the shares follow one another.
+__device__ __forceinline__ long long share_at(long long total, int i, int W) {
+    return total < (1 << 22) ? (long long)((unsigned)total * (unsigned)i / (unsigned)W) : total * i / W;      // (W < 512)
 }
 
 // Two fp32 values in one 64-bit register, for the packed fp32 instructions of sm_100 (one issue slot for two lanes).
