@@ -239,6 +239,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         const int me = blockIdx.x, W = (int)max(min((long long)gridDim.x, total / kMinShare), 1ll);
         // this worker's share of the list
         const long long begin = share_at(total, min(me, W), W), end = share_at(total, min(me + 1, W), W);
+        // (sequence, block, KV head), KV head fastest: with ALiBi the heads' tiles cost differently (weights that are all zero
+        // need no exponentials), and workers side by side walk the same keys
         Seq x = {};
         int s = 0, kvh = 0, mt = 0, jt = 0, t0 = 0, t1 = 0;        // the item's tiles t0 .. t1 - 1, jt of them done
         long long pos = end;                                        // in the list: the next tile's place
@@ -257,14 +259,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 before += units * (long long)p.Hkv;
             }
             if (s < p.B) {                                          // (always so: the shares end where the items do)
-                const long long r = begin - before;
-                kvh = r < 0x7fffffff ? (int)r / units : (int)(r / units);
-                int in_item = (int)(r - (long long)kvh * units) - item_cost(x);
-                for (mt = x.first;; ++mt) {                         // an item's tile j lies its cost + j behind its begin
+                long long r = begin - before;
+                for (mt = x.first;; ++mt) {
                     block_tiles<TQ>(x, mt, p.window, t0, t1);
-                    if (in_item < t1 - t0 || mt == x.blocks - 1) break;
-                    in_item -= t1 - t0 + item_cost(x);
+                    units = t1 - t0 + item_cost(x);
+                    if (r < units * (long long)p.Hkv || mt == x.blocks - 1) break;
+                    r -= units * (long long)p.Hkv;
                 }
+                kvh = r < 0x7fffffff ? (int)r / units : (int)(r / units);
+                const int in_item = (int)(r - (long long)kvh * units) - item_cost(x);      // an item's tile j lies its cost + j behind its begin
                 jt = max(in_item, 0);
                 pos = begin + jt - in_item;
             }
@@ -359,18 +362,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             pos += len;
             jt = 0;
             if (pos < end) {
-                if (++mt == x.blocks) {
-                    if (++kvh == p.Hkv) {
-                        kvh = 0;
+                if (++kvh == p.Hkv) {
+                    kvh = 0;
+                    if (++mt == x.blocks) {
                         for (++s; s < p.B; ++s) {
                             x = sequence<TQ>(p, s);
                             if (x.first < x.blocks) break;
                         }
                         if (s == p.B) pos = end;        // cannot happen: the shares end where the items do
+                        mt = x.first;
                     }
-                    mt = x.first;
+                    block_tiles<TQ>(x, mt, p.window, t0, t1);
                 }
-                block_tiles<TQ>(x, mt, p.window, t0, t1);
                 pos += item_cost(x);
             }
         }
@@ -628,8 +631,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                             for (int e = 0; e < 32; ++e) v[c][e] = __uint_as_float(raw[c][e]);
                         }
                     }
-                    if (__any_sync(kFull, j0 + kTN - 1 > pos || j0 <= lo)) {
-                        // -inf in the place of what the row does not see: both passes then run as they are
+                    if (__any_sync(kFull, (sees || begun) && (j0 + kTN - 1 > pos || j0 <= lo))) {
+                        // -inf in the place of what the row does not see: both passes then run as they are.  (Rows that have not
+                        // begun, or are not there, may weigh what they like: see above.  Without the first condition every tile of a
+                        // block whose last warp is part full came here.)
                         const int top = pos - j0, bottom = lo - j0;
 #pragma unroll
                         for (int e = 0; e < kTN; ++e)
