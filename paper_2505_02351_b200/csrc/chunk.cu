@@ -30,13 +30,25 @@ constexpr int kTN = 64;                    // keys per tile
 constexpr int kStages = 2;                 // of the K ring and of the V ring
 constexpr int kCtasPerSm = 2;
 constexpr int kThreads = 256;
-// The cut counts tiles, and for an item besides (the next one's Q, the wait for its last P V, storing the rows) about as many of
-// them as it costs time: a block of more than 32 rows occupies the row warps all together.
-constexpr int kFullItem = 3, kSmallItem = 1;
-constexpr int kMinShare = 2;               // a worker's share at least
+// The cut counts in quarters of a tile's time, tiles at kTileCost and an item at what it costs besides (the next one's Q, the wait for
+// its last P V, storing the rows): fitted to the times of 296 workers with different numbers of tiles and pieces, a tile 1.0 to 1.1
+// us of any kind (two CTAs per SM), an item 1.2 to 1.6, one of more than 64 rows, which takes the row warps all together, 3.4.
+constexpr int kTileCost = 4, kSmallItem = 5, kFullItem = 13;
+constexpr int kMinShare = 8;               // a worker's share at least, in the same
 constexpr int kNarrowRows = 16;            // up to which the products take 64 rows: row 16 w + i lies in lane 32 w + i
+// The second half of the workers begins later, 1 us where the GPU is idle and 4 to 6 where a call follows another (an SM's second
+// CTA finds its registers when the merge before is done): what a worker of it has less, and one of the first half more.
+#ifndef KLATE
+#define KLATE 5
+#endif
+constexpr int kLateCost = KLATE;
+#ifndef KDIRECT
+#define KDIRECT 11
+#endif
+constexpr int kDirectTiles = KDIRECT;
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr int kDescBytes = 64;
+constexpr int kOpens = 1, kContinues = 2, kCloses = 4;      // a worker's flags: see ChunkLayout
 constexpr unsigned kFull = 0xffffffffu;
 constexpr float kRescaleThreshold = 8.f;   // log2 units: O is rescaled only when a row's maximum grew by more
 
@@ -78,12 +90,13 @@ struct ChunkParams {
     const int32_t* block_tables;
     const int32_t* context_lens;
     const float* slopes;
-    int32_t* info;              // see ChunkLayout, as the pieces below
+    int32_t* flags;             // see ChunkLayout, as the parts below
+    int4* items;
     float* lse;
     float* part;
     int* status;
     float scale;
-    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows;
+    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows, direct;
 };
 
 // A sequence of the batch: its rows of q, context, position of its first new token, and its blocks first .. blocks - 1 that see a key.
@@ -154,7 +167,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
-    auto item_cost = [&](const Seq& x) { return x.q * G > 32 ? kFullItem : kSmallItem; };
+    auto item_cost = [&](const Seq& x) { return x.q * G > 64 ? kFullItem : kSmallItem; };
     auto seq_units = [&](const Seq& x) {
         int sum = 0;
         for (int mt = x.first; mt < x.blocks; ++mt) {
@@ -162,13 +175,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             block_tiles<TQ>(x, mt, p.window, lo, hi);
             sum += hi - lo;
         }
-        return sum + (x.blocks - x.first) * item_cost(x);
+        return sum * kTileCost + (x.blocks - x.first) * item_cost(x);
     };
 
     // ------------------------------------------------------------------ the items (the index arrays are read before the
     // wait for the preceding kernel: see the ordering contract in the header)
     const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
-    {
+    if (!p.direct) {
         long long sum = 0;
         for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) sum += seq_units(sequence<TQ>(p, s));
         long long incl = sum;
@@ -233,44 +246,92 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
 
     if (warp == 4) {
         // ------------------------------------------------------------------ the list of pieces, Q and K
-        long long total = 0;
-        for (int w = 0; w < kThreads / 32; ++w) total += w_units[w];
-        total *= p.Hkv;
-        const int me = blockIdx.x, W = (int)max(min((long long)gridDim.x, total / kMinShare), 1ll);
-        // this worker's share of the list
-        const long long begin = share_at(total, min(me, W), W), end = share_at(total, min(me + 1, W), W);
         // (sequence, block, KV head), KV head fastest: with ALiBi the heads' tiles cost differently (weights that are all zero
         // need no exponentials), and workers side by side walk the same keys
         Seq x = {};
         int s = 0, kvh = 0, mt = 0, jt = 0, t0 = 0, t1 = 0;        // the item's tiles t0 .. t1 - 1, jt of them done
-        long long pos = end;                                        // in the list: the next tile's place
-        if (begin < end) {
+        long long pos = 0, end = 0;                                 // in the list: the next tile's place, and the share's end
+        const int me = blockIdx.x;
+        // Where the share begins in the list.  (In 32 bits where they do: N is int or long long.)
+        auto locate = [&](auto total_units) {
+            using N = decltype(total_units);
+            const N total = total_units;
+            const int W = (int)max(min((N)gridDim.x, total / kMinShare), (N)1);
+            const int skew = total / W >= 4 * kLateCost ? kLateCost : 0;
+            auto share = [&](int i) { return (N)share_at(total, i, W) + skew * min(i, W - i); };
+            const N begin = share(min(me, W));
+            end = share(min(me + 1, W));
+            pos = end;
+            if (begin >= end) return;
             // the last thread's chunk that begins at or before the share, and its begin
-            int at = 0;
-            long long before = 0;
-            while (at < kThreads / 32 - 1 && before + w_units[at] * p.Hkv <= begin) before += w_units[at++] * p.Hkv;
-            at = at * 32 + __popc(__ballot_sync(kFull, before + c_units[at * 32 + lane] * p.Hkv <= begin)) - 1;
-            before += c_units[at] * p.Hkv;
+            const N sum = (N)w_units[lane & 7] * p.Hkv;
+            N upto = sum;
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) {
+                const N v = __shfl_up_sync(kFull, upto, o, 8);
+                if ((lane & 7) >= o) upto += v;
+            }
+            int at = __popc(__ballot_sync(kFull, upto - sum <= begin) & 0xff) - 1;
+            N before = __shfl_sync(kFull, upto - sum, at);
+            const N mine = before + (N)c_units[at * 32 + lane] * p.Hkv;
+            const int in_warp = __popc(__ballot_sync(kFull, mine <= begin)) - 1;
+            before = __shfl_sync(kFull, mine, in_warp);
+            at = at * 32 + in_warp;
             int units = 0;
             for (s = at * chunk; s < p.B; ++s) {
                 x = sequence<TQ>(p, s);
                 units = seq_units(x);
-                if (before + units * (long long)p.Hkv > begin) break;
-                before += units * (long long)p.Hkv;
+                if (before + units * (N)p.Hkv > begin) break;
+                before += units * (N)p.Hkv;
             }
-            if (s < p.B) {                                          // (always so: the shares end where the items do)
-                long long r = begin - before;
-                for (mt = x.first;; ++mt) {
-                    block_tiles<TQ>(x, mt, p.window, t0, t1);
-                    units = t1 - t0 + item_cost(x);
-                    if (r < units * (long long)p.Hkv || mt == x.blocks - 1) break;
-                    r -= units * (long long)p.Hkv;
+            if (s >= p.B) return;                                   // (cannot happen: the shares end where the items do)
+            N r = begin - before;
+            for (mt = x.first;; ++mt) {
+                block_tiles<TQ>(x, mt, p.window, t0, t1);
+                units = (t1 - t0) * kTileCost + item_cost(x);
+                if (r < units * (N)p.Hkv || mt == x.blocks - 1) break;
+                r -= units * (N)p.Hkv;
+            }
+            kvh = (int)(r / units);
+            // an item's tile j lies its cost + j tiles behind its begin; a share has those whose place lies in it
+            const int in_item = (int)(r - (N)kvh * units) - item_cost(x);
+            jt = max((in_item + kTileCost - 1) / kTileCost, 0);
+            pos = begin + jt * kTileCost - in_item;
+        };
+        // on to the next item, where there is one
+        auto next_item = [&]() {
+            jt = 0;
+            if (pos >= end) return;
+            if (++kvh == p.Hkv) {
+                kvh = 0;
+                if (++mt == x.blocks) {
+                    for (++s; s < p.B; ++s) {
+                        x = sequence<TQ>(p, s);
+                        if (x.first < x.blocks) break;
+                    }
+                    if (s == p.B) pos = end;            // cannot happen: the shares end where the items do
+                    mt = x.first;
                 }
-                kvh = r < 0x7fffffff ? (int)r / units : (int)(r / units);
-                const int in_item = (int)(r - (long long)kvh * units) - item_cost(x);      // an item's tile j lies its cost + j behind its begin
-                jt = max(in_item, 0);
-                pos = begin + jt - in_item;
+                block_tiles<TQ>(x, mt, p.window, t0, t1);
             }
+            pos += item_cost(x);
+        };
+        if (p.direct) {
+            s = blockIdx.z;
+            kvh = blockIdx.y;
+            x = sequence<TQ>(p, s);
+            mt = blockIdx.x;
+            if (mt >= x.first && mt < x.blocks) {
+                block_tiles<TQ>(x, mt, p.window, t0, t1);
+                end = (t1 - t0) * kTileCost;
+            }
+        } else {
+            long long total = 0;
+            for (int w = 0; w < kThreads / 32; ++w) total += w_units[w];
+            total *= p.Hkv;
+            if (total < 0x40000000) locate((int)total);
+            else locate(total);
+            if (jt > 0 && jt == t1 - t0) next_item();                  // the share begins inside an item's last tile
         }
         fence_proxy_async();
         __syncwarp();
@@ -283,11 +344,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         uint32_t owner = 0xffff, q_ph = 0;  // per quarter of Q (4 bits) whose block it holds (by its first row warp; f: none that
                                             // has not been seen done), and the parity of that barrier's next release
         int next_warp = 0;
-        // what the merge needs to know: the part of an item at the share's end that others continue, and at its begin
-        int4 open_a = make_int4(0, 0, 0, 0), open_b = make_int4(0, 0, 0, 0);
+        // what the merge needs to know: the parts of items at the share's begin and end
+        int4 first_item = make_int4(0, 0, 0, 0), last_item = first_item;
+        int flags = 0;
         bool waited = false;
         for (int pc = 0;; ++pc) {
-            const unsigned room = (unsigned)max(min(end - pos, (long long)0x3fffffff), 0ll);
+            const unsigned room = (unsigned)max(min((end - pos + kTileCost - 1) / kTileCost, (long long)0x3fffffff), 0ll);
             const int len = (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
             const int rows = min(TQ, x.q - mt * TQ) * G, wide = rows > 64 ? 4 : rows > 32 ? 2 : 1;
             const bool opens = jt == 0, closes = jt + len == t1 - t0, once = x.blocks - x.first <= 1;
@@ -306,8 +368,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 mbar_arrive(&desc_full[pc % kDescs]);
             }
             if (len == 0) break;
-            if (!opens) open_b.x = closes ? 2 : 1;
-            else if (!closes) open_a = make_int4(1, q0, rows, kvh), open_b.y = pos0;
+            if (!opens) flags = closes ? kCloses : kContinues, first_item = make_int4(q0, rows, kvh, pos0);
+            else if (!closes) flags |= kOpens, last_item = make_int4(q0, rows, kvh, pos0);
             const int32_t* table = p.block_tables + (size_t)s * p.max_blocks;
             const int pages = min((x.n + p.bs - 1) >> p.bs_log2, p.max_blocks);       // the table is not read past them
             auto page_of = [&](int j) {
@@ -358,30 +420,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 }
             }
             if (!ok) break;
-            // on to the next item, where there is one
-            pos += len;
-            jt = 0;
-            if (pos < end) {
-                if (++kvh == p.Hkv) {
-                    kvh = 0;
-                    if (++mt == x.blocks) {
-                        for (++s; s < p.B; ++s) {
-                            x = sequence<TQ>(p, s);
-                            if (x.first < x.blocks) break;
-                        }
-                        if (s == p.B) pos = end;        // cannot happen: the shares end where the items do
-                        mt = x.first;
-                    }
-                    block_tiles<TQ>(x, mt, p.window, t0, t1);
-                }
-                pos += item_cost(x);
-            }
+            pos += len * kTileCost;
+            next_item();
         }
         if (!waited) grid_dependency_wait();
-        if (lane == 0) {
-            int4* info = reinterpret_cast<int4*>(p.info + kChunkInfoWords * me);
-            info[0] = open_a;
-            info[1] = open_b;
+        if (lane == 0 && !p.direct) {
+            p.flags[me] = flags;
+            p.items[2 * me] = first_item;
+            p.items[2 * me + 1] = last_item;
         }
     } else {
         // before any wait with a limit: what the producers wait for may take as long as it likes
@@ -571,7 +617,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
             const int r = threadIdx.x, hg = r % G;       // (32 is a multiple of G)
             // rows before position 0 (more new tokens than context: padding) see nothing and are zero
-            for (int s = blockIdx.x * 4 + warp; s < p.B; s += gridDim.x * 4) {
+            const int cta = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), ctas = gridDim.x * gridDim.y * gridDim.z;
+            for (int s = cta * 4 + warp; s < p.B; s += ctas * 4) {
                 const Seq x = sequence<TQ>(p, s);
                 const int none = min(x.q, -x.pos0);
                 uint4* o = reinterpret_cast<uint4*>(p.out + (size_t)x.q0 * p.Hq * D);
@@ -705,6 +752,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                     tc_fence_after();
                     const float inv = 1.f / l;
                     __nv_bfloat16* orow = p.out + ((size_t)(d.q0 + rr / G) * p.Hq + d.kvh * G + hg) * D;
+                    const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;
                     // a part is [D][rows], so that 32 neighbouring rows are one line
                     float* part = p.part + (size_t)d.slot * D * p.slot_rows + rr;
 #pragma unroll 1
@@ -716,11 +764,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                             mbar_arrive(&o_empty[warp]);
                         }
                         if (begun && d.slot < 0) {
-                            uint4* po = reinterpret_cast<uint4*>(orow + c * 32);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                po[e] = make_uint4(pack2(o[8 * e] * inv, o[8 * e + 1] * inv), pack2(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                                   pack2(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack2(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                            for (int e = 0; e < 2; ++e) {
+                                uint32_t w[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) w[i] = pack2(o[16 * e + 2 * i] * inv, o[16 * e + 2 * i + 1] * inv);
+                                st_global_32(orow + c * 32 + e * 16, w, wide);
+                            }
                         } else if (begun) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) part[(size_t)(c * 32 + e) * p.slot_rows] = o[e] * inv;
@@ -749,83 +799,113 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
 }
 
 // ----------------------------------------------------------------------------- merge
-// blockIdx.x: a worker whose last piece others continue; its parts are that one and the first ones of the workers behind it up
-// to the one that closes the item.  A CTA merges 32 rows of it, a lane per row, its eight warps C columns each.
-constexpr int kMergeWarps = 8;
+// An item in parts is the last piece of one worker, the leader, and the first ones of the workers behind it up to the one that
+// closes it.  A CTA stands in the place of each worker (so that the grid is one wave, and the next kernel's CTAs may begin beside
+// it), half its warps for the item of the worker's first piece, half for that of its last; an item is merged by the warps of all its
+// parts together, in units of 32 rows times 4 C columns.  A thread has four rows and C columns; kBatch parts are requested together.
+constexpr int kMergeWarps = 16;
 
 struct ChunkMergeParams {
     __nv_bfloat16* out;
-    const int32_t* info;
+    const int32_t* flags;
+    const int4* items;
     const float* lse;
     const float* part;
     int W, Hq, total_q, slot_rows;
 };
 
-template <int D, int G, int C>
-__global__ void __launch_bounds__(kMergeWarps * 32)
+template <int D, int G, int C, int kBatch>
+__device__ __forceinline__ void merge_units(const ChunkMergeParams& p, int leader, int parts, int first_unit, int step, const int4& item) {
+    const int lane = threadIdx.x & 31, slabs = (item.y + 31) / 32;
+    for (int unit = first_unit; unit < slabs * (D / (4 * C)); unit += step) {
+        const int row = unit % slabs * 32 + (lane & 7) * 4, d0 = unit / slabs * (4 * C) + (lane >> 3) * C;
+        float M[4], den[4], num[C][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            M[i] = -INFINITY;
+            den[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) num[c][i] = 0.f;
+        }
+        for (int first = 0; first < parts; first += kBatch) {
+            __align__(16) float lw[kBatch][4], x[kBatch][C][4];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                // (the workspace has less than 2^32 numbers)
+                const unsigned slot = first + u == 0 ? 2 * leader + 1 : 2 * (leader + min(first + u, parts - 1));
+                *reinterpret_cast<float4*>(lw[u]) = *reinterpret_cast<const float4*>(p.lse + slot * p.slot_rows + row);
+                const unsigned at = (slot * D + d0) * p.slot_rows + row;
+#pragma unroll
+                for (int c = 0; c < C; ++c) *reinterpret_cast<float4*>(x[u][c]) = *reinterpret_cast<const float4*>(p.part + at + c * p.slot_rows);
+                if (kBatch > 1 && first + u >= parts) lw[u][0] = lw[u][1] = lw[u][2] = lw[u][3] = -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float top = M[i];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u][i]);
+                const float f = top > M[i] ? ex2((M[i] - top) * kLog2e) : 1.f;       // 0 the first time
+                M[i] = top;
+                den[i] *= f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) num[c][i] *= f;
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    // -inf: no part, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
+                    const bool holds = lw[u][i] != -INFINITY;
+                    const float w = holds ? ex2((lw[u][i] - top) * kLog2e) : 0.f;
+                    den[i] += w;
+#pragma unroll
+                    for (int c = 0; c < C; ++c) num[c][i] = fmaf(w, holds ? x[u][c][i] : 0.f, num[c][i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = row + i, t = item.x + r / G;
+            if (r >= item.y || item.w + r / G < 0 || (unsigned)t >= (unsigned)p.total_q) continue;
+            const float inv = 1.f / den[i];
+            __nv_bfloat16* o = p.out + ((size_t)t * p.Hq + item.z * G + r % G) * D + d0;
+            if constexpr (C == 4) *reinterpret_cast<uint2*>(o) = make_uint2(pack2(num[0][i] * inv, num[1][i] * inv), pack2(num[2][i] * inv, num[3][i] * inv));
+            else *reinterpret_cast<uint32_t*>(o) = pack2(num[0][i] * inv, num[1][i] * inv);
+        }
+    }
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(kMergeWarps * 32, 2)
 chunk_merge_kernel(const ChunkMergeParams p) {
-    constexpr int kBatch = 32 / C;
+    __shared__ int flags[kChunkMaxWorkers];
     grid_dependency_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, me = blockIdx.x;
+    const int last = warp / (kMergeWarps / 2);                  // in the place of the worker's first piece, or of its last
     grid_dependency_wait();
-    const int4 open = *reinterpret_cast<const int4*>(p.info + kChunkInfoWords * me);
-    const int row = blockIdx.y * 32 + lane;
-    if (open.x != 1 || (int)blockIdx.y * 32 >= open.z) return;
-    const int pos0 = p.info[kChunkInfoWords * me + 5];
-    int parts = 1;                                          // workers behind this one that go on with its item
-    for (int at = me + 1;; at += 32) {
-        const bool more = at + lane < p.W && p.info[kChunkInfoWords * (at + lane) + 4] == 1;
-        const unsigned run = __ballot_sync(kFull, more);
+    for (int i = threadIdx.x; i < p.W; i += kMergeWarps * 32) flags[i] = p.flags[i];
+    const int4 item = p.items[2 * me + last];
+    __syncthreads();
+    if (!(flags[me] & (last ? kOpens : kContinues | kCloses))) return;
+    int leader = me;
+    if (!last) {                                                // the last one before this that opens
+        for (int hi = me - 1;; hi -= 32) {
+            const unsigned found = __ballot_sync(kFull, hi - lane >= 0 && (flags[max(hi - lane, 0)] & kOpens));
+            leader = hi - (__ffs(found) - 1);
+            if (found || hi < 32) break;
+        }
+        leader = min(max(leader, 0), me - 1);
+    }
+    int parts = 1;
+    for (int at = leader + 1;; at += 32) {
+        const unsigned run = __ballot_sync(kFull, at + lane < p.W && (flags[min(at + lane, p.W - 1)] & kContinues));
         if (run != kFull) {
-            parts += __ffs(~run);                           // and the one that closes it
+            parts += __ffs(~run);                               // and the one that closes it
             break;
         }
         parts += 32;
     }
-    parts = min(parts, p.W - me);
-    const int d0 = (blockIdx.z * kMergeWarps + warp) * C;
-    float M = -INFINITY, den = 0.f, num[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) num[c] = 0.f;
-    for (int i = 0; i < parts; i += kBatch) {
-        float lw[kBatch], x[kBatch][C];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            lw[u] = -INFINITY;
-            if (i + u < parts && row < open.z) {
-                const size_t slot = i + u == 0 ? 2 * (size_t)me + 1 : 2 * (size_t)(me + i + u);
-                lw[u] = p.lse[slot * p.slot_rows + row];
-#pragma unroll
-                for (int c = 0; c < C; ++c) x[u][c] = p.part[(slot * D + d0 + c) * p.slot_rows + row];
-            }
-        }
-        float top = M;
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) top = fmaxf(top, lw[u]);
-        if (top > M) {
-            const float f = ex2((M - top) * kLog2e);        // 0 the first time
-            den *= f;
-#pragma unroll
-            for (int c = 0; c < C; ++c) num[c] *= f;
-            M = top;
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            // -inf: no part, or one the row saw nothing of and whose values mean nothing (a NaN is carried on)
-            const bool holds = lw[u] != -INFINITY;
-            const float w = holds ? ex2((lw[u] - M) * kLog2e) : 0.f;
-            den += w;
-#pragma unroll
-            for (int c = 0; c < C; ++c) num[c] = fmaf(w, holds ? x[u][c] : 0.f, num[c]);
-        }
-    }
-    const int t = open.y + row / G;
-    if (row >= open.z || pos0 + row / G < 0 || (unsigned)t >= (unsigned)p.total_q) return;
-    const float inv = 1.f / den;
-    __nv_bfloat16* o = p.out + ((size_t)t * p.Hq + open.w * G + row % G) * D + d0;
-#pragma unroll
-    for (int c = 0; c < C; c += 4)
-        *reinterpret_cast<uint2*>(o + c) = make_uint2(pack2(num[c] * inv, num[c + 1] * inv), pack2(num[c + 2] * inv, num[c + 3] * inv));
+    parts = min(parts, p.W - leader);
+    const int mine = (me - leader) * (kMergeWarps / 2) + warp % (kMergeWarps / 2), all = parts * (kMergeWarps / 2);
+    if (parts <= 4) merge_units<D, G, 4, 1>(p, leader, parts, mine, all, item);
+    else merge_units<D, G, 2, 2>(p, leader, parts, mine, all, item);
 }
 
 // ----------------------------------------------------------------------------- host
@@ -842,23 +922,22 @@ struct Maps {
 };
 
 template <int D, int G>
-int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, cudaStream_t stream) {
+int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, dim3 grid, cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
     if (!ensure_smem_limit(chunk_kernel<D, G>, ChLayout<D>::kSmemBytes, configured)) return OPT_GQA_ERR_CUDA;
-    const int rc = launch_dependent(chunk_kernel<D, G>, dim3((unsigned)m.W), dim3(kThreads), ChLayout<D>::kSmemBytes, stream,
-                                    maps.q32, maps.q16, maps.k, maps.v, p);
-    if (rc != OPT_GQA_OK || m.W == 1) return rc;            // (one worker has nothing to merge)
-    const unsigned slabs = (unsigned)((m.slot_rows + 31) / 32);
-    return launch_dependent(chunk_merge_kernel<D, G, 4>, dim3((unsigned)m.W - 1, slabs, D / 32), dim3(kMergeWarps * 32), 0, stream, m);
+    const int rc = launch_dependent(chunk_kernel<D, G>, grid, dim3(kThreads), ChLayout<D>::kSmemBytes, stream, maps.q32, maps.q16, maps.k,
+                                    maps.v, p);
+    if (rc != OPT_GQA_OK || m.W <= 1) return rc;            // (one worker has nothing to merge)
+    return launch_dependent(chunk_merge_kernel<D, G>, dim3((unsigned)m.W), dim3(kMergeWarps * 32), 0, stream, m);
 }
 
 template <int D>
-int launch_g(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, int G, cudaStream_t stream) {
+int launch_g(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, int G, dim3 grid, cudaStream_t stream) {
     switch (G) {
-        case 1: return launch_both<D, 1>(maps, p, m, stream);
-        case 2: return launch_both<D, 2>(maps, p, m, stream);
-        case 4: return launch_both<D, 4>(maps, p, m, stream);
-        case 8: return launch_both<D, 8>(maps, p, m, stream);
+        case 1: return launch_both<D, 1>(maps, p, m, grid, stream);
+        case 2: return launch_both<D, 2>(maps, p, m, grid, stream);
+        case 4: return launch_both<D, 4>(maps, p, m, grid, stream);
+        case 8: return launch_both<D, 8>(maps, p, m, grid, stream);
     }
     return OPT_GQA_ERR_SHAPE;
 }
@@ -886,7 +965,8 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     p.block_tables = block_tables;
     p.context_lens = context_lens;
     p.slopes = alibi_slopes;
-    p.info = reinterpret_cast<int32_t*>(ws + L.info);
+    p.flags = reinterpret_cast<int32_t*>(ws + L.flags);
+    p.items = reinterpret_cast<int4*>(ws + L.items);
     p.lse = reinterpret_cast<float*>(ws + L.lse);
     p.part = reinterpret_cast<float*>(ws + L.part);
     p.status = device_status;
@@ -903,20 +983,31 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     p.slot_rows = L.slot_rows;
     ChunkMergeParams m;
     m.out = p.out;
-    m.info = p.info;
+    m.flags = p.flags;
+    m.items = p.items;
     m.lse = p.lse;
     m.part = p.part;
     m.Hq = Hq;
     m.total_q = total_q_tokens;
     m.slot_rows = L.slot_rows;
-    // one resident wave, and no more workers than there can be tiles
-    const long long blocks = (long long)Hkv * ((long long)total_q_tokens * G / kRows + B);
-    const long long most = blocks * ((long long)max_blocks_per_seq * bs / kTN + 1);
-    long long ctas = (long long)sms * kCtasPerSm;
-    if (ctas > kChunkMaxWorkers) ctas = kChunkMaxWorkers;
-    if (ctas > most) ctas = most;
-    m.W = (int)ctas;
-    return D == 128 ? launch_g<128>(maps, p, m, G, stream) : launch_g<64>(maps, p, m, G, stream);
+    // Few items of few tiles, as far as the host can bound them: a CTA each, no list, nothing to merge.
+    const long long blocks = ((long long)max_q_len * G + kRows - 1) / kRows, items = blocks * Hkv * B;
+    long long tiles = (long long)max_blocks_per_seq * bs / kTN + 1;
+    if (window > 0) {
+        const long long seen = ((long long)window + kRows / G + kTN - 2) / kTN + 1;
+        if (seen < tiles) tiles = seen;
+    }
+    const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
+    p.direct = items <= wave && tiles <= kDirectTiles;
+    dim3 grid((unsigned)blocks, (unsigned)Hkv, (unsigned)B);
+    m.W = 1;
+    if (!p.direct) {
+        // one resident wave, and no more workers than there can be tiles
+        const long long most = Hkv * ((long long)total_q_tokens * G / kRows + B) * tiles;
+        m.W = (int)(most < wave ? most : wave);
+        grid = dim3((unsigned)m.W);
+    }
+    return D == 128 ? launch_g<128>(maps, p, m, G, grid, stream) : launch_g<64>(maps, p, m, G, grid, stream);
 }
 
 }  // namespace optgqa

@@ -340,23 +340,22 @@ int launch_prompt_umma(void* out, const void* q, const void* k, const void* v, c
                        int total_q_tokens, int max_q_len, const float* alibi_slopes, float scale, int B, int Hq,
                        int Hkv, int D, int* device_status, cudaStream_t stream);
 
-// Workspace of the chunk attention.  Per worker: what the merge needs to know {1 where its last piece is one that others continue,
-// that item's first row of q, rows, KV head; 1 / 2 where its first piece continues / closes an item that others began, position of
-// the last piece's first token}, and two places for parts of items -- its first piece and its last -- of slot_rows rows: log-sum-exps
-// lse[2 w + i][rows], normalised partial results part[2 w + i][D][rows].
+// Workspace of the chunk attention.  Per worker: flags (1: its last piece is the beginning of an item that others go on with;
+// 2 / 4: its first piece goes on with an item that others began / closes it), {first row of q, rows, KV head, position of the first
+// token} of either item, and two places for parts of items -- its first piece and its last -- of slot_rows rows: log-sum-exps lse[2 w + i][rows], normalised partial results part[2 w + i][D][rows].
 constexpr int kChunkRows = 128;
 constexpr int kChunkMaxWorkers = 296;
-constexpr int kChunkInfoWords = 8;
 struct ChunkLayout {
-    size_t info, lse, part, total;
+    size_t flags, items, lse, part, total;
     int slot_rows;
 };
 inline ChunkLayout chunk_layout(int Hq, int Hkv, int D, int max_q_len) {
     ChunkLayout L;
     const long long rows = (long long)max_q_len * (Hq / Hkv);
     L.slot_rows = rows >= kChunkRows ? kChunkRows : (int)(rows + 31) / 32 * 32;
-    L.info = 0;
-    L.lse = round_up_256((size_t)kChunkMaxWorkers * kChunkInfoWords * 4);
+    L.flags = 0;
+    L.items = round_up_256((size_t)kChunkMaxWorkers * 4);
+    L.lse = L.items + round_up_256((size_t)kChunkMaxWorkers * 32);
     L.part = L.lse + round_up_256((size_t)kChunkMaxWorkers * 2 * L.slot_rows * 4);
     L.total = L.part + (size_t)kChunkMaxWorkers * 2 * L.slot_rows * D * 4;
     return L;

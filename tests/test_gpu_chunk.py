@@ -163,6 +163,16 @@ def test_q_as_a_slice_of_wider_rows(wide):
     b.check()
 
 
+def test_out_aligned_to_16_bytes_and_no_more():
+    for n in (90, 9000):
+        b = Batch(16, 4, 128, 16, q_lens=[5, 40, 1], lens=[n, n, 70], seed=n)
+        want = b.run(0.1)
+        room = torch.full((b.q.numel() + 16,), 7.0, device=DEV, dtype=torch.bfloat16)
+        out = room[8:-8].view(b.q.shape)
+        assert out.data_ptr() % 32 == 16
+        assert torch.equal(b.run(0.1, out=out), want) and bool((room[:8] == 7).all()) and bool((room[-8:] == 7).all())
+
+
 def test_one_token_with_any_stride():
     b = Batch(16, 4, 128, 16, q_lens=[1], lens=[300], wide=7, seed=10)       # the stride of a single token says nothing
     b.check()
