@@ -503,7 +503,9 @@ int opt_gqa_cache_copy_pages(void* const* pools, int num_pools, const int32_t* s
     if (rc != OPT_GQA_OK) return rc;
     if (n == 0) return OPT_GQA_OK;
     if (!src_pages || !dst_pages) return OPT_GQA_ERR_NULL;
-    return launch_copy_pages(set, sh, src_pages, dst_pages, n, static_cast<cudaStream_t>(stream));
+    int* status = device_status_ptr();
+    if (!status) return OPT_GQA_ERR_CUDA;
+    return launch_copy_pages(set, sh, src_pages, dst_pages, n, status, static_cast<cudaStream_t>(stream));
 }
 
 static int requests_checked(bool fork, void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
@@ -518,11 +520,14 @@ static int requests_checked(bool fork, void* const* pools, int num_pools, int32_
     if (!block_tables || !context_lens || !ref_counts || !a || !b || !done || !workspace) return OPT_GQA_ERR_NULL;
     if (workspace_bytes < page_work_layout(n, (int)num_blocks, nullptr, nullptr)) return OPT_GQA_ERR_SHAPE;
     if (!aligned16(ref_counts) || !aligned16(workspace)) return OPT_GQA_ERR_ALIGN;
+    int* status = device_status_ptr();
+    if (!status) return OPT_GQA_ERR_CUDA;
     PageWork w;
     page_work_layout(n, (int)num_blocks, static_cast<char*>(workspace), &w);
     const PageTables t = {block_tables, context_lens, ref_counts, num_seqs, max_blocks_per_seq, bs, (int)num_blocks};
     const PageRequests r = {a, b, done, n};
-    return fork ? launch_fork(set, sh, t, r, w, static_cast<cudaStream_t>(stream)) : launch_resize(set, sh, t, r, w, static_cast<cudaStream_t>(stream));
+    return fork ? launch_fork(set, sh, t, r, w, status, static_cast<cudaStream_t>(stream))
+                : launch_resize(set, sh, t, r, w, status, static_cast<cudaStream_t>(stream));
 }
 
 int opt_gqa_cache_fork(void* const* pools, int num_pools, int32_t* block_tables, int max_blocks_per_seq, int32_t* context_lens,
@@ -552,11 +557,13 @@ int opt_gqa_cache_compact(void* const* pools, int num_pools, const int32_t* bloc
         return OPT_GQA_ERR_NULL;
     if (workspace_bytes < page_work_layout(1, (int)num_blocks, nullptr, nullptr)) return OPT_GQA_ERR_SHAPE;
     if (!aligned16(ref_counts) || !aligned16(workspace)) return OPT_GQA_ERR_ALIGN;
+    int* status = device_status_ptr();
+    if (!status) return OPT_GQA_ERR_CUDA;
     PageWork w;
     page_work_layout(1, (int)num_blocks, static_cast<char*>(workspace), &w);
     const PageTables t = {const_cast<int32_t*>(block_tables), const_cast<int32_t*>(context_lens), const_cast<int32_t*>(ref_counts),
                           num_seqs, max_blocks_per_seq, bs, (int)num_blocks};
-    return launch_compact(set, sh, t, block_tables_out, ref_counts_out, page_map, used_out, w, static_cast<cudaStream_t>(stream));
+    return launch_compact(set, sh, t, block_tables_out, ref_counts_out, page_map, used_out, w, status, static_cast<cudaStream_t>(stream));
 }
 
 // Bytes of `workspace` a decode step of these sizes uses: the balanced split's layout for bf16 caches, one

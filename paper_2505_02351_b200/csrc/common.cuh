@@ -411,10 +411,12 @@ inline size_t page_work_layout(int n, int num_blocks, char* base, PageWork* w) {
     if (w) *w = l;
     return off;
 }
-int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, int n, cudaStream_t stream);
-int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream);
-int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream);
+int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, int n, int* status, cudaStream_t stream);
+int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
+                cudaStream_t stream);
+int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
+                  cudaStream_t stream);
 int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& t, int* tables_out, int* refs_out, int* page_map, int* used,
-                   const PageWork& w, cudaStream_t stream);
+                   const PageWork& w, int* status, cudaStream_t stream);
 
 }  // namespace optgqa

@@ -3,12 +3,13 @@
 //
 // A page is free where its count is 0, and free pages are handed out lowest number first in the order of the requests: ranks
 // (prefix sums) of the free pages and of what is asked, whose results do not depend on the order of any atomic.  That part is one
-// cluster of kClusterCtas CTAs, which exchanges its sums through distributed shared memory and takes a few barriers: a grid
-// would need a launch per step, one CTA an eighth of the loads in flight.  What scales with the batch's tables and the pools --
-// dropping and sharing a table's pages, moving data -- runs on the whole GPU before and behind it.
+// cluster of kClusterCtas CTAs, which exchanges its sums through distributed shared memory and takes a few barriers (a grid
+// would need a launch per step), or one CTA where the pool and the requests are few.  What scales with the batch's tables and the
+// pools -- dropping and sharing a table's pages, moving data -- runs on the whole GPU before and behind it.
 //
-// Data moves in pieces of 2 KB, one per warp and step, four independent 16-byte vectors per lane; a page's run of one head (bs
-// rows) is always whole pieces, so the first rows of a page are the first vectors of each head's pieces.
+// Data moves by bulk copies through shared memory, a ring of slots per warp that its first lane fills and empties: 64 pages of 64
+// pools (264 MB read and written) 45 us, 5.9 TB/s, where loads and stores through registers took 51; the part-full page of a
+// 16383-token prompt for 128 samples (504 MB, the reads from L2) 63 us against 85.
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -21,10 +22,11 @@ namespace {
 
 constexpr int kClusterCtas = 8;
 constexpr int kClusterThreads = 1024;
-constexpr int kAll = kClusterCtas * kClusterThreads;
-constexpr int kPieceBytes = 2048;
-constexpr int kCopyThreads = 256;
-constexpr int kCopyCtasPerSm = 8;
+constexpr int kCopyThreads = 128;
+constexpr int kCopyWarps = kCopyThreads / 32;
+constexpr int kCopyCtasPerSm = 3;
+constexpr int kSlots = 4;                   // of a warp's ring
+constexpr int kSlotBytes = 4096;
 constexpr unsigned kFull = 0xffffffffu;
 
 // Read of what other multiprocessors wrote in this launch: past L1.
@@ -33,37 +35,102 @@ __device__ __forceinline__ int ld_cg(const int* p) { return __ldcg(p); }
 __device__ __forceinline__ bool in_pool(int page, int num_blocks) { return (unsigned)page < (unsigned)num_blocks; }
 
 // ----------------------------------------------------------------------------- moving data
-// Every warp of the grid takes pieces in turn.  rows: how many of a page's rows are copied (null: all).
-__device__ __forceinline__ void copy_pieces(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, const int* rows,
-                                            int n) {
-    const int lane = threadIdx.x & 31;
-    const long long warp = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), warps = (long long)gridDim.x * (blockDim.x >> 5);
-    const unsigned per_page = sh.page_bytes / kPieceBytes, per_pair = per_page * (unsigned)sh.num_pools;
-    const long long total = (long long)n * per_pair;
-    for (long long i = warp; i < total; i += warps) {
-        const int pair = total <= 0xffffffffll ? (int)((unsigned)i / per_pair) : (int)(i / per_pair);
-        const unsigned rest = (unsigned)(i - (long long)pair * per_pair), pool = rest / per_page, at = (rest - pool * per_page) * kPieceBytes;
-        const int s = ld_cg(src + pair), d = ld_cg(dst + pair);
-        if (!in_pool(s, sh.num_blocks) || !in_pool(d, sh.num_blocks)) continue;
-        const unsigned in_head = at % sh.head_bytes + lane * 16;
-        const unsigned limit = rows ? (unsigned)ld_cg(rows + pair) * sh.row_bytes : sh.head_bytes;
-        const uint4* from = reinterpret_cast<const uint4*>(pools.p[pool] + (size_t)s * sh.page_bytes + at) + lane;
-        uint4* to = reinterpret_cast<uint4*>(pools.p[pool] + (size_t)d * sh.page_bytes + at) + lane;
-        uint4 v[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (in_head + u * 512 < limit) v[u] = __ldcs(from + u * 32);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (in_head + u * 512 < limit) __stcs(to + u * 32, v[u]);
-    }
+// Where share i of W begins in a list of `total`.
+__device__ __forceinline__ long long share_of(long long total, long long i, long long W) {
+    return total < (1ll << 40) ? total * i / W : total / W * i + total % W * i / W;
 }
 
+struct CopyRing {
+    alignas(128) char data[kCopyWarps][kSlots][kSlotBytes];
+    uint64_t full[kCopyWarps][kSlots];
+};
+
+__device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+
+// Page src[i] to page dst[i] in every pool for i < n; kRows: the first rows[i] rows of every head alone.  A piece is up to
+// kSlotBytes of a page, or of one head's rows.  Whole pages: the warps take the pieces in turn (in runs of their own, 47 us against
+// 45 for the 64 pages).  Part-full ones: each warp takes a run of pieces, so that it looks a pair up once and not for every
+// 4 KB (63 us against 70).
+template <bool kRows>
+__device__ __forceinline__ void copy_pages(CopyRing& ring, const PoolSet& pools, const PageShape& sh, const int* src, const int* dst,
+                                           const int* rows, int n, int* status) {
+    if (threadIdx.x & 31) return;
+    const int w = threadIdx.x >> 5;
+    uint64_t* full = ring.full[w];
+    const unsigned run = kRows ? sh.head_bytes : sh.page_bytes, per_run = (run + kSlotBytes - 1) / kSlotBytes, runs = sh.page_bytes / run;
+    const unsigned per_pool = per_run * runs, per_pair = per_pool * (unsigned)sh.num_pools;
+    const long long total = (long long)n * per_pair;
+    const long long warp = (long long)blockIdx.x * kCopyWarps + w, warps = (long long)gridDim.x * kCopyWarps;
+    const long long step = kRows ? 1 : warps, stop = kRows ? share_of(total, warp + 1, warps) : total;
+    long long next = kRows ? share_of(total, warp, warps) : warp;
+    if (next >= stop) return;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) mbar_init(&full[i], 1);
+    fence_barrier_init();
+    char* to[kSlots];
+    unsigned bytes[kSlots];
+    int pair = -1, from_page = 0, to_page = 0;
+    unsigned limit = 0;
+    // the next piece there is, into slot k; false at the end
+    auto fill = [&](int k) -> bool {
+        for (; next < stop; next += step) {
+            const int i = total <= 0xffffffffll ? (int)((unsigned)next / per_pair) : (int)(next / per_pair);
+            if (i != pair) {
+                pair = i;
+                from_page = ld_cg(src + i), to_page = ld_cg(dst + i);
+                limit = kRows ? (unsigned)ld_cg(rows + i) * sh.row_bytes : run;
+                if (!in_pool(from_page, sh.num_blocks) || !in_pool(to_page, sh.num_blocks)) limit = 0;
+            }
+            const unsigned rest = (unsigned)(next - (long long)i * per_pair), pool = rest / per_pool, in = rest - pool * per_pool;
+            const unsigned r = in / per_run, off = (in - r * per_run) * kSlotBytes;
+            if (off >= limit) {
+                if (kRows && limit == 0) next = (long long)(i + 1) * per_pair - 1;      // nothing of this pair
+                continue;
+            }
+            const size_t at = (size_t)r * run + off;
+            const char* base = pools.p[pool];
+            char* out = pools.p[pool] + (size_t)to_page * sh.page_bytes + at;
+            const unsigned size = min(limit - off, (unsigned)kSlotBytes);
+#pragma unroll
+            for (int u = 0; u < kSlots; ++u)
+                if (u == k) to[u] = out, bytes[u] = size;
+            mbar_expect_tx(&full[k], size);
+            bulk_g2s(ring.data[w][k], base + (size_t)from_page * sh.page_bytes + at, size, &full[k]);
+            next += step;
+            return true;
+        }
+        return false;
+    };
+    int filled = 0;
+    while (filled < kSlots - 1 && fill(filled)) ++filled;
+    for (int done = 0; done < filled; ++done) {
+        const int k = done % kSlots;
+        if (!mbar_wait(&full[k], (done / kSlots) & 1, status)) {
+            for (int i = 0; i < 200; ++i) __nanosleep(1000);        // let what is in flight land
+            break;
+        }
+        char* out = to[0];
+        unsigned size = bytes[0];
+#pragma unroll
+        for (int u = 1; u < kSlots; ++u)
+            if (u == k) out = to[u], size = bytes[u];
+        bulk_s2g(out, ring.data[w][k], size);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the slot before this one has been read: it is next
+        if (fill(filled % kSlots)) ++filled;
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+template <bool kRows>
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PoolSet pools, const PageShape sh, const int* src,
-                                                                  const int* dst, const int* rows, int n, bool last) {
-    if (last) grid_dependency_launch();     // (behind a table's kernel nothing may start early: see below)
+                                                                  const int* dst, const int* rows, int n, int* status) {
+    extern __shared__ __align__(128) char smem[];
+    if (!kRows) grid_dependency_launch();   // (behind a table's kernel nothing may start early: see below)
     grid_dependency_wait();
-    copy_pieces(pools, sh, src, dst, rows, n);
+    copy_pages<kRows>(*reinterpret_cast<CopyRing*>(smem), pools, sh, src, dst, rows, n, status);
 }
 
 // ----------------------------------------------------------------------------- tables
@@ -74,13 +141,18 @@ __device__ __forceinline__ int pages_of(int tokens, const PageTables& t) {
     return min((max(tokens, 0) + t.bs - 1) / t.bs, t.width);
 }
 
-// Entries [from, to) of a table's row let go.
+// Entries [from, to) of a table's row let go, four loads in flight per thread.
 __device__ __forceinline__ void drop_pages(const PageTables& t, int row, int from, int to, int first, int step) {
     int* entry = t.tables + (size_t)row * t.width;
-    for (int i = from + first; i < to; i += step) {
-        const int page = entry[i];
-        if (in_pool(page, t.num_blocks)) atomicSub(t.refs + page, 1);
-        entry[i] = -1;
+    for (long long i = from + first; i < to; i += 4ll * step) {
+        int page[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) page[u] = i + (long long)u * step < to ? entry[i + (long long)u * step] : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (in_pool(page[u], t.num_blocks)) atomicSub(t.refs + page[u], 1);
+            if (i + (long long)u * step < to) entry[i + (long long)u * step] = -1;
+        }
     }
 }
 
@@ -104,6 +176,31 @@ __global__ void __launch_bounds__(256) fork_drop_kernel(const PageTables t, cons
     const int step = gridDim.x * 8 * 128;
     for (int from = (blockIdx.x * 8 + (threadIdx.x >> 5)) * 128; from < pages; from += step)
         drop_pages(t, row, from, min(from + 128, pages), lane, 32);
+}
+
+// The CTAs of a cluster, or the one there is.
+template <int kCtas>
+__device__ __forceinline__ void sync_all() {
+    if constexpr (kCtas > 1) {
+        cg::this_cluster().sync();
+    } else {
+        __threadfence();            // counts are changed and read past L1
+        __syncthreads();
+    }
+}
+template <int kCtas>
+__device__ __forceinline__ int cta_rank() {
+    if constexpr (kCtas > 1) return (int)cg::this_cluster().block_rank();
+    else return 0;
+}
+// `v` to place `rank` of every CTA's `all`.
+template <int kCtas>
+__device__ __forceinline__ void tell_all(long long* all, int rank, long long v) {
+    if constexpr (kCtas > 1) {
+        if (threadIdx.x < kCtas) *cg::this_cluster().map_shared_rank(all + rank, threadIdx.x) = v;
+    } else if (threadIdx.x == 0) {
+        all[0] = v;
+    }
 }
 
 // Sum over the CTA's threads of `v`, of the threads before this one (exclusive) and in all (total); scratch [33].
@@ -148,21 +245,22 @@ __device__ __forceinline__ int4 four_counts(const int* refs, int at, int num_blo
 struct Slice {
     int begin, end;
 };
+template <int kCtas>
 __device__ __forceinline__ Slice slice_of(int num_blocks, int rank) {
-    const int fours = num_blocks / 4 + (num_blocks % 4 != 0), per = (fours + kClusterCtas - 1) / kClusterCtas;
+    const int fours = num_blocks / 4 + (num_blocks % 4 != 0), per = (fours + kCtas - 1) / kCtas;
     const long long b = 4ll * per * rank, e = b + 4ll * per;
     return {(int)min(b, (long long)num_blocks), (int)min(e, (long long)num_blocks)};
 }
 
 // The cluster: what is asked and what is free is counted, the free pages that are handed out are listed, and every request that
 // can be served is.  Request i is served where its own pages and those asked before it are there.
-template <bool kFork>
-__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads)
+template <bool kFork, int kCtas>
+__global__ void __launch_bounds__(kClusterThreads)
 give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bool drops) {
+    constexpr int kAll = kCtas * kClusterThreads;
     __shared__ long long scratch[33];
-    __shared__ long long all_need[kClusterCtas], all_free[kClusterCtas];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), tid = threadIdx.x;
+    __shared__ long long all_need[kCtas], all_free[kCtas];
+    const int rank = cta_rank<kCtas>(), tid = threadIdx.x;
     grid_dependency_launch();
     grid_dependency_wait();
     // 2^k threads for one request, of the whole cluster
@@ -176,11 +274,11 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
             if (row < 0) continue;
             drop_pages(t, row, kFork ? 0 : pages_of(r.b[i], t), pages_of(t.lens[row], t), sub, lanes);
         }
-        cluster.sync();
+        sync_all<kCtas>();
     }
 
     // what is asked, request by request in the order of the list: a share of the list per CTA
-    const int share = (r.n + kClusterCtas - 1) / kClusterCtas;
+    const int share = (r.n + kCtas - 1) / kCtas;
     const int mine = min(share * rank, r.n), mine_end = min(share * (rank + 1), r.n);
     long long asked = 0;
     for (int base = mine; base < mine_end; base += kClusterThreads) {
@@ -225,7 +323,7 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
         asked += total;
     }
     // what is free
-    const Slice s = slice_of(t.num_blocks, rank);
+    const Slice s = slice_of<kCtas>(t.num_blocks, rank);
     long long zeros = 0;
     for (int at = s.begin + 4 * tid; at < s.end; at += 4 * kClusterThreads) {
         const int4 v = four_counts(t.refs, at, t.num_blocks);
@@ -233,13 +331,11 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
     }
     long long here;
     block_scan(zeros, scratch, here);
-    if (tid < kClusterCtas) {
-        *cluster.map_shared_rank(&all_need[rank], tid) = asked;
-        *cluster.map_shared_rank(&all_free[rank], tid) = here;
-    }
-    cluster.sync();
+    tell_all<kCtas>(all_need, rank, asked);
+    tell_all<kCtas>(all_free, rank, here);
+    sync_all<kCtas>();
     long long total_need = 0, total_free = 0, rank_free = 0;
-    for (int c = 0; c < kClusterCtas; ++c) {
+    for (int c = 0; c < kCtas; ++c) {
         if (c == rank) rank_free = total_free;
         total_need += all_need[c];
         total_free += all_free[c];
@@ -257,7 +353,7 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
         if (v.w == 0 && k++ < total_need) w.free_list[k - 1] = at + 3;
         rank_free += total;
     }
-    cluster.sync();
+    sync_all<kCtas>();
 
     for (int i = group; i < r.n; i += groups) {
         const int need = ld_cg(w.need + i), rows = ld_cg(w.rows + i);
@@ -267,10 +363,16 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
         if (served && need > 0) {
             const int first = ld_cg(w.first + i);
             int* entry = t.tables + (size_t)(kFork ? r.b[i] : r.a[i]) * t.width;
-            for (int k = sub; k < need; k += lanes) {
-                const int page = ld_cg(w.free_list + from + k);
-                if (first + k < t.width) entry[first + k] = page;
-                t.refs[page] = 1;
+            for (long long k = sub; k < need; k += 4ll * lanes) {
+                int page[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) page[u] = k + (long long)u * lanes < need ? ld_cg(w.free_list + from + k + (long long)u * lanes) : -1;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if (page[u] < 0) break;
+                    if (first + k + (long long)u * lanes < t.width) entry[first + k + (long long)u * lanes] = page[u];
+                    t.refs[page[u]] = 1;
+                }
             }
         }
         if (sub == 0) {
@@ -289,10 +391,11 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
 // The parents' whole pages shared with their children, then the part-full ones copied.  Neighbouring requests of one parent are
 // a run: the first of them adds for all.
 __global__ void __launch_bounds__(kCopyThreads) fork_share_kernel(const __grid_constant__ PoolSet pools, const PageShape sh, const PageTables t,
-                                                                  const PageRequests r, const PageWork w, int chunks) {
+                                                                  const PageRequests r, const PageWork w, int chunks, int* status) {
+    extern __shared__ __align__(128) char smem[];
     grid_dependency_wait();
-    const int lane = threadIdx.x & 31, warps = gridDim.x * (kCopyThreads / 32);
-    for (long long c = (long long)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); c < (long long)r.n * chunks; c += warps) {
+    const int lane = threadIdx.x & 31, warps = gridDim.x * kCopyWarps;
+    for (long long c = (long long)blockIdx.x * kCopyWarps + (threadIdx.x >> 5); c < (long long)r.n * chunks; c += warps) {
         const int i = (int)(c / chunks), from = (int)(c - (long long)i * chunks) * 128;
         const int parent = r.a[i];
         if ((unsigned)parent >= (unsigned)t.rows) continue;
@@ -320,20 +423,21 @@ __global__ void __launch_bounds__(kCopyThreads) fork_share_kernel(const __grid_c
             if (times && in_pool(page, t.num_blocks)) atomicAdd(t.refs + page, times);
         }
     }
-    copy_pieces(pools, sh, w.src, w.dst, w.rows, r.n);
+    __syncwarp();
+    copy_pages<true>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, w.rows, r.n, status);
 }
 
 // ----------------------------------------------------------------------------- compaction
 // U pages are in use.  The k-th page in use at or past U goes to the k-th free one below U.
-__global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kClusterThreads)
+template <int kCtas>
+__global__ void __launch_bounds__(kClusterThreads)
 compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out, const PageWork w, int num_blocks) {
     __shared__ long long scratch[33];
-    __shared__ long long all_used[kClusterCtas];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int rank = (int)cluster.block_rank(), tid = threadIdx.x;
+    __shared__ long long all_used[kCtas], all_low[kCtas];
+    const int rank = cta_rank<kCtas>(), tid = threadIdx.x;
     grid_dependency_launch();
     grid_dependency_wait();
-    const Slice s = slice_of(num_blocks, rank);
+    const Slice s = slice_of<kCtas>(num_blocks, rank);
     long long count = 0, here;
     for (int at = s.begin + 4 * tid; at < s.end; at += 4 * kClusterThreads) {
         const int4 v = four_counts(refs, at, num_blocks);
@@ -341,25 +445,24 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
         count += (v.x > 0) + (v.y > 0) + (v.z > 0) + (v.w > 0) - (4 - live);
     }
     block_scan(count, scratch, here);
-    if (tid < kClusterCtas) *cluster.map_shared_rank(&all_used[rank], tid) = here;
-    cluster.sync();
+    tell_all<kCtas>(all_used, rank, here);
+    sync_all<kCtas>();
     long long before = 0, U = 0;
-    for (int c = 0; c < kClusterCtas; ++c) {
+    for (int c = 0; c < kCtas; ++c) {
         if (c == rank) before = U;
         U += all_used[c];
     }
     // pages in use below U: the holes and the movers are as many, U less those
-    __shared__ long long all_low[kClusterCtas];
     count = 0;
     for (int at = s.begin + 4 * tid; at < s.end && at < U; at += 4 * kClusterThreads) {
         const int4 v = four_counts(refs, at, num_blocks);
         count += (at < U && v.x > 0) + (at + 1 < U && v.y > 0) + (at + 2 < U && v.z > 0) + (at + 3 < U && v.w > 0);
     }
     block_scan(count, scratch, here);
-    if (tid < kClusterCtas) *cluster.map_shared_rank(&all_low[rank], tid) = here;
-    cluster.sync();
+    tell_all<kCtas>(all_low, rank, here);
+    sync_all<kCtas>();
     long long low = 0;
-    for (int c = 0; c < kClusterCtas; ++c) low += all_low[c];
+    for (int c = 0; c < kCtas; ++c) low += all_low[c];
     for (int base = s.begin; base < s.end; base += 4 * kClusterThreads) {
         const int at = base + 4 * tid;
         int ref[4] = {0, 0, 0, 0};
@@ -397,9 +500,9 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
             }
         }
     }
-    cluster.sync();
+    sync_all<kCtas>();
     const long long moves = U - low;
-    for (long long k = rank * kClusterThreads + tid; k < moves; k += kAll) {
+    for (long long k = rank * kClusterThreads + tid; k < moves; k += kCtas * kClusterThreads) {
         const int from = ld_cg(w.src + k), to = ld_cg(w.dst + k);
         page_map[from] = to;
         refs_out[to] = ld_cg(w.rows + k);
@@ -412,7 +515,8 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
 
 __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid_constant__ PoolSet pools, const PageShape sh, const int* tables,
                                                                     int* tables_out, const int* lens, const int* page_map, const PageWork w,
-                                                                    int rows, int width, int bs) {
+                                                                    int rows, int width, int bs, int* status) {
+    extern __shared__ __align__(128) char smem[];
     grid_dependency_wait();
     const long long entries = (long long)rows * width;
     for (long long e = (long long)blockIdx.x * kCopyThreads + threadIdx.x; e < entries; e += (long long)gridDim.x * kCopyThreads) {
@@ -420,54 +524,99 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid
         const bool held = (long long)k * bs < lens[row] && in_pool(page, sh.num_blocks);
         tables_out[e] = held ? page_map[page] : page;
     }
-    copy_pieces(pools, sh, w.src, w.dst, nullptr, w.first[0]);
+    __syncwarp();
+    copy_pages<false>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, nullptr, w.first[0], status);
 }
 
-unsigned copy_ctas(const PageShape& sh, long long pairs) {
-    const long long warps = pairs * sh.num_pools * (sh.page_bytes / kPieceBytes), most = (long long)sm_count() * kCopyCtasPerSm;
-    const long long ctas = (warps + kCopyThreads / 32 - 1) / (kCopyThreads / 32);
+// One resident wave, or fewer where there are fewer pieces (and chunks of tables).
+unsigned copy_ctas(const PageShape& sh, long long pairs, long long chunks = 0) {
+    const long long per_page = (sh.page_bytes + kSlotBytes - 1) / kSlotBytes;
+    const long long pieces = pairs * sh.num_pools * per_page, most = (long long)sm_count() * kCopyCtasPerSm;
+    const long long ctas = ((pieces > chunks ? pieces : chunks) + kCopyWarps - 1) / kCopyWarps;
     return (unsigned)(ctas < 1 ? 1 : ctas < most ? ctas : most);
 }
 
-}  // namespace
-
-int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, int n, cudaStream_t stream) {
-    if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    return launch_dependent(copy_pages_kernel, dim3(copy_ctas(sh, n)), dim3(kCopyThreads), 0, stream, pools, sh, src, dst, nullptr, n, true);
+// A launch of the kernels with a ring.
+template <typename... KArgs, typename... Args>
+int launch_copying(void (*kernel)(KArgs...), unsigned ctas, std::atomic<bool>* configured, cudaStream_t stream, Args... args) {
+    if (!ensure_smem_limit(kernel, sizeof(CopyRing), configured)) return OPT_GQA_ERR_CUDA;
+    return launch_dependent(kernel, dim3(ctas), dim3(kCopyThreads), sizeof(CopyRing), stream, args...);
 }
 
-// Entries of the children's tables up to which the cluster drops them itself.
-static constexpr long long kClusterDrop = 16384;
+// launch_dependent for a cluster, or one CTA alone.
+template <typename... KArgs, typename... Args>
+int launch_cluster(void (*kernel)(KArgs...), int ctas, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kClusterThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? OPT_GQA_OK : OPT_GQA_ERR_CUDA;
+}
 
-int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream) {
+// Up to this many pages (two vectors of counts per thread) and entries of tables one CTA does what the cluster would: its barriers
+// take a tenth of the cluster's time.
+constexpr int kOneCtaPages = 8192;
+constexpr long long kOneCtaEntries = 16384;
+// Entries of the children's tables up to which the cluster drops them itself, without a launch of the whole GPU before it.
+constexpr long long kClusterDrop = 16384;
+
+}  // namespace
+
+int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src, const int* dst, int n, int* status, cudaStream_t stream) {
+    static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    const bool drops = (long long)r.n * t.width <= kClusterDrop;
+    return launch_copying(copy_pages_kernel<false>, copy_ctas(sh, n), configured, stream, pools, sh, src, dst, nullptr, n, status);
+}
+
+int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
+                cudaStream_t stream) {
+    static std::atomic<bool> configured[kMaxDevices];
+    if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
+    const long long entries = (long long)r.n * t.width;
+    const bool drops = entries <= kClusterDrop;
     int rc = OPT_GQA_OK;
     if (!drops) {
         const unsigned x = (unsigned)((t.width + 1023) / 1024);
         rc = launch_dependent(fork_drop_kernel, dim3(x < 64 ? x : 64, (unsigned)r.n), dim3(256), 0, stream, t, r);
         if (rc != OPT_GQA_OK) return rc;
     }
-    rc = launch_dependent(give_pages_kernel<true>, dim3(kClusterCtas), dim3(kClusterThreads), 0, stream, t, r, w, drops);
+    rc = t.num_blocks <= kOneCtaPages && entries <= kOneCtaEntries
+             ? launch_cluster(give_pages_kernel<true, 1>, 1, stream, t, r, w, drops)
+             : launch_cluster(give_pages_kernel<true, kClusterCtas>, kClusterCtas, stream, t, r, w, drops);
     if (rc != OPT_GQA_OK) return rc;
-    return launch_dependent(fork_share_kernel, dim3(copy_ctas(sh, r.n)), dim3(kCopyThreads), 0, stream, pools, sh, t, r, w, (t.width + 127) / 128);
+    const int chunks = (t.width + 127) / 128;
+    return launch_copying(fork_share_kernel, copy_ctas(sh, r.n, (long long)r.n * chunks), configured, stream, pools, sh, t, r, w, chunks, status);
 }
 
-int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, cudaStream_t stream) {
+int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
+                  cudaStream_t stream) {
+    static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    const int rc = launch_dependent(give_pages_kernel<false>, dim3(kClusterCtas), dim3(kClusterThreads), 0, stream, t, r, w, true);
+    const int rc = t.num_blocks <= kOneCtaPages && (long long)r.n * t.width <= kOneCtaEntries
+                       ? launch_cluster(give_pages_kernel<false, 1>, 1, stream, t, r, w, true)
+                       : launch_cluster(give_pages_kernel<false, kClusterCtas>, kClusterCtas, stream, t, r, w, true);
     if (rc != OPT_GQA_OK) return rc;
-    return launch_dependent(copy_pages_kernel, dim3(copy_ctas(sh, r.n)), dim3(kCopyThreads), 0, stream, pools, sh, w.src, w.dst, w.rows, r.n, false);
+    return launch_copying(copy_pages_kernel<true>, copy_ctas(sh, r.n), configured, stream, pools, sh, w.src, w.dst, w.rows, r.n, status);
 }
 
 int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& t, int* tables_out, int* refs_out, int* page_map, int* used,
-                   const PageWork& w, cudaStream_t stream) {
+                   const PageWork& w, int* status, cudaStream_t stream) {
+    static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    const int rc = launch_dependent(compact_plan_kernel, dim3(kClusterCtas), dim3(kClusterThreads), 0, stream, t.refs, refs_out, page_map, used, w,
-                                    t.num_blocks);
+    const int rc = t.num_blocks <= kOneCtaPages
+                       ? launch_cluster(compact_plan_kernel<1>, 1, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
+                       : launch_cluster(compact_plan_kernel<kClusterCtas>, kClusterCtas, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
     if (rc != OPT_GQA_OK) return rc;
-    return launch_dependent(compact_move_kernel, dim3(copy_ctas(sh, t.num_blocks / 2 + 1)), dim3(kCopyThreads), 0, stream, pools, sh, t.tables,
-                            tables_out, t.lens, page_map, w, t.rows, t.width, t.bs);
+    return launch_copying(compact_move_kernel, copy_ctas(sh, t.num_blocks / 2 + 1, (long long)t.rows * t.width / 32), configured, stream, pools,
+                          sh, t.tables, tables_out, t.lens, page_map, w, t.rows, t.width, t.bs, status);
 }
 
 }  // namespace optgqa
