@@ -38,14 +38,15 @@ constexpr int kMinShare = 8;               // a worker's share at least, in the 
 constexpr int kNarrowRows = 16;            // up to which the products take 64 rows: row 16 w + i lies in lane 32 w + i
 // The second half of the workers begins later, 1 us where the GPU is idle and 4 to 6 where a call follows another (an SM's second
 // CTA finds its registers when the merge before is done): what a worker of it has less, and one of the first half more.
-#ifndef KLATE
-#define KLATE 5
-#endif
-constexpr int kLateCost = KLATE;
-#ifndef KDIRECT
-#define KDIRECT 11
-#endif
-constexpr int kDirectTiles = KDIRECT;
+constexpr int kLateCost = 5;
+// Where there are no more items than workers, nothing is cut -- one item each, and nothing to merge -- if the longest is not much
+// above a worker's share: what cutting costs is kCutCost (with blocks of more than 64 rows kCutCostFull), and alone on its
+// multiprocessor a worker is a fifth faster.  (In a graph, us, tables so wide that the host does not know, not cut against cut: 128
+// items of 9 and 16 tiles 16.3 and 21.9 against 20.5 and 23.9, 256 of 9 and 24 19.6 and 37.0 against 25.7 and 42.1, 32 of 7 and 9
+// 13.3 and 14.9 against 13.7 and 13.0, 72 of 128 rows and 9 and 11 tiles 17.2 and 19.0 against 21.2 and 21.6.)
+constexpr int kCutCost = 28, kCutCostFull = 36;
+// A CTA for each item, and no list, where they are one wave of at most kDirectTiles + items / kDirectItems tiles each.
+constexpr int kDirectTiles = 8, kDirectItems = 16;
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr int kDescBytes = 64;
 constexpr int kOpens = 1, kContinues = 2, kCloses = 4;      // a worker's flags: see ChunkLayout
@@ -155,10 +156,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     uint64_t* desc_full = p_full + 2;
     uint64_t* desc_empty = desc_full + kDescs;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kNumBars);
-    // units (one head) of the sequences before each thread's chunk, from its warp's first on, and of each warp's chunks; gone
-    // once the K ring is in use
+    // units and blocks (of one head) of the sequences before each thread's chunk, from its warp's first on, and of each warp's
+    // chunks, and the most units of a block; gone once the K ring is in use
     long long* c_units = reinterpret_cast<long long*>(smem + kOffK);
     long long* w_units = c_units + kThreads;
+    long long* c_blocks = w_units + kThreads / 32;
+    long long* w_blocks = c_blocks + kThreads;
+    int* w_most = reinterpret_cast<int*>(w_blocks + kThreads / 32);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 192) {
@@ -168,12 +172,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
     auto item_cost = [&](const Seq& x) { return x.q * G > 64 ? kFullItem : kSmallItem; };
-    auto seq_units = [&](const Seq& x) {
-        int sum = 0;
+    auto seq_units = [&](const Seq& x, int& most) {
+        long long sum = 0;
         for (int mt = x.first; mt < x.blocks; ++mt) {
             int lo, hi;
             block_tiles<TQ>(x, mt, p.window, lo, hi);
             sum += hi - lo;
+            most = max(most, (hi - lo) * kTileCost + item_cost(x));
         }
         return sum * kTileCost + (x.blocks - x.first) * item_cost(x);
     };
@@ -182,16 +187,27 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     // wait for the preceding kernel: see the ordering contract in the header)
     const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
     if (!p.direct) {
-        long long sum = 0;
-        for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) sum += seq_units(sequence<TQ>(p, s));
-        long long incl = sum;
+        long long units = 0, blocks = 0;
+        int most = 0;
+        for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) {
+            const Seq x = sequence<TQ>(p, s);
+            units += seq_units(x, most);
+            blocks += x.blocks - x.first;
+        }
+        long long upto = units, upto_b = blocks;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(kFull, incl, o);
-            if (lane >= o) incl += v;
+            const long long v = __shfl_up_sync(kFull, upto, o), b = __shfl_up_sync(kFull, upto_b, o);
+            if (lane >= o) upto += v, upto_b += b;
         }
-        c_units[threadIdx.x] = incl - sum;
-        if (lane == 31) w_units[warp] = incl;
+        most = __reduce_max_sync(kFull, most);
+        c_units[threadIdx.x] = upto - units;
+        c_blocks[threadIdx.x] = upto_b - blocks;
+        if (lane == 31) {
+            w_units[warp] = upto;
+            w_blocks[warp] = upto_b;
+            w_most[warp] = most;
+        }
     }
     if (threadIdx.x == 128) {
 #pragma unroll
@@ -252,19 +268,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         int s = 0, kvh = 0, mt = 0, jt = 0, t0 = 0, t1 = 0;        // the item's tiles t0 .. t1 - 1, jt of them done
         long long pos = 0, end = 0;                                 // in the list: the next tile's place, and the share's end
         const int me = blockIdx.x;
+        bool whole = false;                                         // items are not cut: the list counts them, not their units
         // Where the share begins in the list.  (In 32 bits where they do: N is int or long long.)
         auto locate = [&](auto total_units) {
             using N = decltype(total_units);
             const N total = total_units;
-            const int W = (int)max(min((N)gridDim.x, total / kMinShare), (N)1);
-            const int skew = total / W >= 4 * kLateCost ? kLateCost : 0;
+            const int W = (int)max(min((N)gridDim.x, whole ? total : total / kMinShare), (N)1);
+            const int skew = !whole && total / W >= 4 * kLateCost ? kLateCost : 0;
             auto share = [&](int i) { return (N)share_at(total, i, W) + skew * min(i, W - i); };
             const N begin = share(min(me, W));
             end = share(min(me + 1, W));
             pos = end;
             if (begin >= end) return;
             // the last thread's chunk that begins at or before the share, and its begin
-            const N sum = (N)w_units[lane & 7] * p.Hkv;
+            const long long *warps = whole ? w_blocks : w_units, *chunks = whole ? c_blocks : c_units;
+            const N sum = (N)warps[lane & 7] * p.Hkv;
             N upto = sum;
 #pragma unroll
             for (int o = 1; o < 8; o <<= 1) {
@@ -273,26 +291,29 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             }
             int at = __popc(__ballot_sync(kFull, upto - sum <= begin) & 0xff) - 1;
             N before = __shfl_sync(kFull, upto - sum, at);
-            const N mine = before + (N)c_units[at * 32 + lane] * p.Hkv;
+            const N mine = before + (N)chunks[at * 32 + lane] * p.Hkv;
             const int in_warp = __popc(__ballot_sync(kFull, mine <= begin)) - 1;
             before = __shfl_sync(kFull, mine, in_warp);
             at = at * 32 + in_warp;
-            int units = 0;
+            int most = 0;
             for (s = at * chunk; s < p.B; ++s) {
                 x = sequence<TQ>(p, s);
-                units = seq_units(x);
-                if (before + units * (N)p.Hkv > begin) break;
-                before += units * (N)p.Hkv;
+                const N all = (whole ? (N)(x.blocks - x.first) : (N)seq_units(x, most)) * p.Hkv;
+                if (before + all > begin) break;
+                before += all;
             }
             if (s >= p.B) return;                                   // (cannot happen: the shares end where the items do)
             N r = begin - before;
+            int units;
             for (mt = x.first;; ++mt) {
                 block_tiles<TQ>(x, mt, p.window, t0, t1);
-                units = (t1 - t0) * kTileCost + item_cost(x);
+                units = whole ? 1 : (t1 - t0) * kTileCost + item_cost(x);
                 if (r < units * (N)p.Hkv || mt == x.blocks - 1) break;
                 r -= units * (N)p.Hkv;
             }
             kvh = (int)(r / units);
+            pos = begin;
+            if (whole) return;
             // an item's tile j lies its cost + j tiles behind its begin; a share has those whose place lies in it
             const int in_item = (int)(r - (N)kvh * units) - item_cost(x);
             jt = max((in_item + kTileCost - 1) / kTileCost, 0);
@@ -314,7 +335,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 }
                 block_tiles<TQ>(x, mt, p.window, t0, t1);
             }
-            pos += item_cost(x);
+            if (!whole) pos += item_cost(x);
         };
         if (p.direct) {
             s = blockIdx.z;
@@ -326,9 +347,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 end = (t1 - t0) * kTileCost;
             }
         } else {
-            long long total = 0;
-            for (int w = 0; w < kThreads / 32; ++w) total += w_units[w];
+            long long total = 0, items = 0;
+            int most = 0;
+            for (int w = 0; w < kThreads / 32; ++w) {
+                total += w_units[w];
+                items += w_blocks[w];
+                most = max(most, w_most[w]);
+            }
             total *= p.Hkv;
+            items *= p.Hkv;
+            const int alone = 2 * items <= gridDim.x ? most - most / 5 : most;
+            whole = items <= gridDim.x && alone <= total / gridDim.x + (p.max_q > 64 / G ? kCutCostFull : kCutCost);
+            if (whole) total = items;
             if (total < 0x40000000) locate((int)total);
             else locate(total);
             if (jt > 0 && jt == t1 - t0) next_item();                  // the share begins inside an item's last tile
@@ -350,7 +380,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         bool waited = false;
         for (int pc = 0;; ++pc) {
             const unsigned room = (unsigned)max(min((end - pos + kTileCost - 1) / kTileCost, (long long)0x3fffffff), 0ll);
-            const int len = (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
+            const int len = whole ? (pos < end ? t1 - t0 : 0) : (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
             const int rows = min(TQ, x.q - mt * TQ) * G, wide = rows > 64 ? 4 : rows > 32 ? 2 : 1;
             const bool opens = jt == 0, closes = jt + len == t1 - t0, once = x.blocks - x.first <= 1;
             const int tile_hi = t0 + jt + len - 1, q0 = x.q0 + mt * TQ, pos0 = x.pos0 + mt * TQ;
@@ -420,7 +450,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 }
             }
             if (!ok) break;
-            pos += len * kTileCost;
+            pos += whole ? 1 : len * kTileCost;
             next_item();
         }
         if (!waited) grid_dependency_wait();
@@ -891,7 +921,7 @@ chunk_merge_kernel(const ChunkMergeParams p) {
             leader = hi - (__ffs(found) - 1);
             if (found || hi < 32) break;
         }
-        leader = min(max(leader, 0), me - 1);
+        leader = max(min(leader, me - 1), 0);
     }
     int parts = 1;
     for (int at = leader + 1;; at += 32) {
@@ -998,7 +1028,10 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    p.direct = items <= wave && tiles <= kDirectTiles;
+    // (In a graph, us, a CTA each against the list that is cut: 32 items of 4, 7, 10, 11 and 16 tiles 7.7 10.1 12.6 13.4 17.4 against
+    // 12.8 13.3 12.7 12.8 15.1; 64 of 11, 13 and 16 17.6 19.5 22.6 against 20.1 20.8 21.7; 128 of 13, 16 and 24 16.7 19.3 26.3 against
+    // 22.1 23.4 27.2; 256 of 16 and 24 23.9 33.0 against 32.4 41.5.)
+    p.direct = items <= wave && tiles <= kDirectTiles + items / kDirectItems;
     dim3 grid((unsigned)blocks, (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.direct) {
