@@ -9,13 +9,27 @@
 // two per SM), so that one long context fills the GPU as well as a large ragged batch.  A range covers whole items, written
 // out at once, and at its two ends parts of items: normalised partial rows and log-sum-exps in the workspace, two places a worker,
 // merged by chunk_merge_kernel.  (The chunked prefill gives a block of rows to one CTA whatever the context: with few new tokens
-// most of the GPU is idle.)
+// most of the GPU is idle.)  Few items are not cut, and few items of few tiles need no list: see kCutCost and kDirectTiles.
 //
-// Blocks of up to 32 rows lie in the lanes of one row warp, those of up to 64 in two: items take the warps in turns, so that one
-// block's last product and its storing overlap the next one's first scores.  Warps none of whose rows see a tile skip its softmax.
+// Products take 64 rows for blocks of up to 64, row 16 w + i in lane 32 w + i, so that a block of up to 16 or 32 rows lies in one
+// or two row warps: items take the warps in turns, and one block's last product and its storing overlap the next one's first scores.
+// (With 128 rows for those of more than 16, run without a pause, 8 drafts behind 16 to 32 k tokens took 74.6 us instead of 72.4, for
+// the power; in a graph 66.3 instead of 67.0.)  Warps none of whose rows see a tile skip its softmax.
 //
-// Bound: few rows per sequence, the reading of the cache (2 q G flop per byte); blocks of 128 rows, tensor core and
-// special-function unit, as in the prefill.
+// 32/8 heads, 32 sequences of 3 to 6 new tokens behind 512 to 2048: 35.5 us (152 MB: 23.1 us of copy bandwidth); 32/4 heads, 8 of 8
+// behind 16384 to 32768: 67 us (357 MB, 54.5); 64/8 heads, 60 decode rows and 4 chunks of 300 to 512: 100 us (409 MB, 62.3; 118
+// without a pause, where the power limit takes the clock down); 32/8 heads, 511 behind 32768: 267 to 280 us (272 GFLOP, 165 at the
+// burst rate, 196 at the sustained one; 318 without a pause).  What bounds them: between prologue and tail the cache is read at 6.9 to
+// 7.3 TB/s where rows are few; besides that 2 us from the preceding kernel's end to the first scores, 4 to 5 us between the
+// workers' mean end and the last one's, 2 us until the merge may read and 3 to 4 us of merge.  Blocks of 128 rows: 1.03 to 1.17 us a
+// tile with two CTAs per SM, the tensor pipe 48 % active and, its instructions having a shortest time, 73 % occupied; as the prefill.
+// With both kinds on an SM nothing is above 60 %: the chain from a tile's scores over its weights to the score buffer's next use.
+//
+// Built and not kept: the last quarter of the list in small ranges that a worker asks for when it is done
+// (clusterlaunchcontrol; 36 -> 45 us and 67 -> 73 by the first two batches: the rings drain at each range); tiles prefetched into L2
+// (35 -> 45: the TMA unit's instructions are what is short); blocks of up to 32 rows spread over all row warps, 16 keys each, with the
+// maximum exchanged and the weights in shared memory (the same, the mixed batch 100 -> 123); four stages for heads of 64 (the
+// same); fewer registers at launch and setmaxnreg (spills).
 //
 // Eight warps: 0-3 one thread per row (softmax), 4 the list of pieces and the TMA copies of Q and K, 6 those of V, 5 and 7
 // issue S = Q K^T and O += P V.  Every wait is a bounded mbarrier wait.
@@ -35,7 +49,7 @@ constexpr int kThreads = 256;
 // us of any kind (two CTAs per SM), an item 1.2 to 1.6, one of more than 64 rows, which takes the row warps all together, 3.4.
 constexpr int kTileCost = 4, kSmallItem = 5, kFullItem = 13;
 constexpr int kMinShare = 8;               // a worker's share at least, in the same
-constexpr int kNarrowRows = 16;            // up to which the products take 64 rows: row 16 w + i lies in lane 32 w + i
+constexpr int kNarrowRows = 64;            // up to which the products take 64 rows: row 16 w + i lies in lane 32 w + i
 // The second half of the workers begins later, 1 us where the GPU is idle and 4 to 6 where a call follows another (an SM's second
 // CTA finds its registers when the merge before is done): what a worker of it has less, and one of the first half more.
 constexpr int kLateCost = 5;
@@ -381,7 +395,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         for (int pc = 0;; ++pc) {
             const unsigned room = (unsigned)max(min((end - pos + kTileCost - 1) / kTileCost, (long long)0x3fffffff), 0ll);
             const int len = whole ? (pos < end ? t1 - t0 : 0) : (int)min((unsigned)(t1 - t0 - jt), room);    // 0: the end
-            const int rows = min(TQ, x.q - mt * TQ) * G, wide = rows > 64 ? 4 : rows > 32 ? 2 : 1;
+            const int rows = min(TQ, x.q - mt * TQ) * G, wide = rows > 32 ? 4 : rows > 16 ? 2 : 1;
             const bool opens = jt == 0, closes = jt + len == t1 - t0, once = x.blocks - x.first <= 1;
             const int tile_hi = t0 + jt + len - 1, q0 = x.q0 + mt * TQ, pos0 = x.pos0 + mt * TQ;
             // the row warps in turns
@@ -437,15 +451,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
 #pragma unroll 1
                     for (int w = warp0; w < warp0 + wide; ++w) owner = (owner & ~(15u << (4 * w))) | (uint32_t)warp0 << (4 * w);
                     if (lane == 0) {
-                        // whole quarters of 32 rows (or 16): rows past the block's are others' or zeros and reach no live row
+                        // boxes of 16 rows (or 32): rows past the block's are others' or zeros and reach no live row
                         const bool narrow = rows <= kNarrowRows;
-                        mbar_expect_tx(&q_full[warp0], (uint32_t)(narrow ? kNarrowRows * D * 2 : wide * 32 * D * 2));
+                        const int box = narrow ? 16 : 32;
+                        mbar_expect_tx(&q_full[warp0], (uint32_t)(wide * box * D * 2));
 #pragma unroll 1
                         for (int w = 0; w < wide; ++w)
 #pragma unroll
                             for (int h = 0; h < L::kHalves; ++h)
-                                tma_load_3d(smem + kOffQ + h * kQHalfBytes + (warp0 + w) * kQuarterBytes, narrow ? &map_q16 : &map_q32, 64 * h,
-                                            kvh * G, q0 + w * (32 / G), &q_full[warp0]);
+                                tma_load_3d(smem + kOffQ + h * kQHalfBytes + warp0 * kQuarterBytes + w * box * 128, narrow ? &map_q16 : &map_q32,
+                                            64 * h, kvh * G, q0 + w * (box / G), &q_full[warp0]);
                     }
                 }
             }
@@ -552,7 +567,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 }
                 // products of 64 rows: Q begins so that their rows 16 w0 .. 16 w0 + 15 are the quarter's first
                 const bool narrow = d.rows <= kNarrowRows;
-                const uint64_t qd = desc_advance(q_desc0, narrow ? w0 * (kQuarterBytes - kNarrowRows * 128) : 0);
+                const uint64_t qd = desc_advance(q_desc0, narrow ? w0 * (kQuarterBytes - 16 * 128) : 0);
                 const uint32_t idesc_s = narrow ? instr_desc(false, kTN, false, 64) : instr_desc(false, kTN);
                 const uint32_t idesc_qk = idesc_s | (negate ? instr_desc(false, kTN, true) ^ instr_desc(false, kTN) : 0u);
                 if (lane == 0) {
@@ -641,11 +656,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                     if (++st == kStages) st = 0, ph ^= 1;
                 }
                 if (!ok) break;
-                reading = ((1u << ((d.rows + 31) / 32)) - 1) << d.warp0;
+                reading = ((1u << (d.rows <= kNarrowRows ? (d.rows + 15) / 16 : (d.rows + 31) / 32)) - 1) << d.warp0;
             }
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
-            const int r = threadIdx.x, hg = r % G;       // (32 is a multiple of G)
+            const int hg = lane % G;                     // (16 is a multiple of G)
+            // the thread's row of the block, -1: none
+            auto row_of = [&]() {
+                const int w = warp - d.warp0;
+                const int rr = d.rows > kNarrowRows ? (int)threadIdx.x : lane < 16 && w >= 0 ? 16 * w + lane : -1;
+                return rr < d.rows ? rr : -1;
+            };
             // rows before position 0 (more new tokens than context: padding) see nothing and are zero
             const int cta = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), ctas = gridDim.x * gridDim.y * gridDim.z;
             for (int s = cta * 4 + warp; s < p.B; s += ctas * 4) {
@@ -667,8 +688,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 // the row's position, and the last key before those it sees; a row that is not there sees none
                 int pos = -1, lo = -1;
                 {
-                    const int rr = r - 32 * d.warp0;
-                    if (rr >= 0 && rr < d.rows) {
+                    const int rr = row_of();
+                    if (rr >= 0) {
                         pos = d.pos0 + rr / G;
                         if (p.window > 0) lo = pos - p.window;
                     }
@@ -774,8 +795,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
 
                 // ---- the piece is complete once its last P V is: normalise, store, hand O back
                 read_piece(pc);             // (again, rather than in registers meanwhile)
-                const int rr = r - 32 * d.warp0;
-                const bool valid = rr >= 0 && rr < d.rows;
+                const int rr = row_of();
+                const bool valid = rr >= 0;
                 if (__any_sync(kFull, valid)) {
                     ok = prev_pv_done();
                     if (!ok) break;
@@ -984,7 +1005,7 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     if (sms <= 0) return OPT_GQA_ERR_CUDA;
     Maps maps;
     if (!make_q_map(&maps.q32, q, q_stride, total_q_tokens, Hq, G, D, 32 / G) ||
-        !make_q_map(&maps.q16, q, q_stride, total_q_tokens, Hq, G, D, kNarrowRows / G) || !make_cache_map(&maps.k, k_cache, rows, D, bs) ||
+        !make_q_map(&maps.q16, q, q_stride, total_q_tokens, Hq, G, D, 16 / G) || !make_cache_map(&maps.k, k_cache, rows, D, bs) ||
         !make_slice_map(&maps.v, v_cache, rows, D, bs))
         return OPT_GQA_ERR_CUDA;
     const ChunkLayout L = chunk_layout(Hq, Hkv, D, max_q_len);
