@@ -25,11 +25,11 @@
 // tile with two CTAs per SM, the tensor pipe 48 % active and, its instructions having a shortest time, 73 % occupied; as the prefill.
 // With both kinds on an SM nothing is above 60 %: the chain from a tile's scores over its weights to the score buffer's next use.
 //
-// Built and not kept: the last quarter of the list in small ranges that a worker asks for when it is done
-// (clusterlaunchcontrol; 36 -> 45 us and 67 -> 73 by the first two batches: the rings drain at each range); tiles prefetched into L2
-// (35 -> 45: the TMA unit's instructions are what is short); blocks of up to 32 rows spread over all row warps, 16 keys each, with the
-// maximum exchanged and the weights in shared memory (the same, the mixed batch 100 -> 123); four stages for heads of 64 (the
-// same); fewer registers at launch and setmaxnreg (spills).
+// Built and not kept (the first two batches above, as the kernel then was): the last quarter of the list in small ranges that a worker
+// asks for when it is done (clusterlaunchcontrol; 41 -> 53 us and 67 -> 79: the rings drain at each range); tiles prefetched into L2 (41
+// -> 45 to 52, 67 -> 70 to 85: the TMA unit's instructions are what is short); blocks of up to 32 rows spread over all row warps, 16 keys
+// each, with the maximum exchanged and the weights in shared memory (the same; the mixed batch 99 -> 123); four stages for heads of
+// 64 (the same); fewer registers at launch and setmaxnreg (ptxas spilled 2.4 KB).
 //
 // Eight warps: 0-3 one thread per row (softmax), 4 the list of pieces and the TMA copies of Q and K, 6 those of V, 5 and 7
 // issue S = Q K^T and O += P V.  Every wait is a bounded mbarrier wait.
