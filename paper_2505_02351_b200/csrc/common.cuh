@@ -386,10 +386,10 @@ struct PageRequests {
     int n;
 };
 // Workspace of the page calls.  Per request: pages asked (-1: void), the table entry they begin at, rows of a part-full page to
-// copy, from which page to which, pages asked before it (in its CTA's share of the list); and the free pages to hand out.  The
-// compaction keeps the pages it moves (from, to, count) in src, dst and rows, and how many in first[0].
+// copy, from which page to which, table entries to let go, pages asked before it (in its CTA's share of the list); and the free
+// pages to hand out.  The compaction keeps the pages it moves (from, to, count) in src, dst and rows, and how many in first[0].
 struct PageWork {
-    int *need, *first, *rows, *src, *dst, *free_list;
+    int *need, *first, *from, *to, *rows, *src, *dst, *free_list;
     long long* before;
 };
 inline size_t page_work_layout(int n, int num_blocks, char* base, PageWork* w) {
@@ -404,6 +404,8 @@ inline size_t page_work_layout(int n, int num_blocks, char* base, PageWork* w) {
     l.before = reinterpret_cast<long long*>(take((size_t)(n > 0 ? n : 1) * 8));
     l.need = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
     l.first = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
+    l.from = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
+    l.to = reinterpret_cast<int*>(take((size_t)(n > 0 ? n : 1) * 4));
     l.rows = reinterpret_cast<int*>(take(requests * 4));
     l.src = reinterpret_cast<int*>(take(requests * 4));
     l.dst = reinterpret_cast<int*>(take(requests * 4));

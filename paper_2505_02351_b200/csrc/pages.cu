@@ -164,11 +164,6 @@ __device__ __forceinline__ int fork_row(const PageTables& t, const PageRequests&
     const int parent = r.a[i], child = r.b[i];
     return (unsigned)parent < (unsigned)t.rows && (unsigned)child < (unsigned)t.rows ? child : -1;
 }
-__device__ __forceinline__ int resize_row(const PageTables& t, const PageRequests& r, int i) {
-    const int row = r.a[i], tokens = r.b[i];
-    return (unsigned)row < (unsigned)t.rows && tokens >= 0 && tokens <= (long long)t.width * t.bs ? row : -1;
-}
-
 // What the children held is dropped (the whole grid: a warp per 128 entries of a table's row).
 __global__ void __launch_bounds__(256) fork_drop_kernel(const PageTables t, const PageRequests r) {
     grid_dependency_launch();
@@ -255,121 +250,165 @@ __device__ __forceinline__ Slice slice_of(int num_blocks, int rank) {
     return {(int)min(b, (long long)num_blocks), (int)min(e, (long long)num_blocks)};
 }
 
-// The cluster: what is asked and what is free is counted, the free pages that are handed out are listed, and every request that
-// can be served is.  Request i is served where its own pages and those asked before it are there.
+// The cluster: what the requests let go is dropped, what they ask for and what is free is counted, the free pages that are handed
+// out are listed, and every request that can be served is: where its own pages and those asked before it are there.  Each CTA has a
+// share of the requests, in the order of the list, and a slice of the pool.  A round trip to L2 is 0.7 us, so what does not depend on
+// one another is loaded together, and what a request needs later stays in shared memory (of up to kTold requests per CTA).
+constexpr int kTold = kClusterThreads;
+constexpr int kListed = 1024;               // free pages listed in shared memory, by one CTA
+
+// What is known of the requests of a CTA's share.
+struct Told {
+    int need[kTold];        // pages asked, -1: void
+    int first[kTold];       // the table entry they begin at
+    int rows[kTold];        // rows of a part-full page to copy
+    int src[kTold];         // from which page
+    int from[kTold];        // table entries to let go: from .. to - 1
+    int to[kTold];
+    long long before[kTold];        // pages asked before it in the share
+};
+
 template <bool kFork, int kCtas>
 __global__ void __launch_bounds__(kClusterThreads)
 give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bool drops) {
-    constexpr int kAll = kCtas * kClusterThreads;
+    extern __shared__ __align__(128) char smem[];
     __shared__ long long scratch[33];
     __shared__ long long all_need[kCtas], all_free[kCtas];
+    __shared__ int listed[kListed];
     const int rank = cta_rank<kCtas>(), tid = threadIdx.x;
     grid_dependency_launch();
     grid_dependency_wait();
-    // 2^k threads for one request, of the whole cluster
+    const int share = (r.n + kCtas - 1) / kCtas, mine = min(share * rank, r.n), count = min(share, r.n - mine);
+    // in shared memory, or in the workspace where there are more
+    Told& told = *reinterpret_cast<Told*>(smem);
+    const bool few = share <= kTold;
+    int* const need_of = few ? told.need : w.need + mine;
+    int* const first_of = few ? told.first : w.first + mine;
+    int* const rows_of = few ? told.rows : w.rows + mine;
+    int* const src_of = few ? told.src : w.src + mine;
+    int* const from_of = few ? told.from : w.from + mine;
+    int* const to_of = few ? told.to : w.to + mine;
+    long long* const before_of = few ? told.before : w.before + mine;
+    // 2^k threads of the CTA for one request
     int lanes = 1;
-    while (lanes < kAll && (long long)r.n * (lanes * 2) <= kAll) lanes *= 2;
-    const int group = (rank * kClusterThreads + tid) / lanes, sub = (rank * kClusterThreads + tid) % lanes, groups = kAll / lanes;
+    while (lanes < kClusterThreads && (long long)share * (lanes * 2) <= kClusterThreads) lanes *= 2;
+    const int group = tid / lanes, sub = tid % lanes, groups = kClusterThreads / lanes;
 
-    if (drops) {
-        for (int i = group; i < r.n; i += groups) {
-            const int row = kFork ? fork_row(t, r, i) : resize_row(t, r, i);
-            if (row < 0) continue;
-            drop_pages(t, row, kFork ? 0 : pages_of(r.b[i], t), pages_of(t.lens[row], t), sub, lanes);
-        }
-        sync_all<kCtas>();
-    }
-
-    // what is asked, request by request in the order of the list: a share of the list per CTA
-    const int share = (r.n + kCtas - 1) / kCtas;
-    const int mine = min(share * rank, r.n), mine_end = min(share * (rank + 1), r.n);
-    long long asked = 0;
-    for (int base = mine; base < mine_end; base += kClusterThreads) {
-        const int i = base + tid;
-        int need = 0, first = 0, rows = 0, last = -1;
-        if (i < mine_end) {
-            const int row = kFork ? fork_row(t, r, i) : resize_row(t, r, i);
-            if (row < 0) {
-                need = -1;
-            } else if (kFork) {
-                const int n = min(max(t.lens[r.a[i]], 0), t.width * t.bs);
+    for (int i = tid; i < count; i += kClusterThreads) {
+        const int a = r.a[mine + i], b = r.b[mine + i];
+        const bool real = (unsigned)a < (unsigned)t.rows && (kFork ? (unsigned)b < (unsigned)t.rows : b >= 0 && b <= (long long)t.width * t.bs);
+        int need = -1, first = 0, rows = 0, from = 0, to = 0;
+        if (real) {
+            const int tokens = t.lens[a], have = pages_of(tokens, t);
+            if (kFork) {
+                const int n = min(max(tokens, 0), t.width * t.bs);
                 first = n / t.bs;
                 rows = n % t.bs;
                 need = rows != 0;
-                if (rows) last = ld_cg(t.tables + (size_t)r.a[i] * t.width + first);
+                to = pages_of(t.lens[b], t);
             } else {
-                const int n = t.lens[row], want = pages_of(r.b[i], t);
-                first = pages_of(n, t);
-                if (r.b[i] > n) {
-                    need = want - first;
-                    // a part-full last page that another sequence holds too is replaced before this one writes into it
-                    if (n > 0 && n % t.bs != 0 && first > 0) {
-                        last = ld_cg(t.tables + (size_t)row * t.width + first - 1);
-                        if (in_pool(last, t.num_blocks) && ld_cg(t.refs + last) > 1) {
-                            rows = n % t.bs;
-                            --first;
-                            ++need;
-                        }
-                    }
+                const int want = pages_of(b, t);
+                first = have;
+                need = max(want - have, 0);
+                from = want;
+                to = have;
+                if (b > tokens && tokens > 0 && have > 0) rows = tokens % t.bs;     // (whether they are copied is seen below)
+            }
+        }
+        need_of[i] = need;
+        first_of[i] = first;
+        rows_of[i] = rows;
+        from_of[i] = from;
+        to_of[i] = drops ? to : from;
+    }
+    __syncthreads();
+    // the pages that may be copied from (parents and sequences that grow drop nothing), requested beside what is dropped
+    for (int i = tid; i < count; i += kClusterThreads) {
+        int last = -1;
+        if (rows_of[i] > 0) last = t.tables[(size_t)r.a[mine + i] * t.width + (kFork ? first_of[i] : first_of[i] - 1)];
+        src_of[i] = last;
+    }
+    for (int i = group; i < count; i += groups)
+        if (from_of[i] < to_of[i]) drop_pages(t, kFork ? r.b[mine + i] : r.a[mine + i], from_of[i], to_of[i], sub, lanes);
+    if (drops) sync_all<kCtas>();
+    else __syncthreads();
+
+    // what is free: of the slice's first pages, which is mostly all of it, the counts are kept
+    const Slice s = slice_of<kCtas>(t.num_blocks, rank);
+    const bool one_tile = s.end - s.begin <= 4 * kClusterThreads;
+    int4 v = make_int4(1, 1, 1, 1);
+    if (s.begin + 4 * tid < s.end) v = four_counts(t.refs, s.begin + 4 * tid, t.num_blocks);
+    // what is asked, request by request
+    long long asked = 0;
+    for (int base = 0; base < count; base += kClusterThreads) {
+        const int i = base + tid;
+        int need = 0;
+        if (i < count) {
+            need = need_of[i];
+            // a part-full last page that another sequence holds too is replaced before this one writes into it
+            if (!kFork && rows_of[i] > 0) {
+                const int last = src_of[i];
+                if (in_pool(last, t.num_blocks) && ld_cg(t.refs + last) > 1) {
+                    need_of[i] = ++need;
+                    --first_of[i];
+                } else {
+                    rows_of[i] = 0;
                 }
             }
         }
         long long total;
         const long long before = block_scan(max(need, 0), scratch, total);
-        if (i < mine_end) {
-            w.need[i] = need;
-            w.first[i] = first;
-            w.rows[i] = rows;
-            w.src[i] = last;
-            w.before[i] = asked + before;
-        }
+        if (i < count) before_of[i] = asked + before;
         asked += total;
     }
-    // what is free
-    const Slice s = slice_of<kCtas>(t.num_blocks, rank);
-    long long zeros = 0;
-    for (int at = s.begin + 4 * tid; at < s.end; at += 4 * kClusterThreads) {
-        const int4 v = four_counts(t.refs, at, t.num_blocks);
-        zeros += (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0);
+    long long zeros = (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0), here;
+    for (int at = s.begin + 4 * (tid + kClusterThreads); at < s.end; at += 4 * kClusterThreads) {
+        const int4 u = four_counts(t.refs, at, t.num_blocks);
+        zeros += (u.x == 0) + (u.y == 0) + (u.z == 0) + (u.w == 0);
     }
-    long long here;
-    block_scan(zeros, scratch, here);
+    const long long zeros_before = block_scan(zeros, scratch, here);        // (in the order of the pages where there is one tile)
     tell_all<kCtas>(all_need, rank, asked);
     tell_all<kCtas>(all_free, rank, here);
     sync_all<kCtas>();
-    long long total_need = 0, total_free = 0, rank_free = 0;
+    long long total_need = 0, total_free = 0, rank_need = 0, rank_free = 0;
     for (int c = 0; c < kCtas; ++c) {
-        if (c == rank) rank_free = total_free;
+        if (c == rank) rank_need = total_need, rank_free = total_free;
         total_need += all_need[c];
         total_free += all_free[c];
     }
     // the list of the pages to hand out
+    const bool near = kCtas == 1 && total_need <= kListed;
+    int* const list = near ? listed : w.free_list;
     for (int base = s.begin; base < s.end && rank_free < total_need; base += 4 * kClusterThreads) {
         const int at = base + 4 * tid;
-        int4 v = make_int4(1, 1, 1, 1);
-        if (at < s.end) v = four_counts(t.refs, at, t.num_blocks);
-        long long total;
-        long long k = rank_free + block_scan((v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0), scratch, total);
-        if (v.x == 0 && k++ < total_need) w.free_list[k - 1] = at;
-        if (v.y == 0 && k++ < total_need) w.free_list[k - 1] = at + 1;
-        if (v.z == 0 && k++ < total_need) w.free_list[k - 1] = at + 2;
-        if (v.w == 0 && k++ < total_need) w.free_list[k - 1] = at + 3;
+        long long k = zeros_before, total = here;
+        if (!one_tile) {
+            v = make_int4(1, 1, 1, 1);
+            if (at < s.end) v = four_counts(t.refs, at, t.num_blocks);
+            k = block_scan((v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0), scratch, total);
+        }
+        k += rank_free;
+        if (v.x == 0 && k++ < total_need) list[k - 1] = at;
+        if (v.y == 0 && k++ < total_need) list[k - 1] = at + 1;
+        if (v.z == 0 && k++ < total_need) list[k - 1] = at + 2;
+        if (v.w == 0 && k++ < total_need) list[k - 1] = at + 3;
         rank_free += total;
     }
-    sync_all<kCtas>();
+    if constexpr (kCtas > 1) sync_all<kCtas>();
+    else __syncthreads();               // (one CTA reads its own list)
 
-    for (int i = group; i < r.n; i += groups) {
-        const int need = ld_cg(w.need + i), rows = ld_cg(w.rows + i);
-        long long from = __ldcg(w.before + i);
-        for (int c = 0; c < i / share; ++c) from += all_need[c];
+    for (int i = group; i < count; i += groups) {
+        const int need = need_of[i], rows = rows_of[i], a = r.a[mine + i], b = r.b[mine + i];
+        const long long from = rank_need + before_of[i];
         const bool served = need >= 0 && (need == 0 || from + need <= total_free);
+        auto page_at = [&](long long k) { return near || kCtas == 1 ? list[from + k] : ld_cg(w.free_list + from + k); };
         if (served && need > 0) {
-            const int first = ld_cg(w.first + i);
-            int* entry = t.tables + (size_t)(kFork ? r.b[i] : r.a[i]) * t.width;
+            const int first = first_of[i];
+            int* entry = t.tables + (size_t)(kFork ? b : a) * t.width;
             for (long long k = sub; k < need; k += 4ll * lanes) {
                 int page[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) page[u] = k + (long long)u * lanes < need ? ld_cg(w.free_list + from + k + (long long)u * lanes) : -1;
+                for (int u = 0; u < 4; ++u) page[u] = k + (long long)u * lanes < need ? page_at(k + (long long)u * lanes) : -1;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                     if (page[u] < 0) break;
@@ -379,13 +418,17 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
             }
         }
         if (sub == 0) {
-            if (!kFork && served && rows > 0) atomicSub(t.refs + ld_cg(w.src + i), 1);
-            w.dst[i] = served && rows > 0 ? ld_cg(w.free_list + from) : -1;
-            r.done[i] = served;
+            const int src = src_of[i];
+            const bool copies = served && rows > 0;
+            if (!kFork && copies) atomicSub(t.refs + src, 1);
+            w.rows[mine + i] = copies ? rows : 0;
+            w.src[mine + i] = src;
+            w.dst[mine + i] = copies ? page_at(0) : -1;
+            r.done[mine + i] = served;
             if (kFork) {
-                if (need >= 0) t.lens[r.b[i]] = served ? t.lens[r.a[i]] : 0;
+                if (need >= 0) t.lens[b] = served ? t.lens[a] : 0;
             } else if (served) {
-                t.lens[r.a[i]] = r.b[i];
+                t.lens[a] = b;
             }
         }
     }
@@ -441,9 +484,13 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
     grid_dependency_launch();
     grid_dependency_wait();
     const Slice s = slice_of<kCtas>(num_blocks, rank);
+    // of the slice's first pages, which is mostly all of it, the counts are kept
+    int4 kept = make_int4(0, 0, 0, 0);
+    if (s.begin + 4 * tid < s.end) kept = four_counts(refs, s.begin + 4 * tid, num_blocks);
+    auto counts = [&](int at) { return at < s.begin + 4 * kClusterThreads ? kept : four_counts(refs, at, num_blocks); };
     long long count = 0, here;
     for (int at = s.begin + 4 * tid; at < s.end; at += 4 * kClusterThreads) {
-        const int4 v = four_counts(refs, at, num_blocks);
+        const int4 v = counts(at);
         const int live = min(4, num_blocks - at);       // past the end reads as in use
         count += (v.x > 0) + (v.y > 0) + (v.z > 0) + (v.w > 0) - (4 - live);
     }
@@ -458,7 +505,7 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
     // pages in use below U: the holes and the movers are as many, U less those
     count = 0;
     for (int at = s.begin + 4 * tid; at < s.end && at < U; at += 4 * kClusterThreads) {
-        const int4 v = four_counts(refs, at, num_blocks);
+        const int4 v = counts(at);
         count += (at < U && v.x > 0) + (at + 1 < U && v.y > 0) + (at + 2 < U && v.z > 0) + (at + 3 < U && v.w > 0);
     }
     block_scan(count, scratch, here);
@@ -470,7 +517,7 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
         const int at = base + 4 * tid;
         int ref[4] = {0, 0, 0, 0};
         if (at < s.end) {
-            const int4 v = four_counts(refs, at, num_blocks);
+            const int4 v = counts(at);
             ref[0] = v.x, ref[1] = v.y, ref[2] = v.z, ref[3] = v.w;
         }
         int live = 0;
@@ -548,10 +595,11 @@ int launch_copying(void (*kernel)(KArgs...), unsigned ctas, std::atomic<bool>* c
 
 // launch_dependent for a cluster, or one CTA alone.
 template <typename... KArgs, typename... Args>
-int launch_cluster(void (*kernel)(KArgs...), int ctas, cudaStream_t stream, Args... args) {
+int launch_cluster(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t stream, Args... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kClusterThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -592,8 +640,8 @@ int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, 
         if (rc != OPT_GQA_OK) return rc;
     }
     rc = t.num_blocks <= kOneCtaPages && entries <= kOneCtaEntries
-             ? launch_cluster(give_pages_kernel<true, 1>, 1, stream, t, r, w, drops)
-             : launch_cluster(give_pages_kernel<true, kClusterCtas>, kClusterCtas, stream, t, r, w, drops);
+             ? launch_cluster(give_pages_kernel<true, 1>, 1, sizeof(Told), stream, t, r, w, drops)
+             : launch_cluster(give_pages_kernel<true, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, drops);
     if (rc != OPT_GQA_OK) return rc;
     const int chunks = (t.width + 127) / 128;
     return launch_copying(fork_share_kernel, copy_ctas(sh, r.n, (long long)r.n * chunks), configured, stream, pools, sh, t, r, w, chunks, status);
@@ -604,8 +652,8 @@ int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
     const int rc = t.num_blocks <= kOneCtaPages && (long long)r.n * t.width <= kOneCtaEntries
-                       ? launch_cluster(give_pages_kernel<false, 1>, 1, stream, t, r, w, true)
-                       : launch_cluster(give_pages_kernel<false, kClusterCtas>, kClusterCtas, stream, t, r, w, true);
+                       ? launch_cluster(give_pages_kernel<false, 1>, 1, sizeof(Told), stream, t, r, w, true)
+                       : launch_cluster(give_pages_kernel<false, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, true);
     if (rc != OPT_GQA_OK) return rc;
     return launch_copying(copy_pages_kernel<true>, copy_ctas(sh, r.n), configured, stream, pools, sh, w.src, w.dst, w.rows, r.n, status);
 }
@@ -615,8 +663,8 @@ int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& 
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
     const int rc = t.num_blocks <= kOneCtaPages
-                       ? launch_cluster(compact_plan_kernel<1>, 1, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
-                       : launch_cluster(compact_plan_kernel<kClusterCtas>, kClusterCtas, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
+                       ? launch_cluster(compact_plan_kernel<1>, 1, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
+                       : launch_cluster(compact_plan_kernel<kClusterCtas>, kClusterCtas, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
     if (rc != OPT_GQA_OK) return rc;
     return launch_copying(compact_move_kernel, copy_ctas(sh, t.num_blocks / 2 + 1, (long long)t.rows * t.width / 32), configured, stream, pools,
                           sh, t.tables, tables_out, t.lens, page_map, w, t.rows, t.width, t.bs, status);

@@ -25,9 +25,9 @@ POOLS = addresses(256, 512)
 
 def test_workspace_grows_with_requests_and_pages(lib):
     f = binding.pages_workspace_bytes
-    # per request five words and a 64-bit one, per page one word and, of half the pages, three
-    assert 65535 * 28 + 4 * 1000 <= f(65535, 1000) <= 65535 * 28 + 4 * 1000 + 8 * 256
-    assert 4 * 100000 + 3 * 4 * 50000 <= f(1, 100000) <= 4 * 100000 + 3 * 4 * 50001 + 28 + 8 * 256
+    # per request seven words and a 64-bit one, per page one word and, of half the pages, three
+    assert 65535 * 36 + 4 * 1000 <= f(65535, 1000) <= 65535 * 36 + 4 * 1000 + 10 * 256
+    assert 4 * 100000 + 3 * 4 * 50000 <= f(1, 100000) <= 4 * 100000 + 3 * 4 * 50001 + 36 + 10 * 256
     sizes = [f(n, b) for n, b in ((1, 1), (1, 10), (9, 10), (9, 5000), (300, 5000), (3000, 5000), (3000, 1 << 28))]
     assert sizes == sorted(sizes) and sizes[0] > 0
     for bad in ((0, 10), (-1, 10), (65536, 10), (1, 0), (1, -5), (1, (1 << 28) + 1)):
