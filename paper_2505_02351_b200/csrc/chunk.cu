@@ -124,9 +124,10 @@ __device__ __forceinline__ Seq sequence(const ChunkParams& p, int s) {
     Seq x;
     // (inside the rows and the promised length, whatever the arrays hold)
     x.q0 = min(max(__ldg(p.q_start_loc + s), 0), p.total_q);
-    x.q = min(max(min(__ldg(p.q_start_loc + s + 1), p.total_q) - x.q0, 0), p.max_q);
+    const int q = max(min(__ldg(p.q_start_loc + s + 1), p.total_q) - x.q0, 0);
+    x.q = min(q, p.max_q);
     x.n = max(__ldg(p.context_lens + s), 0);
-    x.pos0 = x.n - x.q;
+    x.pos0 = x.n - q;
     x.blocks = x.n > 0 ? (x.q + TQ - 1) / TQ : 0;
     x.first = x.pos0 < 0 ? min(-x.pos0 / TQ, x.blocks) : 0;
     return x;
