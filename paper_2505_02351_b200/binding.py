@@ -355,7 +355,7 @@ def _rows(name: str, t: torch.Tensor, shape, dtype, device: int):
 
 
 def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
-    if t.dtype != dtype or (n >= 0 and t.numel() != n) or t.get_device() != device or not t.is_contiguous():
+    if t.dtype is not dtype or (n >= 0 and t.numel() != n) or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name}: expected {'any number of' if n < 0 else n} contiguous {dtype} values on the current "
                          "CUDA device")
     return t.data_ptr()
@@ -449,22 +449,21 @@ def chunk_workspace_bytes(Hq: int, Hkv: int, D: int, max_q_len: int) -> int:
 def paged_attention_chunk(out, q, q_start_loc, max_q_len: int, k_cache, v_cache, block_tables, context_lens, alibi_slopes,
                           scale: float, workspace, window: int = 0, stream=None) -> None:
     """Causal attention of any mix of new tokens per sequence over the paged cache; q may be a slice of wider rows."""
-    shape, pool, dtype, dev = q.shape, k_cache.shape, q.dtype, _current_device(q)
+    shape, pool, dtype, dev, i32 = q.shape, k_cache.shape, q.dtype, _current_device(q), torch.int32
     T, Hq, D = shape
-    num_blocks, Hkv, bs, _ = pool
-    B = context_lens.numel()
-    if out.shape != shape or pool != (num_blocks, Hkv, bs, D) or v_cache.shape != pool:
+    num_blocks, Hkv, bs, dims = pool
+    rows, width = block_tables.shape if block_tables.dim() == 2 else (-1, 0)
+    if dims != D or out.shape != shape or v_cache.shape != pool:
         raise ValueError("expected out like q and k_cache, v_cache [blocks, heads, block size, dims of q]")
-    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+    if rows != context_lens.numel():
         raise ValueError("block_tables: expected a row per sequence")
     qp, qs = _rows("q", q, shape, dtype, dev)
     _check(load().opt_gqa_paged_attention_chunk(
-        _index("out", out, dtype, -1, dev), qp, qs, _index("q_start_loc", q_start_loc, torch.int32, B + 1, dev), T, max_q_len,
+        _index("out", out, dtype, -1, dev), qp, qs, _index("q_start_loc", q_start_loc, i32, rows + 1, dev), T, max_q_len,
         _index("k_cache", k_cache, dtype, -1, dev), _index("v_cache", v_cache, dtype, -1, dev),
-        _index("block_tables", block_tables, torch.int32, -1, dev), block_tables.shape[1],
-        _index("context_lens", context_lens, torch.int32, B, dev),
-        None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, B, Hq, Hkv, D, bs,
-        num_blocks, window, _ptr(workspace), _nbytes(workspace), _DTYPE_CODE[dtype], _stream(stream, dev)),
+        _index("block_tables", block_tables, i32, -1, dev), width, _index("context_lens", context_lens, i32, -1, dev),
+        None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, rows, Hq, Hkv, D,
+        bs, num_blocks, window, _ptr(workspace), _nbytes(workspace), _DTYPE_CODE[dtype], _stream(stream, dev)),
         "opt_gqa_paged_attention_chunk")
 
 
@@ -524,12 +523,11 @@ def cache_copy_pages(pools: PagePools, src_pages, dst_pages, stream=None) -> Non
 
 
 def _pages(entry: str, pools, block_tables, context_lens, ref_counts, a, b, done, workspace, stream) -> None:
-    dev, n = _pools_device(pools), a.numel()
+    dev, n, i32 = _pools_device(pools), a.numel(), torch.int32
     bt, S, W, lens = _table(block_tables, context_lens, dev)
     _check(getattr(load(), entry)(
-        pools.address, pools.count, bt, W, lens, _index("ref_counts", ref_counts, torch.int32, pools.num_blocks, dev),
-        _index("requests", a, torch.int32, n, dev), _index("requests", b, torch.int32, n, dev), n,
-        _index("done", done, torch.int32, n, dev), S, pools.Hkv, pools.D, pools.bs, pools.num_blocks, _ptr(workspace),
+        pools.address, pools.count, bt, W, lens, _index("ref_counts", ref_counts, i32, pools.num_blocks, dev),
+        _index("requests", a, i32, -1, dev), _index("requests", b, i32, n, dev), n, _index("done", done, i32, n, dev), S, pools.Hkv, pools.D, pools.bs, pools.num_blocks, _ptr(workspace),
         _nbytes(workspace), pools.code, _stream(stream, dev)), entry)
 
 

@@ -1005,9 +1005,11 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     const int G = Hq / Hkv, sms = sm_count();
     if (sms <= 0) return OPT_GQA_ERR_CUDA;
     Maps maps;
-    if (!make_q_map(&maps.q32, q, q_stride, total_q_tokens, Hq, G, D, 32 / G) ||
-        !make_q_map(&maps.q16, q, q_stride, total_q_tokens, Hq, G, D, 16 / G) || !make_cache_map(&maps.k, k_cache, rows, D, bs) ||
+    if (!make_q_map(&maps.q16, q, q_stride, total_q_tokens, Hq, G, D, 16 / G) || !make_cache_map(&maps.k, k_cache, rows, D, bs) ||
         !make_slice_map(&maps.v, v_cache, rows, D, bs))
+        return OPT_GQA_ERR_CUDA;
+    maps.q32 = maps.q16;                // blocks of more than kNarrowRows take boxes of 32 rows
+    if ((long long)max_q_len * G > kNarrowRows && !make_q_map(&maps.q32, q, q_stride, total_q_tokens, Hq, G, D, 32 / G))
         return OPT_GQA_ERR_CUDA;
     const ChunkLayout L = chunk_layout(Hq, Hkv, D, max_q_len);
     char* ws = static_cast<char*>(workspace);
