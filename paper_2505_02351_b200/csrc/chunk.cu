@@ -59,8 +59,6 @@ constexpr int kLateCost = 5;
 // items of 9 and 16 tiles 16.3 and 21.9 against 20.5 and 23.9, 256 of 9 and 24 19.6 and 37.0 against 25.7 and 42.1, 32 of 7 and 9
 // 13.3 and 14.9 against 13.7 and 13.0, 72 of 128 rows and 9 and 11 tiles 17.2 and 19.0 against 21.2 and 21.6.)
 constexpr int kCutCost = 28, kCutCostFull = 36;
-// A CTA for each item, and no list, where they are one wave of at most kDirectTiles + items / kDirectItems tiles each.
-constexpr int kDirectTiles = 8, kDirectItems = 16;
 constexpr int kDescs = 4;                  // pieces described ahead
 constexpr int kDescBytes = 64;
 constexpr int kOpens = 1, kContinues = 2, kCloses = 4;      // a worker's flags: see ChunkLayout
@@ -973,6 +971,25 @@ struct Maps {
     CUtensorMap q32, q16, k, v;
 };
 
+// Whether every item gets a CTA of its own: no list and nothing to merge, but the longest item's time, or one wave of CTAs after the
+// other.  items and tiles (of the longest) are what the host can bound them by; wide: blocks of more than 64 rows.
+//
+// In a graph, us, a CTA each against the list that is cut.  One wave: 32 items of 4, 7, 10, 11 and 16 tiles 7.7 10.1 12.6 13.4 17.4 against
+// 12.8 13.3 12.7 12.8 15.1; 64 of 11, 13 and 16, wide, 17.6 19.5 22.6 against 20.1 20.8 21.7; 128 of 13, 16 and 24 16.7 19.3 26.3 against
+// 22.1 23.4 27.2; 256 of 16 and 24 23.9 33.0 against 32.4 41.5: worth it up to 8 tiles and one more per 16 items.  More waves: 320
+// items of 2, 4, 8 and 16 tiles 13.1 17.0 24.8 41.7 against 17.6 21.2 26.9 37.1; 448 14.6 18.2 26.9 45.0 against 17.6 25.3 32.5 46.9; 600 20.0
+// 25.9 38.0 65.3 against 21.0 28.4 37.5 58.3; 896 of 1, 2 and 4 23.4 26.9 34.8 against 17.4 26.1 34.6; 448 wide of 2, 4, 8 and 16 19.0 23.2 32.9
+// 52.9 against 24.2 33.5 41.9 59.3.  There it goes by estimates of both, in us: a wave 6 and 1.06 a tile (wide 8.3 and 1.2), the list 17 (12
+// where nothing can be cut) and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25).  A last wave that is not full counts 0.8.
+bool prefers_direct(long long items, long long wave, long long tiles, bool wide) {
+    if (items <= wave) return tiles <= 8 + items / 16;
+    if (items > 4 * wave) return false;
+    const double waves = (double)(items / wave) + (items % wave ? 0.8 : 0.0), share = (double)items / (double)wave, t = (double)tiles;
+    const double direct = waves * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
+    const double list = (tiles > 1 ? 17.0 : 12.0) + share * (wide ? 3.4 + 1.25 * t : 1.2 + 1.06 * t);
+    return direct < list;
+}
+
 template <int D, int G>
 int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, dim3 grid, cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
@@ -1044,7 +1061,6 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     m.Hq = Hq;
     m.total_q = total_q_tokens;
     m.slot_rows = L.slot_rows;
-    // Few items of few tiles, as far as the host can bound them: a CTA each, no list, nothing to merge.
     const long long blocks = ((long long)max_q_len * G + kRows - 1) / kRows, items = blocks * Hkv * B;
     long long tiles = (long long)max_blocks_per_seq * bs / kTN + 1;
     if (window > 0) {
@@ -1052,10 +1068,7 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    // (In a graph, us, a CTA each against the list that is cut: 32 items of 4, 7, 10, 11 and 16 tiles 7.7 10.1 12.6 13.4 17.4 against
-    // 12.8 13.3 12.7 12.8 15.1; 64 of 11, 13 and 16 17.6 19.5 22.6 against 20.1 20.8 21.7; 128 of 13, 16 and 24 16.7 19.3 26.3 against
-    // 22.1 23.4 27.2; 256 of 16 and 24 23.9 33.0 against 32.4 41.5.)
-    p.direct = items <= wave && tiles <= kDirectTiles + items / kDirectItems;
+    p.direct = blocks <= 65535 && prefers_direct(items, wave, tiles, (long long)max_q_len * G > 64);
     dim3 grid((unsigned)blocks, (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.direct) {
