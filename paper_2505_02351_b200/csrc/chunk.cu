@@ -9,7 +9,7 @@
 // two per SM), so that one long context fills the GPU as well as a large ragged batch.  A range covers whole items, written
 // out at once, and at its two ends parts of items: normalised partial rows and log-sum-exps in the workspace, two places a worker,
 // merged by chunk_merge_kernel.  (The chunked prefill gives a block of rows to one CTA whatever the context: with few new tokens
-// most of the GPU is idle.)  Few items are not cut, and few items of few tiles need no list: see kCutCost and kDirectTiles.
+// most of the GPU is idle.)  Few items are not cut, and items of few tiles need no list: see kCutCost and prefers_direct.
 //
 // Products take 64 rows for blocks of up to 64, row 16 w + i in lane 32 w + i, so that a block of up to 16 or 32 rows lies in one
 // or two row warps: items take the warps in turns, and one block's last product and its storing overlap the next one's first scores.
@@ -184,7 +184,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
-    auto item_cost = [&](const Seq& x) { return x.q * G > 64 ? kFullItem : kSmallItem; };
+    auto item_cost = [&](const Seq& x) { return x.q * G > kNarrowRows ? kFullItem : kSmallItem; };
     auto seq_units = [&](const Seq& x, int& most) {
         long long sum = 0;
         for (int mt = x.first; mt < x.blocks; ++mt) {
@@ -370,7 +370,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             total *= p.Hkv;
             items *= p.Hkv;
             const int alone = 2 * items <= gridDim.x ? most - most / 5 : most;
-            whole = items <= gridDim.x && alone <= total / gridDim.x + (p.max_q > 64 / G ? kCutCostFull : kCutCost);
+            whole = items <= gridDim.x && alone <= total / gridDim.x + (p.max_q > kNarrowRows / G ? kCutCostFull : kCutCost);
             if (whole) total = items;
             if (total < 0x40000000) locate((int)total);
             else locate(total);
@@ -1068,7 +1068,7 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    p.direct = blocks <= 65535 && prefers_direct(items, wave, tiles, (long long)max_q_len * G > 64);
+    p.direct = blocks <= 65535 && prefers_direct(items, wave, tiles, (long long)max_q_len * G > kNarrowRows);
     dim3 grid((unsigned)blocks, (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.direct) {

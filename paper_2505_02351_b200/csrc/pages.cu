@@ -9,8 +9,8 @@
 //
 // Data moves by bulk copies through shared memory, a ring of slots per warp that its first lane fills and empties: 64 pages of 64
 // pools (264 MB read and written) 46 us, 5.7 TB/s, where loads and stores through registers took 51 to 52; the part-full page of a
-// 16383-token prompt for 128 samples (504 MB, the reads from L2) 64 us against 79 to 85; 129 of 512 pages compacted (528 MB) 97 to 98.
-// Rings of 8 or 16 KB slots and one or two CTAs per SM are within 3 % of that.  Few pages: 11 to 13 us for a call's two or three launches,
+// 16383-token prompt for 128 samples (504 MB, the reads from L2) 64 us against 79 to 85; 129 of 512 pages compacted (528 MB) 96.
+// Rings of 8 or 16 KB slots and one or two CTAs per SM are within 3 % of that.  Few pages: 8 to 12 us for a call's two or three launches,
 // a chain of dependent loads of tables and counts (about 0.7 us each) and barriers between.
 //
 #include <cooperative_groups.h>
@@ -612,12 +612,19 @@ int launch_cluster(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? OPT_GQA_OK : OPT_GQA_ERR_CUDA;
 }
 
-// Up to this many pages (two vectors of counts per thread) and entries of tables one CTA does what the cluster would: its barriers
-// take a tenth of the cluster's time.
-constexpr int kOneCtaPages = 8192;
-constexpr long long kOneCtaEntries = 16384;
-// Entries of the children's tables up to which the cluster drops them itself, without a launch of the whole GPU before it.
-constexpr long long kClusterDrop = 16384;
+// One CTA instead of the cluster, whose barriers and sums through distributed shared memory cost 1 us, where its threads have one vector
+// of counts each and there are no more than half as many requests.  (In a graph, us, one CTA against the cluster.  Steps that resize 32
+// sequences in pools of 512, 4096, 8192 and 32768 pages: 8.3 8.2 9.3 10.6 against 9.4 9.7 9.6 9.2; of 256 and 1024 in 4096: 9.1 and 11.1
+// against 9.7 and 10.9.)
+constexpr int kOneCtaPages = 4 * kClusterThreads, kOneCtaRequests = kClusterThreads / 2;
+bool one_cta(int num_blocks, int n) { return num_blocks <= kOneCtaPages && n <= kOneCtaRequests; }
+// The compaction goes over the counts again and again and writes as much: 512, 2048, 4096 and 8192 pages 7.3 8.9 10.4 13.7 against 7.9 8.6
+// 8.8 9.0.
+constexpr int kOneCtaCompact = 1024;
+// Entries of the children's tables up to which give_pages_kernel drops them itself, without a launch of the whole GPU before it.  (Forks
+// of a parent whose pages fill the tables, us, itself against with that launch: one CTA, 256, 4096, 8192 and 16384 entries 9.8 11.6 14.4
+// 15.4 against 10.3 11.4 12.0 11.9; the cluster, 2048, 16384, 32768 and 131072 entries 11.8 12.0 12.3 17.4 against 12.1 12.6 13.0 14.3.)
+constexpr long long kOneCtaDrop = 4096, kClusterDrop = 32768;
 
 }  // namespace
 
@@ -632,15 +639,14 @@ int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, 
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
     const long long entries = (long long)r.n * t.width;
-    const bool drops = entries <= kClusterDrop;
+    const bool one = one_cta(t.num_blocks, r.n), drops = entries <= (one ? kOneCtaDrop : kClusterDrop);
     int rc = OPT_GQA_OK;
     if (!drops) {
         const unsigned x = (unsigned)((t.width + 1023) / 1024);
         rc = launch_dependent(fork_drop_kernel, dim3(x < 64 ? x : 64, (unsigned)r.n), dim3(256), 0, stream, t, r);
         if (rc != OPT_GQA_OK) return rc;
     }
-    rc = t.num_blocks <= kOneCtaPages && entries <= kOneCtaEntries
-             ? launch_cluster(give_pages_kernel<true, 1>, 1, sizeof(Told), stream, t, r, w, drops)
+    rc = one ? launch_cluster(give_pages_kernel<true, 1>, 1, sizeof(Told), stream, t, r, w, drops)
              : launch_cluster(give_pages_kernel<true, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, drops);
     if (rc != OPT_GQA_OK) return rc;
     const int chunks = (t.width + 127) / 128;
@@ -651,7 +657,7 @@ int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t
                   cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    const int rc = t.num_blocks <= kOneCtaPages && (long long)r.n * t.width <= kOneCtaEntries
+    const int rc = one_cta(t.num_blocks, r.n)
                        ? launch_cluster(give_pages_kernel<false, 1>, 1, sizeof(Told), stream, t, r, w, true)
                        : launch_cluster(give_pages_kernel<false, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, true);
     if (rc != OPT_GQA_OK) return rc;
@@ -662,7 +668,7 @@ int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& 
                    const PageWork& w, int* status, cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
-    const int rc = t.num_blocks <= kOneCtaPages
+    const int rc = t.num_blocks <= kOneCtaCompact
                        ? launch_cluster(compact_plan_kernel<1>, 1, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
                        : launch_cluster(compact_plan_kernel<kClusterCtas>, kClusterCtas, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
     if (rc != OPT_GQA_OK) return rc;

@@ -267,6 +267,27 @@ def test_compact_leaves_the_old_tables_readable():
         assert torch.equal(p[before[0, :19].long()], o) and torch.equal(p[c.tables[0, :19].long()], o)
 
 
+@pytest.mark.parametrize("blocks", [4096, 4097])
+@pytest.mark.parametrize("n,wide", [(40, 64), (60, 68), (61, 68), (40, 900), (512, 8), (513, 8)])
+def test_fork_and_resize_on_both_sides_of_the_launches_choice(blocks, n, wide):
+    """One CTA or a cluster, the children's pages dropped by it or before it."""
+    rng = np.random.default_rng(n + wide)
+    c = Cache([16 * (wide - 2) + 9, 50] + [0] * n, blocks, wide=wide, Hkv=1, pools=1, seed=n)
+    for turn in range(2):                                          # the second time the children hold what they got before
+        c.call("fork", rng.integers(0, 2, size=n), 2 + rng.permutation(n))
+        c.consistent()
+    c.call("resize", 2 + rng.permutation(n), rng.integers(0, 16 * wide + 1, size=n))
+    c.consistent()
+
+
+@pytest.mark.parametrize("blocks", [1024, 1025, 4096, 4097])
+def test_compact_on_both_sides_of_the_launches_choice(blocks):
+    rng = np.random.default_rng(blocks)
+    c = Cache([int(x) for x in rng.integers(0, 16 * blocks // 64, size=80)], blocks, Hkv=1, pools=2, seed=blocks)
+    c.compact(True)
+    c.consistent()
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_a_run_of_steps(seed):
     """Forks, steps, ends and compactions in turn, each checked."""
