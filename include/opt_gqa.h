@@ -335,7 +335,8 @@ int opt_gqa_paged_attention_prefill_local(void* out, const void* q, const int32_
  * with one new token (decode rows), with a few (drafts to verify) and with many (a prompt's chunk); few new tokens behind
  * long contexts fill the GPU (the prefill gives a block of rows to one CTA).
  *
- *   out           [total_q_tokens, Hq, D]  bf16; rows no sequence has (behind q_start_loc[B], say) are left as they are
+ *   out           [total_q_tokens, Hq, D]  bf16; rows no sequence has (behind q_start_loc[B], say) are left as they are; overlaps
+ *                 no input
  *   q             bf16 rows of Hq * D values, q_stride (a HOST value, elements, a multiple of 8, >= Hq * D) from token to token,
  *                 so that q may be a slice of the fused projection's rows
  *   q_start_loc   [B+1] int32, total_q_tokens, max_q_len, block_tables, context_lens  as in opt_gqa_paged_attention_prefill: new

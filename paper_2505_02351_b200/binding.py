@@ -361,6 +361,15 @@ def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
     return t.data_ptr()
 
 
+def _scratch(t: Optional[torch.Tensor], device: int):
+    """(address, bytes) of a workspace."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor on the current CUDA device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _current_device(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor")
@@ -458,12 +467,13 @@ def paged_attention_chunk(out, q, q_start_loc, max_q_len: int, k_cache, v_cache,
     if rows != context_lens.numel():
         raise ValueError("block_tables: expected a row per sequence")
     qp, qs = _rows("q", q, shape, dtype, dev)
+    ws, wsb = _scratch(workspace, dev)
     _check(load().opt_gqa_paged_attention_chunk(
         _index("out", out, dtype, -1, dev), qp, qs, _index("q_start_loc", q_start_loc, i32, rows + 1, dev), T, max_q_len,
         _index("k_cache", k_cache, dtype, -1, dev), _index("v_cache", v_cache, dtype, -1, dev),
         _index("block_tables", block_tables, i32, -1, dev), width, _index("context_lens", context_lens, i32, -1, dev),
         None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, rows, Hq, Hkv, D,
-        bs, num_blocks, window, _ptr(workspace), _nbytes(workspace), _DTYPE_CODE[dtype], _stream(stream, dev)),
+        bs, num_blocks, window, ws, wsb, _DTYPE_CODE[dtype], _stream(stream, dev)),
         "opt_gqa_paged_attention_chunk")
 
 
@@ -525,10 +535,11 @@ def cache_copy_pages(pools: PagePools, src_pages, dst_pages, stream=None) -> Non
 def _pages(entry: str, pools, block_tables, context_lens, ref_counts, a, b, done, workspace, stream) -> None:
     dev, n, i32 = _pools_device(pools), a.numel(), torch.int32
     bt, S, W, lens = _table(block_tables, context_lens, dev)
+    ws, wsb = _scratch(workspace, dev)
     _check(getattr(load(), entry)(
         pools.address, pools.count, bt, W, lens, _index("ref_counts", ref_counts, i32, pools.num_blocks, dev),
-        _index("requests", a, i32, -1, dev), _index("requests", b, i32, n, dev), n, _index("done", done, i32, n, dev), S, pools.Hkv, pools.D, pools.bs, pools.num_blocks, _ptr(workspace),
-        _nbytes(workspace), pools.code, _stream(stream, dev)), entry)
+        _index("requests", a, i32, -1, dev), _index("requests", b, i32, n, dev), n, _index("done", done, i32, n, dev), S,
+        pools.Hkv, pools.D, pools.bs, pools.num_blocks, ws, wsb, pools.code, _stream(stream, dev)), entry)
 
 
 def cache_fork(pools: PagePools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream=None) -> None:
@@ -548,11 +559,12 @@ def cache_compact(pools: PagePools, block_tables, context_lens, ref_counts, bloc
     bt, S, W, lens = _table(block_tables, context_lens, dev)
     if block_tables_out.shape != block_tables.shape:
         raise ValueError("block_tables_out: expected the shape of block_tables")
+    ws, wsb = _scratch(workspace, dev)
     _check(load().opt_gqa_cache_compact(
         pools.address, pools.count, bt, _index("block_tables_out", block_tables_out, torch.int32, -1, dev), W, lens,
         _index("ref_counts", ref_counts, torch.int32, nb, dev), _index("ref_counts_out", ref_counts_out, torch.int32, nb, dev),
         _index("page_map", page_map, torch.int32, nb, dev), _index("used_out", used_out, torch.int32, 1, dev), S, pools.Hkv,
-        pools.D, pools.bs, nb, _ptr(workspace), _nbytes(workspace), pools.code, _stream(stream, dev)), "opt_gqa_cache_compact")
+        pools.D, pools.bs, nb, ws, wsb, pools.code, _stream(stream, dev)), "opt_gqa_cache_compact")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

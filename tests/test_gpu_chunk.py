@@ -375,3 +375,24 @@ def test_refusals_of_the_binding():
         with pytest.raises(binding.OptGqaError) as e:
             binding.paged_attention_chunk(**dict(good, **bad))
         assert e.value.code == code
+
+
+class Elsewhere:
+    """A workspace on another device, as the binding sees it."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return self.t.get_device() + 1
+
+
+def test_workspaces_of_another_device_or_with_gaps_are_refused():
+    b = Batch(8, 2, 64, 16, [2], [30])
+    for ws in (Elsewhere(b.workspace()), torch.empty(1 << 24, device=DEV)[::2], torch.empty(1 << 24)):
+        with pytest.raises(ValueError):
+            b.run(0.125, ws=ws)
+    b.run(0.125)

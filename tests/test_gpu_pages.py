@@ -356,3 +356,28 @@ def test_refusals_of_the_binding():
         binding.page_pools([c.pools[0].half()])
     torch.cuda.synchronize()
     c.same()
+
+
+class Elsewhere:
+    """A workspace on another device, as the binding sees it."""
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return self.t.get_device() + 1
+
+
+def test_workspaces_of_another_device_or_with_gaps_are_refused():
+    c = Cache([30, 0], 8)
+    to, used = [torch.empty_like(x) for x in (c.tables, c.refs, c.refs)], dev([0])
+    for ws in (Elsewhere(c.workspace(1)), torch.empty(1 << 16, device=DEV)[::2], torch.empty(1 << 16)):
+        for f in (binding.cache_fork, binding.cache_resize):
+            with pytest.raises(ValueError):
+                f(c.handle, c.tables, c.lens, c.refs, dev([0]), dev([1]), dev([0]), ws)
+        with pytest.raises(ValueError):
+            binding.cache_compact(c.handle, c.tables, c.lens, c.refs, *to, used, ws)
+    assert c.call("fork", [0], [1]) == [1]
