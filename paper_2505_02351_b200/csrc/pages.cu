@@ -9,7 +9,7 @@
 //
 // Data moves by bulk copies through shared memory, a ring of slots per warp that its first lane fills and empties: 64 pages of 64
 // pools (264 MB read and written) 46 us, 5.7 TB/s, where loads and stores through registers took 51 to 52; the part-full page of a
-// 16383-token prompt for 128 samples (504 MB, the reads from L2) 64 us against 79 to 85; 129 of 512 pages compacted (528 MB) 96.
+// 16383-token prompt for 128 samples (504 MB, the reads from L2) 62 to 64 us against 79 to 85; 129 of 512 pages compacted (528 MB) 96 to 98.
 // Rings of 8 or 16 KB slots and one or two CTAs per SM are within 3 % of that.  Few pages: 8 to 12 us for a call's two or three launches,
 // a chain of dependent loads of tables and counts (about 0.7 us each) and barriers between.
 //
