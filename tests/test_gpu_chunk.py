@@ -207,6 +207,16 @@ def test_a_mixed_batch():
     Batch(32, 4, 128, 32, q_lens=[int(x) for x in q[order]], lens=[int(x) for x in lens[order]], seed=11, slopes=True, extra_pages=9).check()
 
 
+@pytest.mark.parametrize("B,window", [(257, 0), (700, 90), (1500, 0)])
+def test_batches_of_more_sequences_than_threads(B, window):
+    """Each thread of the list's first pass has several sequences, some without new tokens, without a context, or padding."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 200, size=B)
+    q = np.where(rng.random(B) < 0.3, 0, rng.integers(1, 6, size=B))
+    q[B // 2], lens[B // 2] = 150, 180
+    Batch(4, 2, 64, 16, q_lens=[int(x) for x in q], lens=[int(x) for x in lens], seed=B, slopes=window > 0, lead=3, tail=5).check(window=window)
+
+
 def test_every_key_counts_once_wherever_the_list_is_cut():
     """Equal scores, values that name their token: each row is the mean of the numbers it sees, so a key too many or too few
     shows.  Numbers below 256 are whole in bf16, and so is what the tensor core sums."""

@@ -280,6 +280,17 @@ def test_fork_and_resize_on_both_sides_of_the_launches_choice(blocks, n, wide):
     c.consistent()
 
 
+def test_more_requests_than_shared_memory_holds():
+    rng = np.random.default_rng(12)
+    n, parents = 8200, 3
+    c = Cache([75, 64, 5] + [0] * n, 3 * n, wide=8, Hkv=1, pools=1, seed=12)
+    c.call("fork", np.sort(rng.integers(0, parents, size=n)), parents + rng.permutation(n))
+    c.consistent()
+    for _ in range(2):
+        c.call("resize", parents + rng.permutation(n), rng.integers(-1, 100, size=n))
+        c.consistent()
+
+
 @pytest.mark.parametrize("blocks", [1024, 1025, 4096, 4097])
 def test_compact_on_both_sides_of_the_launches_choice(blocks):
     rng = np.random.default_rng(blocks)
