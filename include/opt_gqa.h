@@ -28,9 +28,10 @@
  *    freq are read BEFORE that wait (the split of the work and the angles are computed
  *    from them while the preceding kernel drains).  They must therefore not be
  *    produced by a kernel that signals its dependents early (griddepcontrol
- *    .launch_dependents / cudaTriggerProgrammaticLaunchCompletion); no kernel of this
- *    library writes them except the gather of opt_gqa_decode_step_host, which does not
- *    signal early.  Ordinary producers (copies, kernels without that signal) are fine.
+ *    .launch_dependents / cudaTriggerProgrammaticLaunchCompletion); of this library
+ *    the gather of opt_gqa_decode_step_host and the calls on the cache's pages write
+ *    them, whose last kernels do not signal early.  Ordinary producers (copies, kernels
+ *    without that signal) are fine.
  *  - dtype: OPT_GQA_FP32 (0) or OPT_GQA_BF16 (1).  q, k_new/v_new, the cache and out
  *    share it.  Slopes, scale, partials are always fp32.  All arithmetic is fp32;
  *    results are rounded once (to nearest even) when stored.
@@ -535,6 +536,21 @@ int opt_gqa_cache_compact(void* const* pools, int num_pools, const int32_t* bloc
                           int max_blocks_per_seq, const int32_t* context_lens, const int32_t* ref_counts, int32_t* ref_counts_out,
                           int32_t* page_map, int32_t* used_out, int num_seqs, int Hkv, int D, int bs, int64_t num_blocks,
                           void* workspace, size_t workspace_bytes, int dtype, void* stream);
+
+/*
+ * The chunk attention and the calls on the pages with their arguments in one HOST record, for bindings that pay by the argument
+ * (Python's ctypes: 2 of the 10 us of a small call).  args: the arguments of the call in their order, 8 bytes each -- pointers and
+ * integers as int64, scale as double.  The result is that call's; OPT_GQA_ERR_SHAPE where an int argument does not fit an int or
+ * there is no such call.
+ */
+enum {
+    OPT_GQA_CALL_CHUNK = 0,          /* opt_gqa_paged_attention_chunk */
+    OPT_GQA_CALL_COPY_PAGES = 1,     /* opt_gqa_cache_copy_pages */
+    OPT_GQA_CALL_FORK = 2,           /* opt_gqa_cache_fork */
+    OPT_GQA_CALL_RESIZE = 3,         /* opt_gqa_cache_resize */
+    OPT_GQA_CALL_COMPACT = 4         /* opt_gqa_cache_compact */
+};
+int opt_gqa_call_record(int call, const int64_t* args);
 
 /*
  * One decode step of the attention layer, Algorithm 2 from "Store reshaped K, V

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -68,6 +69,7 @@ SIGNATURES = {
     "opt_gqa_cache_fork": (_i, [_vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
     "opt_gqa_cache_resize": (_i, [_vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
     "opt_gqa_cache_compact": (_i, [_vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i64, _vp, _sz, _i, _vp]),
+    "opt_gqa_call_record": (_i, [_i, _vp]),
     "opt_gqa_decode_step": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp, _f, _i, _i, _i, _i, _i, _i64,
                                  _i, _vp, _sz, _i, _i, _vp]),
     "opt_gqa_decode_step_host": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _f, _i, _i, _i, _i,
@@ -347,11 +349,14 @@ def _rows(name: str, t: torch.Tensor, shape, dtype, device: int):
     """(address, elements from token to token) of a CUDA tensor [T, heads, D] whose heads lie side by side."""
     if t is None or t.shape != shape or t.dtype != dtype or t.get_device() != device:
         raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on the current CUDA device")
-    T, H, D = shape
+    return t.data_ptr(), _token_stride(name, t, *shape)
+
+
+def _token_stride(name: str, t: torch.Tensor, T: int, H: int, D: int) -> int:
     st, sh, sd = t.stride()
     if sd != 1 or (sh != D and H > 1):
         raise ValueError(f"{name}: expected the heads of a token side by side")
-    return t.data_ptr(), st if T > 1 else H * D      # the stride of a single token says nothing
+    return st if T > 1 else H * D                    # the stride of a single token says nothing
 
 
 def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
@@ -364,10 +369,10 @@ def _index(name: str, t: torch.Tensor, dtype, n: int, device: int) -> int:
 def _scratch(t: Optional[torch.Tensor], device: int):
     """(address, bytes) of a workspace."""
     if t is None:
-        return None, 0
+        return 0, 0
     if t.get_device() != device or not t.is_contiguous():
         raise ValueError("workspace: expected a contiguous tensor on the current CUDA device")
-    return t.data_ptr(), t.numel() * t.element_size()
+    return t.data_ptr(), t.nbytes
 
 
 def _current_device(t: torch.Tensor) -> int:
@@ -451,6 +456,13 @@ def paged_attention_decode_shared(out, q, k_cache, v_cache, block_tables, contex
         _DTYPE_CODE[dtype], _stream(stream, dev)), "opt_gqa_paged_attention_decode_shared")
 
 
+# Calls with their arguments in one record (opt_gqa_call_record): ctypes converts each argument of the others, 2 us for these.
+_CALL_CHUNK, _CALL_COPY_PAGES, _CALL_FORK, _CALL_RESIZE, _CALL_COMPACT = range(5)
+_chunk_record = struct.Struct("=12qd11q").pack
+_copy_record = struct.Struct("=11q").pack
+_pages_record = struct.Struct("=19q").pack
+
+
 def chunk_workspace_bytes(Hq: int, Hkv: int, D: int, max_q_len: int) -> int:
     return int(load().opt_gqa_chunk_workspace_bytes(Hq, Hkv, D, max_q_len))
 
@@ -461,20 +473,21 @@ def paged_attention_chunk(out, q, q_start_loc, max_q_len: int, k_cache, v_cache,
     shape, pool, dtype, dev, i32 = q.shape, k_cache.shape, q.dtype, _current_device(q), torch.int32
     T, Hq, D = shape
     num_blocks, Hkv, bs, dims = pool
-    rows, width = block_tables.shape if block_tables.dim() == 2 else (-1, 0)
+    tables, rows = block_tables.shape, context_lens.numel()
     if dims != D or out.shape != shape or v_cache.shape != pool:
         raise ValueError("expected out like q and k_cache, v_cache [blocks, heads, block size, dims of q]")
-    if rows != context_lens.numel():
+    if len(tables) != 2 or tables[0] != rows:
         raise ValueError("block_tables: expected a row per sequence")
-    qp, qs = _rows("q", q, shape, dtype, dev)
+    if q.get_device() != dev:
+        raise ValueError("q: expected a tensor on the current CUDA device")
     ws, wsb = _scratch(workspace, dev)
-    _check(load().opt_gqa_paged_attention_chunk(
-        _index("out", out, dtype, -1, dev), qp, qs, _index("q_start_loc", q_start_loc, i32, rows + 1, dev), T, max_q_len,
-        _index("k_cache", k_cache, dtype, -1, dev), _index("v_cache", v_cache, dtype, -1, dev),
-        _index("block_tables", block_tables, i32, -1, dev), width, _index("context_lens", context_lens, i32, -1, dev),
-        None if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, rows, Hq, Hkv, D,
-        bs, num_blocks, window, ws, wsb, _DTYPE_CODE[dtype], _stream(stream, dev)),
-        "opt_gqa_paged_attention_chunk")
+    _check(load().opt_gqa_call_record(_CALL_CHUNK, _chunk_record(
+        _index("out", out, dtype, -1, dev), q.data_ptr(), _token_stride("q", q, T, Hq, D),
+        _index("q_start_loc", q_start_loc, i32, rows + 1, dev), T, max_q_len, _index("k_cache", k_cache, dtype, -1, dev),
+        _index("v_cache", v_cache, dtype, -1, dev), _index("block_tables", block_tables, i32, -1, dev), tables[1],
+        _index("context_lens", context_lens, i32, -1, dev),
+        0 if alibi_slopes is None else _index("alibi_slopes", alibi_slopes, torch.float32, Hq, dev), scale, rows, Hq, Hkv, D, bs,
+        num_blocks, window, ws, wsb, _DTYPE_CODE[dtype], _stream(stream, dev))), "opt_gqa_paged_attention_chunk")
 
 
 class PagePools:
@@ -516,55 +529,55 @@ def _pools_device(pools: PagePools) -> int:
 
 
 def _table(block_tables, context_lens, dev: int):
-    if block_tables.dim() != 2:
+    shape = block_tables.shape
+    if len(shape) != 2:
         raise ValueError("block_tables: expected a row per sequence")
-    S, W = block_tables.shape
+    S, W = shape
     return (_index("block_tables", block_tables, torch.int32, -1, dev), S, W,
             _index("context_lens", context_lens, torch.int32, S, dev))
 
 
 def cache_copy_pages(pools: PagePools, src_pages, dst_pages, stream=None) -> None:
     """Page dst_pages[i] becomes a copy of page src_pages[i] in every pool (int32; a pair with a number outside is skipped)."""
-    dev, n = _pools_device(pools), src_pages.numel()
-    _check(load().opt_gqa_cache_copy_pages(
-        pools.address, pools.count, _index("src_pages", src_pages, torch.int32, n, dev),
-        _index("dst_pages", dst_pages, torch.int32, n, dev), n, pools.Hkv, pools.D, pools.bs, pools.num_blocks, pools.code,
-        _stream(stream, dev)), "opt_gqa_cache_copy_pages")
+    dev, n, i32 = _pools_device(pools), src_pages.numel(), torch.int32
+    _check(load().opt_gqa_call_record(_CALL_COPY_PAGES, _copy_record(
+        pools.address, pools.count, _index("src_pages", src_pages, i32, -1, dev), _index("dst_pages", dst_pages, i32, n, dev), n,
+        pools.Hkv, pools.D, pools.bs, pools.num_blocks, pools.code, _stream(stream, dev))), "opt_gqa_cache_copy_pages")
 
 
-def _pages(entry: str, pools, block_tables, context_lens, ref_counts, a, b, done, workspace, stream) -> None:
+def _pages(call: int, where: str, pools, block_tables, context_lens, ref_counts, a, b, done, workspace, stream) -> None:
     dev, n, i32 = _pools_device(pools), a.numel(), torch.int32
     bt, S, W, lens = _table(block_tables, context_lens, dev)
     ws, wsb = _scratch(workspace, dev)
-    _check(getattr(load(), entry)(
+    _check(load().opt_gqa_call_record(call, _pages_record(
         pools.address, pools.count, bt, W, lens, _index("ref_counts", ref_counts, i32, pools.num_blocks, dev),
         _index("requests", a, i32, -1, dev), _index("requests", b, i32, n, dev), n, _index("done", done, i32, n, dev), S,
-        pools.Hkv, pools.D, pools.bs, pools.num_blocks, ws, wsb, pools.code, _stream(stream, dev)), entry)
+        pools.Hkv, pools.D, pools.bs, pools.num_blocks, ws, wsb, pools.code, _stream(stream, dev))), where)
 
 
 def cache_fork(pools: PagePools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream=None) -> None:
     """Rows `children` continue rows `parents`: full pages shared, a part-full last page copied.  done [n] int32: 1 where it was."""
-    _pages("opt_gqa_cache_fork", pools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream)
+    _pages(_CALL_FORK, "opt_gqa_cache_fork", pools, block_tables, context_lens, ref_counts, parents, children, done, workspace, stream)
 
 
 def cache_resize(pools: PagePools, block_tables, context_lens, ref_counts, seqs, new_lens, done, workspace, stream=None) -> None:
     """Rows `seqs` get the lengths `new_lens`: pages dropped (0 frees a sequence) or given.  done [n] int32: 1 where it was."""
-    _pages("opt_gqa_cache_resize", pools, block_tables, context_lens, ref_counts, seqs, new_lens, done, workspace, stream)
+    _pages(_CALL_RESIZE, "opt_gqa_cache_resize", pools, block_tables, context_lens, ref_counts, seqs, new_lens, done, workspace, stream)
 
 
 def cache_compact(pools: PagePools, block_tables, context_lens, ref_counts, block_tables_out, ref_counts_out, page_map, used_out,
                   workspace, stream=None) -> None:
     """The pages in use move to the front of the pools; outputs may be their inputs.  page_map: old number -> new one or -1."""
-    dev, nb = _pools_device(pools), pools.num_blocks
+    dev, nb, i32 = _pools_device(pools), pools.num_blocks, torch.int32
     bt, S, W, lens = _table(block_tables, context_lens, dev)
     if block_tables_out.shape != block_tables.shape:
         raise ValueError("block_tables_out: expected the shape of block_tables")
     ws, wsb = _scratch(workspace, dev)
-    _check(load().opt_gqa_cache_compact(
-        pools.address, pools.count, bt, _index("block_tables_out", block_tables_out, torch.int32, -1, dev), W, lens,
-        _index("ref_counts", ref_counts, torch.int32, nb, dev), _index("ref_counts_out", ref_counts_out, torch.int32, nb, dev),
-        _index("page_map", page_map, torch.int32, nb, dev), _index("used_out", used_out, torch.int32, 1, dev), S, pools.Hkv,
-        pools.D, pools.bs, nb, ws, wsb, pools.code, _stream(stream, dev)), "opt_gqa_cache_compact")
+    _check(load().opt_gqa_call_record(_CALL_COMPACT, _pages_record(
+        pools.address, pools.count, bt, _index("block_tables_out", block_tables_out, i32, -1, dev), W, lens,
+        _index("ref_counts", ref_counts, i32, nb, dev), _index("ref_counts_out", ref_counts_out, i32, nb, dev),
+        _index("page_map", page_map, i32, nb, dev), _index("used_out", used_out, i32, 1, dev), S, pools.Hkv, pools.D, pools.bs, nb,
+        ws, wsb, pools.code, _stream(stream, dev))), "opt_gqa_cache_compact")
 
 
 def step_staging_bytes(B: int, Hq: int, Hkv: int, D: int, max_blocks_per_seq: int, dtype: torch.dtype) -> int:

@@ -1,6 +1,9 @@
 // extern "C" boundary of the Opt-GQA library: host-side argument checks, then one
 // launcher per operation.  Nothing here allocates or keeps caller pointers; the only state of the
 // library is per device: a status word on the GPU and host-side caches of addresses and attributes.
+#include <cstring>
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace optgqa {
@@ -36,6 +39,19 @@ static bool shape_ok(int Hq, int Hkv, int D, int bs) {
 }  // namespace optgqa
 
 using namespace optgqa;
+
+// A call's arguments in a record, in their order.
+struct Record {
+    const int64_t* a;
+    template <typename T = void>
+    T* P(int k) const { return reinterpret_cast<T*>(a[k]); }
+    int I(int k) const { return (int)a[k]; }
+    bool ints(std::initializer_list<int> which) const {         // whether they fit an int
+        for (const int k : which)
+            if (a[k] != (int)a[k]) return false;
+        return true;
+    }
+};
 
 extern "C" {
 
@@ -564,6 +580,38 @@ int opt_gqa_cache_compact(void* const* pools, int num_pools, const int32_t* bloc
     const PageTables t = {const_cast<int32_t*>(block_tables), const_cast<int32_t*>(context_lens), const_cast<int32_t*>(ref_counts),
                           num_seqs, max_blocks_per_seq, bs, (int)num_blocks};
     return launch_compact(set, sh, t, block_tables_out, ref_counts_out, page_map, used_out, w, status, static_cast<cudaStream_t>(stream));
+}
+
+int opt_gqa_call_record(int call, const int64_t* args) {
+    if (!args) return OPT_GQA_ERR_NULL;
+    const Record r{args};
+    const int64_t* a = args;
+    switch (call) {
+    case OPT_GQA_CALL_CHUNK: {
+        if (!r.ints({4, 5, 9, 13, 14, 15, 16, 17, 19, 22})) return OPT_GQA_ERR_SHAPE;
+        double scale;
+        std::memcpy(&scale, a + 12, sizeof scale);
+        return opt_gqa_paged_attention_chunk(r.P(0), r.P(1), a[2], r.P<int32_t>(3), r.I(4), r.I(5), r.P(6), r.P(7), r.P<int32_t>(8), r.I(9),
+                                             r.P<int32_t>(10), r.P<float>(11), (float)scale, r.I(13), r.I(14), r.I(15), r.I(16), r.I(17), a[18],
+                                             r.I(19), r.P(20), (size_t)a[21], r.I(22), r.P(23));
+    }
+    case OPT_GQA_CALL_COPY_PAGES:
+        if (!r.ints({1, 4, 5, 6, 7, 9})) return OPT_GQA_ERR_SHAPE;
+        return opt_gqa_cache_copy_pages(r.P<void*>(0), r.I(1), r.P<int32_t>(2), r.P<int32_t>(3), r.I(4), r.I(5), r.I(6), r.I(7), a[8], r.I(9),
+                                        r.P(10));
+    case OPT_GQA_CALL_FORK:
+    case OPT_GQA_CALL_RESIZE:
+        if (!r.ints({1, 3, 8, 10, 11, 12, 13, 17})) return OPT_GQA_ERR_SHAPE;
+        return requests_checked(call == OPT_GQA_CALL_FORK, r.P<void*>(0), r.I(1), r.P<int32_t>(2), r.I(3), r.P<int32_t>(4), r.P<int32_t>(5),
+                                r.P<int32_t>(6), r.P<int32_t>(7), r.I(8), r.P<int32_t>(9), r.I(10), r.I(11), r.I(12), r.I(13), a[14], r.P(15),
+                                (size_t)a[16], r.I(17), r.P(18));
+    case OPT_GQA_CALL_COMPACT:
+        if (!r.ints({1, 4, 10, 11, 12, 13, 17})) return OPT_GQA_ERR_SHAPE;
+        return opt_gqa_cache_compact(r.P<void*>(0), r.I(1), r.P<int32_t>(2), r.P<int32_t>(3), r.I(4), r.P<int32_t>(5), r.P<int32_t>(6),
+                                     r.P<int32_t>(7), r.P<int32_t>(8), r.P<int32_t>(9), r.I(10), r.I(11), r.I(12), r.I(13), a[14], r.P(15),
+                                     (size_t)a[16], r.I(17), r.P(18));
+    }
+    return OPT_GQA_ERR_SHAPE;
 }
 
 // Bytes of `workspace` a decode step of these sizes uses: the balanced split's layout for bf16 caches, one

@@ -1,5 +1,6 @@
 """Host side of the chunk attention: workspace size and refusals (no GPU needed)."""
 import ctypes
+import struct
 
 import pytest
 import torch
@@ -59,3 +60,24 @@ def test_binding_refuses_tensors_that_do_not_fit(lib):
                       workspace=None), **kw)
         with pytest.raises(ValueError):
             binding.paged_attention_chunk(**a)
+
+
+def test_a_record_of_the_arguments_is_refused_as_the_call_is(lib):
+    wsb = binding.chunk_workspace_bytes(32, 4, 128, 4)
+    good = dict(out=256, q=256, stride=4096, qsl=256, T=9, most=4, k=256, v=256, bt=256, maxb=8, n=256, sl=256, scale=1.0, B=4, Hq=32, Hkv=4,
+                D=128, bs=16, blocks=100, window=0, ws=256, wsb=wsb, dtype=1, stream=0)
+
+    def call(which=0, **kw):
+        return lib.opt_gqa_call_record(which, struct.pack("=12qd11q", *dict(good, **kw).values()))
+
+    for code, cases in ((-3, (dict(dtype=0), dict(dtype=7))),
+                        (-2, (dict(B=-1), dict(B=70000), dict(T=-1), dict(most=-1), dict(Hq=33), dict(Hkv=3), dict(D=96), dict(bs=8),
+                              dict(maxb=0), dict(blocks=0), dict(window=-1), dict(stride=4088), dict(stride=1 << 40), dict(wsb=wsb - 1))),
+                        (-1, [{name: 0} for name in ("out", "q", "qsl", "k", "v", "bt", "n", "ws")]),
+                        (-4, [{name: 264} for name in ("out", "q", "k", "v", "ws")] + [dict(stride=4100)]),
+                        (0, (dict(B=0), dict(T=0), dict(most=0)))):
+        for bad in cases:
+            assert call(**bad) == code, bad
+    for name in ("T", "most", "maxb", "B", "Hq", "Hkv", "D", "bs", "window", "dtype"):          # not cut to 32 bits
+        assert call(**{name: good[name] + (1 << 32)}) == -2, name
+    assert call(which=5) == -2 and call(which=-1) == -2 and lib.opt_gqa_call_record(0, None) == -1

@@ -1,5 +1,6 @@
 """Host side of the page operators: workspace size and refusals (no GPU needed)."""
 import ctypes
+import struct
 
 import pytest
 import torch
@@ -99,3 +100,41 @@ def test_binding_refuses_host_tensors_and_no_pools(lib):
         binding.page_pools([])
     with pytest.raises(ValueError):
         binding.page_pools([torch.zeros(2, 2, 16, 64)])
+
+
+def host(pools):
+    return 0 if pools is None else ctypes.addressof(pools)
+
+
+@pytest.mark.parametrize("entry,where", [(1, "copy"), (2, "fork"), (3, "resize"), (4, "compact")])
+def test_a_record_of_the_arguments_is_refused_as_the_call_is(lib, entry, where):
+    fixed = dict(Hkv=8, D=128, bs=16, blocks=10)
+    n = 1 if where == "compact" else 3
+    wsb = binding.pages_workspace_bytes(n, 10)
+    last = dict(ws=256, wsb=wsb, dtype=1, stream=0)
+    good = dict(pools=POOLS, num=2)
+    if where == "copy":
+        good |= dict(src=256, dst=256, n=3) | fixed | dict(dtype=1, stream=0)
+    elif where == "compact":
+        good |= dict(bt=256, bto=256, W=8, lens=256, refs=256, refs_out=256, pm=256, used=256, S=4) | fixed | last
+    else:
+        good |= dict(bt=256, W=8, lens=256, refs=256, a=256, b=256, n=3, done=256, S=4) | fixed | last
+
+    def call(**kw):
+        values = dict(good, **kw)
+        values["pools"] = host(values["pools"])
+        return lib.opt_gqa_call_record(entry, struct.pack("=%dq" % len(values), *values.values()))
+
+    for want, bad in bad_pools():
+        assert call(**bad) == want, bad
+    for name in set(good) & {"src", "dst", "bt", "bto", "lens", "refs", "refs_out", "pm", "used", "a", "b", "done", "ws"}:
+        assert call(**{name: 0}) == -1, name
+    for name in set(good) & {"refs", "ws"}:
+        assert call(**{name: 260}) == -4, name
+    for bad in (dict(n=-1), dict(S=0), dict(W=0), dict(W=1 << 27), dict(wsb=wsb - 1)):
+        if set(bad) <= set(good):
+            assert call(**bad) == -2, bad
+    for name in set(good) & {"num", "W", "n", "S", "Hkv", "D", "bs", "dtype"}:                  # not cut to 32 bits
+        assert call(**{name: good[name] + (1 << 32)}) == -2, name
+    if "n" in good:
+        assert call(n=0) == 0
