@@ -9,7 +9,7 @@
 // two per SM), so that one long context fills the GPU as well as a large ragged batch.  A range covers whole items, written
 // out at once, and at its two ends parts of items: normalised partial rows and log-sum-exps in the workspace, two places a worker,
 // merged by chunk_merge_kernel.  (The chunked prefill gives a block of rows to one CTA whatever the context: with few new tokens
-// most of the GPU is idle.)  Few items are not cut, and items of few tiles need no list: see kCutCost and prefers_direct.
+// most of the GPU is idle.)  Few items are not cut, and items of few tiles need no list: see kCutCost and ctas_per_item.
 //
 // Products take 64 rows for blocks of up to 64, row 16 w + i in lane 32 w + i, so that a block of up to 16 or 32 rows lies in one
 // or two row warps: items take the warps in turns, and one block's last product and its storing overlap the next one's first scores.
@@ -78,6 +78,9 @@ constexpr int kKpBytes = kTN / 8 * kExtRowGroupBytes;
 constexpr int kNumBars = 12 + 4 * kStages + 4 + 2 * kDescs;
 constexpr int kDescReaders = 7;            // warps that read a descriptor: all but the one that writes it
 
+constexpr int kMaxSplit = 8;               // CTAs that share an item at most
+constexpr size_t kSmemPerSm = 228 * 1024;
+
 template <int D>
 struct ChLayout {
     static constexpr int kHalves = D / 64;
@@ -90,7 +93,9 @@ struct ChLayout {
     static constexpr int kOffKp = kOffQx + kQxBytes;
     static constexpr int kOffBar = kOffKp + kKpBytes;
     static constexpr int kOffDesc = kOffBar + kNumBars * 8 + 16;
-    static constexpr int kSmemBytes = kOffDesc + kDescs * kDescBytes + 1024;
+    static constexpr int kOffParts = kOffDesc + kDescs * kDescBytes;       // of a cluster's item: see merge_cluster
+    static constexpr int kSmemBytes = kOffParts + 1024;
+    static constexpr int kMostBytes = kSmemBytes + kRows * D * 4 + kMaxSplit * kRows * 4;
 };
 
 constexpr uint32_t kColS = 0;              // S buffers at 0 and kTN, P over the first half of its S
@@ -109,7 +114,7 @@ struct ChunkParams {
     float* part;
     int* status;
     float scale;
-    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows, direct;
+    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows, direct, recv_rows;
 };
 
 // A sequence of the batch: its rows of q, context, position of its first new token, and its blocks first .. blocks - 1 that see a key.
@@ -131,6 +136,63 @@ __device__ __forceinline__ Seq sequence(const ChunkParams& p, int s) {
     return x;
 }
 
+__device__ __forceinline__ int linear_cta() { return blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z); }
+
+// ----------------------------------------------------------------------------- an item shared by a cluster
+// The CTAs of a cluster have a share of the item's tiles each and merge their rows through distributed shared memory: CTA c gets
+// every part's columns c D / C and on, and writes them out.  What a CTA receives, behind its own buffers: four columns of a part by
+// rows of 16 bytes, and the parts' log-sum-exps.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, int rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+
+// 32 columns of a part's row to the CTAs that own them.
+template <int D>
+__device__ __forceinline__ void send_columns(uint32_t parts, int part, int C, int slot_rows, int row, int col, const float (&o)[32], float inv) {
+    const int width = D / C;
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        const int own = (col + e) / width, four = (col + e) % width / 4;
+        const uint32_t at = in_cta(parts + ((part * (width / 4) + four) * slot_rows + row) * 16, own);
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(o[e] * inv), "f"(o[e + 1] * inv), "f"(o[e + 2] * inv),
+                     "f"(o[e + 3] * inv)
+                     : "memory");
+    }
+}
+
+// The parts' rows joined: this CTA's columns, a thread a row of eight.
+template <int D, int G>
+__device__ __forceinline__ void merge_cluster(const char* received, __nv_bfloat16* out, int rank, int C, int parts, int slot_rows, int rows,
+                                              int q0, int pos0, int kvh, int Hq, int total_q) {
+    const int width = D / C, padded = (rows + 15) / 16 * 16;
+    const float4* x = reinterpret_cast<const float4*>(received);
+    const float* lse = reinterpret_cast<const float*>(received + (size_t)slot_rows * D * 4);
+    for (int i = threadIdx.x; i < padded * (width / 8); i += kThreads) {
+        const int row = i % padded, eight = i / padded, t = q0 + row / G;
+        if (row >= rows || pos0 + row / G < 0 || (unsigned)t >= (unsigned)total_q) continue;
+        float top = -INFINITY, den = 0.f, num[8] = {};
+        for (int u = 0; u < parts; ++u) top = fmaxf(top, lse[u * slot_rows + row]);
+#pragma unroll 2
+        for (int u = 0; u < parts; ++u) {
+            const float l = lse[u * slot_rows + row];
+            if (l == -INFINITY) continue;               // a part the row saw nothing of: its values mean nothing (a NaN is carried on)
+            const float w = ex2((l - top) * kLog2e);
+            const float4 a = x[(u * (width / 4) + 2 * eight) * slot_rows + row], b = x[(u * (width / 4) + 2 * eight + 1) * slot_rows + row];
+            den += w;
+            num[0] = fmaf(w, a.x, num[0]), num[1] = fmaf(w, a.y, num[1]), num[2] = fmaf(w, a.z, num[2]), num[3] = fmaf(w, a.w, num[3]);
+            num[4] = fmaf(w, b.x, num[4]), num[5] = fmaf(w, b.y, num[5]), num[6] = fmaf(w, b.z, num[6]), num[7] = fmaf(w, b.w, num[7]);
+        }
+        const float inv = 1.f / den;
+        *reinterpret_cast<uint4*>(out + ((size_t)t * Hq + kvh * G + row % G) * D + rank * width + eight * 8) =
+            make_uint4(pack2(num[0] * inv, num[1] * inv), pack2(num[2] * inv, num[3] * inv), pack2(num[4] * inv, num[5] * inv),
+                       pack2(num[6] * inv, num[7] * inv));
+    }
+}
+
 // The tiles lo .. hi - 1 that the rows of block mt see.
 template <int TQ>
 __device__ __forceinline__ void block_tiles(const Seq& x, int mt, int window, int& lo, int& hi) {
@@ -146,7 +208,9 @@ struct Piece {
                                     // whether the tiles are read for this block alone
 };
 
-template <int D, int G>
+// kShared: an item's tiles are shared by the CTAs of a cluster, p.direct of them (a kernel of its own: with its code in the other, that
+// one's list took 3 to 9 % longer).
+template <int D, int G, bool kShared>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant__ CUtensorMap map_q16,
              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const ChunkParams p) {
@@ -199,7 +263,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     // ------------------------------------------------------------------ the items (the index arrays are read before the
     // wait for the preceding kernel: see the ordering contract in the header)
     const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
-    if (!p.direct) {
+    if (!kShared && !p.direct) {
         long long units = 0, blocks = 0;
         int most = 0;
         for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) {
@@ -272,6 +336,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     grid_dependency_launch();           // not before this CTA has its tensor memory: a later grid's could take it and wait for this one
+    const uint32_t received = smem_u32(smem + L::kOffParts);
+    if constexpr (kShared) cluster_arrive();
 
     if (warp == 4) {
         // ------------------------------------------------------------------ the list of pieces, Q and K
@@ -350,14 +416,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             }
             if (!whole) pos += item_cost(x);
         };
-        if (p.direct) {
+        if (kShared || p.direct) {
+            const int split = kShared ? p.direct : 1;
             s = blockIdx.z;
             kvh = blockIdx.y;
             x = sequence<TQ>(p, s);
-            mt = blockIdx.x;
+            mt = blockIdx.x / split;
             if (mt >= x.first && mt < x.blocks) {
                 block_tiles<TQ>(x, mt, p.window, t0, t1);
-                end = (t1 - t0) * kTileCost;
+                // this CTA's share of them
+                const int parts = min(split, t1 - t0), part = blockIdx.x % split;
+                if (part < parts) {
+                    jt = (t1 - t0) * part / parts;
+                    end = ((t1 - t0) * (part + 1) / parts - jt) * kTileCost;
+                }
             }
         } else {
             long long total = 0, items = 0;
@@ -468,7 +540,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             next_item();
         }
         if (!waited) grid_dependency_wait();
-        if (lane == 0 && !p.direct) {
+        if (!kShared && lane == 0 && !p.direct) {
             p.flags[me] = flags;
             p.items[2 * me] = first_item;
             p.items[2 * me + 1] = last_item;
@@ -660,6 +732,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
             const int hg = lane % G;                     // (16 is a multiple of G)
+            if constexpr (kShared) cluster_wait();       // every CTA is there to be written to
             // the thread's row of the block, -1: none
             auto row_of = [&]() {
                 const int w = warp - d.warp0;
@@ -667,7 +740,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                 return rr < d.rows ? rr : -1;
             };
             // rows before position 0 (more new tokens than context: padding) see nothing and are zero
-            const int cta = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), ctas = gridDim.x * gridDim.y * gridDim.z;
+            const int cta = linear_cta(), ctas = gridDim.x * gridDim.y * gridDim.z;
             for (int s = cta * 4 + warp; s < p.B; s += ctas * 4) {
                 const Seq x = sequence<TQ>(p, s);
                 const int none = min(x.q, -x.pos0);
@@ -821,13 +894,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                                 for (int i = 0; i < 8; ++i) w[i] = pack2(o[16 * e + 2 * i] * inv, o[16 * e + 2 * i + 1] * inv);
                                 st_global_32(orow + c * 32 + e * 16, w, wide);
                             }
+                        } else if (begun && kShared) {
+                            send_columns<D>(received, blockIdx.x % p.direct, p.direct, p.recv_rows, rr, c * 32, o, inv);
                         } else if (begun) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) part[(size_t)(c * 32 + e) * p.slot_rows] = o[e] * inv;
                         }
                     }
                     // a row that saw nothing of the piece: weight zero
-                    if (valid && d.slot >= 0) p.lse[(size_t)d.slot * p.slot_rows + rr] = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
+                    if (valid && d.slot >= 0) {
+                        const float lse = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
+                        if constexpr (kShared) {
+                            const uint32_t at = received + p.recv_rows * D * 4 + (blockIdx.x % p.direct * p.recv_rows + rr) * 4;
+                            for (int c = 0; c < p.direct; ++c) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(in_cta(at, c)), "f"(lse) : "memory");
+                        } else {
+                            p.lse[(size_t)d.slot * p.slot_rows + rr] = lse;
+                        }
+                    }
                 }
                 release_piece(pc);
             }
@@ -845,6 +928,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     if (warp == 5) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+    }
+
+    if constexpr (kShared) {
+        __syncwarp();
+        if (warp >= 4) cluster_wait();
+        const Seq x = sequence<TQ>(p, blockIdx.z);
+        const int mt = blockIdx.x / p.direct;
+        int t0 = 0, t1 = 0;
+        if (mt >= x.first && mt < x.blocks) block_tiles<TQ>(x, mt, p.window, t0, t1);
+        const int parts = min(p.direct, t1 - t0);
+        if (parts > 1) {                    // (the same in the whole cluster)
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+            merge_cluster<D, G>(smem + L::kOffParts, p.out, blockIdx.x % p.direct, p.direct, parts, p.recv_rows, min(TQ, x.q - mt * TQ) * G,
+                                x.q0 + mt * TQ, x.pos0 + mt * TQ, blockIdx.y, p.Hq, p.total_q);
+        }
     }
 }
 
@@ -971,31 +1071,89 @@ struct Maps {
     CUtensorMap q32, q16, k, v;
 };
 
-// Whether every item gets a CTA of its own: no list and nothing to merge, but the longest item's time, or one wave of CTAs after the
-// other.  items and tiles (of the longest) are what the host can bound them by; wide: blocks of more than 64 rows.
+// Shared memory of a launch whose items have `split` CTAs each.
+size_t chunk_smem(int D, int split, int recv_rows) {
+    return (D == 128 ? ChLayout<128>::kSmemBytes : ChLayout<64>::kSmemBytes) + (split > 1 ? (size_t)recv_rows * (D + split) * 4 : 0);
+}
+
+// Clusters of 2^k of the kernel's CTAs that are resident together, of one CTA per multiprocessor (148, 74, 33, 15: a cluster's lie in
+// one part of the GPU); 0 where that cannot be found out.
+int resident_clusters(int k) {
+    static std::atomic<int> known[kMaxDevices][4];
+    static std::atomic<bool> configured[kMaxDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+    int n = known[dev][k].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (!ensure_smem_limit(chunk_kernel<128, 1, true>, ChLayout<128>::kMostBytes, configured)) return 0;
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        cfg.gridDim = dim3(8);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = ChLayout<128>::kMostBytes;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 1u << k;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, chunk_kernel<128, 1, true>, &cfg) != cudaSuccess || n <= 0) return 0;
+        known[dev][k].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+// How many CTAs every item gets: one, or a cluster that shares its tiles; 0: the list.  items and tiles (of the longest) are what the
+// host can bound them by; wide: blocks of more than 64 rows; wave: the CTAs that are resident together.
 //
-// In a graph, us, a CTA each against the list that is cut.  One wave: 32 items of 4, 7, 10, 11 and 16 tiles 7.7 10.1 12.6 13.4 17.4 against
-// 12.8 13.3 12.7 12.8 15.1; 64 of 11, 13 and 16, wide, 17.6 19.5 22.6 against 20.1 20.8 21.7; 128 of 13, 16 and 24 16.7 19.3 26.3 against
-// 22.1 23.4 27.2; 256 of 16 and 24 23.9 33.0 against 32.4 41.5: worth it up to 8 tiles and one more per 16 items.  More waves: 320
-// items of 2, 4, 8 and 16 tiles 13.1 17.0 24.8 41.7 against 17.6 21.2 26.9 37.1; 448 14.6 18.2 26.9 45.0 against 17.6 25.3 32.5 46.9; 600 20.0
-// 25.9 38.0 65.3 against 21.0 28.4 37.5 58.3; 896 of 1, 2 and 4 23.4 26.9 34.8 against 17.4 26.1 34.6; 448 wide of 2, 4, 8 and 16 19.0 23.2 32.9
-// 52.9 against 24.2 33.5 41.9 59.3.  There it goes by estimates of both, in us: a wave 6 and 1.06 a tile (wide 8.3 and 1.2), the list 17 (12
-// where nothing can be cut) and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25).  A last wave that is not full counts 0.8.
-bool prefers_direct(long long items, long long wave, long long tiles, bool wide) {
-    if (items <= wave) return tiles <= 8 + items / 16;
-    if (items > 4 * wave) return false;
-    const double waves = (double)(items / wave) + (items % wave ? 0.8 : 0.0), share = (double)items / (double)wave, t = (double)tiles;
-    const double direct = waves * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
-    const double list = (tiles > 1 ? 17.0 : 12.0) + share * (wide ? 3.4 + 1.25 * t : 1.2 + 1.06 * t);
-    return direct < list;
+// The list takes a prologue and a launch for the merge, and cuts evenly; clusters cost their barriers and the exchange, 3 us, and go
+// with the longest item.  In a graph, us, the list against 1, 2, 4 and 8 CTAs an item:
+//   8 items of 5, 9, 17, 33, 65, 129 and 257 tiles: 8.6 11.7 13.0 16.0 21.3 26.4 32.4 against 7.4 10.4 16.5 28.4 .. (1), 7.9 8.4 10.1 13.2
+//     19.3 31.2 55 (4) and 8.4 8.9 9.4 11.0 14.1 20.1 32.2 (8);
+//   32 items of 5, 9, 17, 33 and 65: 10.3 14.3 15.5 19.5 23.9 against 7.7 10.9 17.4 30 56 (1), 8.8 10.4 13.6 19.6 31.7 (2), 9.8 10.3 11.8
+//     15.0 21.2 (4); wide 12.5 15.9 18.1 20.7 25.4 against 9.5 13.4 20.7 35 64 (1) and 11.5 12.2 13.9 17.3 23.9 (4);
+//   128 items of 9, 17 and 33: 15.8 22.0 33.7 against 12.2 19.2 33.4 (1) and 13.2 17.6 27.1 (2);
+//   64-dim heads, 128 items of 66 rows and 18 tiles: 23.3 against 23.9 (1) and 20.2 (2).
+// So: by estimates in us, a CTA 4.3 and 0.8 a tile (wide 6 and 0.9), a cluster 6.8 (8.7) and 0.013 per CTA of all, where they fit the GPU at
+// once -- 16 clusters of 8 with a multiprocessor for each CTA, in two waves, took 16.1 us where 8 took 8.2 -- and a CTA has few tiles:
+// up to 8 and one more per 16 items of one CTA, 16 and one more per 32 CTAs of clusters.
+//
+// More items than a wave: a CTA each against the list that is cut, 320 items of 2, 4, 8 and 16 tiles 13.1 17.0 24.8 41.7 against 17.6 21.2
+// 26.9 37.1; 448 14.6 18.2 26.9 45.0 against 17.6 25.3 32.5 46.9; 600 20.0 25.9 38.0 65.3 against 21.0 28.4 37.5 58.3; 896 of 1, 2 and 4 23.4
+// 26.9 34.8 against 17.4 26.1 34.6; 448 wide of 2, 4, 8 and 16 19.0 23.2 32.9 52.9 against 24.2 33.5 41.9 59.3.  There it goes by estimates of
+// both, in us: a wave 6 and 1.06 a tile (wide 8.3 and 1.2), the list 17 (12 where nothing can be cut) and of each worker's items 1.2 and
+// 1.06 a tile (wide 3.4 and 1.25).  A last wave that is not full counts 0.8.
+int ctas_per_item(long long items, long long wave, long long tiles, bool wide, int D, int recv_rows) {
+    const double t = (double)tiles;
+    if (items > 4 * wave) return 0;
+    if (items > wave) {
+        const double waves = (double)(items / wave) + (items % wave ? 0.8 : 0.0), share = (double)items / (double)wave;
+        const double direct = waves * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
+        const double list = (tiles > 1 ? 17.0 : 12.0) + share * (wide ? 3.4 + 1.25 * t : 1.2 + 1.06 * t);
+        return direct < list;
+    }
+    const double per_tile = wide ? 0.9 : 0.8;
+    double best = (wide ? 6.0 : 4.3) + per_tile * t;
+    int split = 1;
+    for (int k = 1; k <= 3; ++k) {
+        const int C = 1 << k, per_sm = 2 * (chunk_smem(D, C, recv_rows) + 1024) <= kSmemPerSm ? 2 : 1;
+        if (items * C > wave || tiles < C) break;
+        const double time = (wide ? 8.7 : 6.8) + 0.013 * (double)(items * C) + per_tile * (double)((tiles + C - 1) / C);
+        if (time < best && items <= (long long)per_sm * resident_clusters(k)) best = time, split = C;
+    }
+    const long long each = (tiles + split - 1) / split;
+    return each <= (split == 1 ? 8 + items / 16 : 16 + items * split / 32) ? split : 0;
 }
 
 template <int D, int G>
 int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, dim3 grid, cudaStream_t stream) {
-    static std::atomic<bool> configured[kMaxDevices];
-    if (!ensure_smem_limit(chunk_kernel<D, G>, ChLayout<D>::kSmemBytes, configured)) return OPT_GQA_ERR_CUDA;
-    const int rc = launch_dependent(chunk_kernel<D, G>, grid, dim3(kThreads), ChLayout<D>::kSmemBytes, stream, maps.q32, maps.q16, maps.k,
-                                    maps.v, p);
+    static std::atomic<bool> configured[2][kMaxDevices];
+    const size_t smem = chunk_smem(D, p.direct, p.recv_rows);
+    if (p.direct > 1) {
+        if (!ensure_smem_limit(chunk_kernel<D, G, true>, ChLayout<D>::kMostBytes, configured[1])) return OPT_GQA_ERR_CUDA;
+        return launch_clusters(chunk_kernel<D, G, true>, grid, dim3(kThreads), p.direct, smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
+    }
+    if (!ensure_smem_limit(chunk_kernel<D, G, false>, ChLayout<D>::kSmemBytes, configured[0])) return OPT_GQA_ERR_CUDA;
+    const int rc = launch_dependent(chunk_kernel<D, G, false>, grid, dim3(kThreads), smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
     if (rc != OPT_GQA_OK || m.W <= 1) return rc;            // (one worker has nothing to merge)
     return launch_dependent(chunk_merge_kernel<D, G>, dim3((unsigned)m.W), dim3(kMergeWarps * 32), 0, stream, m);
 }
@@ -1052,6 +1210,7 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     p.bs_log2 = bs == 32 ? 5 : 4;
     p.window = window;
     p.slot_rows = L.slot_rows;
+    p.recv_rows = (long long)max_q_len * G <= 16 ? 16 : L.slot_rows;
     ChunkMergeParams m;
     m.out = p.out;
     m.flags = p.flags;
@@ -1068,8 +1227,8 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    p.direct = blocks <= 65535 && prefers_direct(items, wave, tiles, (long long)max_q_len * G > kNarrowRows);
-    dim3 grid((unsigned)blocks, (unsigned)Hkv, (unsigned)B);
+    p.direct = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, D, p.recv_rows) : 0;
+    dim3 grid((unsigned)blocks * (p.direct > 1 ? p.direct : 1), (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.direct) {
         // one resident wave, and no more workers than there can be tiles

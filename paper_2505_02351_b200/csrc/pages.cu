@@ -593,25 +593,6 @@ int launch_copying(void (*kernel)(KArgs...), unsigned ctas, std::atomic<bool>* c
     return launch_dependent(kernel, dim3(ctas), dim3(kCopyThreads), sizeof(CopyRing), stream, args...);
 }
 
-// launch_dependent for a cluster, or one CTA alone.
-template <typename... KArgs, typename... Args>
-int launch_cluster(void (*kernel)(KArgs...), int ctas, size_t smem, cudaStream_t stream, Args... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kClusterThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)ctas;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = ctas > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? OPT_GQA_OK : OPT_GQA_ERR_CUDA;
-}
-
 // One CTA instead of the cluster, whose barriers and sums through distributed shared memory cost 1 us, where its threads have one vector
 // of counts each and there are no more than half as many requests.  (In a graph, us, one CTA against the cluster.  Steps that resize 32
 // sequences in pools of 512, 4096, 8192 and 32768 pages: 8.3 8.2 9.3 10.6 against 9.4 9.7 9.6 9.2; of 256 and 1024 in 4096: 9.1 and 11.1
@@ -646,8 +627,8 @@ int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, 
         rc = launch_dependent(fork_drop_kernel, dim3(x < 64 ? x : 64, (unsigned)r.n), dim3(256), 0, stream, t, r);
         if (rc != OPT_GQA_OK) return rc;
     }
-    rc = one ? launch_cluster(give_pages_kernel<true, 1>, 1, sizeof(Told), stream, t, r, w, drops)
-             : launch_cluster(give_pages_kernel<true, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, drops);
+    rc = one ? launch_clusters(give_pages_kernel<true, 1>, dim3(1), dim3(kClusterThreads), 1, sizeof(Told), stream, t, r, w, drops)
+             : launch_clusters(give_pages_kernel<true, kClusterCtas>, dim3(kClusterCtas), dim3(kClusterThreads), kClusterCtas, sizeof(Told), stream, t, r, w, drops);
     if (rc != OPT_GQA_OK) return rc;
     const int chunks = (t.width + 127) / 128;
     return launch_copying(fork_share_kernel, copy_ctas(sh, r.n, (long long)r.n * chunks), configured, stream, pools, sh, t, r, w, chunks, status);
@@ -658,8 +639,8 @@ int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
     const int rc = one_cta(t.num_blocks, r.n)
-                       ? launch_cluster(give_pages_kernel<false, 1>, 1, sizeof(Told), stream, t, r, w, true)
-                       : launch_cluster(give_pages_kernel<false, kClusterCtas>, kClusterCtas, sizeof(Told), stream, t, r, w, true);
+                       ? launch_clusters(give_pages_kernel<false, 1>, dim3(1), dim3(kClusterThreads), 1, sizeof(Told), stream, t, r, w, true)
+                       : launch_clusters(give_pages_kernel<false, kClusterCtas>, dim3(kClusterCtas), dim3(kClusterThreads), kClusterCtas, sizeof(Told), stream, t, r, w, true);
     if (rc != OPT_GQA_OK) return rc;
     return launch_copying(copy_pages_kernel<true>, copy_ctas(sh, r.n), configured, stream, pools, sh, w.src, w.dst, w.rows, r.n, status);
 }
@@ -669,8 +650,8 @@ int launch_compact(const PoolSet& pools, const PageShape& sh, const PageTables& 
     static std::atomic<bool> configured[kMaxDevices];
     if (sm_count() <= 0) return OPT_GQA_ERR_CUDA;
     const int rc = t.num_blocks <= kOneCtaCompact
-                       ? launch_cluster(compact_plan_kernel<1>, 1, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
-                       : launch_cluster(compact_plan_kernel<kClusterCtas>, kClusterCtas, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
+                       ? launch_clusters(compact_plan_kernel<1>, dim3(1), dim3(kClusterThreads), 1, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks)
+                       : launch_clusters(compact_plan_kernel<kClusterCtas>, dim3(kClusterCtas), dim3(kClusterThreads), kClusterCtas, 0, stream, t.refs, refs_out, page_map, used, w, t.num_blocks);
     if (rc != OPT_GQA_OK) return rc;
     return launch_copying(compact_move_kernel, copy_ctas(sh, t.num_blocks / 2 + 1, (long long)t.rows * t.width / 32), configured, stream, pools,
                           sh, t.tables, tables_out, t.lens, page_map, w, t.rows, t.width, t.bs, status);
