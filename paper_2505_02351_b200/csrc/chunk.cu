@@ -9,7 +9,8 @@
 // two per SM), so that one long context fills the GPU as well as a large ragged batch.  A range covers whole items, written
 // out at once, and at its two ends parts of items: normalised partial rows and log-sum-exps in the workspace, two places a worker,
 // merged by chunk_merge_kernel.  (The chunked prefill gives a block of rows to one CTA whatever the context: with few new tokens
-// most of the GPU is idle.)  Few items are not cut, and items of few tiles need no list: see kCutCost and ctas_per_item.
+// most of the GPU is idle.)  Few items are not cut (kCutCost).  Items of few tiles need no list but get a CTA each, and few items of
+// longer contexts a cluster each, whose CTAs share the tiles and merge their rows through distributed shared memory (ctas_per_item).
 //
 // Products take 64 rows for blocks of up to 64, row 16 w + i in lane 32 w + i, so that a block of up to 16 or 32 rows lies in one
 // or two row warps: items take the warps in turns, and one block's last product and its storing overlap the next one's first scores.
@@ -114,7 +115,7 @@ struct ChunkParams {
     float* part;
     int* status;
     float scale;
-    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows, direct, recv_rows;
+    int B, total_q, max_q, max_blocks, Hq, Hkv, bs, bs_log2, window, slot_rows, split, recv_rows;
 };
 
 // A sequence of the batch: its rows of q, context, position of its first new token, and its blocks first .. blocks - 1 that see a key.
@@ -208,9 +209,11 @@ struct Piece {
                                     // whether the tiles are read for this block alone
 };
 
-// kShared: an item's tiles are shared by the CTAs of a cluster, p.direct of them (a kernel of its own: with its code in the other, that
-// one's list took 3 to 9 % longer).
-template <int D, int G, bool kShared>
+// Where a CTA's items come from.  kList: its share of the list; kOne: the grid, an item each; kShared: the same with an item's tiles
+// shared by the CTAs of a cluster, p.split of them.  Kernels of their own: with the clusters' code in the list's, that took 3 to 9 %
+// longer, with the single items' 1 to 2 %.
+enum Route { kList, kOne, kShared };
+template <int D, int G, Route kRoute>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant__ CUtensorMap map_q16,
              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const ChunkParams p) {
@@ -263,7 +266,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     // ------------------------------------------------------------------ the items (the index arrays are read before the
     // wait for the preceding kernel: see the ordering contract in the header)
     const int chunk = (p.B + kThreads - 1) / kThreads;          // sequences per thread
-    if (!kShared && !p.direct) {
+    if constexpr (kRoute == kList) {
         long long units = 0, blocks = 0;
         int most = 0;
         for (int s = threadIdx.x * chunk; s < min((int)(threadIdx.x + 1) * chunk, p.B); ++s) {
@@ -337,7 +340,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     const uint32_t tmem_base = *tmem_slot;
     grid_dependency_launch();           // not before this CTA has its tensor memory: a later grid's could take it and wait for this one
     const uint32_t received = smem_u32(smem + L::kOffParts);
-    if constexpr (kShared) cluster_arrive();
+    if constexpr (kRoute == kShared) cluster_arrive();
 
     if (warp == 4) {
         // ------------------------------------------------------------------ the list of pieces, Q and K
@@ -416,8 +419,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             }
             if (!whole) pos += item_cost(x);
         };
-        if (kShared || p.direct) {
-            const int split = kShared ? p.direct : 1;
+        if constexpr (kRoute != kList) {
+            const int split = kRoute == kShared ? p.split : 1;
             s = blockIdx.z;
             kvh = blockIdx.y;
             x = sequence<TQ>(p, s);
@@ -540,7 +543,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
             next_item();
         }
         if (!waited) grid_dependency_wait();
-        if (!kShared && lane == 0 && !p.direct) {
+        if (kRoute == kList && lane == 0) {
             p.flags[me] = flags;
             p.items[2 * me] = first_item;
             p.items[2 * me + 1] = last_item;
@@ -732,7 +735,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         } else {
             // -------------------------------------------------------------- one thread per row: softmax, rescale, store
             const int hg = lane % G;                     // (16 is a multiple of G)
-            if constexpr (kShared) cluster_wait();       // every CTA is there to be written to
+            if constexpr (kRoute == kShared) cluster_wait();        // every CTA is there to be written to
             // the thread's row of the block, -1: none
             auto row_of = [&]() {
                 const int w = warp - d.warp0;
@@ -894,8 +897,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                                 for (int i = 0; i < 8; ++i) w[i] = pack2(o[16 * e + 2 * i] * inv, o[16 * e + 2 * i + 1] * inv);
                                 st_global_32(orow + c * 32 + e * 16, w, wide);
                             }
-                        } else if (begun && kShared) {
-                            send_columns<D>(received, blockIdx.x % p.direct, p.direct, p.recv_rows, rr, c * 32, o, inv);
+                        } else if (begun && kRoute == kShared) {
+                            send_columns<D>(received, blockIdx.x % p.split, p.split, p.recv_rows, rr, c * 32, o, inv);
                         } else if (begun) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) part[(size_t)(c * 32 + e) * p.slot_rows] = o[e] * inv;
@@ -904,9 +907,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                     // a row that saw nothing of the piece: weight zero
                     if (valid && d.slot >= 0) {
                         const float lse = begun ? (m_used + lg2(l)) * kLn2 : -INFINITY;
-                        if constexpr (kShared) {
-                            const uint32_t at = received + p.recv_rows * D * 4 + (blockIdx.x % p.direct * p.recv_rows + rr) * 4;
-                            for (int c = 0; c < p.direct; ++c) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(in_cta(at, c)), "f"(lse) : "memory");
+                        if constexpr (kRoute == kShared) {
+                            const uint32_t at = received + p.recv_rows * D * 4 + (blockIdx.x % p.split * p.recv_rows + rr) * 4;
+                            for (int c = 0; c < p.split; ++c) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(in_cta(at, c)), "f"(lse) : "memory");
                         } else {
                             p.lse[(size_t)d.slot * p.slot_rows + rr] = lse;
                         }
@@ -930,19 +933,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
     }
 
-    if constexpr (kShared) {
+    if constexpr (kRoute == kShared) {
         __syncwarp();
         if (warp >= 4) cluster_wait();
         const Seq x = sequence<TQ>(p, blockIdx.z);
-        const int mt = blockIdx.x / p.direct;
+        const int mt = blockIdx.x / p.split;
         int t0 = 0, t1 = 0;
         if (mt >= x.first && mt < x.blocks) block_tiles<TQ>(x, mt, p.window, t0, t1);
-        const int parts = min(p.direct, t1 - t0);
+        const int parts = min(p.split, t1 - t0);
         if (parts > 1) {                    // (the same in the whole cluster)
             __syncwarp();
             cluster_arrive();
             cluster_wait();
-            merge_cluster<D, G>(smem + L::kOffParts, p.out, blockIdx.x % p.direct, p.direct, parts, p.recv_rows, min(TQ, x.q - mt * TQ) * G,
+            merge_cluster<D, G>(smem + L::kOffParts, p.out, blockIdx.x % p.split, p.split, parts, p.recv_rows, min(TQ, x.q - mt * TQ) * G,
                                 x.q0 + mt * TQ, x.pos0 + mt * TQ, blockIdx.y, p.Hq, p.total_q);
         }
     }
@@ -1085,7 +1088,7 @@ int resident_clusters(int k) {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
     int n = known[dev][k].load(std::memory_order_relaxed);
     if (n == 0) {
-        if (!ensure_smem_limit(chunk_kernel<128, 1, true>, ChLayout<128>::kMostBytes, configured)) return 0;
+        if (!ensure_smem_limit(chunk_kernel<128, 1, kShared>, ChLayout<128>::kMostBytes, configured)) return 0;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         cfg.gridDim = dim3(8);
@@ -1096,7 +1099,7 @@ int resident_clusters(int k) {
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        if (cudaOccupancyMaxActiveClusters(&n, chunk_kernel<128, 1, true>, &cfg) != cudaSuccess || n <= 0) return 0;
+        if (cudaOccupancyMaxActiveClusters(&n, chunk_kernel<128, 1, kShared>, &cfg) != cudaSuccess || n <= 0) return 0;
         known[dev][k].store(n, std::memory_order_relaxed);
     }
     return n;
@@ -1146,14 +1149,18 @@ int ctas_per_item(long long items, long long wave, long long tiles, bool wide, i
 
 template <int D, int G>
 int launch_both(const Maps& maps, const ChunkParams& p, const ChunkMergeParams& m, dim3 grid, cudaStream_t stream) {
-    static std::atomic<bool> configured[2][kMaxDevices];
-    const size_t smem = chunk_smem(D, p.direct, p.recv_rows);
-    if (p.direct > 1) {
-        if (!ensure_smem_limit(chunk_kernel<D, G, true>, ChLayout<D>::kMostBytes, configured[1])) return OPT_GQA_ERR_CUDA;
-        return launch_clusters(chunk_kernel<D, G, true>, grid, dim3(kThreads), p.direct, smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
+    static std::atomic<bool> configured[3][kMaxDevices];
+    const size_t smem = chunk_smem(D, p.split, p.recv_rows);
+    if (p.split > 1) {
+        if (!ensure_smem_limit(chunk_kernel<D, G, kShared>, ChLayout<D>::kMostBytes, configured[kShared])) return OPT_GQA_ERR_CUDA;
+        return launch_clusters(chunk_kernel<D, G, kShared>, grid, dim3(kThreads), p.split, smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
     }
-    if (!ensure_smem_limit(chunk_kernel<D, G, false>, ChLayout<D>::kSmemBytes, configured[0])) return OPT_GQA_ERR_CUDA;
-    const int rc = launch_dependent(chunk_kernel<D, G, false>, grid, dim3(kThreads), smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
+    if (p.split == 1) {
+        if (!ensure_smem_limit(chunk_kernel<D, G, kOne>, smem, configured[kOne])) return OPT_GQA_ERR_CUDA;
+        return launch_dependent(chunk_kernel<D, G, kOne>, grid, dim3(kThreads), smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
+    }
+    if (!ensure_smem_limit(chunk_kernel<D, G, kList>, smem, configured[kList])) return OPT_GQA_ERR_CUDA;
+    const int rc = launch_dependent(chunk_kernel<D, G, kList>, grid, dim3(kThreads), smem, stream, maps.q32, maps.q16, maps.k, maps.v, p);
     if (rc != OPT_GQA_OK || m.W <= 1) return rc;            // (one worker has nothing to merge)
     return launch_dependent(chunk_merge_kernel<D, G>, dim3((unsigned)m.W), dim3(kMergeWarps * 32), 0, stream, m);
 }
@@ -1227,10 +1234,10 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    p.direct = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, D, p.recv_rows) : 0;
-    dim3 grid((unsigned)blocks * (p.direct > 1 ? p.direct : 1), (unsigned)Hkv, (unsigned)B);
+    p.split = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, D, p.recv_rows) : 0;
+    dim3 grid((unsigned)blocks * (p.split > 1 ? p.split : 1), (unsigned)Hkv, (unsigned)B);
     m.W = 1;
-    if (!p.direct) {
+    if (!p.split) {
         // one resident wave, and no more workers than there can be tiles
         const long long most = Hkv * ((long long)total_q_tokens * G / kRows + B) * tiles;
         m.W = (int)(most < wave ? most : wave);

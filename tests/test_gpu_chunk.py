@@ -199,6 +199,20 @@ def test_cuts(B, Hq, Hkv, m, n):
     Batch(Hq, Hkv, 128, 16, q_lens=[int(x) for x in q], lens=[int(x) for x in lens], seed=B, slopes=B < 3).check()
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,bs", [(8, 1, 128, 16), (32, 4, 128, 32), (16, 8, 64, 16), (4, 4, 64, 32), (64, 8, 128, 16)])
+@pytest.mark.parametrize("m", [1, 2, 4, 9, 16, 33])
+@pytest.mark.parametrize("window", [0, 200])
+def test_few_items_of_long_contexts(Hq, Hkv, D, bs, m, window):
+    """Items whose tiles a cluster shares: some with fewer tiles than CTAs, padding, none, rows that see nothing of a share."""
+    lens = [1500 + m, 700, 65, 64, 1, 0, 130 + m, 5]
+    q = [m, m, min(m, 65), 1, 1, 0, m, m]
+    b = Batch(Hq, Hkv, D, bs, q_lens=q, lens=lens, seed=Hq + m, slopes=m % 2 == 0, lead=2, tail=3)
+    got = b.check(window=window)
+    scale = D ** -0.5
+    for _ in range(2):
+        assert torch.equal(b.run(scale, window).view(torch.int16), got.view(torch.int16))
+
+
 def test_a_mixed_batch():
     rng = np.random.default_rng(0)
     q = np.concatenate([np.ones(40, dtype=int), rng.integers(2, 9, size=10), [257, 512, 100]])
