@@ -920,6 +920,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
         }
     }
 
+    if constexpr (kRoute == kShared) {
+        __syncwarp();
+        if (warp >= 4) cluster_wait();
+        cluster_arrive();                   // (this warp's rows are where they are merged)
+    }
     // ---- every role is done with tensor memory: give it back (after a wait that gave up, let what is in flight drain)
     if (*reinterpret_cast<volatile int*>(p.status) != 0) tmem_slot[1] = 1;
     tc_fence_before();
@@ -934,20 +939,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
     }
 
     if constexpr (kRoute == kShared) {
-        __syncwarp();
-        if (warp >= 4) cluster_wait();
         const Seq x = sequence<TQ>(p, blockIdx.z);
         const int mt = blockIdx.x / p.split;
         int t0 = 0, t1 = 0;
         if (mt >= x.first && mt < x.blocks) block_tiles<TQ>(x, mt, p.window, t0, t1);
         const int parts = min(p.split, t1 - t0);
-        if (parts > 1) {                    // (the same in the whole cluster)
-            __syncwarp();
-            cluster_arrive();
-            cluster_wait();
+        __syncwarp();
+        cluster_wait();                     // (and only then may a CTA end: the others write into it)
+        if (parts > 1)
             merge_cluster<D, G>(smem + L::kOffParts, p.out, blockIdx.x % p.split, p.split, parts, p.recv_rows, min(TQ, x.q - mt * TQ) * G,
                                 x.q0 + mt * TQ, x.pos0 + mt * TQ, blockIdx.y, p.Hq, p.total_q);
-        }
     }
 }
 
