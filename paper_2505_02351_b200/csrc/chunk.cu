@@ -17,10 +17,10 @@
 // (With 128 rows for those of more than 16, run without a pause, 8 drafts behind 16 to 32 k tokens took 74.6 us instead of 72.4, for
 // the power; in a graph 66.3 instead of 67.0.)  Warps none of whose rows see a tile skip its softmax.
 //
-// 32/8 heads, 32 sequences of 3 to 6 new tokens behind 512 to 2048: 35.5 us (152 MB: 23.1 us of copy bandwidth); 32/4 heads, 8 of 8
-// behind 16384 to 32768: 67 us (357 MB, 54.5); 64/8 heads, 60 decode rows and 4 chunks of 300 to 512: 100 us (409 MB, 62.3; 118
-// without a pause, where the power limit takes the clock down); 32/8 heads, 511 behind 32768: 267 to 280 us (272 GFLOP, 165 at the
-// burst rate, 196 at the sustained one; 318 without a pause).  What bounds them: between prologue and tail the cache is read at 6.9 to
+// 32/8 heads, 32 sequences of 3 to 6 new tokens behind 512 to 2048: 34.4 us (152 MB: 23.1 us of copy bandwidth); 32/4 heads, 8 of 8
+// behind 16384 to 32768: 67 us (357 MB, 54.5); 64/8 heads, 60 decode rows and 4 chunks of 300 to 512: 97 us (409 MB, 62.3; 115
+// without a pause, where the power limit takes the clock down); 32/8 heads, 511 behind 32768: 267 to 277 us (272 GFLOP, 165 at the
+// burst rate, 196 at the sustained one; 315 without a pause).  What bounds them: between prologue and tail the cache is read at 6.9 to
 // 7.3 TB/s where rows are few; besides that 2 us from the preceding kernel's end to the first scores, 4 to 5 us between the
 // workers' mean end and the last one's, 2 us until the merge may read and 3 to 4 us of merge.  Blocks of 128 rows: 1.03 to 1.17 us a
 // tile with two CTAs per SM, the tensor pipe 48 % active and, its instructions having a shortest time, 73 % occupied; as the prefill.
