@@ -58,14 +58,14 @@ __device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t by
 // 4 KB (63 us against 70).
 template <bool kRows>
 __device__ __forceinline__ void copy_pages(CopyRing& ring, const PoolSet& pools, const PageShape& sh, const int* src, const int* dst,
-                                           const int* rows, int n, int* status) {
+                                           const int* rows, int n, int* status, int block, int blocks) {
     if (threadIdx.x & 31) return;
     const int w = threadIdx.x >> 5;
     uint64_t* full = ring.full[w];
     const unsigned run = kRows ? sh.head_bytes : sh.page_bytes, per_run = (run + kSlotBytes - 1) / kSlotBytes, runs = sh.page_bytes / run;
     const unsigned per_pool = per_run * runs, per_pair = per_pool * (unsigned)sh.num_pools;
     const long long total = (long long)n * per_pair;
-    const long long warp = (long long)blockIdx.x * kCopyWarps + w, warps = (long long)gridDim.x * kCopyWarps;
+    const long long warp = (long long)block * kCopyWarps + w, warps = (long long)blocks * kCopyWarps;
     const long long step = kRows ? 1 : warps, stop = kRows ? share_of(total, warp + 1, warps) : total;
     long long next = kRows ? share_of(total, warp, warps) : warp;
     if (next >= stop) return;
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
     extern __shared__ __align__(128) char smem[];
     if (!kRows) grid_dependency_launch();   // (behind a table's kernel nothing may start early: see below)
     grid_dependency_wait();
-    copy_pages<kRows>(*reinterpret_cast<CopyRing*>(smem), pools, sh, src, dst, rows, n, status);
+    copy_pages<kRows>(*reinterpret_cast<CopyRing*>(smem), pools, sh, src, dst, rows, n, status, blockIdx.x, gridDim.x);
 }
 
 // ----------------------------------------------------------------------------- tables
@@ -434,14 +434,18 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
     }
 }
 
-// The parents' whole pages shared with their children, then the part-full ones copied.  Neighbouring requests of one parent are
-// a run: the first of them adds for all.
+// The parents' whole pages shared with their children, and the part-full ones copied: by CTAs of their own, the first `sharing` and the
+// others, or one behind the other (sharing 0).  Neighbouring requests of one parent are a run: the first of them adds for all.
 __global__ void __launch_bounds__(kCopyThreads) fork_share_kernel(const __grid_constant__ PoolSet pools, const PageShape sh, const PageTables t,
-                                                                  const PageRequests r, const PageWork w, int chunks, int* status) {
+                                                                  const PageRequests r, const PageWork w, int chunks, int sharing, int* status) {
     extern __shared__ __align__(128) char smem[];
     grid_dependency_wait();
-    const int lane = threadIdx.x & 31, warps = gridDim.x * kCopyWarps;
-    for (long long c = (long long)blockIdx.x * kCopyWarps + (threadIdx.x >> 5); c < (long long)r.n * chunks; c += warps) {
+    const int lane = threadIdx.x & 31, block = blockIdx.x, warps = (sharing ? sharing : gridDim.x) * kCopyWarps;
+    if (sharing && block >= sharing) {
+        copy_pages<true>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, w.rows, r.n, status, block - sharing, gridDim.x - sharing);
+        return;
+    }
+    for (long long c = (long long)block * kCopyWarps + (threadIdx.x >> 5); c < (long long)r.n * chunks; c += warps) {
         const int i = (int)(c / chunks), from = (int)(c - (long long)i * chunks) * 128;
         const int parent = r.a[i];
         if ((unsigned)parent >= (unsigned)t.rows) continue;
@@ -469,8 +473,9 @@ __global__ void __launch_bounds__(kCopyThreads) fork_share_kernel(const __grid_c
             if (times && in_pool(page, t.num_blocks)) atomicAdd(t.refs + page, times);
         }
     }
+    if (sharing) return;
     __syncwarp();
-    copy_pages<true>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, w.rows, r.n, status);
+    copy_pages<true>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, w.rows, r.n, status, block, gridDim.x);
 }
 
 // ----------------------------------------------------------------------------- compaction
@@ -575,7 +580,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid
         tables_out[e] = held ? page_map[page] : page;
     }
     __syncwarp();
-    copy_pages<false>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, nullptr, w.first[0], status);
+    copy_pages<false>(*reinterpret_cast<CopyRing*>(smem), pools, sh, w.src, w.dst, nullptr, w.first[0], status, blockIdx.x, gridDim.x);
 }
 
 // One resident wave, or fewer where there are fewer pieces (and chunks of tables).
@@ -615,6 +620,9 @@ int launch_copy_pages(const PoolSet& pools, const PageShape& sh, const int* src,
     return launch_copying(copy_pages_kernel<false>, copy_ctas(sh, n), configured, stream, pools, sh, src, dst, nullptr, n, status);
 }
 
+// Sharing has CTAs of its own where they are few or fit beside the copying ones.  (In a graph, us, one behind the other against that: a
+// prompt of 541 tokens to 4, 32 and 64 children in 8 pools 10.0 11.2 13.2 against 8.9 10.7 12.8; but 16383 tokens to 30 in 64 pools, where
+// sharing would take 60 of 444 CTAs, 22.3 against 23.7.)
 int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
                 cudaStream_t stream) {
     static std::atomic<bool> configured[kMaxDevices];
@@ -631,7 +639,11 @@ int launch_fork(const PoolSet& pools, const PageShape& sh, const PageTables& t, 
              : launch_clusters(give_pages_kernel<true, kClusterCtas>, dim3(kClusterCtas), dim3(kClusterThreads), kClusterCtas, sizeof(Told), stream, t, r, w, drops);
     if (rc != OPT_GQA_OK) return rc;
     const int chunks = (t.width + 127) / 128;
-    return launch_copying(fork_share_kernel, copy_ctas(sh, r.n, (long long)r.n * chunks), configured, stream, pools, sh, t, r, w, chunks, status);
+    const long long wave = (long long)sm_count() * kCopyCtasPerSm, share = ((long long)r.n * chunks + kCopyWarps - 1) / kCopyWarps;
+    const int sharing = 16 * share <= wave || share + copy_ctas(sh, r.n) <= wave ? (int)share : 0;
+    const long long copy = copy_ctas(sh, r.n, sharing ? 0 : (long long)r.n * chunks);
+    return launch_copying(fork_share_kernel, (unsigned)(sharing + (copy < wave - sharing ? copy : wave - sharing)), configured, stream, pools, sh,
+                          t, r, w, chunks, sharing, status);
 }
 
 int launch_resize(const PoolSet& pools, const PageShape& sh, const PageTables& t, const PageRequests& r, const PageWork& w, int* status,
