@@ -351,7 +351,8 @@ int opt_gqa_paged_attention_prefill_local(void* out, const void* q, const int32_
  *                 the one for 128 tokens serves all calls of the same heads.  Calls that can overlap on the GPU need one each.
  * bf16 only.  Weights are rounded to bf16 for the product with V and the denominator sums the rounded ones.  Keys and values past
  * a sequence's end never reach a row, whatever they hold; new tokens of one sequence share tiles, so a V row that is not
- * finite can reach those of them that do not see its key.
+ * finite can reach those of them that do not see its key.  A call gives the same bits in every run; where contexts are cut goes by
+ * its sizes, so other bounds (max_q_len, max_blocks_per_seq) for the same data can give other last bits.
  */
 int opt_gqa_paged_attention_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_start_loc, int total_q_tokens,
                                   int max_q_len, const void* k_cache, const void* v_cache, const int32_t* block_tables,
