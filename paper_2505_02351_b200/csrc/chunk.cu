@@ -81,6 +81,7 @@ constexpr int kDescReaders = 7;            // warps that read a descriptor: all 
 
 constexpr int kMaxSplit = 8;               // CTAs that share an item at most
 constexpr size_t kSmemPerSm = 228 * 1024;
+constexpr double kFarBytes = 126e6;         // what L2 holds
 
 template <int D>
 struct ChLayout {
@@ -1122,17 +1123,28 @@ int resident_clusters(int k) {
 // up to 8 and one more per 16 items of one CTA, 16 and one more per 32 CTAs of clusters.
 //
 // More items than a wave: a CTA each against the list that is cut, 320 items of 2, 4, 8 and 16 tiles 13.1 17.0 24.8 41.7 against 17.6 21.2
-// 26.9 37.1; 448 14.6 18.2 26.9 45.0 against 17.6 25.3 32.5 46.9; 600 20.0 25.9 38.0 65.3 against 21.0 28.4 37.5 58.3; 896 of 1, 2 and 4 23.4
-// 26.9 34.8 against 17.4 26.1 34.6; 448 wide of 2, 4, 8 and 16 19.0 23.2 32.9 52.9 against 24.2 33.5 41.9 59.3.  There it goes by estimates of
-// both, in us: a wave 6 and 1.06 a tile (wide 8.3 and 1.2), the list 17 (12 where nothing can be cut) and of each worker's items 1.2 and
-// 1.06 a tile (wide 3.4 and 1.25).  A last wave that is not full counts 0.8.
-int ctas_per_item(long long items, long long wave, long long tiles, bool wide, int D, int recv_rows) {
-    const double t = (double)tiles;
-    if (items > 4 * wave) return 0;
+// 26.9 37.1; 448 14.6 18.2 26.9 45.0 against 17.6 25.3 32.5 46.9; 600 of 2, 4 and 8 19.5 25.1 37.9 against 22.7 28.2 37.1; 896 25.9 33.7 51.0
+// against 25.2 33.1 48.0; wide, 448 of 2, 4, 8 and 16 18.3 22.5 31.7 51.5 against 23.7 31.9 40.3 58.9, 600 26.7 32.8 45.7 74.7 against 28.2
+// 36.7 48.7 72.9, 896 36.5 46.3 63.9 103.6 against 35.3 46.3 64.7 101.3.  There it goes by estimates of both, in us.  Up to two waves:
+// a wave 6 and 1.06 a tile (wide 8.3 and 1.2), a last one that is not full counting 0.8, and the list 17 (12 where nothing can be cut)
+// and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25); from there on straight lines in the number of items.
+//
+// far: the batch's keys and values are more than L2 holds and the sequences have several blocks, which read the same ones.  Side by side
+// as the grid has them they find them there, over the list's ranges not: 4 blocks each behind 1024 tokens, 172, 264 and 403 MB, 117 170 253
+// against 128 194 289 us; 8 blocks, 130 and 197 MB, 164 243 against 166 280 (65 MB: 103 against 95).
+int ctas_per_item(long long items, long long wave, long long tiles, bool wide, bool far, int D, int recv_rows) {
+    const double t = (double)tiles, share = (double)items / (double)wave;
     if (items > wave) {
-        const double waves = (double)(items / wave) + (items % wave ? 0.8 : 0.0), share = (double)items / (double)wave;
-        const double direct = waves * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
-        const double list = (tiles > 1 ? 17.0 : 12.0) + share * (wide ? 3.4 + 1.25 * t : 1.2 + 1.06 * t);
+        if (far) return 1;
+        if (items > 4 * wave) return 0;
+        double direct, list;
+        if (items <= 2 * wave) {
+            direct = (1.0 + 0.8) * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
+            list = (tiles > 1 ? 17.0 : 12.0) + share * (wide ? 3.4 + 1.25 * t : 1.2 + 1.06 * t);
+        } else {
+            direct = wide ? 3.0 + 0.9 * t + share * (6.2 + 1.17 * t) : 4.0 + 0.8 * t + share * (3.3 + t);
+            list = wide ? (tiles > 2 ? 17.0 : 10.0) + share * (2.2 + 1.35 * t) : (tiles > 2 ? 15.0 : 11.0) + share * (1.25 * t - 0.5);
+        }
         return direct < list;
     }
     const double per_tile = wide ? 0.9 : 0.8;
@@ -1235,7 +1247,10 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
         if (seen < tiles) tiles = seen;
     }
     const long long wave = (long long)sms * kCtasPerSm < kChunkMaxWorkers ? (long long)sms * kCtasPerSm : kChunkMaxWorkers;
-    p.split = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, D, p.recv_rows) : 0;
+    // several blocks of most sequences, by the number of new tokens, and more than kFarBytes of keys and values, by the tables' width
+    const bool far = blocks > 1 && blocks * B <= 2 * ((long long)total_q_tokens * G / kRows + B) &&
+                     (double)B * Hkv * D * 4 * kTN * (double)tiles > kFarBytes;
+    p.split = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, far, D, p.recv_rows) : 0;
     dim3 grid((unsigned)blocks * (p.split > 1 ? p.split : 1), (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.split) {
