@@ -213,6 +213,14 @@ def test_few_items_of_long_contexts(Hq, Hkv, D, bs, m, window):
         assert torch.equal(b.run(scale, window).view(torch.int16), got.view(torch.int16))
 
 
+@pytest.mark.parametrize("D,bs,window", [(128, 16, 0), (64, 32, 150)])
+def test_many_blocks_whose_tables_say_that_l2_does_not_hold_them(D, bs, window):
+    rng = np.random.default_rng(D)
+    q = rng.integers(130, 161, size=9)
+    lens = q + rng.integers(0, 400, size=9)
+    Batch(32, 8, D, bs, q_lens=[int(x) for x in q], lens=[int(x) for x in lens], seed=D, slopes=D == 64, extra_pages=300).check(window=window)
+
+
 def test_a_mixed_batch():
     rng = np.random.default_rng(0)
     q = np.concatenate([np.ones(40, dtype=int), rng.integers(2, 9, size=10), [257, 512, 100]])
