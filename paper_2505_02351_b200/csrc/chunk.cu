@@ -1101,7 +1101,10 @@ int resident_clusters(int k) {
         attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        if (cudaOccupancyMaxActiveClusters(&n, chunk_kernel<128, 1, kShared>, &cfg) != cudaSuccess || n <= 0) return 0;
+        if (cudaOccupancyMaxActiveClusters(&n, chunk_kernel<128, 1, kShared>, &cfg) != cudaSuccess || n <= 0) {
+            (void)cudaGetLastError();       // not the call's: it goes without clusters
+            return 0;
+        }
         known[dev][k].store(n, std::memory_order_relaxed);
     }
     return n;
