@@ -144,8 +144,6 @@ __device__ __forceinline__ int linear_cta() { return blockIdx.x + gridDim.x * (b
 // The CTAs of a cluster have a share of the item's tiles each and merge their rows through distributed shared memory: CTA c gets
 // every part's columns c D / C and on, and writes them out.  What a CTA receives, behind its own buffers: four columns of a part by
 // rows of 16 bytes, and the parts' log-sum-exps.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, int rank) {
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));

@@ -122,6 +122,12 @@ __device__ __forceinline__ float lg2(float x) {
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependency_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// The barrier of a thread-block cluster, by whole warps.  Another CTA's shared memory may be written once that CTA has begun: every
+// kernel that does so arrives at its start and waits before its first such store, and no CTA ends before the last of those
+// stores into it (another arrival and wait).
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // Launch that may begin while the preceding kernel of the stream is still draining (programmatic
 // stream serialisation).  The kernel must execute grid_dependency_wait() before it touches anything
 // the preceding kernel writes; with a predecessor that never signals, this is an ordinary launch.

@@ -191,6 +191,15 @@ __device__ __forceinline__ int cta_rank() {
     if constexpr (kCtas > 1) return (int)cg::this_cluster().block_rank();
     else return 0;
 }
+// Every CTA of the cluster has begun, and may be written to, where all arrived and one has waited.  (Whole warps.)
+template <int kCtas>
+__device__ __forceinline__ void arrive_begun() {
+    if constexpr (kCtas > 1) cluster_arrive();
+}
+template <int kCtas>
+__device__ __forceinline__ void wait_begun() {
+    if constexpr (kCtas > 1) cluster_wait();
+}
 // `v` to place `rank` of every CTA's `all`.
 template <int kCtas>
 __device__ __forceinline__ void tell_all(long long* all, int rank, long long v) {
@@ -276,6 +285,7 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
     __shared__ long long all_need[kCtas], all_free[kCtas];
     __shared__ int listed[kListed];
     const int rank = cta_rank<kCtas>(), tid = threadIdx.x;
+    arrive_begun<kCtas>();
     grid_dependency_launch();
     grid_dependency_wait();
     const int share = (r.n + kCtas - 1) / kCtas, mine = min(share * rank, r.n), count = min(share, r.n - mine);
@@ -322,6 +332,7 @@ give_pages_kernel(const PageTables t, const PageRequests r, const PageWork w, bo
         to_of[i] = drops ? to : from;
     }
     __syncthreads();
+    wait_begun<kCtas>();
     // the pages that may be copied from (parents and sequences that grow drop nothing), requested beside what is dropped
     for (int i = tid; i < count; i += kClusterThreads) {
         int last = -1;
@@ -486,6 +497,7 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
     __shared__ long long scratch[33];
     __shared__ long long all_used[kCtas], all_low[kCtas];
     const int rank = cta_rank<kCtas>(), tid = threadIdx.x;
+    arrive_begun<kCtas>();
     grid_dependency_launch();
     grid_dependency_wait();
     const Slice s = slice_of<kCtas>(num_blocks, rank);
@@ -500,6 +512,7 @@ compact_plan_kernel(const int* refs, int* refs_out, int* page_map, int* used_out
         count += (v.x > 0) + (v.y > 0) + (v.z > 0) + (v.w > 0) - (4 - live);
     }
     block_scan(count, scratch, here);
+    wait_begun<kCtas>();
     tell_all<kCtas>(all_used, rank, here);
     sync_all<kCtas>();
     long long before = 0, U = 0;
