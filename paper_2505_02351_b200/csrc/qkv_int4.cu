@@ -93,8 +93,8 @@ __device__ __forceinline__ void store_pair(const ProjParams& p, int t, int n, fl
     }
 }
 
-// Thread-block cluster: this CTA's rank and the cluster's size, the cluster-wide barrier, and a store to the same
-// shared-memory location in another CTA of the cluster.
+// Thread-block cluster: this CTA's rank and the cluster's size, and a store to the same shared-memory location in
+// another CTA of the cluster.
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -104,9 +104,6 @@ __device__ __forceinline__ uint32_t cluster_size() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void st_cluster_float2(const void* local_smem, uint32_t rank, float2 v) {
     uint32_t remote;
@@ -136,6 +133,7 @@ __global__ void __launch_bounds__(kProjWarps * 32, 2) qkv_int4_kernel(const Proj
     // the CTA's tile and its slice of the tile's quantisation groups; the warps split the slice
     const bool sliced = (int)blockIdx.x >= p.whole_ctas;
     const int csize = sliced ? (int)cluster_size() : 1, crank = sliced ? (int)cluster_rank() : 0;
+    if (sliced) cluster_arrive();
     const int tile = sliced ? p.whole_ctas + ((int)blockIdx.x - p.whole_ctas) / csize : (int)blockIdx.x;
     const int tile_groups = KC / CPG;
     const int g0 = tile_groups * crank / csize, groups = tile_groups * (crank + 1) / csize - g0;
@@ -273,12 +271,16 @@ __global__ void __launch_bounds__(kProjWarps * 32, 2) qkv_int4_kernel(const Proj
         return;
     }
     // a K slice: CTA o of the cluster finishes an equal share of the outputs; every CTA writes its sums for that
-    // share into slot `crank` of o's shared memory, and after one cluster barrier each CTA adds up what it received,
+    // share into slot `crank` of o's shared memory, and after a cluster barrier each CTA adds up what it received,
     // in rank order.  (Nothing touches another CTA's shared memory after the barrier, so a CTA may end at once.)
     const int share = 16 * 8 * NT / csize;
+    __syncwarp();
+    cluster_wait();                     // every CTA has begun and can be written to
     if (threadIdx.x < 16 * 8 * NT)
         st_cluster_float2(&recv[crank][tl][f], (uint32_t)(threadIdx.x / share), make_float2(s0, s1));
-    cluster_sync_all();
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
     if ((int)threadIdx.x < share) {
         const int idx = crank * share + threadIdx.x;
         const int tk = idx >> 4, fk = (idx & 15) * 2;

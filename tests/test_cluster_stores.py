@@ -25,7 +25,8 @@ def kernels(source):
         yield m.group(1), text[m.end():at - 1]
 
 
-@pytest.mark.parametrize("source,name", [("pages.cu", "give_pages_kernel"), ("pages.cu", "compact_plan_kernel"), ("chunk.cu", "chunk_kernel")])
+@pytest.mark.parametrize("source,name", [("pages.cu", "give_pages_kernel"), ("pages.cu", "compact_plan_kernel"), ("chunk.cu", "chunk_kernel"),
+                                         ("qkv_int4.cu", "qkv_int4_kernel")])
 def test_the_first_store_waits_until_the_cluster_has_begun(source, name):
     body = dict(kernels(source))[name]
     store, wait, arrive = (r.search(body) for r in (STORES, WAITS, ARRIVES))
