@@ -41,7 +41,7 @@ def test_compact(blocks):
     torch.cuda.synchronize()
     want = c.host.compact()
     for got in outs:
-        assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got, want)) and got[3].tolist() == [want[3]]
+        assert all(np.array_equal(g.cpu().numpy(), w) for g, w in zip(got[:3], want)) and got[3].tolist() == [want[3]]
     for got, w in zip(c.pools, c.host.pools):
         assert np.array_equal(got.view(c.bits).cpu().numpy(), w)
     assert binding.device_status() == 0
