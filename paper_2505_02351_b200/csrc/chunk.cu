@@ -197,7 +197,7 @@ __device__ __forceinline__ void merge_cluster(const char* received, __nv_bfloat1
 template <int TQ>
 __device__ __forceinline__ void block_tiles(const Seq& x, int mt, int window, int& lo, int& hi) {
     hi = (x.pos0 + min((mt + 1) * TQ, x.q) - 1) / kTN + 1;
-    lo = window > 0 ? max(0, x.pos0 + mt * TQ - window + 1) / kTN : 0;
+    lo = window > 0 ? max(0, max(0, x.pos0 + mt * TQ) - window + 1) / kTN : 0;      // (from 0 on no window takes it past 32 bits)
 }
 
 // What the other warps need to know of a piece.
@@ -765,7 +765,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_q32, const __grid_constant_
                     const int rr = row_of();
                     if (rr >= 0) {
                         pos = d.pos0 + rr / G;
-                        if (p.window > 0) lo = pos - p.window;
+                        if (p.window > 0) lo = max(max(pos, 0) - p.window, -1);
                     }
                 }
                 const float slope2 = p.slopes ? __ldg(p.slopes + d.kvh * G + hg) * kLog2e : 0.f;
