@@ -133,7 +133,7 @@ __device__ __forceinline__ Seq sequence(const ChunkParams& p, int s) {
     x.q = min(q, p.max_q);
     x.n = max(__ldg(p.context_lens + s), 0);
     x.pos0 = x.n - q;
-    x.blocks = x.n > 0 ? (x.q + TQ - 1) / TQ : 0;
+    x.blocks = x.pos0 + x.q > 0 ? (x.q + TQ - 1) / TQ : 0;      // (of more tokens than promised the first may all lie before position 0)
     x.first = x.pos0 < 0 ? min(-x.pos0 / TQ, x.blocks) : 0;
     return x;
 }
