@@ -493,8 +493,10 @@ int opt_gqa_rotary_append(void* q_out, const void* q, void* k_out, const void* k
  * Free pages are handed out lowest number first, in the order of the requests, and a request is carried out where as many are
  * free as it and all requests before it ask for: one whose pages are not there is left out, and so are those behind it that ask
  * for any.  Results are the same in every run.  num_seqs rows, n <= 65535, max_blocks_per_seq * 32 and context lengths below 2^31,
- * num_blocks <= 2^28; fp32 or bf16 pools.  The calls read their arrays behind the wait for the preceding kernel and let no later kernel
- * start before they have ended, so that attention calls may follow on the same stream.
+ * num_blocks <= 2^28; fp32 or bf16 pools.  The calls read their arrays behind the wait for the preceding kernel.  Fork, resize and
+ * compaction let no later kernel start before they have ended, with the tables, lengths and counts in memory, so that attention
+ * calls, which read those before they wait, may follow on the same stream.  The copy of pages writes none of them and lets a later
+ * kernel start once all that precedes it has ended.
  *
  * opt_gqa_cache_copy_pages: page dst_pages[i] becomes a copy of page src_pages[i] in every pool, n pairs in one launch; a pair
  *   with a number outside the pool (-1, say) is skipped.  The pages written are distinct and none of them is read by the same call.

@@ -131,14 +131,16 @@ template <bool kRows>
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PoolSet pools, const PageShape sh, const int* src,
                                                                   const int* dst, const int* rows, int n, int* status) {
     extern __shared__ __align__(128) char smem[];
-    if (!kRows) grid_dependency_launch();   // (behind a table's kernel nothing may start early: see below)
     grid_dependency_wait();
+    if (!kRows) grid_dependency_launch();   // (not before the wait, nor at all behind a table's kernel of the same call: see below)
     copy_pages<kRows>(*reinterpret_cast<CopyRing*>(smem), pools, sh, src, dst, rows, n, status, blockIdx.x, gridDim.x);
 }
 
 // ----------------------------------------------------------------------------- tables
-// The kernels that write tables and lengths never let the next kernel of another call start early: the attention kernels read
-// those before they wait.  Those behind which another kernel of the same call follows, which waits first, do.
+// The attention kernels read tables and lengths before they wait, so a call that writes those lets no other call's kernel start
+// before its own last kernel has ended.  A kernel behind which another one of the same call follows, which waits first, signals early.
+// The last ones never do: behind a grid that does not signal, a dependent one starts when it has ended and its memory can be seen.
+// A kernel that writes no table (copy_pages_kernel<false>) signals once it has waited, and so behind the tables' writer.
 
 __device__ __forceinline__ int pages_of(int tokens, const PageTables& t) {
     return min((max(tokens, 0) + t.bs - 1) / t.bs, t.width);
