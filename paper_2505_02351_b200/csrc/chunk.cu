@@ -82,6 +82,8 @@ constexpr int kDescReaders = 7;            // warps that read a descriptor: all 
 constexpr int kMaxSplit = 8;               // CTAs that share an item at most
 constexpr size_t kSmemPerSm = 228 * 1024;
 constexpr double kFarBytes = 126e6;         // what L2 holds
+// Contexts, as the host can bound them, up to which more items than a wave get a CTA each: see ctas_per_item.
+constexpr int kOneTiles = 1024 / kTN + 1, kFarTiles = 1536 / kTN + 1;
 
 template <int D>
 struct ChLayout {
@@ -1128,16 +1130,22 @@ int resident_clusters(int k) {
 // against 25.2 33.1 48.0; wide, 448 of 2, 4, 8 and 16 18.3 22.5 31.7 51.5 against 23.7 31.9 40.3 58.9, 600 26.7 32.8 45.7 74.7 against 28.2
 // 36.7 48.7 72.9, 896 36.5 46.3 63.9 103.6 against 35.3 46.3 64.7 101.3.  There it goes by estimates of both, in us.  Up to two waves:
 // a wave 6 and 1.06 a tile (wide 8.3 and 1.2), a last one that is not full counting 0.8, and the list 17 (12 where nothing can be cut)
-// and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25); from there on straight lines in the number of items.
+// and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25); from there on straight lines in the number of items.  Only up to
+// kOneTiles: the estimates take every context for the longest, and what the host knows of that is the tables' width.  One item of 8,
+// 16, 24, 32 and 48 tiles among 320 of 1: 11.7 17.4 23.3 29.1 41.1 against 16.0 15.9 16.8 17.6 19.0, among 560 of 4 18.9 20.2 26.4 32.4 44.4
+// against 26.4 26.9 27.1 27.9 27.8; one of 512 among 560 of 16 403 against 76.  Where all are as long a CTA each would gain up to 9 % past
+// the bound (592 of 20, 32, 64 and 128: 59 94 180 354 against 65 99 188 363; 320 73 142 278 against 59 107 200 for 32, 64 and 128).
 //
 // far: the batch's keys and values are more than L2 holds and the sequences have several blocks, which read the same ones.  Side by side
 // as the grid has them they find them there, over the list's ranges not: 4 blocks each behind 1024 tokens, 172, 264 and 403 MB, 117 170 253
 // against 128 194 289 us; 8 blocks, 130 and 197 MB, 164 243 against 166 280 (65 MB: 103 against 95).
+// Up to kFarTiles, by the same reason: 768 items, one of 16, 24, 32 and 48 tiles among others of 4, 35 41 48 62 against 39 42 43 45; one of 512
+// among 512 of 16, 451 against 104.  (All as long, 768 items of 24, 32 and 64 tiles 97 123 236 against 100 128 254; 1600 203 264 496 against 228 297 574.)
 int ctas_per_item(long long items, long long wave, long long tiles, bool wide, bool far, int D, int recv_rows) {
     const double t = (double)tiles, share = (double)items / (double)wave;
     if (items > wave) {
-        if (far) return 1;
-        if (items > 4 * wave) return 0;
+        if (far && tiles <= kFarTiles) return 1;
+        if (items > 4 * wave || tiles > kOneTiles) return 0;
         double direct, list;
         if (items <= 2 * wave) {
             direct = (1.0 + 0.8) * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
