@@ -82,7 +82,7 @@ constexpr int kDescReaders = 7;            // warps that read a descriptor: all 
 constexpr int kMaxSplit = 8;               // CTAs that share an item at most
 constexpr size_t kSmemPerSm = 228 * 1024;
 constexpr double kFarBytes = 126e6;         // what L2 holds
-// Contexts, as the host can bound them, up to which more items than a wave get a CTA each: see ctas_per_item.
+// Contexts, as the host can bound them, up to which more items than a wave may get a CTA each: see ctas_per_item.
 constexpr int kOneTiles = 1024 / kTN + 1, kFarTiles = 1536 / kTN + 1;
 
 template <int D>
@@ -1110,8 +1110,8 @@ int resident_clusters(int k) {
     return n;
 }
 
-// How many CTAs every item gets: one, or a cluster that shares its tiles; 0: the list.  items and tiles (of the longest) are what the
-// host can bound them by; wide: blocks of more than 64 rows; wave: the CTAs that are resident together.
+// How many CTAs every item gets: one, or a cluster that shares its tiles; 0: the list.  items, seq_items (of one sequence) and tiles (of the
+// longest) are what the host can bound them by; wide: blocks of more than 64 rows; wave: the CTAs that are resident together.
 //
 // The list takes a prologue and a launch for the merge, and cuts evenly; clusters cost their barriers and the exchange, 3 us, and go
 // with the longest item.  In a graph, us, the list against 1, 2, 4 and 8 CTAs an item:
@@ -1130,22 +1130,26 @@ int resident_clusters(int k) {
 // against 25.2 33.1 48.0; wide, 448 of 2, 4, 8 and 16 18.3 22.5 31.7 51.5 against 23.7 31.9 40.3 58.9, 600 26.7 32.8 45.7 74.7 against 28.2
 // 36.7 48.7 72.9, 896 36.5 46.3 63.9 103.6 against 35.3 46.3 64.7 101.3.  There it goes by estimates of both, in us.  Up to two waves:
 // a wave 6 and 1.06 a tile (wide 8.3 and 1.2), a last one that is not full counting 0.8, and the list 17 (12 where nothing can be cut)
-// and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25); from there on straight lines in the number of items.  Only up to
-// kOneTiles: the estimates take every context for the longest, and what the host knows of that is the tables' width.  One item of 8,
-// 16, 24, 32 and 48 tiles among 320 of 1: 11.7 17.4 23.3 29.1 41.1 against 16.0 15.9 16.8 17.6 19.0, among 560 of 4 18.9 20.2 26.4 32.4 44.4
-// against 26.4 26.9 27.1 27.9 27.8; one of 512 among 560 of 16 403 against 76.  Where all are as long a CTA each would gain up to 9 % past
-// the bound (592 of 20, 32, 64 and 128: 59 94 180 354 against 65 99 188 363; 320 73 142 278 against 59 107 200 for 32, 64 and 128).
+// and of each worker's items 1.2 and 1.06 a tile (wide 3.4 and 1.25); from there on straight lines in the number of items.
 //
 // far: the batch's keys and values are more than L2 holds and the sequences have several blocks, which read the same ones.  Side by side
 // as the grid has them they find them there, over the list's ranges not: 4 blocks each behind 1024 tokens, 172, 264 and 403 MB, 117 170 253
 // against 128 194 289 us; 8 blocks, 130 and 197 MB, 164 243 against 166 280 (65 MB: 103 against 95).
-// Up to kFarTiles, by the same reason: 768 items, one of 16, 24, 32 and 48 tiles among others of 4, 35 41 48 62 against 39 42 43 45; one of 512
-// among 512 of 16, 451 against 104.  (All as long, 768 items of 24, 32 and 64 tiles 97 123 236 against 100 128 254; 1600 203 264 496 against 228 297 574.)
-int ctas_per_item(long long items, long long wave, long long tiles, bool wide, bool far, int D, int recv_rows) {
+//
+// Both take every context for the longest, and what the host knows of that is the tables' width.  Where a batch is not so, the longest
+// item is walked by one CTA alone.  So they hold up to kOneTiles and kFarTiles, where that costs little -- one item of 8, 16, 24, 32 and
+// 48 tiles among 320 of 1, a CTA each against the list, 11.7 17.4 23.3 29.1 41.1 against 16.0 15.9 16.8 17.6 19.0, among 560 of 4 18.9 20.2 26.4
+// 32.4 44.4 against 26.4 26.9 27.1 27.9 27.8; of 16, 24, 32 and 48 among 768 wide ones of 4 35 41 48 62 against 39 42 43 45; but one of 512
+// among 560 of 16 403 against 76 -- and beyond where a sequence's items alone are a third of a wave, which leaves few CTAs without work:
+// with 16, 32, 64, 128 and 256 items one sequence of 32768 tokens among others of 1024 took 490 603 733 752 763 against 116 232 327 432 1009,
+// all of 8192 431 466 568 1091 1152 against 457 504 657 1348 1262, all of 32768 (32 to 256) 1925 2301 4661 4675 against 2129 3257 6431 6346.
+// (Short of that, batches of long and like contexts would gain: 592 items of 20, 32, 64 and 128 tiles 59 94 180 354 against 65 99 188 363.)
+int ctas_per_item(long long items, long long seq_items, long long wave, long long tiles, bool wide, bool far, int D, int recv_rows) {
     const double t = (double)tiles, share = (double)items / (double)wave;
     if (items > wave) {
-        if (far && tiles <= kFarTiles) return 1;
-        if (items > 4 * wave || tiles > kOneTiles) return 0;
+        const bool fills = 3 * seq_items >= wave;
+        if (far && (fills || tiles <= kFarTiles)) return 1;
+        if (items > 4 * wave || !(fills || tiles <= kOneTiles)) return 0;
         double direct, list;
         if (items <= 2 * wave) {
             direct = (1.0 + 0.8) * (wide ? 8.3 + 1.2 * (t - 1) : 6.0 + 1.06 * (t - 1));
@@ -1259,7 +1263,7 @@ int launch_chunk(void* out, const void* q, int64_t q_stride, const int32_t* q_st
     // several blocks of most sequences, by the number of new tokens, and more than kFarBytes of keys and values, by the tables' width
     const bool far = blocks > 1 && blocks * B <= 2 * ((long long)total_q_tokens * G / kRows + B) &&
                      (double)B * Hkv * D * 4 * kTN * (double)tiles > kFarBytes;
-    p.split = blocks <= 65535 ? ctas_per_item(items, wave, tiles, (long long)max_q_len * G > kNarrowRows, far, D, p.recv_rows) : 0;
+    p.split = blocks <= 65535 ? ctas_per_item(items, blocks * Hkv, wave, tiles, (long long)max_q_len * G > kNarrowRows, far, D, p.recv_rows) : 0;
     dim3 grid((unsigned)blocks * (p.split > 1 ? p.split : 1), (unsigned)Hkv, (unsigned)B);
     m.W = 1;
     if (!p.split) {

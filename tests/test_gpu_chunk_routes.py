@@ -69,3 +69,12 @@ def test_more_items_than_a_wave_up_to_the_measured_contexts(tokens, one):
     b = Batch(8, 8, 64, 16, q_lens=[3] * 70, lens=lens, seed=tokens)
     assert bounds(b)[1] == (17 if one else 18)
     assert by_list(b) != one
+
+
+@pytest.mark.parametrize("m,one", [(416, True), (385, True), (384, False)])
+def test_many_blocks_of_each_sequence_get_a_cta_each_at_any_context(m, one):
+    """13 blocks of 8 heads are a third of a wave, 12 are not."""
+    b = Batch(32, 8, 64, 16, q_lens=[m, 300, m, 290], lens=[m, 900, m + 100, 400], seed=m, extra_pages=1200)
+    items, tiles, size = bounds(b)
+    assert items == 4 * 8 * (13 if one else 12) > 296 and tiles > 300 and size > 126e6
+    assert by_list(b) != one
