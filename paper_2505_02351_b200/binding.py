@@ -1,9 +1,10 @@
 """ctypes binding of ``libopt_gqa.so``: argument marshalling only.
 
 Each function has the name of the C entry point it calls (without the
-``opt_gqa_`` prefix), takes CUDA torch tensors, passes their ``data_ptr()``
-and sizes straight through, and raises :class:`OptGqaError` on a non-zero
-status.  There is no fallback of any kind: if the shared library is missing
+``opt_gqa_`` prefix; the chunk attention and the page operators go through
+``opt_gqa_call_record``, which makes the call of their name), takes CUDA torch
+tensors, passes their ``data_ptr()`` and sizes straight through, and raises
+:class:`OptGqaError` on a non-zero status.  There is no fallback of any kind: if the shared library is missing
 or a tensor is not on a CUDA device the call fails.
 """
 from __future__ import annotations
