@@ -124,7 +124,9 @@ __device__ __forceinline__ void grid_dependency_launch() { asm volatile("griddep
 
 // The barrier of a thread-block cluster, by whole warps.  Another CTA's shared memory may be written once that CTA has begun: every
 // kernel that does so arrives at its start and waits before its first such store, and no CTA ends before the last of those
-// stores into it (another arrival and wait).
+// stores into it (another arrival and wait).  The arrival that only says that the CTA has begun orders no memory (with one that
+// releases, the 4-bit projection took 14.2 us instead of 13.5).
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 

@@ -196,7 +196,7 @@ __device__ __forceinline__ int cta_rank() {
 // Every CTA of the cluster has begun, and may be written to, where all arrived and one has waited.  (Whole warps.)
 template <int kCtas>
 __device__ __forceinline__ void arrive_begun() {
-    if constexpr (kCtas > 1) cluster_arrive();
+    if constexpr (kCtas > 1) cluster_arrive_relaxed();
 }
 template <int kCtas>
 __device__ __forceinline__ void wait_begun() {

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kProjWarps * 32, 2) qkv_int4_kernel(const Proj
     // the CTA's tile and its slice of the tile's quantisation groups; the warps split the slice
     const bool sliced = (int)blockIdx.x >= p.whole_ctas;
     const int csize = sliced ? (int)cluster_size() : 1, crank = sliced ? (int)cluster_rank() : 0;
-    if (sliced) cluster_arrive();
+    if (sliced) cluster_arrive_relaxed();
     const int tile = sliced ? p.whole_ctas + ((int)blockIdx.x - p.whole_ctas) / csize : (int)blockIdx.x;
     const int tile_groups = KC / CPG;
     const int g0 = tile_groups * crank / csize, groups = tile_groups * (crank + 1) / csize - g0;

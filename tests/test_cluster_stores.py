@@ -11,7 +11,7 @@ from paper_2505_02351_b200 import build
 # what stores into other CTAs, and what waits until all have begun; none of either is conditional but on the kernel's own form
 STORES = re.compile(r"\b(tell_all<|send_columns<|st_cluster_float2\()")
 WAITS = re.compile(r"\b(wait_begun<kCtas>\(\)|cluster_wait\(\))")
-ARRIVES = re.compile(r"\b(arrive_begun<kCtas>\(\)|cluster_arrive\(\))")
+ARRIVES = re.compile(r"\b(arrive_begun<kCtas>\(\)|cluster_arrive(_relaxed)?\(\))")
 
 
 def kernels(source):
